@@ -26,7 +26,7 @@
  * QLLM_ERR_CUDA.
  *
  * DEVICE MEMORY.  Which calls may call cudaMalloc / cudaFree:
- *   never      qllm_qgemm_noalloc, qllm_quantize_rows, qllm_calib_absmax, qllm_layernorm_rows,
+ *   never      qllm_qgemm_noalloc, qllm_quantize_rows, qllm_calib_absmax, qllm_layernorm_rows, qllm_kv_*,
  *              qllm_channel_distance, qllm_layer_forward / _reassemble_quant / _qgemm / _forward_host (everything a
  *              layer needs is taken in qllm_layer_create and returned in qllm_layer_destroy);
  *   grow-only  qllm_reassemble_quant (compiled-map scratch per (device, stream): grown on the first call
@@ -61,6 +61,8 @@ extern "C" {
 #define QLLM_ERR_ALIGN       (-9)  /* a main device tensor is not 16-byte aligned         */
 #define QLLM_ERR_UNSUPPORTED (-10) /* size beyond a documented limit                      */
 #define QLLM_ERR_NOMEM       (-11) /* allocation failed                                   */
+#define QLLM_ERR_PAGE        (-12) /* a page, length, row range or index found on the device is out of
+                                      range, or the cache has too few free pages (qllm_poll_status) */
 
 #define QLLM_F32  0
 #define QLLM_BF16 1
@@ -371,13 +373,136 @@ int qllm_layer_workspace(qllm_layer_t* layer, uint8_t** codes, float** a_scale, 
                          int32_t** a_rowsum, int* lane_bits);
 
 /* ==========================================================================
- * 6. Diagnostics
+ * 6. Key/value cache in 4 bits                    (device, asynchronous)
+ * ==========================================================================
+ * What follows the QKV projection: its keys and values are stored with the per-token quantizer of Eq. 2, one scale
+ * and zero-point for each token and head, and attention reads them in that form.
+ *
+ * THE CACHE is four caller-owned device arrays over `layers` layers and `pages` pages of page_size tokens:
+ *   k_codes, v_codes  uint8 [layers][pages][kv_heads][page_size][head_dim / 2], byte i of a row holds channel 2i in its
+ *                     low nibble and channel 2i + 1 in its high nibble (the 4-bit layout of qllm_quantize_rows)
+ *   k_param, v_param  float [layers][pages][kv_heads][page_size][2]: scale alpha, zero-point; value = alpha (code - zero)
+ * page_size is 16, 32, 64, 128 or 256, head_dim 64, 128 or 256 (QLLM_ERR_UNSUPPORTED otherwise); all four arrays are 16-byte
+ * aligned.  A token's keys and values take 2 (head_dim / 2 + 8) bytes per head.
+ *
+ * A BATCH names the sequences that a call works on and their newest tokens:
+ *   table     device int32 [seqs][table_width]: table[s][j] is the page of positions j page_size .. of sequence s.  Only the
+ *             entries that seq_lens reaches are read.
+ *   seq_lens  device int32 [seqs]: tokens of the sequence in the cache, the new ones included
+ *   q_start   device int32 [seqs + 1], not decreasing: rows q_start[s] .. q_start[s+1] - 1 of the call's packed tensors are the
+ *             new tokens of sequence s, its last positions in order.  A sequence may have none.
+ *   rows      rows of the packed tensors, at least q_start[seqs]; rows in front of q_start[0] and from q_start[seqs] on are
+ *             left as they are
+ *   max_new   the most new tokens of one sequence.  A hint: it selects kernels and sizes the workspace of the attention,
+ *             results do not depend on its being right.
+ * Where a sequence has more new tokens than length, the first of them have no position: qllm_kv_append skips them,
+ * qllm_kv_read writes zeros, and causal attention rows see no key.
+ *
+ * Everything in the batch is read on the device when the kernels run, so a captured graph follows its contents.  Values that
+ * are out of range there (a page outside [0, pages), a length outside [0, table_width page_size], q_start decreasing or
+ * beyond rows) fault nothing: lengths and row ranges are cut to what exists, tokens of a page that does not exist are taken
+ * as absent (not stored, read as zero, not attended to), and the device's status word becomes QLLM_ERR_PAGE
+ * (qllm_poll_status).
+ *
+ * Packed tensors are [rows][heads][head_dim] with head_dim contiguous and head_dim elements from head to head; *_stride is the
+ * distance between rows in elements (at least heads * head_dim, QLLM_ERR_SHAPE), so the three parts of a fused QKV
+ * projection's rows can be passed as they lie.  Their addresses and row strides are multiples of 16 bytes (QLLM_ERR_ALIGN).
+ */
+typedef struct qllm_kv_cache {
+    uint8_t* k_codes;
+    float*   k_param;
+    uint8_t* v_codes;
+    float*   v_param;
+    int layers, pages, kv_heads, page_size, head_dim;
+} qllm_kv_cache_t;
+
+typedef struct qllm_kv_batch {
+    const int32_t* table;
+    const int32_t* seq_lens;
+    const int32_t* q_start;
+    int     seqs, table_width;
+    int64_t rows;
+    int     max_new;
+} qllm_kv_batch_t;
+
+/* Quantizes the new tokens' keys and values and stores them at their positions.  A row is quantized as by
+ * qllm_quantize_rows(bits = 4) on its head_dim channels, x / alpha taken as the exact product of x with the float32 reciprocal
+ * of alpha and rounded once (as that call's one-pass kernels do; its kernel for other channel counts rounds the product to
+ * float32 first, which can differ where a quotient lies within a float32 rounding of a tie).  k, v: device, QLLM_F32 or
+ * QLLM_BF16 (dtype).  A row holding an infinity has no finite scale and reads back as infinities and NaN.  Pages that receive
+ * tokens must belong to one position of one sequence. */
+int qllm_kv_append(const qllm_kv_cache_t* cache, int layer, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                   int dtype, const qllm_kv_batch_t* batch, void* stream);
+
+/* The inverse: the stored values alpha (code - zero) of the batch's tokens as packed rows (rounded to nearest even for
+ * QLLM_BF16).  With q_start counting every token of a sequence it reads the whole sequence back. */
+int qllm_kv_read(const qllm_kv_cache_t* cache, int layer, void* k, int64_t k_stride, void* v, int64_t v_stride, int dtype,
+                 const qllm_kv_batch_t* batch, void* stream);
+
+/* Attention of the new tokens over their sequence's cache (the new tokens' own keys included, so append first):
+ *
+ *   s_j = scale * q . k_j,   out = sum_j exp(s_j - max s) v_j / sum_j exp(s_j - max s),   lse = log sum_j exp(s_j)
+ *
+ * over the positions j < length for causal = 0, and j <= the token's own position for causal = 1.  Query head h reads
+ * key/value head h / (q_heads / kv_heads); q_heads is a multiple of kv_heads (QLLM_ERR_SHAPE).  A token that sees no key gets
+ * zeros and lse = -infinity.
+ *  q, out     device, QLLM_F32 or QLLM_BF16 (dtype, the same for both), packed rows of q_heads heads
+ *  lse        device float [rows][q_heads] or NULL (natural logarithm): what parts of a context that were attended to
+ *             separately are joined with
+ *  workspace  device, 16-byte aligned, qllm_kv_attention_workspace(...) bytes for the same arguments (QLLM_ERR_SHAPE when
+ *             smaller), written before it is read: calls that may run at the same time need one each
+ *  scale      finite (QLLM_ERR_SHAPE)
+ * The workspace size depends on the device, the cache's shape, q_heads, dtype and the batch's seqs, rows and max_new; it is
+ * negative (a status) for arguments that the call itself would refuse. */
+int64_t qllm_kv_attention_workspace(const qllm_kv_cache_t* cache, int q_heads, int dtype, const qllm_kv_batch_t* batch);
+int qllm_kv_attention(const qllm_kv_cache_t* cache, int layer, const void* q, int64_t q_stride, void* out, int64_t out_stride,
+                      int dtype, int q_heads, float scale, int causal, float* lse, const qllm_kv_batch_t* batch,
+                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/* THE POOL says who uses which page, for all layers at once (a page id stands for that page in every layer):
+ *   refs      device int32 [pages]: how many table entries name the page; 0 = free
+ *   table     device int32 [seqs][table_width]; entries beyond a sequence's pages are -1
+ *   seq_lens  device int32 [seqs]; 0 = the sequence is unused
+ * pool->pages equals cache->pages (QLLM_ERR_SHAPE).  A program starts from refs = 0, table = -1, seq_lens = 0.  Pages are taken lowest free index first, in list order, so results
+ * do not depend on timing.  seqs <= 8192 and lists of at most 8192 entries (QLLM_ERR_UNSUPPORTED).  The calls change the pool
+ * on the device; an entry that cannot be served (an index out of range, too few free pages, no room in the table) changes
+ * nothing, the others are served, and the status word becomes QLLM_ERR_PAGE.  Calls on one pool must be ordered (one stream). */
+typedef struct qllm_kv_pool {
+    int32_t* refs;
+    int32_t* table;
+    int32_t* seq_lens;
+    int pages, seqs, table_width;
+} qllm_kv_pool_t;
+
+/* seq_lens[s] += add[s] (device int32 [seqs], >= 0), with the pages that takes.  Whether sequence s is served goes by the pages
+ * that it and all sequences in front of it ask for. */
+int qllm_kv_pages_extend(const qllm_kv_cache_t* cache, const qllm_kv_pool_t* pool, const int32_t* add, void* stream);
+/* child[i] becomes a copy of parent[i] (device int32 [n]): full pages are shared, a partly filled last page is copied into a
+ * free one in all layers, so both can be appended to.  A child must be unused (length 0) and is served once; a parent may
+ * occur any number of times, but not as a child of the same list.  fresh (device int32 [n]) receives the page that was copied
+ * into, -1 where none was needed, -2 where the entry was not served. */
+int qllm_kv_pages_fork(const qllm_kv_cache_t* cache, const qllm_kv_pool_t* pool, const int32_t* parent, const int32_t* child,
+                       int n, int32_t* fresh, void* stream);
+/* The sequences seqs[i] (device int32 [n]) end: their pages lose a reference, their table rows become -1, their length 0.  A
+ * sequence listed twice ends once. */
+int qllm_kv_pages_free(const qllm_kv_pool_t* pool, const int32_t* seqs, int n, void* stream);
+/* Moves the used pages into the lowest indices (a page moves only when it lies behind the last of them; the k-th such page
+ * goes to the k-th hole), in all layers, and renames them in refs and table.  remap (device int32 [pages]) receives each used
+ * page's new index, -1 for free ones. */
+int qllm_kv_pages_compact(const qllm_kv_cache_t* cache, const qllm_kv_pool_t* pool, int32_t* remap, void* stream);
+/* Copies page src[i] to page dst[i] (device int32 [n]) in all layers.  The pages in dst must be different from one another and
+ * from all those in src.  Touches no pool. */
+int qllm_kv_pages_copy(const qllm_kv_cache_t* cache, const int32_t* src, const int32_t* dst, int n, void* stream);
+
+/* ==========================================================================
+ * 7. Diagnostics
  * ========================================================================== */
 const char* qllm_status_string(int status);
 /* Last cudaError_t seen by this library on the calling thread (0 = none). */
 int qllm_last_cuda_error(void);
 /* Reads (and clears) the device-side status word of the current device: QLLM_OK, or
- * QLLM_ERR_TIMEOUT if a bounded wait inside a kernel expired since the last poll.
+ * QLLM_ERR_TIMEOUT if a bounded wait inside a kernel expired since the last poll, or
+ * QLLM_ERR_PAGE if only an index of the key/value cache was out of range.
  * Synchronizes the device. */
 int qllm_poll_status(void);
 /* Exercises the expiry path of the bounded device-side waits (every mbarrier wait of the tensor-core GEMM

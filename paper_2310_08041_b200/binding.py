@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libqllm_b200.so")
 QLLM_OK = 0
 QLLM_ERR_NULL, QLLM_ERR_SHAPE, QLLM_ERR_BITS, QLLM_ERR_DTYPE = -1, -2, -3, -4
 QLLM_ERR_MAP, QLLM_ERR_INFEASIBLE, QLLM_ERR_CUDA, QLLM_ERR_TIMEOUT = -5, -6, -7, -8
-QLLM_ERR_ALIGN, QLLM_ERR_UNSUPPORTED, QLLM_ERR_NOMEM = -9, -10, -11
+QLLM_ERR_ALIGN, QLLM_ERR_UNSUPPORTED, QLLM_ERR_NOMEM, QLLM_ERR_PAGE = -9, -10, -11, -12
 QLLM_F32, QLLM_BF16 = 0, 1
 
 # every symbol include/qllm.h declares
@@ -31,6 +31,8 @@ EXPORTS = [
     "qllm_layer_create", "qllm_layer_destroy", "qllm_layer_forward", "qllm_layer_forward_host",
     "qllm_layer_reassemble_quant", "qllm_layer_qgemm",
     "qllm_layer_workspace", "qllm_layer_keep_byte_weights",
+    "qllm_kv_append", "qllm_kv_read", "qllm_kv_attention", "qllm_kv_attention_workspace",
+    "qllm_kv_pages_extend", "qllm_kv_pages_fork", "qllm_kv_pages_free", "qllm_kv_pages_compact", "qllm_kv_pages_copy",
     "qllm_status_string", "qllm_last_cuda_error", "qllm_poll_status", "qllm_launch_count", "qllm_debug_wait_expiry",
 ]
 
@@ -79,6 +81,16 @@ _lib.qllm_status_string.argtypes = [_i]
 _lib.qllm_status_string.restype = ctypes.c_char_p
 _lib.qllm_launch_count.restype = _i64
 _lib.qllm_debug_wait_expiry.argtypes = [_vp, _vp]
+_lib.qllm_kv_append.argtypes = [_vp, _i, _vp, _i64, _vp, _i64, _i, _vp, _vp]
+_lib.qllm_kv_read.argtypes = [_vp, _i, _vp, _i64, _vp, _i64, _i, _vp, _vp]
+_lib.qllm_kv_attention.argtypes = [_vp, _i, _vp, _i64, _vp, _i64, _i, _i, _f, _i, _vp, _vp, _vp, _i64, _vp]
+_lib.qllm_kv_attention_workspace.argtypes = [_vp, _i, _i, _vp]
+_lib.qllm_kv_attention_workspace.restype = _i64
+_lib.qllm_kv_pages_extend.argtypes = [_vp, _vp, _vp, _vp]
+_lib.qllm_kv_pages_fork.argtypes = [_vp, _vp, _vp, _vp, _i, _vp, _vp]
+_lib.qllm_kv_pages_free.argtypes = [_vp, _vp, _i, _vp]
+_lib.qllm_kv_pages_compact.argtypes = [_vp, _vp, _vp, _vp]
+_lib.qllm_kv_pages_copy.argtypes = [_vp, _vp, _vp, _i, _vp]
 
 
 class QllmError(RuntimeError):
@@ -375,3 +387,166 @@ class Layer:
         _check(_lib.qllm_layer_workspace(self._h, ctypes.byref(c), ctypes.byref(s), ctypes.byref(z), ctypes.byref(r),
                                          ctypes.byref(lanes)))
         return c.value, s.value, z.value, r.value, lanes.value
+
+
+# --------------------------------------------------------------------------- key/value cache in 4 bits
+class _KvCacheStruct(ctypes.Structure):
+    _fields_ = [("k_codes", _vp), ("k_param", _vp), ("v_codes", _vp), ("v_param", _vp),
+                ("layers", _i), ("pages", _i), ("kv_heads", _i), ("page_size", _i), ("head_dim", _i)]
+
+
+class _KvBatchStruct(ctypes.Structure):
+    _fields_ = [("table", _vp), ("seq_lens", _vp), ("q_start", _vp), ("seqs", _i), ("table_width", _i), ("rows", _i64), ("max_new", _i)]
+
+
+class _KvPoolStruct(ctypes.Structure):
+    _fields_ = [("refs", _vp), ("table", _vp), ("seq_lens", _vp), ("pages", _i), ("seqs", _i), ("table_width", _i)]
+
+
+def _want(cond):
+    if not cond:
+        raise QllmError(QLLM_ERR_SHAPE)
+
+
+def _ints(*ts):
+    for t in ts:
+        if t.dtype != torch.int32:
+            raise QllmError(QLLM_ERR_DTYPE)
+        _dp(t)
+
+
+class KvCache:
+    """qllm_kv_cache_t over four tensors, which it keeps: codes uint8 [layers][pages][kv_heads][page_size][head_dim / 2], parameters
+    float32 [layers][pages][kv_heads][page_size][2].  KvCache.empty makes them."""
+
+    def __init__(self, k_codes, k_param, v_codes, v_param):
+        if not (k_codes.dtype == v_codes.dtype == torch.uint8 and k_param.dtype == v_param.dtype == torch.float32):
+            raise QllmError(QLLM_ERR_DTYPE)
+        _want(k_codes.dim() == 5 and k_codes.shape == v_codes.shape)
+        layers, pages, heads, page, half = k_codes.shape
+        _want(tuple(k_param.shape) == tuple(v_param.shape) == (layers, pages, heads, page, 2))
+        self.k_codes, self.k_param, self.v_codes, self.v_param = k_codes, k_param, v_codes, v_param
+        self.layers, self.pages, self.kv_heads, self.page_size, self.head_dim = layers, pages, heads, page, 2 * half
+        self._s = _KvCacheStruct(_dp(k_codes), _dp(k_param), _dp(v_codes), _dp(v_param), layers, pages, heads, page, 2 * half)
+        self._p = ctypes.addressof(self._s)
+
+    @classmethod
+    def empty(cls, layers, pages, kv_heads, page_size, head_dim, device="cuda"):
+        shape = (layers, pages, kv_heads, page_size)
+        make = lambda last, t: torch.zeros(*shape, last, dtype=t, device=device)  # noqa: E731
+        return cls(make(head_dim // 2, torch.uint8), make(2, torch.float32), make(head_dim // 2, torch.uint8), make(2, torch.float32))
+
+
+class KvBatch:
+    """qllm_kv_batch_t: table int32 [seqs][table_width], seq_lens int32 [seqs], q_start int32 [seqs + 1] (device tensors, kept;
+    their contents may change between calls), rows of the packed tensors, most new tokens of a sequence."""
+
+    def __init__(self, table, seq_lens, q_start, rows, max_new):
+        _ints(table, seq_lens, q_start)
+        _want(table.dim() == 2 and seq_lens.numel() == table.shape[0] and q_start.numel() == table.shape[0] + 1)
+        self.table, self.seq_lens, self.q_start, self.rows, self.max_new = table, seq_lens, q_start, rows, max_new
+        self._s = _KvBatchStruct(_dp(table), _dp(seq_lens), _dp(q_start), table.shape[0], table.shape[1], rows, max_new)
+        self._p = ctypes.addressof(self._s)
+
+
+class KvPool:
+    """qllm_kv_pool_t: refs int32 [pages], table int32 [seqs][table_width], seq_lens int32 [seqs] (device tensors, kept)."""
+
+    def __init__(self, refs, table, seq_lens):
+        _ints(refs, table, seq_lens)
+        _want(table.dim() == 2 and seq_lens.numel() == table.shape[0])
+        self.refs, self.table, self.seq_lens = refs, table, seq_lens
+        self._s = _KvPoolStruct(_dp(refs), _dp(table), _dp(seq_lens), refs.numel(), table.shape[0], table.shape[1])
+        self._p = ctypes.addressof(self._s)
+
+    @classmethod
+    def empty(cls, pages, seqs, table_width, device="cuda"):
+        return cls(torch.zeros(pages, dtype=torch.int32, device=device),
+                   torch.full((seqs, table_width), -1, dtype=torch.int32, device=device),
+                   torch.zeros(seqs, dtype=torch.int32, device=device))
+
+
+def _packed(t, rows, heads, head_dim):
+    """Address and row stride of a packed tensor [rows][heads][head_dim]: any row stride, the rest contiguous."""
+    assert t.is_cuda, "device arguments must be CUDA tensors"
+    _want(tuple(t.shape) == (rows, heads, head_dim))
+    st = t.stride()
+    _want(st[2] == 1 and (st[1] == head_dim or heads == 1))
+    return t.data_ptr(), st[0] if rows > 1 else max(st[0], heads * head_dim)
+
+
+def qllm_kv_append(cache, layer, k, v, batch, stream=None):
+    """k, v [rows][kv_heads][head_dim] (any row stride): the batch's new tokens, quantized into the cache."""
+    kp, ks = _packed(k, batch.rows, cache.kv_heads, cache.head_dim)
+    vp, vs = _packed(v, batch.rows, cache.kv_heads, cache.head_dim)
+    _want(k.dtype == v.dtype)
+    _check(_lib.qllm_kv_append(cache._p, layer, kp, ks, vp, vs, _xdtype(k), batch._p, _stream(stream)))
+
+
+def qllm_kv_read(cache, layer, k, v, batch, stream=None):
+    """The stored values of the batch's tokens into k, v [rows][kv_heads][head_dim]."""
+    kp, ks = _packed(k, batch.rows, cache.kv_heads, cache.head_dim)
+    vp, vs = _packed(v, batch.rows, cache.kv_heads, cache.head_dim)
+    _want(k.dtype == v.dtype)
+    _check(_lib.qllm_kv_read(cache._p, layer, kp, ks, vp, vs, _xdtype(k), batch._p, _stream(stream)))
+
+
+def qllm_kv_attention_workspace(cache, q_heads, q, batch):
+    """Bytes of workspace for qllm_kv_attention with these arguments (of q only the dtype counts)."""
+    n = _lib.qllm_kv_attention_workspace(cache._p, q_heads, _xdtype(q), batch._p)
+    _check(min(n, 0))
+    return n
+
+
+def qllm_kv_attention(cache, layer, q, out, scale, batch, workspace, causal=True, lse=None, stream=None):
+    """q, out [rows][q_heads][head_dim] (any row stride); workspace: uint8 tensor of qllm_kv_attention_workspace bytes; lse: None
+    or float32 [rows][q_heads]."""
+    heads = q.shape[1] if q.dim() == 3 else 0
+    qp, qs = _packed(q, batch.rows, heads, cache.head_dim)
+    op, os_ = _packed(out, batch.rows, heads, cache.head_dim)
+    _want(q.dtype == out.dtype)
+    if lse is not None:
+        _want(lse.dtype == torch.float32 and tuple(lse.shape) == (batch.rows, heads))
+    _check(_lib.qllm_kv_attention(cache._p, layer, qp, qs, op, os_, _xdtype(q), heads, scale, 1 if causal else 0, _dp(lse),
+                                  batch._p, _dp(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                  _stream(stream)))
+
+
+def qllm_kv_pages_extend(cache, pool, add, stream=None):
+    """add: int32 [seqs], tokens to make room for."""
+    _ints(add)
+    _want(add.numel() == pool.seq_lens.numel())
+    _check(_lib.qllm_kv_pages_extend(cache._p, pool._p, _dp(add), _stream(stream)))
+
+
+def qllm_kv_pages_fork(cache, pool, parent, child, fresh=None, stream=None):
+    """parent, child: int32 [n].  Returns fresh, int32 [n] (made here when not given, which goes with the current stream only)."""
+    _ints(parent, child)
+    _want(parent.numel() == child.numel())
+    if fresh is None:
+        _want(stream is None)
+        fresh = torch.empty_like(parent)
+    _ints(fresh)
+    _want(fresh.numel() == parent.numel())
+    _check(_lib.qllm_kv_pages_fork(cache._p, pool._p, _dp(parent), _dp(child), parent.numel(), _dp(fresh), _stream(stream)))
+    return fresh
+
+
+def qllm_kv_pages_free(pool, seqs, stream=None):
+    """seqs: int32 [n], the sequences that have ended."""
+    _ints(seqs)
+    _check(_lib.qllm_kv_pages_free(pool._p, _dp(seqs), seqs.numel(), _stream(stream)))
+
+
+def qllm_kv_pages_compact(cache, pool, remap, stream=None):
+    """remap: int32 [pages], receives every page's new index (-1: free)."""
+    _ints(remap)
+    _want(remap.numel() == pool.refs.numel())
+    _check(_lib.qllm_kv_pages_compact(cache._p, pool._p, _dp(remap), _stream(stream)))
+
+
+def qllm_kv_pages_copy(cache, src, dst, stream=None):
+    """src, dst: int32 [n]."""
+    _ints(src, dst)
+    _want(src.numel() == dst.numel())
+    _check(_lib.qllm_kv_pages_copy(cache._p, _dp(src), _dp(dst), src.numel(), _stream(stream)))

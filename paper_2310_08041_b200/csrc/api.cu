@@ -600,6 +600,7 @@ const char* qllm_status_string(int s) {
         case QLLM_ERR_ALIGN: return "device tensor not 16-byte aligned";
         case QLLM_ERR_UNSUPPORTED: return "size beyond a documented limit";
         case QLLM_ERR_NOMEM: return "out of memory";
+        case QLLM_ERR_PAGE: return "a page, length or index of the key/value cache is out of range";
         default: return "unknown status";
     }
 }
@@ -613,7 +614,7 @@ int qllm_poll_status(void) {
     if (v != 0) {
         const int zero = 0;
         QLLM_CUDA_TRY(cudaMemcpyToSymbol(g_status_word, &zero, sizeof(int)));
-        return QLLM_ERR_TIMEOUT;
+        return v == QLLM_ERR_PAGE ? QLLM_ERR_PAGE : QLLM_ERR_TIMEOUT;
     }
     return QLLM_OK;
 }
