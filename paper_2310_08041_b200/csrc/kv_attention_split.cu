@@ -1,0 +1,704 @@
+// Attention over the 4-bit cache for few query rows per key head: decode steps, drafted tokens, odd shapes.
+//
+// s_j = scale q . k_j, k_j = ks_j (ck_j - kz_j), so s_j = ks_j (scale q . ck_j - kz_j scale sum q): the keys enter the
+// tensor cores as bare codes, scale and zero-point act on finished sums.  Likewise sum_j p_j v_j = sum_j (p_j vs_j) cv_j -
+// sum_j (p_j vs_j) vz_j.  HBM bounds it: a token's keys and values are D + 16 bytes a head, read once per 8 NT query rows.
+//
+// Work split: an item is (sequence, key head, tile of 8 NT query rows); its keys are tiles of T tokens.  All items' tiles form
+// one line, which the CTAs of one resident wave cut into equal shares, each working out its own from the lengths on the
+// device: a batch of any lengths keeps every SM busy, and a captured graph follows them.  An item that lies in several shares
+// leaves one piece per share (sum, running maximum, weights) in the workspace, which a second kernel joins; at most two pieces
+// per CTA.  No CTA waits for another, and the order of all additions is fixed by the shapes and lengths.
+//
+// In a CTA: one warp fetches a tile's codes and parameters with bulk copies, one per page and array, several tiles ahead; four
+// warps own 32 of its tokens each, with a softmax state of their own that meets at the item's end.  Both products run
+// transposed (S^T = K Q^T, O^T = V^T P^T) so that 16 tokens or channels fill the 16 rows of the warp-level MMA and the 8
+// query rows its 8 columns: a decode step's few rows waste nothing.  A nibble masked in place is a denormal fp16 number
+// (c 2^-24, or c 2^-20 from the upper half of a byte), which the MMA takes exactly: five logical instructions turn 8 key codes
+// into operands.  Channel and token order inside an operand is free as long as both sides agree, so the codes of one 16-byte
+// read are used where they lie, and the factor 16 of the upper nibbles is taken out of the queries, or of the output's odd
+// channels at the end.
+//
+// Precision: queries are scaled by a power of two per row into fp16's range (a bf16 query's 8 bits stay exact) and float32
+// queries are split in two; weights p_j vs_j are rounded to fp16, 11 bits, for bf16 results (which carry 8) and split in two
+// for float32 ones.  So that no weight leaves fp16's range whatever the value scales are, the running maximum is that of
+// s_j + log2 vs_j (exponent of vs_j only, cut to +-80), 14 below which the largest weight is placed.  Sums, maxima and
+// zero-point corrections are float32, the latter with the rounded weight, so that the two parts of a value cancel as they should.
+
+#include <cuda_fp16.h>
+
+#include "kv_attention.h"
+#include "ptx_sm100.cuh"
+#include "qgemm_tc_common.cuh"
+
+namespace qllm {
+namespace {
+
+using namespace kv;
+using tc::Abort;
+using tc::wait_bounded;
+
+constexpr int T = 128;                                     // tokens of a tile
+constexpr int kWarps = 4;                                  // consumer warps, 32 tokens each
+constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kCombineThreads = 128;
+
+template <int D, int NT, bool F32>
+struct Shape {
+    static constexpr int R = 8 * NT;                       // query rows of an item
+    static constexpr int KW = D / 32, VW = D / 64, MT = D / 16;
+    static constexpr int STAGE = T * (D + 16);
+    static constexpr int STAGES = D == 256 ? 2 : 3;
+    static constexpr int OROW = D + 4;                     // floats of a merged row (padded)
+    static constexpr int MERGE = kWarps * R * (OROW + 4) * 4;
+    static constexpr int SMEM = STAGES * STAGE + MERGE + 256;
+    static constexpr int CTAS = SMEM <= 75 * 1024 && NT * D * (F32 ? 3 : 2) <= 256 ? 3 : 2;
+};
+
+// ---- the line of tiles ---------------------------------------------------------------------------------------------------
+struct Plan {
+    Batch b;
+    int heads, group, rows, most_rows;                     // key heads, query heads per key head, rows of an item
+    __device__ __forceinline__ int64_t qrows(int n) const { return int64_t(n) * group; }
+    __device__ __forceinline__ int qtiles(int n) const { return int((qrows(n) + rows - 1) / rows); }
+    __device__ __forceinline__ int ktiles(int len) const { return len <= T ? 1 : int((int64_t(len) + T - 1) / T); }
+    __device__ __forceinline__ int64_t work(int s) const {
+        const int n = b.count(s);
+        return n == 0 || qrows(n) > most_rows ? 0 : int64_t(heads) * qtiles(n) * ktiles(b.len(s));
+    }
+};
+
+// Called by a whole CTA of NTHREADS threads: total work, and (in every thread) the first sequence whose range of the line
+// ends behind `x`, with the work in front of it.  want >= 0: that sequence instead.
+template <int NTHREADS, typename XFn>
+__device__ __forceinline__ int64_t locate(const Plan& p, int64_t* s_mem, XFn x_of_total, int want, int& seq, int64_t& before) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (p.b.seqs + NTHREADS - 1) / NTHREADS, first = min(tid * per, p.b.seqs), last = min(first + per, p.b.seqs);
+    int64_t mine = 0;
+    for (int s = first; s < last; ++s) mine += p.work(s);
+    int64_t incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    if (lane == 31) s_mem[warp] = incl;
+    __syncthreads();
+    int64_t base = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < NTHREADS / 32; ++w) {
+        if (w < warp) base += s_mem[w];
+        total += s_mem[w];
+    }
+    const int64_t pre = base + incl - mine, x = x_of_total(total);
+    if (want >= 0 ? (want >= first && want < last) : (x >= pre && x < pre + mine)) {
+        int64_t at = pre;
+        int s = first;
+        for (; s < last; ++s) {
+            const int64_t w = p.work(s);
+            if (want >= 0 ? s == want : x < at + w) break;
+            at += w;
+        }
+        s_mem[NTHREADS / 32] = s;
+        s_mem[NTHREADS / 32 + 1] = at;
+    }
+    __syncthreads();
+    seq = int(s_mem[NTHREADS / 32]);
+    before = s_mem[NTHREADS / 32 + 1];
+    return total;
+}
+
+__device__ __forceinline__ int64_t share_begin(int64_t c, int64_t total, int ctas) { return c * total / ctas; }
+
+// The part of an item that lies in a share.
+struct Part {
+    int s, g, qt, n, len, tile, tiles, count;              // sequence .., first tile, tiles of the item, tiles of the part
+    int64_t row0;                                          // first packed row of the sequence
+    int keys;                                              // keys that the item's last row sees
+};
+// Walks the parts of [x, end).  Every role of the CTA walks for itself.
+struct Walk {
+    const Plan& p;
+    int64_t x, end, before;
+    int s;
+    bool causal;
+    __device__ __forceinline__ bool next(Part& o) {
+        if (x >= end) return false;
+        int64_t w;
+        while ((w = p.work(s)) <= x - before) { before += w; ++s; }      // x < total: a sequence with work follows
+        o.s = s;
+        o.n = p.b.count(s);
+        o.len = p.b.len(s);
+        o.row0 = p.b.row(s);
+        o.tiles = p.ktiles(o.len);
+        const int64_t at = x - before, item = at / o.tiles;
+        const int qts = p.qtiles(o.n);
+        o.g = int(item / qts);
+        o.qt = int(item - int64_t(o.g) * qts);
+        o.tile = int(at - item * o.tiles);
+        o.count = int(min(int64_t(o.tiles - o.tile), end - x));
+        const int64_t last = min(int64_t(o.qt + 1) * p.rows, p.qrows(o.n)) - 1;
+        const int64_t own = int64_t(o.len) - o.n + last / p.group + 1;
+        o.keys = !causal ? o.len : own < 0 ? 0 : int(own);
+        x += o.count;
+        return true;
+    }
+};
+
+// ---- warp-level pieces ---------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+__device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }     // -126 <= e <= 127
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ptx::smem_addr(dst)),
+                 "l"(src), "r"(bytes), "r"(ptx::smem_addr(bar))
+                 : "memory");
+}
+// Row r of an 8-token block of the MMA holds token order(r) of it: neighbours differ in parity and the even rows' tokens do
+// too, which spreads the key reads (rows 2i, 2i + 1 in a phase) and the value reads (rows 0, 2, 4, 6) over the banks.
+__device__ __forceinline__ int order(int r) { return r ^ ((r >> 1) & 1); }
+
+// The query rows of a column group: 8 channels of column `r` at a time as B operands.  Returns the row's power of two.
+template <typename QT, int D, bool F32>
+__device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi)[D / 8], uint32_t (&lo)[F32 ? D / 8 : 1], float& unit, float& sum) {
+    constexpr int N = D / 4;                               // channels of this lane: N t .. N t + N - 1
+    float top = 0.f;
+    sum = 0.f;
+    if (row) {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) {
+            float f[8];
+            load8<QT>(row + t * N + 8 * i, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { top = fmaxf(top, fabsf(f[j])); sum += f[j]; }
+        }
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    const int e = max(int(__float_as_uint(top) >> 23) - 127, -100);      // 2^e <= top < 2^(e+1); infinities: 128
+    const float up = pow2i(min(13 - e, 126));
+    unit = e > 115 ? INFINITY : pow2i(e + 11);             // 2^24 / 2^(13 - e)
+#pragma unroll
+    for (int i = 0; i < N / 8; ++i) {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = 0.f;
+        if (row) load8<QT>(row + t * N + 8 * i, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] *= (j & 1) ? up * 0.0625f : up;
+        // word 8i of the codes gives the pairs (0, 4), (1, 5) x 16, (2, 6), (3, 7) x 16
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t h = pack2(f[j], f[j + 4]);
+            hi[4 * i + j] = h;
+            if (F32) {
+                const float2 b = unpack2(h);
+                lo[4 * i + j] = pack2(f[j] - b.x, f[j + 4] - b.y);
+            }
+        }
+    }
+}
+
+template <int W>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
+    if constexpr (W == 1) {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (W == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < W / 4; ++i) {
+            const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
+    }
+}
+
+template <typename QT, int D, int NT>
+__global__ void __launch_bounds__(kThreads, Shape<D, NT, sizeof(QT) == 4>::CTAS)
+kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT* __restrict__ out, int64_t out_stride, float scale,
+                int causal, float* __restrict__ lse, float* __restrict__ part_o, float2* __restrict__ part_ml, int* status) {
+    constexpr bool F32 = sizeof(QT) == 4;
+    using S = Shape<D, NT, F32>;
+    constexpr int R = S::R, HALF = T * (D / 2);
+    extern __shared__ __align__(128) uint8_t smem[];
+    uint8_t* merge = smem + S::STAGES * S::STAGE;
+    __shared__ uint64_t s_full[S::STAGES], s_empty[S::STAGES];
+    __shared__ uint32_t s_pieces[S::STAGES];
+    __shared__ int64_t s_plan[kThreads / 32 + 2];
+    __shared__ int s_abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::STAGES; ++i) {
+            ptx::mbar_init(&s_full[i], 1);
+            ptx::mbar_init(&s_empty[i], kWarps);
+        }
+        s_abort = 0;
+        ptx::fence_barrier_init();
+        ptx::fence_proxy_async_smem();
+    }
+    if (blockIdx.x == 0) p.b.report(status);
+    int seq;
+    int64_t before, begin = 0;
+    const int64_t total = locate<kThreads>(p, s_plan, [&](int64_t tot) { return begin = share_begin(blockIdx.x, tot, gridDim.x); }, -1, seq, before);
+    const int64_t end = share_begin(blockIdx.x + 1, total, gridDim.x);
+    if (begin >= end) return;
+    const Abort ab{&s_abort, status};
+    Walk walk{p, begin, end, before, seq, causal != 0};
+    Part it;
+    uint32_t k = 0;                                        // tiles passed so far
+    const int log2p = p.b.page_log2, piece_log2 = log2p < 7 ? log2p : 7;
+
+    if (warp == kWarps) {
+        // ---------------------------------------------------------------- producer: lane = 4 * piece + array
+        const int piece = lane >> 2, array = lane & 3, piece_tokens = 1 << piece_log2;
+        bool ok = true;
+        while (ok && walk.next(it)) {
+            const int32_t* row = p.b.table + int64_t(it.s) * p.b.width;
+            for (int j = it.tile; j < it.tile + it.count; ++j) {
+                const int t0 = j * T + (piece << piece_log2);
+                if (j * T >= it.keys) break;               // nothing there that a row of this item sees
+                const bool mine = (piece << piece_log2) < T && t0 < it.keys;
+                const int page = mine ? row[t0 >> log2p] : 0;
+                const bool good = mine && page >= 0 && page < c.pages;
+                if (mine && !good) raise_page(status);
+                const uint32_t bytes = uint32_t(piece_tokens) * ((array & 1) ? 8 : D / 2);
+                const uint32_t got = __ballot_sync(0xffffffffu, good), total_bytes = __reduce_add_sync(0xffffffffu, good ? bytes : 0);
+                const int st = k % S::STAGES;
+                if (!wait_bounded(&s_empty[st], ((k / S::STAGES) & 1) ^ 1, ab)) { ok = false; break; }
+                if (lane == 0) {
+                    s_pieces[st] = got;
+                    ptx::mbar_arrive_expect_tx(&s_full[st], total_bytes);
+                }
+                __syncwarp();
+                if (good) {
+                    const int64_t r = c.row(page, it.g, t0 & ((1 << log2p) - 1));
+                    uint8_t* base = smem + st * S::STAGE;
+                    const int place = piece << piece_log2;
+                    if (array == 0) bulk_load(base + place * (D / 2), c.kc + r * (D / 2), bytes, &s_full[st]);
+                    else if (array == 2) bulk_load(base + HALF + place * (D / 2), c.vc + r * (D / 2), bytes, &s_full[st]);
+                    else if (array == 1) bulk_load(base + 2 * HALF + place * 8, c.kp + r, bytes, &s_full[st]);
+                    else bulk_load(base + 2 * HALF + T * 8 + place * 8, c.vp + r, bytes, &s_full[st]);
+                }
+                ++k;
+            }
+        }
+        if (!ok) {                                         // give copies still in flight a bounded chance to land
+            for (uint32_t j = 0; j < S::STAGES && j < k; ++j) {
+                const uint32_t i = k - 1 - j;
+                const long long t0 = clock64();
+                while (!ptx::mbar_try_wait(&s_full[i % S::STAGES], (i / S::STAGES) & 1) && clock64() - t0 < (1ll << 24)) {}
+            }
+        }
+        return;
+    }
+
+    // -------------------------------------------------------------------- consumers
+    const int r = lane >> 2, t = lane & 3, rt = order(r);
+    const float to_log2 = scale * 1.4426950408889634f;
+    bool ok = true;                                        // false: a wait ran out; go through the motions without waiting
+    while (walk.next(it)) {
+        uint32_t qh[NT][D / 8], ql[NT][F32 ? D / 8 : 1];
+        float qn[NT][2], qs[NT][2];                        // per column 2t, 2t + 1: factor of the sum of codes, scaled sum of q
+        int limit[NT][2], low = 0x7fffffff;                // keys that the column sees; the fewest of all columns
+#pragma unroll
+        for (int a = 0; a < NT; ++a) {
+            const int64_t rr = int64_t(it.qt) * R + a * 8 + r, i = rr / p.group;
+            const bool real = i < it.n;
+            const QT* row = real ? q + (it.row0 + i) * q_stride + (int64_t(it.g) * p.group + (rr - i * p.group)) * D : nullptr;
+            float unit, sum;
+            load_queries<QT, D, F32>(row, t, qh[a], ql[a], unit, sum);
+            const int64_t own = int64_t(it.len) - it.n + i + 1;
+            const int lim = !real ? 0x7fffffff : !causal ? it.len : own < 0 ? 0 : int(own);
+            low = min(low, lim);
+            unit *= to_log2;
+            sum *= to_log2;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {                  // column 2t + e is lane group 2t + e
+                qn[a][e] = __shfl_sync(0xffffffffu, unit, (2 * t + e) * 4);
+                qs[a][e] = __shfl_sync(0xffffffffu, sum, (2 * t + e) * 4);
+                limit[a][e] = __shfl_sync(0xffffffffu, lim, (2 * t + e) * 4);
+            }
+        }
+        low = __reduce_min_sync(0xffffffffu, low);
+        float o[NT][S::MT][4], top[NT][2], l[NT][2], zs[NT][2];
+#pragma unroll
+        for (int a = 0; a < NT; ++a) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) { top[a][e] = -INFINITY; l[a][e] = 0.f; zs[a][e] = 0.f; }
+#pragma unroll
+            for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[a][m][e] = 0.f;
+        }
+        for (int j = it.tile; j < it.tile + it.count; ++j) {
+            if (j * T >= it.keys) break;
+            const int st = k % S::STAGES;
+            if (ok && !wait_bounded(&s_full[st], (k / S::STAGES) & 1, ab)) ok = false;
+            ++k;
+            if (!ok) continue;
+            const uint8_t* base = smem + st * S::STAGE;
+            const uint8_t* kc = base + (warp * 32) * (D / 2);
+            const uint8_t* vc = base + HALF + (warp * 32) * (D / 2);
+            const float2* kp = reinterpret_cast<const float2*>(base + 2 * HALF) + warp * 32;
+            const float2* vp = kp + T;
+            const int first = j * T + warp * 32;           // token of this warp's row 0
+            // which 8-token blocks of this warp's 32 tokens lie in pages that exist
+            const uint32_t pieces = s_pieces[st];
+            uint32_t there = 0;
+#pragma unroll
+            for (int b8 = 0; b8 < 4; ++b8) there |= ((pieces >> (4 * ((warp * 32 + b8 * 8) >> piece_log2))) & 1u) << b8;
+            if (first < it.keys) {
+                const bool masked = first + 32 > low || first + 32 > it.len || there != 15u;
+                float s[NT][2][4], vs[2][2], vz[2][2];
+                // ---- S^T = K Q^T, 16 tokens at a time
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    uint32_t w0[S::KW], w1[S::KW];
+                    load_words<S::KW>(kc + (b * 16 + rt) * (D / 2) + t * (D / 8), w0);
+                    load_words<S::KW>(kc + (b * 16 + 8 + rt) * (D / 2) + t * (D / 8), w1);
+#pragma unroll
+                    for (int a = 0; a < NT; ++a)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[a][b][e] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < S::KW; ++i) {
+                        const uint32_t u0 = w0[i] >> 8, u1 = w1[i] >> 8;
+                        const uint32_t a0 = w0[i] & 0x000F000Fu, a1 = w1[i] & 0x000F000Fu, a2 = w0[i] & 0x00F000F0u, a3 = w1[i] & 0x00F000F0u;
+                        const uint32_t c0 = u0 & 0x000F000Fu, c1 = u1 & 0x000F000Fu, c2 = u0 & 0x00F000F0u, c3 = u1 & 0x00F000F0u;
+#pragma unroll
+                        for (int a = 0; a < NT; ++a) {
+                            mma_f16(s[a][b], a0, a1, a2, a3, qh[a][4 * i], qh[a][4 * i + 1]);
+                            mma_f16(s[a][b], c0, c1, c2, c3, qh[a][4 * i + 2], qh[a][4 * i + 3]);
+                            if (F32) {
+                                mma_f16(s[a][b], a0, a1, a2, a3, ql[a][4 * i], ql[a][4 * i + 1]);
+                                mma_f16(s[a][b], c0, c1, c2, c3, ql[a][4 * i + 2], ql[a][4 * i + 3]);
+                            }
+                        }
+                    }
+                }
+                // ---- scores, in base 2, of tokens (block b, half h) and columns 2t, 2t + 1
+                float ve[2][2];
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int tok = b * 16 + h * 8 + rt;
+                        const float2 kk = kp[tok], vv = vp[tok];
+                        vs[b][h] = vv.x;
+                        vz[b][h] = vv.y;
+                        ve[b][h] = float(min(max(int((__float_as_uint(vv.x) >> 23) & 255u) - 127, -80), 80) - 14);
+#pragma unroll
+                        for (int a = 0; a < NT; ++a)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                s[a][b][2 * h + e] = kk.x * (s[a][b][2 * h + e] * qn[a][e] - kk.y * qs[a][e]);
+                    }
+                if (masked) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int tok = first + b * 16 + h * 8 + rt;
+                            const bool hole = tok >= it.len || !((there >> (2 * b + h)) & 1u);
+                            if (hole) { vs[b][h] = 0.f; vz[b][h] = 0.f; }
+#pragma unroll
+                            for (int a = 0; a < NT; ++a)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e)
+                                    if (hole || tok >= limit[a][e]) s[a][b][2 * h + e] = -INFINITY;
+                        }
+                }
+                uint32_t ph[NT][4], pl[NT][F32 ? 4 : 1];   // weights as B operands of the second product
+#pragma unroll
+                for (int a = 0; a < NT; ++a) {
+                    float fix[2];
+                    bool moved = false;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float m = fmaxf(fmaxf(s[a][0][e] + ve[0][0], s[a][0][2 + e] + ve[0][1]), fmaxf(s[a][1][e] + ve[1][0], s[a][1][2 + e] + ve[1][1]));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                        m = fmaxf(m, top[a][e]);
+                        const float at = m == -INFINITY ? 0.f : m;
+                        fix[e] = ex2(top[a][e] - at);
+                        moved |= m != top[a][e];
+                        top[a][e] = m;
+                        l[a][e] *= fix[e];
+                        zs[a][e] *= fix[e];
+#pragma unroll
+                        for (int b = 0; b < 2; ++b)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const float pw = ex2(s[a][b][2 * h + e] - at);
+                                l[a][e] += pw;
+                                float w = pw * vs[b][h];
+                                // a hidden key's value parameters may be anything
+                                if (masked && first + b * 16 + h * 8 + rt >= limit[a][e]) w = 0.f;
+                                s[a][b][2 * h + e] = w;
+                            }
+                    }
+                    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                        for (int m = 0; m < S::MT; ++m)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[a][m][e] *= fix[e & 1];
+                    }
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float w0 = s[a][b][2 * h], w1 = s[a][b][2 * h + 1];
+                            const uint32_t hi = pack2(w0, w1);
+                            float2 f = unpack2(hi);
+                            ph[a][2 * b + h] = transpose8(hi);
+                            if (F32) {
+                                const uint32_t lo = pack2(w0 - f.x, w1 - f.y);
+                                const float2 g = unpack2(lo);
+                                pl[a][2 * b + h] = transpose8(lo);
+                                f.x += g.x;
+                                f.y += g.y;
+                            }
+                            if (masked) {
+                                const int tok = first + b * 16 + h * 8 + rt;
+                                zs[a][0] += tok >= limit[a][0] ? 0.f : f.x * vz[b][h];
+                                zs[a][1] += tok >= limit[a][1] ? 0.f : f.y * vz[b][h];
+                            } else {
+                                zs[a][0] = fmaf(f.x, vz[b][h], zs[a][0]);
+                                zs[a][1] = fmaf(f.y, vz[b][h], zs[a][1]);
+                            }
+                        }
+                }
+                // ---- O^T += V^T P^T: this lane's channels are D/8 r .. D/8 r + D/8 - 1
+                const int ka = order(2 * t), kb = order(2 * t + 1);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    uint32_t v[4][S::VW];
+                    load_words<S::VW>(vc + (b * 16 + ka) * (D / 2) + r * (D / 16), v[0]);
+                    load_words<S::VW>(vc + (b * 16 + kb) * (D / 2) + r * (D / 16), v[1]);
+                    load_words<S::VW>(vc + (b * 16 + 8 + ka) * (D / 2) + r * (D / 16), v[2]);
+                    load_words<S::VW>(vc + (b * 16 + 8 + kb) * (D / 2) + r * (D / 16), v[3]);
+#pragma unroll
+                    for (int i = 0; i < S::VW; ++i)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const uint32_t x0 = __byte_perm(v[0][i], v[1][i], y ? 0x7632 : 0x5410);
+                            const uint32_t x1 = __byte_perm(v[2][i], v[3][i], y ? 0x7632 : 0x5410);
+#pragma unroll
+                            for (int z = 0; z < 2; ++z) {
+                                const uint32_t y0 = z ? x0 >> 8 : x0, y1 = z ? x1 >> 8 : x1;
+                                const int m = 4 * i + 2 * y + z;
+#pragma unroll
+                                for (int a = 0; a < NT; ++a) {
+                                    mma_f16(o[a][m], y0 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x000F000Fu, y1 & 0x00F000F0u, ph[a][2 * b], ph[a][2 * b + 1]);
+                                    if (F32) mma_f16(o[a][m], y0 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x000F000Fu, y1 & 0x00F000F0u, pl[a][2 * b], pl[a][2 * b + 1]);
+                                }
+                            }
+                        }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&s_empty[st]);
+        }
+        // ---- the four warps' states meet
+        float* m_top = reinterpret_cast<float*>(merge);    // [warps][R], then [warps][R] sums, [warps][R][OROW] outputs
+        float* m_l = m_top + kWarps * R;
+        float* m_o = m_l + kWarps * R;
+#pragma unroll
+        for (int a = 0; a < NT; ++a)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) {
+                    l[a][e] += __shfl_xor_sync(0xffffffffu, l[a][e], x);
+                    zs[a][e] += __shfl_xor_sync(0xffffffffu, zs[a][e], x);
+                }
+                if (r == 0) {
+                    m_top[warp * R + a * 8 + 2 * t + e] = top[a][e];
+                    m_l[warp * R + a * 8 + 2 * t + e] = l[a][e];
+                }
+                float* row = m_o + (warp * R + a * 8 + 2 * t + e) * S::OROW + r * (D / 8);
+#pragma unroll
+                for (int m = 0; m < S::MT; m += 2)
+                    *reinterpret_cast<float4*>(row + 2 * m) =
+                        make_float4(fmaf(o[a][m][e], 16777216.f, -zs[a][e]), fmaf(o[a][m][2 + e], 1048576.f, -zs[a][e]),
+                                    fmaf(o[a][m + 1][e], 16777216.f, -zs[a][e]), fmaf(o[a][m + 1][2 + e], 1048576.f, -zs[a][e]));
+            }
+        ptx::named_bar_sync(1, 32 * kWarps);
+        const bool whole = it.count == it.tiles;
+        const int64_t slot = 2 * int64_t(blockIdx.x) + (it.tile > 0 ? 0 : 1);
+        constexpr int PER = D / 4;                         // threads of a row: 4 channels each
+        for (int u = threadIdx.x; u < R * PER; u += 32 * kWarps) {
+            const int col = u / PER, d4 = (u % PER) * 4;
+            const int64_t rr = int64_t(it.qt) * R + col, i = rr / p.group;
+            if (i >= it.n) continue;
+            float m = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) m = fmaxf(m, m_top[w * R + col]);
+            const float at = m == -INFINITY ? 0.f : m;
+            float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = ex2(m_top[w * R + col] - at);
+                sum += f * m_l[w * R + col];
+                const float4 x = *reinterpret_cast<const float4*>(m_o + (w * R + col) * S::OROW + d4);
+                v[0] += f * x.x; v[1] += f * x.y; v[2] += f * x.z; v[3] += f * x.w;
+            }
+            if (whole) {
+                const int64_t row = it.row0 + i;
+                const int head = it.g * p.group + int(rr - i * p.group);
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                QT* dst = out + row * out_stride + int64_t(head) * D + d4;
+                if constexpr (F32) {
+                    *reinterpret_cast<float4*>(dst) = make_float4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+                } else {
+                    const __nv_bfloat162 x = __floats2bfloat162_rn(v[0] * inv, v[1] * inv), y = __floats2bfloat162_rn(v[2] * inv, v[3] * inv);
+                    *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+                }
+                if (lse && d4 == 0) lse[row * (int64_t(c.heads) * p.group) + head] = sum == 0.f ? -INFINITY : (at + log2f(sum)) * 0.6931471805599453f;
+            } else {
+                *reinterpret_cast<float4*>(part_o + (slot * R + col) * D + d4) = make_float4(v[0], v[1], v[2], v[3]);
+                if (d4 == 0) part_ml[slot * R + col] = make_float2(m, sum);
+            }
+        }
+        ptx::named_bar_sync(1, 32 * kWarps);               // the merge area is free again
+    }
+}
+
+// Joins the pieces of an item that lay in several shares: a CTA per (packed row, query head), its warps take every fourth piece.
+template <typename QT, int D>
+__global__ void __launch_bounds__(kCombineThreads)
+kv_combine_kernel(Plan p, int ctas, QT* __restrict__ out, int64_t out_stride, float* __restrict__ lse, const float* __restrict__ part_o,
+                  const float2* __restrict__ part_ml) {
+    constexpr int V = D / 32;
+    __shared__ int64_t s_plan[kCombineThreads / 32 + 2];
+    __shared__ float s_ml[kCombineThreads / 32][2], s_o[kCombineThreads / 32][D];
+    const int q_heads = p.heads * p.group;
+    const int64_t row = blockIdx.x / q_heads;
+    const int head = int(blockIdx.x - row * q_heads), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int s = p.b.seq_of(row);
+    int seq;
+    int64_t before;
+    const int64_t total = locate<kCombineThreads>(p, s_plan, [](int64_t) { return int64_t(0); }, s < 0 ? 0 : s, seq, before);
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // in every CTA: this kernel is not over before the one it depends on
+    if (s < 0 || p.work(s) == 0) return;                   // nobody's row, or another kernel's
+    const int n = p.b.count(s), tiles = p.ktiles(p.b.len(s)), g = head / p.group;
+    const int64_t rr = (row - p.b.row(s)) * p.group + (head - g * p.group);
+    const int qt = int(rr / p.rows), col = int(rr - int64_t(qt) * p.rows);
+    const int64_t first = before + (int64_t(g) * p.qtiles(n) + qt) * tiles, last = first + tiles - 1;
+    const int c0 = int(((first + 1) * ctas - 1) / total), c1 = int(((last + 1) * ctas - 1) / total);
+    if (c0 == c1) return;                                  // whole: written by its CTA
+    float m = -INFINITY, l = 0.f, o[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = 0.f;
+    for (int cc = c0 + warp; cc <= c1; cc += kCombineThreads / 32) {
+        const int64_t from = share_begin(cc, total, ctas);
+        if (from == share_begin(cc + 1, total, ctas)) continue;          // an empty share
+        const int64_t at = (2 * int64_t(cc) + (from > first ? 0 : 1)) * p.rows + col;
+        const float2 ml = part_ml[at];
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = part_o[at * D + lane * V + i];
+        const float m2 = fmaxf(m, ml.x), ref = m2 == -INFINITY ? 0.f : m2, f0 = ex2(m - ref), f1 = ex2(ml.x - ref);
+        l = l * f0 + ml.y * f1;
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = o[i] * f0 + v[i] * f1;
+        m = m2;
+    }
+    if (lane == 0) { s_ml[warp][0] = m; s_ml[warp][1] = l; }
+#pragma unroll
+    for (int i = 0; i < V; ++i) s_o[warp][lane * V + i] = o[i];
+    __syncthreads();
+    m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kCombineThreads / 32; ++w) m = fmaxf(m, s_ml[w][0]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kCombineThreads / 32; ++w) l += ex2(s_ml[w][0] - ref) * s_ml[w][1];
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    for (int d = threadIdx.x; d < D; d += kCombineThreads) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kCombineThreads / 32; ++w) v += ex2(s_ml[w][0] - ref) * s_o[w][d];
+        out[row * out_stride + int64_t(head) * D + d] = QT(v * inv);
+    }
+    if (lse && threadIdx.x == 0) lse[row * q_heads + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+}
+
+// Query rows of an item: 16 when a key head has more than 8 of them, which halves the passes over its keys; float32 and
+// 256-channel items of 16 would not leave their accumulators in registers.
+inline int rows_of_item(int head_dim, int dtype, int rows_hint) { return rows_hint > 8 && head_dim <= 128 && dtype == QLLM_BF16 ? 16 : 8; }
+
+template <typename QT, int D, int NT>
+int launch(const Cache& c, const Batch& b, const AttnArgs& a, void* workspace, int* status, cudaStream_t st) {
+    using S = Shape<D, NT, sizeof(QT) == 4>;
+    const int ctas = device_sm_count() * S::CTAS;
+    const Plan p{b, c.heads, a.group, S::R, a.most_rows};
+    float* part_o = static_cast<float*>(workspace);
+    float2* part_ml = reinterpret_cast<float2*>(part_o + size_t(2) * ctas * S::R * D);
+    auto kern = kv_split_kernel<QT, D, NT>;
+    QLLM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+    kern<<<ctas, kThreads, S::SMEM, st>>>(c, p, static_cast<const QT*>(a.q), a.q_stride, static_cast<QT*>(a.out), a.out_stride, a.scale,
+                                          a.causal, a.lse, part_o, part_ml, status);
+    const int rc = after_launch();
+    if (rc != QLLM_OK) return rc;
+    const int64_t rows = b.rows * a.q_heads;
+    if (rows > 0x7fffffff) return QLLM_ERR_UNSUPPORTED;
+    QLLM_CUDA_TRY(launch_dependent(kv_combine_kernel<QT, D>, dim3(unsigned(rows)), dim3(kCombineThreads), 0, st, p, ctas,
+                                   static_cast<QT*>(a.out), a.out_stride, a.lse, static_cast<const float*>(part_o),
+                                   static_cast<const float2*>(part_ml)));
+    return after_launch();
+}
+
+}  // namespace
+
+namespace kv {
+
+int64_t split_workspace(int head_dim, int dtype, int rows_hint) {
+    // three CTAs on every SM at most, two pieces each
+    return int64_t(2) * 3 * device_sm_count() * rows_of_item(head_dim, dtype, rows_hint) * (head_dim + 2) * 4;
+}
+
+int launch_attention_split(const Cache& c, const Batch& b, int head_dim, const AttnArgs& a, int rows_hint, void* workspace, int* status,
+                           cudaStream_t st) {
+    const int rows = rows_of_item(head_dim, a.dtype, rows_hint);
+#define QLLM_KV_SPLIT(QT, D, NT) return launch<QT, D, NT>(c, b, a, workspace, status, st)
+    if (a.dtype == QLLM_BF16) {
+        if (head_dim == 64) { if (rows == 16) QLLM_KV_SPLIT(__nv_bfloat16, 64, 2); QLLM_KV_SPLIT(__nv_bfloat16, 64, 1); }
+        if (head_dim == 128) { if (rows == 16) QLLM_KV_SPLIT(__nv_bfloat16, 128, 2); QLLM_KV_SPLIT(__nv_bfloat16, 128, 1); }
+        if (head_dim == 256) QLLM_KV_SPLIT(__nv_bfloat16, 256, 1);
+    } else {
+        if (head_dim == 64) QLLM_KV_SPLIT(float, 64, 1);
+        if (head_dim == 128) QLLM_KV_SPLIT(float, 128, 1);
+        if (head_dim == 256) QLLM_KV_SPLIT(float, 256, 1);
+    }
+#undef QLLM_KV_SPLIT
+    return QLLM_ERR_UNSUPPORTED;
+}
+
+}  // namespace kv
+}  // namespace qllm
