@@ -22,8 +22,8 @@
 // Precision: queries are scaled by a power of two per row into fp16's range (a bf16 query's 8 bits stay exact) and float32
 // queries are split in two; weights p_j vs_j are rounded to fp16, 11 bits, for bf16 results (which carry 8) and split in two
 // for float32 ones.  So that no weight leaves fp16's range whatever the value scales are, the running maximum is that of
-// s_j + log2 vs_j (exponent of vs_j only, cut to +-80), 14 below which the largest weight is placed.  Sums, maxima and
-// zero-point corrections are float32, the latter with the rounded weight, so that the two parts of a value cancel as they should.
+// s_j + log2 vs_j (the logarithm cut to +-80), with the largest weight placed at 2^6; it moves only when a weight would pass 2^14,
+// which spares most steps the reduction over lanes and the rescaling.  Sums, maxima and zero-point corrections are float32.
 
 #include <cuda_fp16.h>
 
@@ -42,6 +42,7 @@ constexpr int T = 128;                                     // tokens of a tile
 constexpr int kWarps = 4;                                  // consumer warps, 32 tokens each
 constexpr int kThreads = 32 * (kWarps + 1);
 constexpr int kCombineThreads = 128;
+constexpr float kPlace = 6.f, kSlack = 8.f;                // where the largest weight is placed (powers of two), how far it may grow
 
 template <int D, int NT, bool F32>
 struct Shape {
@@ -58,10 +59,12 @@ struct Shape {
 // ---- the line of tiles ---------------------------------------------------------------------------------------------------
 struct Plan {
     Batch b;
-    int heads, group, rows, most_rows;                     // key heads, query heads per key head, rows of an item
-    __device__ __forceinline__ int64_t qrows(int n) const { return int64_t(n) * group; }
-    __device__ __forceinline__ int qtiles(int n) const { return int((qrows(n) + rows - 1) / rows); }
-    __device__ __forceinline__ int ktiles(int len) const { return len <= T ? 1 : int((int64_t(len) + T - 1) / T); }
+    int heads, group, row_log2, rows;                      // key heads, query heads per key head, rows of an item
+    unsigned most_rows;                                    // sequences with more query rows are another kernel's
+    // (query rows of a call fit 31 bits: checked before the launch)
+    __device__ __forceinline__ unsigned qrows(int n) const { return unsigned(n) * unsigned(group); }
+    __device__ __forceinline__ unsigned qtiles(int n) const { return (qrows(n) + rows - 1) >> row_log2; }
+    __device__ __forceinline__ int ktiles(int len) const { return len <= T ? 1 : int((unsigned(len) + T - 1) / T); }
     __device__ __forceinline__ int64_t work(int s) const {
         const int n = b.count(s);
         return n == 0 || qrows(n) > most_rows ? 0 : int64_t(heads) * qtiles(n) * ktiles(b.len(s));
@@ -131,15 +134,23 @@ struct Walk {
         o.len = p.b.len(s);
         o.row0 = p.b.row(s);
         o.tiles = p.ktiles(o.len);
-        const int64_t at = x - before, item = at / o.tiles;
-        const int qts = p.qtiles(o.n);
-        o.g = int(item / qts);
-        o.qt = int(item - int64_t(o.g) * qts);
-        o.tile = int(at - item * o.tiles);
+        const int64_t at = x - before;
+        const unsigned qts = p.qtiles(o.n);
+        if (at >> 32) {
+            const int64_t item = at / o.tiles;
+            o.g = int(item / qts);
+            o.qt = int(item - int64_t(o.g) * qts);
+            o.tile = int(at - item * o.tiles);
+        } else {
+            const unsigned item = unsigned(at) / unsigned(o.tiles);
+            o.g = int(item / qts);
+            o.qt = int(item - o.g * qts);
+            o.tile = int(unsigned(at) - item * o.tiles);
+        }
         o.count = int(min(int64_t(o.tiles - o.tile), end - x));
-        const int64_t last = min(int64_t(o.qt + 1) * p.rows, p.qrows(o.n)) - 1;
-        const int64_t own = int64_t(o.len) - o.n + last / p.group + 1;
-        o.keys = !causal ? o.len : own < 0 ? 0 : int(own);
+        const unsigned last = min(unsigned(o.qt + 1) << p.row_log2, p.qrows(o.n)) - 1;
+        const int own = o.len - o.n + int(last / unsigned(p.group)) + 1;
+        o.keys = !causal ? o.len : max(own, 0);
         x += o.count;
         return true;
     }
@@ -161,6 +172,11 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+__device__ __forceinline__ float lg2(float x) {
+    float r;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -176,12 +192,11 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 // too, which spreads the key reads (rows 2i, 2i + 1 in a phase) and the value reads (rows 0, 2, 4, 6) over the banks.
 __device__ __forceinline__ int order(int r) { return r ^ ((r >> 1) & 1); }
 
-// The query rows of a column group: 8 channels of column `r` at a time as B operands.  Returns the row's power of two.
+// The query row of column `r` as B operands; what a unit of the sums made with them stands for, and the row's sum in those units.
 template <typename QT, int D, bool F32>
-__device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi)[D / 8], uint32_t (&lo)[F32 ? D / 8 : 1], float& unit, float& sum) {
+__device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi)[D / 8], uint32_t (&lo)[F32 ? D / 8 : 1], float& unit, float& ratio) {
     constexpr int N = D / 4;                               // channels of this lane: N t .. N t + N - 1
-    float top = 0.f;
-    sum = 0.f;
+    float top = 0.f, sum = 0.f;
     if (row) {
 #pragma unroll
         for (int i = 0; i < N / 8; ++i) {
@@ -197,7 +212,8 @@ __device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     const int e = max(int(__float_as_uint(top) >> 23) - 127, -100);      // 2^e <= top < 2^(e+1); infinities: 128
     const float up = pow2i(min(13 - e, 126));
-    unit = e > 115 ? INFINITY : pow2i(e + 11);             // 2^24 / 2^(13 - e)
+    unit = e > 115 ? INFINITY : pow2i(e + 11);             // 2^24 / 2^(13 - e): what one unit of an MMA sum stands for
+    ratio = e > 115 ? NAN : sum * pow2i(-e - 11);
 #pragma unroll
     for (int i = 0; i < N / 8; ++i) {
         float f[8];
@@ -232,6 +248,162 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
             const uint4 v = reinterpret_cast<const uint4*>(p)[i];
             w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
         }
+    }
+}
+
+// What a warp keeps of an item: lane (r, t) holds columns 2t, 2t + 1 of every column group.
+template <int D, int NT, bool F32>
+struct State {
+    uint32_t qh[NT][D / 8], ql[NT][F32 ? D / 8 : 1];       // queries of column r as B operands
+    float qn[NT][2], qr[NT][2];                            // factor of the key sums (into base 2), sum of the query in their units
+    int limit[NT][2];                                      // keys that the column sees
+    float o[NT][D / 16][4], top[NT][2], l[NT][2], zs[NT][2];
+};
+
+// 32 tokens, from `first` on.  MASKED: some are hidden from some column, or not there.
+template <int D, int NT, bool F32, bool MASKED>
+__device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, const uint8_t* vc, const float2* kp, int first, int len,
+                                     uint32_t there, int r, int t) {
+    constexpr int KW = D / 32, VW = D / 64, MT = D / 16;
+    const int rt = order(r);
+    float s[NT][2][4];
+    // ---- S^T = K Q^T, 16 tokens at a time
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        uint32_t w0[KW], w1[KW];
+        load_words<KW>(kc + (b * 16 + rt) * (D / 2) + t * (D / 8), w0);
+        load_words<KW>(kc + (b * 16 + 8 + rt) * (D / 2) + t * (D / 8), w1);
+#pragma unroll
+        for (int a = 0; a < NT; ++a)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[a][b][e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < KW; ++i) {
+            const uint32_t u0 = w0[i] >> 8, u1 = w1[i] >> 8;
+            const uint32_t a0 = w0[i] & 0x000F000Fu, a1 = w1[i] & 0x000F000Fu, a2 = w0[i] & 0x00F000F0u, a3 = w1[i] & 0x00F000F0u;
+            const uint32_t c0 = u0 & 0x000F000Fu, c1 = u1 & 0x000F000Fu, c2 = u0 & 0x00F000F0u, c3 = u1 & 0x00F000F0u;
+#pragma unroll
+            for (int a = 0; a < NT; ++a) {
+                mma_f16(s[a][b], a0, a1, a2, a3, st.qh[a][4 * i], st.qh[a][4 * i + 1]);
+                mma_f16(s[a][b], c0, c1, c2, c3, st.qh[a][4 * i + 2], st.qh[a][4 * i + 3]);
+                if (F32) {
+                    mma_f16(s[a][b], a0, a1, a2, a3, st.ql[a][4 * i], st.ql[a][4 * i + 1]);
+                    mma_f16(s[a][b], c0, c1, c2, c3, st.ql[a][4 * i + 2], st.ql[a][4 * i + 3]);
+                }
+            }
+        }
+    }
+    // ---- s becomes y, score = qn y in base 2, of tokens (block b, half h) and columns 2t, 2t + 1
+    float vs[2][2], vz[2][2], ve[2][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int tok = b * 16 + h * 8 + rt;
+            const float2 kk = kp[tok], vv = kp[T + tok];
+            vs[b][h] = vv.x;
+            vz[b][h] = vv.y;
+            ve[b][h] = fminf(fmaxf(lg2(fabsf(vv.x)), -80.f), 80.f) - kPlace;
+            if (MASKED && (first + tok >= len || !((there >> (2 * b + h)) & 1u))) vs[b][h] = vz[b][h] = 0.f;
+#pragma unroll
+            for (int a = 0; a < NT; ++a)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) s[a][b][2 * h + e] = kk.x * fmaf(-kk.y, st.qr[a][e], s[a][b][2 * h + e]);
+        }
+    auto hidden = [&](int b, int h, int a, int e) {
+        const int tok = first + b * 16 + h * 8 + rt;
+        return MASKED && (tok >= len || tok >= st.limit[a][e] || !((there >> (2 * b + h)) & 1u));
+    };
+    uint32_t ph[NT][4], pl[NT][F32 ? 4 : 1];               // weights as B operands of the second product
+#pragma unroll
+    for (int a = 0; a < NT; ++a) {
+        float m[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            m[e] = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float x = fmaf(s[a][b][2 * h + e], st.qn[a][e], ve[b][h]);
+                    m[e] = fmaxf(m[e], hidden(b, h, a, e) ? -INFINITY : x);
+                }
+        }
+        // the reference moves only when a weight would pass 2^kSlack times its place
+        if (__any_sync(0xffffffffu, m[0] > st.top[a][0] + kSlack || m[1] > st.top[a][1] + kSlack)) {
+            float fix[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float x = m[e];
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                x = fmaxf(x, st.top[a][e]);
+                fix[e] = x == -INFINITY ? 1.f : ex2(st.top[a][e] - x);
+                st.top[a][e] = x;
+                st.l[a][e] *= fix[e];
+                st.zs[a][e] *= fix[e];
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st.o[a][i][e] *= fix[e & 1];
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float at = MASKED && st.top[a][e] == -INFINITY ? 0.f : st.top[a][e];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    // a hidden key's parameters may be anything
+                    const bool gone = hidden(b, h, a, e);
+                    const float pw = gone ? 0.f : ex2(fmaf(s[a][b][2 * h + e], st.qn[a][e], -at));
+                    const float w = gone ? 0.f : pw * vs[b][h];
+                    st.l[a][e] += pw;
+                    st.zs[a][e] = gone ? st.zs[a][e] : fmaf(w, vz[b][h], st.zs[a][e]);
+                    s[a][b][2 * h + e] = w;
+                }
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float w0 = s[a][b][2 * h], w1 = s[a][b][2 * h + 1];
+                const uint32_t hi = pack2(w0, w1);
+                ph[a][2 * b + h] = transpose8(hi);
+                if (F32) {
+                    const float2 f = unpack2(hi);
+                    pl[a][2 * b + h] = transpose8(pack2(w0 - f.x, w1 - f.y));
+                }
+            }
+    }
+    // ---- O^T += V^T P^T: this lane's channels are D/8 r .. D/8 r + D/8 - 1
+    const int ka = order(2 * t), kb = order(2 * t + 1);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        uint32_t v[4][VW];
+        load_words<VW>(vc + (b * 16 + ka) * (D / 2) + r * (D / 16), v[0]);
+        load_words<VW>(vc + (b * 16 + kb) * (D / 2) + r * (D / 16), v[1]);
+        load_words<VW>(vc + (b * 16 + 8 + ka) * (D / 2) + r * (D / 16), v[2]);
+        load_words<VW>(vc + (b * 16 + 8 + kb) * (D / 2) + r * (D / 16), v[3]);
+#pragma unroll
+        for (int i = 0; i < VW; ++i)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const uint32_t x0 = __byte_perm(v[0][i], v[1][i], y ? 0x7632 : 0x5410);
+                const uint32_t x1 = __byte_perm(v[2][i], v[3][i], y ? 0x7632 : 0x5410);
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const uint32_t y0 = z ? x0 >> 8 : x0, y1 = z ? x1 >> 8 : x1;
+                    const int m = 4 * i + 2 * y + z;
+#pragma unroll
+                    for (int a = 0; a < NT; ++a) {
+                        mma_f16(st.o[a][m], y0 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x000F000Fu, y1 & 0x00F000F0u, ph[a][2 * b], ph[a][2 * b + 1]);
+                        if (F32) mma_f16(st.o[a][m], y0 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x000F000Fu, y1 & 0x00F000F0u, pl[a][2 * b], pl[a][2 * b + 1]);
+                    }
+                }
+            }
     }
 }
 
@@ -316,212 +488,60 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
     }
 
     // -------------------------------------------------------------------- consumers
-    const int r = lane >> 2, t = lane & 3, rt = order(r);
-    const float to_log2 = scale * 1.4426950408889634f;
+    const int r = lane >> 2, t = lane & 3;
     bool ok = true;                                        // false: a wait ran out; go through the motions without waiting
     while (walk.next(it)) {
-        uint32_t qh[NT][D / 8], ql[NT][F32 ? D / 8 : 1];
-        float qn[NT][2], qs[NT][2];                        // per column 2t, 2t + 1: factor of the sum of codes, scaled sum of q
-        int limit[NT][2], low = 0x7fffffff;                // keys that the column sees; the fewest of all columns
+        State<D, NT, F32> st;
+        int low = 0x7fffffff;                              // the fewest keys that a column sees
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
-            const int64_t rr = int64_t(it.qt) * R + a * 8 + r, i = rr / p.group;
-            const bool real = i < it.n;
+            const unsigned rr = unsigned(it.qt) * R + a * 8 + r, i = rr / unsigned(p.group);
+            const bool real = int(i) < it.n;
             const QT* row = real ? q + (it.row0 + i) * q_stride + (int64_t(it.g) * p.group + (rr - i * p.group)) * D : nullptr;
-            float unit, sum;
-            load_queries<QT, D, F32>(row, t, qh[a], ql[a], unit, sum);
-            const int64_t own = int64_t(it.len) - it.n + i + 1;
-            const int lim = !real ? 0x7fffffff : !causal ? it.len : own < 0 ? 0 : int(own);
+            float unit, ratio;
+            load_queries<QT, D, F32>(row, t, st.qh[a], st.ql[a], unit, ratio);
+            const int lim = !real ? 0x7fffffff : !causal ? it.len : max(it.len - it.n + int(i) + 1, 0);
             low = min(low, lim);
-            unit *= to_log2;
-            sum *= to_log2;
+            unit *= scale * 1.4426950408889634f;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {                  // column 2t + e is lane group 2t + e
-                qn[a][e] = __shfl_sync(0xffffffffu, unit, (2 * t + e) * 4);
-                qs[a][e] = __shfl_sync(0xffffffffu, sum, (2 * t + e) * 4);
-                limit[a][e] = __shfl_sync(0xffffffffu, lim, (2 * t + e) * 4);
+                st.qn[a][e] = __shfl_sync(0xffffffffu, unit, (2 * t + e) * 4);
+                st.qr[a][e] = __shfl_sync(0xffffffffu, ratio, (2 * t + e) * 4);
+                st.limit[a][e] = __shfl_sync(0xffffffffu, lim, (2 * t + e) * 4);
             }
         }
         low = __reduce_min_sync(0xffffffffu, low);
-        float o[NT][S::MT][4], top[NT][2], l[NT][2], zs[NT][2];
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { top[a][e] = -INFINITY; l[a][e] = 0.f; zs[a][e] = 0.f; }
+            for (int e = 0; e < 2; ++e) { st.top[a][e] = -INFINITY; st.l[a][e] = 0.f; st.zs[a][e] = 0.f; }
 #pragma unroll
             for (int m = 0; m < S::MT; ++m)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[a][m][e] = 0.f;
+                for (int e = 0; e < 4; ++e) st.o[a][m][e] = 0.f;
         }
         for (int j = it.tile; j < it.tile + it.count; ++j) {
             if (j * T >= it.keys) break;
-            const int st = k % S::STAGES;
-            if (ok && !wait_bounded(&s_full[st], (k / S::STAGES) & 1, ab)) ok = false;
+            const int sg = k % S::STAGES;
+            if (ok && !wait_bounded(&s_full[sg], (k / S::STAGES) & 1, ab)) ok = false;
             ++k;
             if (!ok) continue;
-            const uint8_t* base = smem + st * S::STAGE;
+            const uint8_t* base = smem + sg * S::STAGE;
             const uint8_t* kc = base + (warp * 32) * (D / 2);
-            const uint8_t* vc = base + HALF + (warp * 32) * (D / 2);
+            const uint8_t* vc = kc + HALF;
             const float2* kp = reinterpret_cast<const float2*>(base + 2 * HALF) + warp * 32;
-            const float2* vp = kp + T;
             const int first = j * T + warp * 32;           // token of this warp's row 0
-            // which 8-token blocks of this warp's 32 tokens lie in pages that exist
-            const uint32_t pieces = s_pieces[st];
-            uint32_t there = 0;
-#pragma unroll
-            for (int b8 = 0; b8 < 4; ++b8) there |= ((pieces >> (4 * ((warp * 32 + b8 * 8) >> piece_log2))) & 1u) << b8;
             if (first < it.keys) {
-                const bool masked = first + 32 > low || first + 32 > it.len || there != 15u;
-                float s[NT][2][4], vs[2][2], vz[2][2];
-                // ---- S^T = K Q^T, 16 tokens at a time
+                // which 8-token blocks of this warp's 32 tokens lie in pages that exist
+                uint32_t there = 0;
+                const uint32_t pieces = s_pieces[sg];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    uint32_t w0[S::KW], w1[S::KW];
-                    load_words<S::KW>(kc + (b * 16 + rt) * (D / 2) + t * (D / 8), w0);
-                    load_words<S::KW>(kc + (b * 16 + 8 + rt) * (D / 2) + t * (D / 8), w1);
-#pragma unroll
-                    for (int a = 0; a < NT; ++a)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[a][b][e] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < S::KW; ++i) {
-                        const uint32_t u0 = w0[i] >> 8, u1 = w1[i] >> 8;
-                        const uint32_t a0 = w0[i] & 0x000F000Fu, a1 = w1[i] & 0x000F000Fu, a2 = w0[i] & 0x00F000F0u, a3 = w1[i] & 0x00F000F0u;
-                        const uint32_t c0 = u0 & 0x000F000Fu, c1 = u1 & 0x000F000Fu, c2 = u0 & 0x00F000F0u, c3 = u1 & 0x00F000F0u;
-#pragma unroll
-                        for (int a = 0; a < NT; ++a) {
-                            mma_f16(s[a][b], a0, a1, a2, a3, qh[a][4 * i], qh[a][4 * i + 1]);
-                            mma_f16(s[a][b], c0, c1, c2, c3, qh[a][4 * i + 2], qh[a][4 * i + 3]);
-                            if (F32) {
-                                mma_f16(s[a][b], a0, a1, a2, a3, ql[a][4 * i], ql[a][4 * i + 1]);
-                                mma_f16(s[a][b], c0, c1, c2, c3, ql[a][4 * i + 2], ql[a][4 * i + 3]);
-                            }
-                        }
-                    }
-                }
-                // ---- scores, in base 2, of tokens (block b, half h) and columns 2t, 2t + 1
-                float ve[2][2];
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int tok = b * 16 + h * 8 + rt;
-                        const float2 kk = kp[tok], vv = vp[tok];
-                        vs[b][h] = vv.x;
-                        vz[b][h] = vv.y;
-                        ve[b][h] = float(min(max(int((__float_as_uint(vv.x) >> 23) & 255u) - 127, -80), 80) - 14);
-#pragma unroll
-                        for (int a = 0; a < NT; ++a)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                s[a][b][2 * h + e] = kk.x * (s[a][b][2 * h + e] * qn[a][e] - kk.y * qs[a][e]);
-                    }
-                if (masked) {
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int tok = first + b * 16 + h * 8 + rt;
-                            const bool hole = tok >= it.len || !((there >> (2 * b + h)) & 1u);
-                            if (hole) { vs[b][h] = 0.f; vz[b][h] = 0.f; }
-#pragma unroll
-                            for (int a = 0; a < NT; ++a)
-#pragma unroll
-                                for (int e = 0; e < 2; ++e)
-                                    if (hole || tok >= limit[a][e]) s[a][b][2 * h + e] = -INFINITY;
-                        }
-                }
-                uint32_t ph[NT][4], pl[NT][F32 ? 4 : 1];   // weights as B operands of the second product
-#pragma unroll
-                for (int a = 0; a < NT; ++a) {
-                    float fix[2];
-                    bool moved = false;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float m = fmaxf(fmaxf(s[a][0][e] + ve[0][0], s[a][0][2 + e] + ve[0][1]), fmaxf(s[a][1][e] + ve[1][0], s[a][1][2 + e] + ve[1][1]));
-                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                        m = fmaxf(m, top[a][e]);
-                        const float at = m == -INFINITY ? 0.f : m;
-                        fix[e] = ex2(top[a][e] - at);
-                        moved |= m != top[a][e];
-                        top[a][e] = m;
-                        l[a][e] *= fix[e];
-                        zs[a][e] *= fix[e];
-#pragma unroll
-                        for (int b = 0; b < 2; ++b)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const float pw = ex2(s[a][b][2 * h + e] - at);
-                                l[a][e] += pw;
-                                float w = pw * vs[b][h];
-                                // a hidden key's value parameters may be anything
-                                if (masked && first + b * 16 + h * 8 + rt >= limit[a][e]) w = 0.f;
-                                s[a][b][2 * h + e] = w;
-                            }
-                    }
-                    if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-                        for (int m = 0; m < S::MT; ++m)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[a][m][e] *= fix[e & 1];
-                    }
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float w0 = s[a][b][2 * h], w1 = s[a][b][2 * h + 1];
-                            const uint32_t hi = pack2(w0, w1);
-                            float2 f = unpack2(hi);
-                            ph[a][2 * b + h] = transpose8(hi);
-                            if (F32) {
-                                const uint32_t lo = pack2(w0 - f.x, w1 - f.y);
-                                const float2 g = unpack2(lo);
-                                pl[a][2 * b + h] = transpose8(lo);
-                                f.x += g.x;
-                                f.y += g.y;
-                            }
-                            if (masked) {
-                                const int tok = first + b * 16 + h * 8 + rt;
-                                zs[a][0] += tok >= limit[a][0] ? 0.f : f.x * vz[b][h];
-                                zs[a][1] += tok >= limit[a][1] ? 0.f : f.y * vz[b][h];
-                            } else {
-                                zs[a][0] = fmaf(f.x, vz[b][h], zs[a][0]);
-                                zs[a][1] = fmaf(f.y, vz[b][h], zs[a][1]);
-                            }
-                        }
-                }
-                // ---- O^T += V^T P^T: this lane's channels are D/8 r .. D/8 r + D/8 - 1
-                const int ka = order(2 * t), kb = order(2 * t + 1);
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    uint32_t v[4][S::VW];
-                    load_words<S::VW>(vc + (b * 16 + ka) * (D / 2) + r * (D / 16), v[0]);
-                    load_words<S::VW>(vc + (b * 16 + kb) * (D / 2) + r * (D / 16), v[1]);
-                    load_words<S::VW>(vc + (b * 16 + 8 + ka) * (D / 2) + r * (D / 16), v[2]);
-                    load_words<S::VW>(vc + (b * 16 + 8 + kb) * (D / 2) + r * (D / 16), v[3]);
-#pragma unroll
-                    for (int i = 0; i < S::VW; ++i)
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const uint32_t x0 = __byte_perm(v[0][i], v[1][i], y ? 0x7632 : 0x5410);
-                            const uint32_t x1 = __byte_perm(v[2][i], v[3][i], y ? 0x7632 : 0x5410);
-#pragma unroll
-                            for (int z = 0; z < 2; ++z) {
-                                const uint32_t y0 = z ? x0 >> 8 : x0, y1 = z ? x1 >> 8 : x1;
-                                const int m = 4 * i + 2 * y + z;
-#pragma unroll
-                                for (int a = 0; a < NT; ++a) {
-                                    mma_f16(o[a][m], y0 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x000F000Fu, y1 & 0x00F000F0u, ph[a][2 * b], ph[a][2 * b + 1]);
-                                    if (F32) mma_f16(o[a][m], y0 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x000F000Fu, y1 & 0x00F000F0u, pl[a][2 * b], pl[a][2 * b + 1]);
-                                }
-                            }
-                        }
-                }
+                for (int b8 = 0; b8 < 4; ++b8) there |= ((pieces >> (4 * ((warp * 32 + b8 * 8) >> piece_log2))) & 1u) << b8;
+                if (first + 32 > low || there != 15u) step<D, NT, F32, true>(st, kc, vc, kp, first, it.len, there, r, t);
+                else step<D, NT, F32, false>(st, kc, vc, kp, first, it.len, there, r, t);
             }
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&s_empty[st]);
+            if (lane == 0) ptx::mbar_arrive(&s_empty[sg]);
         }
         // ---- the four warps' states meet
         float* m_top = reinterpret_cast<float*>(merge);    // [warps][R], then [warps][R] sums, [warps][R][OROW] outputs
@@ -533,19 +553,19 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
             for (int e = 0; e < 2; ++e) {
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) {
-                    l[a][e] += __shfl_xor_sync(0xffffffffu, l[a][e], x);
-                    zs[a][e] += __shfl_xor_sync(0xffffffffu, zs[a][e], x);
+                    st.l[a][e] += __shfl_xor_sync(0xffffffffu, st.l[a][e], x);
+                    st.zs[a][e] += __shfl_xor_sync(0xffffffffu, st.zs[a][e], x);
                 }
                 if (r == 0) {
-                    m_top[warp * R + a * 8 + 2 * t + e] = top[a][e];
-                    m_l[warp * R + a * 8 + 2 * t + e] = l[a][e];
+                    m_top[warp * R + a * 8 + 2 * t + e] = st.top[a][e];
+                    m_l[warp * R + a * 8 + 2 * t + e] = st.l[a][e];
                 }
                 float* row = m_o + (warp * R + a * 8 + 2 * t + e) * S::OROW + r * (D / 8);
 #pragma unroll
                 for (int m = 0; m < S::MT; m += 2)
                     *reinterpret_cast<float4*>(row + 2 * m) =
-                        make_float4(fmaf(o[a][m][e], 16777216.f, -zs[a][e]), fmaf(o[a][m][2 + e], 1048576.f, -zs[a][e]),
-                                    fmaf(o[a][m + 1][e], 16777216.f, -zs[a][e]), fmaf(o[a][m + 1][2 + e], 1048576.f, -zs[a][e]));
+                        make_float4(fmaf(st.o[a][m][e], 16777216.f, -st.zs[a][e]), fmaf(st.o[a][m][2 + e], 1048576.f, -st.zs[a][e]),
+                                    fmaf(st.o[a][m + 1][e], 16777216.f, -st.zs[a][e]), fmaf(st.o[a][m + 1][2 + e], 1048576.f, -st.zs[a][e]));
             }
         ptx::named_bar_sync(1, 32 * kWarps);
         const bool whole = it.count == it.tiles;
@@ -553,8 +573,8 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
         constexpr int PER = D / 4;                         // threads of a row: 4 channels each
         for (int u = threadIdx.x; u < R * PER; u += 32 * kWarps) {
             const int col = u / PER, d4 = (u % PER) * 4;
-            const int64_t rr = int64_t(it.qt) * R + col, i = rr / p.group;
-            if (i >= it.n) continue;
+            const unsigned rr = unsigned(it.qt) * R + col, i = rr / unsigned(p.group);
+            if (int(i) >= it.n) continue;
             float m = -INFINITY;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) m = fmaxf(m, m_top[w * R + col]);
@@ -611,21 +631,44 @@ kv_combine_kernel(Plan p, int ctas, QT* __restrict__ out, int64_t out_stride, fl
     const int64_t first = before + (int64_t(g) * p.qtiles(n) + qt) * tiles, last = first + tiles - 1;
     const int c0 = int(((first + 1) * ctas - 1) / total), c1 = int(((last + 1) * ctas - 1) / total);
     if (c0 == c1) return;                                  // whole: written by its CTA
+    // this warp's pieces, 8 at a time: one lane looks up each, then all of their loads are in flight together
     float m = -INFINITY, l = 0.f, o[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) o[i] = 0.f;
-    for (int cc = c0 + warp; cc <= c1; cc += kCombineThreads / 32) {
-        const int64_t from = share_begin(cc, total, ctas);
-        if (from == share_begin(cc + 1, total, ctas)) continue;          // an empty share
-        const int64_t at = (2 * int64_t(cc) + (from > first ? 0 : 1)) * p.rows + col;
-        const float2 ml = part_ml[at];
-        float v[V];
+    for (int base = c0 + warp * 8; base <= c1; base += 8 * (kCombineThreads / 32)) {
+        const int cc = base + (lane & 7);
+        int64_t at = 0;
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (cc <= c1) {
+            const int64_t from = share_begin(cc, total, ctas);
+            if (from != share_begin(cc + 1, total, ctas)) {              // not an empty share
+                at = (2 * int64_t(cc) + (from > first ? 0 : 1)) * p.rows + col;
+                ml = part_ml[at];
+            }
+        }
+        float m2 = ml.x;
+        m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, 1));
+        m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, 2));
+        m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, 4));
+        m2 = fmaxf(m2, m);
+        const float ref = m2 == -INFINITY ? 0.f : m2, f0 = ex2(m - ref), f1 = ml.y == 0.f ? 0.f : ml.x == -INFINITY ? 1.f : ex2(ml.x - ref);   // (a NaN sum goes through)
+        float v[8][V], f[8];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = part_o[at * D + lane * V + i];
-        const float m2 = fmaxf(m, ml.x), ref = m2 == -INFINITY ? 0.f : m2, f0 = ex2(m - ref), f1 = ex2(ml.x - ref);
-        l = l * f0 + ml.y * f1;
+        for (int j = 0; j < 8; ++j) {
+            const int64_t a = __shfl_sync(0xffffffffu, at, j);
+            f[j] = __shfl_sync(0xffffffffu, f1, j);
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = o[i] * f0 + v[i] * f1;
+            for (int i = 0; i < V; ++i) v[j][i] = f[j] != 0.f ? part_o[a * D + lane * V + i] : 0.f;
+        }
+        l *= f0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] *= f0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            l = fmaf(f[j], __shfl_sync(0xffffffffu, ml.y, j), l);
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[i] = fmaf(f[j], v[j][i], o[i]);
+        }
         m = m2;
     }
     if (lane == 0) { s_ml[warp][0] = m; s_ml[warp][1] = l; }
@@ -657,7 +700,7 @@ template <typename QT, int D, int NT>
 int launch(const Cache& c, const Batch& b, const AttnArgs& a, void* workspace, int* status, cudaStream_t st) {
     using S = Shape<D, NT, sizeof(QT) == 4>;
     const int ctas = device_sm_count() * S::CTAS;
-    const Plan p{b, c.heads, a.group, S::R, a.most_rows};
+    const Plan p{b, c.heads, a.group, NT == 2 ? 4 : 3, S::R, unsigned(a.most_rows)};
     float* part_o = static_cast<float*>(workspace);
     float2* part_ml = reinterpret_cast<float2*>(part_o + size_t(2) * ctas * S::R * D);
     auto kern = kv_split_kernel<QT, D, NT>;
