@@ -17,7 +17,7 @@ int check_attention(const qllm_kv_cache_t* cache, int q_heads, int dtype, const 
     if (rc == QLLM_OK) rc = check_batch(batch);
     if (rc != QLLM_OK) return rc;
     if (q_heads <= 0 || q_heads % cache->kv_heads) return QLLM_ERR_SHAPE;
-    if (q_heads > 65535) return QLLM_ERR_UNSUPPORTED;
+    if (q_heads > 65535 || batch->rows * q_heads > 0x7fffffff) return QLLM_ERR_UNSUPPORTED;   // query rows are counted in 31 bits
     return QLLM_OK;
 }
 

@@ -7,8 +7,8 @@
 // Work split: an item is (sequence, key head, tile of 8 NT query rows); its keys are tiles of T tokens.  All items' tiles form
 // one line, which the CTAs of one resident wave cut into equal shares, each working out its own from the lengths on the
 // device: a batch of any lengths keeps every SM busy, and a captured graph follows them.  An item that lies in several shares
-// leaves one piece per share (sum, running maximum, weights) in the workspace, which a second kernel joins; at most two pieces
-// per CTA.  No CTA waits for another, and the order of all additions is fixed by the shapes and lengths.
+// leaves one piece per share (sum, running maximum, weights) in the workspace, which a second kernel joins by the records that the
+// CTAs leave; at most two pieces per CTA.  No CTA waits for another, and the order of all additions is fixed by the shapes and lengths.
 //
 // In a CTA: one warp fetches a tile's codes and parameters with bulk copies, one per page and array, several tiles ahead; four
 // warps own 32 of its tokens each, with a softmax state of their own that meets at the item's end.  Both products run
@@ -26,6 +26,8 @@
 // which spares most steps the reduction over lanes and the rescaling.  Sums, maxima and zero-point corrections are float32.
 
 #include <cuda_fp16.h>
+
+#include <algorithm>
 
 #include "kv_attention.h"
 #include "ptx_sm100.cuh"
@@ -56,7 +58,12 @@ struct Shape {
     static constexpr int CTAS = SMEM <= 75 * 1024 && NT * D * (F32 ? 3 : 2) <= 256 ? 3 : 2;
 };
 
-// ---- the line of tiles ---------------------------------------------------------------------------------------------------
+// ---- the line of work ----------------------------------------------------------------------------------------------------
+// An item costs kItemCost tiles for its queries, its first loads and its end, then one for each tile of keys: a share that
+// ends in front of the first tile takes none of the item.  (Counting tiles alone gave the CTAs that got the short sequences of
+// a ragged batch half as much work again.)
+constexpr int kItemCost = 3;
+
 struct Plan {
     Batch b;
     int heads, group, row_log2, rows;                      // key heads, query heads per key head, rows of an item
@@ -67,16 +74,38 @@ struct Plan {
     __device__ __forceinline__ int ktiles(int len) const { return len <= T ? 1 : int((unsigned(len) + T - 1) / T); }
     __device__ __forceinline__ int64_t work(int s) const {
         const int n = b.count(s);
-        return n == 0 || qrows(n) > most_rows ? 0 : int64_t(heads) * qtiles(n) * ktiles(b.len(s));
+        return n == 0 || qrows(n) > most_rows ? 0 : int64_t(heads) * qtiles(n) * (ktiles(b.len(s)) + kItemCost);
     }
 };
 
-// Called by a whole CTA of NTHREADS threads: total work, and (in every thread) the first sequence whose range of the line
-// ends behind `x`, with the work in front of it.  want >= 0: that sequence instead.
-template <int NTHREADS, typename XFn>
-__device__ __forceinline__ int64_t locate(const Plan& p, int64_t* s_mem, XFn x_of_total, int want, int& seq, int64_t& before) {
+// quotient and rest, in 32 bits where they suffice
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b, int64_t& rest) {
+    if (((a | b) >> 32) == 0) {
+        const unsigned q = unsigned(a) / unsigned(b);
+        rest = unsigned(a) - q * unsigned(b);
+        return q;
+    }
+    const int64_t q = a / b;
+    rest = a - q * b;
+    return q;
+}
+
+// `total` cut into `ctas` shares that differ by one at most.
+struct Shares {
+    int64_t each, more;                                    // the first `more` shares have each + 1
+    __device__ __forceinline__ Shares(int64_t total, int ctas) { each = divide(total, ctas, more); }
+    __device__ __forceinline__ int64_t begin(int64_t c) const { return c * each + min(c, more); }
+    __device__ __forceinline__ int owner(int64_t x) const {
+        int64_t rest;
+        return x < more * (each + 1) ? int(divide(x, each + 1, rest)) : int(more + divide(x - more * (each + 1), each, rest));
+    }
+};
+
+// Called by a whole CTA of kThreads threads: total work, and (in every thread) the sequence whose range of the line holds
+// the beginning of share c, with the work in front of it.
+__device__ __forceinline__ int64_t locate(const Plan& p, int64_t* s_mem, int c, int ctas, int& seq, int64_t& before) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (p.b.seqs + NTHREADS - 1) / NTHREADS, first = min(tid * per, p.b.seqs), last = min(first + per, p.b.seqs);
+    const int per = (p.b.seqs + kThreads - 1) / kThreads, first = min(tid * per, p.b.seqs), last = min(first + per, p.b.seqs);
     int64_t mine = 0;
     for (int s = first; s < last; ++s) mine += p.work(s);
     int64_t incl = mine;
@@ -89,34 +118,32 @@ __device__ __forceinline__ int64_t locate(const Plan& p, int64_t* s_mem, XFn x_o
     __syncthreads();
     int64_t base = 0, total = 0;
 #pragma unroll
-    for (int w = 0; w < NTHREADS / 32; ++w) {
+    for (int w = 0; w < kThreads / 32; ++w) {
         if (w < warp) base += s_mem[w];
         total += s_mem[w];
     }
-    const int64_t pre = base + incl - mine, x = x_of_total(total);
-    if (want >= 0 ? (want >= first && want < last) : (x >= pre && x < pre + mine)) {
+    const int64_t pre = base + incl - mine, x = Shares(total, ctas).begin(c);
+    if (x >= pre && x < pre + mine) {
         int64_t at = pre;
         int s = first;
-        for (; s < last; ++s) {
+        for (; s < last - 1; ++s) {
             const int64_t w = p.work(s);
-            if (want >= 0 ? s == want : x < at + w) break;
+            if (x < at + w) break;
             at += w;
         }
-        s_mem[NTHREADS / 32] = s;
-        s_mem[NTHREADS / 32 + 1] = at;
+        s_mem[kThreads / 32] = s;
+        s_mem[kThreads / 32 + 1] = at;
     }
     __syncthreads();
-    seq = int(s_mem[NTHREADS / 32]);
-    before = s_mem[NTHREADS / 32 + 1];
+    seq = int(s_mem[kThreads / 32]);
+    before = s_mem[kThreads / 32 + 1];
     return total;
 }
-
-__device__ __forceinline__ int64_t share_begin(int64_t c, int64_t total, int ctas) { return c * total / ctas; }
 
 // The part of an item that lies in a share.
 struct Part {
     int s, g, qt, n, len, tile, tiles, count;              // sequence .., first tile, tiles of the item, tiles of the part
-    int64_t row0;                                          // first packed row of the sequence
+    int64_t row0, first;                                   // first packed row of the sequence, the item's place in the line
     int keys;                                              // keys that the item's last row sees
 };
 // Walks the parts of [x, end).  Every role of the CTA walks for itself.
@@ -126,34 +153,39 @@ struct Walk {
     int s;
     bool causal;
     __device__ __forceinline__ bool next(Part& o) {
-        if (x >= end) return false;
-        int64_t w;
-        while ((w = p.work(s)) <= x - before) { before += w; ++s; }      // x < total: a sequence with work follows
-        o.s = s;
-        o.n = p.b.count(s);
-        o.len = p.b.len(s);
-        o.row0 = p.b.row(s);
-        o.tiles = p.ktiles(o.len);
-        const int64_t at = x - before;
-        const unsigned qts = p.qtiles(o.n);
-        if (at >> 32) {
-            const int64_t item = at / o.tiles;
-            o.g = int(item / qts);
-            o.qt = int(item - int64_t(o.g) * qts);
-            o.tile = int(at - item * o.tiles);
-        } else {
-            const unsigned item = unsigned(at) / unsigned(o.tiles);
-            o.g = int(item / qts);
-            o.qt = int(item - o.g * qts);
-            o.tile = int(unsigned(at) - item * o.tiles);
+        while (x < end) {
+            int64_t w;
+            while ((w = p.work(s)) <= x - before) { before += w; ++s; }  // x < total: a sequence with work follows
+            o.s = s;
+            o.n = p.b.count(s);
+            o.len = p.b.len(s);
+            o.row0 = p.b.row(s);
+            o.tiles = p.ktiles(o.len);
+            int64_t in_item, qt;
+            const int64_t item = divide(x - before, o.tiles + kItemCost, in_item);
+            o.g = int(divide(item, p.qtiles(o.n), qt));
+            o.qt = int(qt);
+            o.first = x - in_item;
+            o.tile = max(int(in_item) - kItemCost, 0);
+            const int64_t stop = min(int64_t(o.tiles + kItemCost), end - o.first);
+            o.count = int(stop) - kItemCost - o.tile;
+            x = o.first + stop;
+            if (o.count <= 0) continue;                    // the share ends in front of the item's first tile
+            const unsigned last = min(unsigned(o.qt + 1) << p.row_log2, p.qrows(o.n)) - 1;
+            const int own = o.len - o.n + int(last / unsigned(p.group)) + 1;
+            o.keys = !causal ? o.len : max(own, 0);
+            return true;
         }
-        o.count = int(min(int64_t(o.tiles - o.tile), end - x));
-        const unsigned last = min(unsigned(o.qt + 1) << p.row_log2, p.qrows(o.n)) - 1;
-        const int own = o.len - o.n + int(last / unsigned(p.group)) + 1;
-        o.keys = !causal ? o.len : max(own, 0);
-        x += o.count;
-        return true;
+        return false;
     }
+};
+
+// What a CTA leaves for the joining kernel: the item that begins in its share and goes on behind it (rows = 0: none).
+struct __align__(16) Record {
+    int64_t row0;                                          // first packed row of the sequence
+    int first_row, rows;                                   // query rows first_row .. first_row + rows - 1 of the key head
+    int head;                                              // first query head of the group
+    int last;                                              // the share that holds its end
 };
 
 // ---- warp-level pieces ---------------------------------------------------------------------------------------------------
@@ -410,7 +442,8 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
 template <typename QT, int D, int NT>
 __global__ void __launch_bounds__(kThreads, Shape<D, NT, sizeof(QT) == 4>::CTAS)
 kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT* __restrict__ out, int64_t out_stride, float scale,
-                int causal, float* __restrict__ lse, float* __restrict__ part_o, float2* __restrict__ part_ml, int* status) {
+                int causal, float* __restrict__ lse, float* __restrict__ part_o, float2* __restrict__ part_ml, Record* __restrict__ record,
+                int* status) {
     constexpr bool F32 = sizeof(QT) == 4;
     using S = Shape<D, NT, F32>;
     constexpr int R = S::R, HALF = T * (D / 2);
@@ -433,19 +466,27 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
     }
     if (blockIdx.x == 0) p.b.report(status);
     int seq;
-    int64_t before, begin = 0;
-    const int64_t total = locate<kThreads>(p, s_plan, [&](int64_t tot) { return begin = share_begin(blockIdx.x, tot, gridDim.x); }, -1, seq, before);
-    const int64_t end = share_begin(blockIdx.x + 1, total, gridDim.x);
+    int64_t before;
+    const int64_t total = locate(p, s_plan, blockIdx.x, gridDim.x, seq, before);
+    const Shares shares(total, gridDim.x);
+    const int64_t begin = shares.begin(blockIdx.x), end = shares.begin(blockIdx.x + 1);
+    const int piece_log2 = min(p.b.page_log2, 7);
+    const uint32_t all_pieces = piece_log2 == 4 ? 0xffffffffu : (1u << (4 * (T >> piece_log2))) - 1;
+    if (threadIdx.x == 0) record[blockIdx.x].rows = 0;
     if (begin >= end) return;
     const Abort ab{&s_abort, status};
     Walk walk{p, begin, end, before, seq, causal != 0};
     Part it;
-    uint32_t k = 0;                                        // tiles passed so far
-    const int log2p = p.b.page_log2, piece_log2 = log2p < 7 ? log2p : 7;
+    int sg = 0;                                            // pipeline stage and the parity of its turn
+    uint32_t turn = 0;
+    auto advance = [&]() {
+        if (++sg == S::STAGES) { sg = 0; turn ^= 1; }
+    };
 
     if (warp == kWarps) {
         // ---------------------------------------------------------------- producer: lane = 4 * piece + array
-        const int piece = lane >> 2, array = lane & 3, piece_tokens = 1 << piece_log2;
+        const int piece = lane >> 2, array = lane & 3, piece_tokens = 1 << piece_log2, log2p = p.b.page_log2;
+        int issued = 0;
         bool ok = true;
         while (ok && walk.next(it)) {
             const int32_t* row = p.b.table + int64_t(it.s) * p.b.width;
@@ -458,30 +499,30 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
                 if (mine && !good) raise_page(status);
                 const uint32_t bytes = uint32_t(piece_tokens) * ((array & 1) ? 8 : D / 2);
                 const uint32_t got = __ballot_sync(0xffffffffu, good), total_bytes = __reduce_add_sync(0xffffffffu, good ? bytes : 0);
-                const int st = k % S::STAGES;
-                if (!wait_bounded(&s_empty[st], ((k / S::STAGES) & 1) ^ 1, ab)) { ok = false; break; }
+                if (!wait_bounded(&s_empty[sg], turn ^ 1, ab)) { ok = false; break; }
                 if (lane == 0) {
-                    s_pieces[st] = got;
-                    ptx::mbar_arrive_expect_tx(&s_full[st], total_bytes);
+                    s_pieces[sg] = got;
+                    ptx::mbar_arrive_expect_tx(&s_full[sg], total_bytes);
                 }
                 __syncwarp();
                 if (good) {
                     const int64_t r = c.row(page, it.g, t0 & ((1 << log2p) - 1));
-                    uint8_t* base = smem + st * S::STAGE;
+                    uint8_t* base = smem + sg * S::STAGE;
                     const int place = piece << piece_log2;
-                    if (array == 0) bulk_load(base + place * (D / 2), c.kc + r * (D / 2), bytes, &s_full[st]);
-                    else if (array == 2) bulk_load(base + HALF + place * (D / 2), c.vc + r * (D / 2), bytes, &s_full[st]);
-                    else if (array == 1) bulk_load(base + 2 * HALF + place * 8, c.kp + r, bytes, &s_full[st]);
-                    else bulk_load(base + 2 * HALF + T * 8 + place * 8, c.vp + r, bytes, &s_full[st]);
+                    if (array == 0) bulk_load(base + place * (D / 2), c.kc + r * (D / 2), bytes, &s_full[sg]);
+                    else if (array == 2) bulk_load(base + HALF + place * (D / 2), c.vc + r * (D / 2), bytes, &s_full[sg]);
+                    else if (array == 1) bulk_load(base + 2 * HALF + place * 8, c.kp + r, bytes, &s_full[sg]);
+                    else bulk_load(base + 2 * HALF + T * 8 + place * 8, c.vp + r, bytes, &s_full[sg]);
                 }
-                ++k;
+                advance();
+                ++issued;
             }
         }
         if (!ok) {                                         // give copies still in flight a bounded chance to land
-            for (uint32_t j = 0; j < S::STAGES && j < k; ++j) {
-                const uint32_t i = k - 1 - j;
+            for (int j = 0; j < S::STAGES && j < issued; ++j) {
+                if (--sg < 0) { sg = S::STAGES - 1; turn ^= 1; }
                 const long long t0 = clock64();
-                while (!ptx::mbar_try_wait(&s_full[i % S::STAGES], (i / S::STAGES) & 1) && clock64() - t0 < (1ll << 24)) {}
+                while (!ptx::mbar_try_wait(&s_full[sg], turn) && clock64() - t0 < (1ll << 24)) {}
             }
         }
         return;
@@ -522,26 +563,25 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
         }
         for (int j = it.tile; j < it.tile + it.count; ++j) {
             if (j * T >= it.keys) break;
-            const int sg = k % S::STAGES;
-            if (ok && !wait_bounded(&s_full[sg], (k / S::STAGES) & 1, ab)) ok = false;
-            ++k;
+            if (ok && !wait_bounded(&s_full[sg], turn, ab)) ok = false;
             if (!ok) continue;
             const uint8_t* base = smem + sg * S::STAGE;
             const uint8_t* kc = base + (warp * 32) * (D / 2);
             const uint8_t* vc = kc + HALF;
             const float2* kp = reinterpret_cast<const float2*>(base + 2 * HALF) + warp * 32;
             const int first = j * T + warp * 32;           // token of this warp's row 0
-            if (first < it.keys) {
-                // which 8-token blocks of this warp's 32 tokens lie in pages that exist
-                uint32_t there = 0;
-                const uint32_t pieces = s_pieces[sg];
+            const uint32_t pieces = s_pieces[sg];
+            if (first + 32 <= low && pieces == all_pieces) {
+                step<D, NT, F32, false>(st, kc, vc, kp, first, it.len, 15u, r, t);
+            } else if (first < it.keys) {
+                uint32_t there = 0;                        // which 8-token blocks of the 32 tokens lie in pages that exist
 #pragma unroll
                 for (int b8 = 0; b8 < 4; ++b8) there |= ((pieces >> (4 * ((warp * 32 + b8 * 8) >> piece_log2))) & 1u) << b8;
-                if (first + 32 > low || there != 15u) step<D, NT, F32, true>(st, kc, vc, kp, first, it.len, there, r, t);
-                else step<D, NT, F32, false>(st, kc, vc, kp, first, it.len, there, r, t);
+                step<D, NT, F32, true>(st, kc, vc, kp, first, it.len, there, r, t);
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&s_empty[sg]);
+            advance();
         }
         // ---- the four warps' states meet
         float* m_top = reinterpret_cast<float*>(merge);    // [warps][R], then [warps][R] sums, [warps][R][OROW] outputs
@@ -569,6 +609,11 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
             }
         ptx::named_bar_sync(1, 32 * kWarps);
         const bool whole = it.count == it.tiles;
+        if (threadIdx.x == 0 && !whole && it.tile == 0) {
+            const int first_row = it.qt * R;
+            record[blockIdx.x] = Record{it.row0, first_row, min(R, int(p.qrows(it.n)) - first_row), it.g * p.group,
+                                        shares.owner(it.first + kItemCost + it.tiles - 1)};
+        }
         const int64_t slot = 2 * int64_t(blockIdx.x) + (it.tile > 0 ? 0 : 1);
         constexpr int PER = D / 4;                         // threads of a row: 4 channels each
         for (int u = threadIdx.x; u < R * PER; u += 32 * kWarps) {
@@ -608,50 +653,34 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
     }
 }
 
-// Joins the pieces of an item that lay in several shares: a CTA per (packed row, query head), its warps take every fourth piece.
-template <typename QT, int D>
+// Joins the pieces of the items that lay in several shares: CTA (c, row) the given row of the item that began in share c, by
+// the record that share's CTA left.  Its four warps take 8 pieces at a time: a lane looks each up, then all loads are in flight.
+template <typename QT, int D, int R>
 __global__ void __launch_bounds__(kCombineThreads)
-kv_combine_kernel(Plan p, int ctas, QT* __restrict__ out, int64_t out_stride, float* __restrict__ lse, const float* __restrict__ part_o,
-                  const float2* __restrict__ part_ml) {
-    constexpr int V = D / 32;
-    __shared__ int64_t s_plan[kCombineThreads / 32 + 2];
-    __shared__ float s_ml[kCombineThreads / 32][2], s_o[kCombineThreads / 32][D];
-    const int q_heads = p.heads * p.group;
-    const int64_t row = blockIdx.x / q_heads;
-    const int head = int(blockIdx.x - row * q_heads), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int s = p.b.seq_of(row);
-    int seq;
-    int64_t before;
-    const int64_t total = locate<kCombineThreads>(p, s_plan, [](int64_t) { return int64_t(0); }, s < 0 ? 0 : s, seq, before);
+kv_combine_kernel(int group, QT* __restrict__ out, int64_t out_stride, float* __restrict__ lse, int q_heads, const float* __restrict__ part_o,
+                  const float2* __restrict__ part_ml, const Record* __restrict__ record) {
+    constexpr int V = D / 32, W = kCombineThreads / 32;
+    __shared__ float s_ml[W][2], s_o[W][D];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c0 = blockIdx.x, col = blockIdx.y;
     asm volatile("griddepcontrol.wait;" ::: "memory");     // in every CTA: this kernel is not over before the one it depends on
-    if (s < 0 || p.work(s) == 0) return;                   // nobody's row, or another kernel's
-    const int n = p.b.count(s), tiles = p.ktiles(p.b.len(s)), g = head / p.group;
-    const int64_t rr = (row - p.b.row(s)) * p.group + (head - g * p.group);
-    const int qt = int(rr / p.rows), col = int(rr - int64_t(qt) * p.rows);
-    const int64_t first = before + (int64_t(g) * p.qtiles(n) + qt) * tiles, last = first + tiles - 1;
-    const int c0 = int(((first + 1) * ctas - 1) / total), c1 = int(((last + 1) * ctas - 1) / total);
-    if (c0 == c1) return;                                  // whole: written by its CTA
-    // this warp's pieces, 8 at a time: one lane looks up each, then all of their loads are in flight together
+    const Record rec = record[c0];
+    if (col >= rec.rows) return;
     float m = -INFINITY, l = 0.f, o[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) o[i] = 0.f;
-    for (int base = c0 + warp * 8; base <= c1; base += 8 * (kCombineThreads / 32)) {
+    for (int base = c0 + warp * 8; base <= rec.last; base += 8 * W) {
         const int cc = base + (lane & 7);
-        int64_t at = 0;
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (cc <= c1) {
-            const int64_t from = share_begin(cc, total, ctas);
-            if (from != share_begin(cc + 1, total, ctas)) {              // not an empty share
-                at = (2 * int64_t(cc) + (from > first ? 0 : 1)) * p.rows + col;
-                ml = part_ml[at];
-            }
-        }
+        // the first piece is the last one its CTA left, the others are the first of theirs
+        const int64_t at = (2 * int64_t(min(cc, rec.last)) + (cc == c0 ? 1 : 0)) * R + col;
+        float2 ml = part_ml[at];
+        if (cc > rec.last) ml = make_float2(-INFINITY, 0.f);
         float m2 = ml.x;
         m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, 1));
         m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, 2));
         m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, 4));
         m2 = fmaxf(m2, m);
-        const float ref = m2 == -INFINITY ? 0.f : m2, f0 = ex2(m - ref), f1 = ml.y == 0.f ? 0.f : ml.x == -INFINITY ? 1.f : ex2(ml.x - ref);   // (a NaN sum goes through)
+        const float ref = m2 == -INFINITY ? 0.f : m2, f0 = ex2(m - ref);
+        const float f1 = ml.y == 0.f ? 0.f : ml.x == -INFINITY ? 1.f : ex2(ml.x - ref);       // (a NaN sum goes through)
         float v[8][V], f[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -665,7 +694,7 @@ kv_combine_kernel(Plan p, int ctas, QT* __restrict__ out, int64_t out_stride, fl
         for (int i = 0; i < V; ++i) o[i] *= f0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            l = fmaf(f[j], __shfl_sync(0xffffffffu, ml.y, j), l);
+            l = f[j] != 0.f ? fmaf(f[j], __shfl_sync(0xffffffffu, ml.y, j), l) : l;
 #pragma unroll
             for (int i = 0; i < V; ++i) o[i] = fmaf(f[j], v[j][i], o[i]);
         }
@@ -677,16 +706,18 @@ kv_combine_kernel(Plan p, int ctas, QT* __restrict__ out, int64_t out_stride, fl
     __syncthreads();
     m = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kCombineThreads / 32; ++w) m = fmaxf(m, s_ml[w][0]);
+    for (int w = 0; w < W; ++w) m = fmaxf(m, s_ml[w][0]);
     const float ref = m == -INFINITY ? 0.f : m;
     l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kCombineThreads / 32; ++w) l += ex2(s_ml[w][0] - ref) * s_ml[w][1];
+    for (int w = 0; w < W; ++w) l += ex2(s_ml[w][0] - ref) * s_ml[w][1];
     const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int rr = rec.first_row + col, i = rr / group, head = rec.head + (rr - i * group);
+    const int64_t row = rec.row0 + i;
     for (int d = threadIdx.x; d < D; d += kCombineThreads) {
         float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < kCombineThreads / 32; ++w) v += ex2(s_ml[w][0] - ref) * s_o[w][d];
+        for (int w = 0; w < W; ++w) v += ex2(s_ml[w][0] - ref) * s_o[w][d];
         out[row * out_stride + int64_t(head) * D + d] = QT(v * inv);
     }
     if (lse && threadIdx.x == 0) lse[row * q_heads + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
@@ -703,17 +734,17 @@ int launch(const Cache& c, const Batch& b, const AttnArgs& a, void* workspace, i
     const Plan p{b, c.heads, a.group, NT == 2 ? 4 : 3, S::R, unsigned(a.most_rows)};
     float* part_o = static_cast<float*>(workspace);
     float2* part_ml = reinterpret_cast<float2*>(part_o + size_t(2) * ctas * S::R * D);
+    Record* record = reinterpret_cast<Record*>(part_ml + size_t(2) * ctas * S::R);
     auto kern = kv_split_kernel<QT, D, NT>;
     QLLM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
     kern<<<ctas, kThreads, S::SMEM, st>>>(c, p, static_cast<const QT*>(a.q), a.q_stride, static_cast<QT*>(a.out), a.out_stride, a.scale,
-                                          a.causal, a.lse, part_o, part_ml, status);
+                                          a.causal, a.lse, part_o, part_ml, record, status);
     const int rc = after_launch();
     if (rc != QLLM_OK) return rc;
-    const int64_t rows = b.rows * a.q_heads;
-    if (rows > 0x7fffffff) return QLLM_ERR_UNSUPPORTED;
-    QLLM_CUDA_TRY(launch_dependent(kv_combine_kernel<QT, D>, dim3(unsigned(rows)), dim3(kCombineThreads), 0, st, p, ctas,
-                                   static_cast<QT*>(a.out), a.out_stride, a.lse, static_cast<const float*>(part_o),
-                                   static_cast<const float2*>(part_ml)));
+    const int live = int(std::min<int64_t>(S::R, b.rows * a.group));     // rows that an item can have
+    QLLM_CUDA_TRY(launch_dependent(kv_combine_kernel<QT, D, S::R>, dim3(ctas, live), dim3(kCombineThreads), 0, st, a.group,
+                                   static_cast<QT*>(a.out), a.out_stride, a.lse, a.q_heads, static_cast<const float*>(part_o),
+                                   static_cast<const float2*>(part_ml), static_cast<const Record*>(record)));
     return after_launch();
 }
 
@@ -723,7 +754,8 @@ namespace kv {
 
 int64_t split_workspace(int head_dim, int dtype, int rows_hint) {
     // three CTAs on every SM at most, two pieces each
-    return int64_t(2) * 3 * device_sm_count() * rows_of_item(head_dim, dtype, rows_hint) * (head_dim + 2) * 4;
+    const int64_t ctas = int64_t(3) * device_sm_count();
+    return 2 * ctas * rows_of_item(head_dim, dtype, rows_hint) * (head_dim + 2) * 4 + ctas * int64_t(sizeof(Record));
 }
 
 int launch_attention_split(const Cache& c, const Batch& b, int head_dim, const AttnArgs& a, int rows_hint, void* workspace, int* status,
