@@ -15,7 +15,7 @@
 // transposed (S^T = K Q^T, O^T = V^T P^T) so that 16 tokens or channels fill the 16 rows of the warp-level MMA and the 8
 // query rows its 8 columns: a decode step's few rows waste nothing.  A nibble masked in place is a denormal fp16 number
 // (c 2^-24, or c 2^-20 from the upper half of a byte), which the MMA takes exactly: five logical instructions turn 8 key codes
-// into operands.  Channel and token order inside an operand is free as long as both sides agree, so the codes of one 16-byte
+// (eight of 16-bit units that a transposing load has paired, 16 value codes) into operands.  Channel and token order inside an operand is free as long as both sides agree, so the codes of one 16-byte
 // read are used where they lie, and the factor 16 of the upper nibbles is taken out of the queries, or of the output's odd
 // channels at the end.
 //
@@ -49,7 +49,7 @@ constexpr float kPlace = 6.f, kSlack = 8.f;                // where the largest 
 template <int D, int NT, bool F32>
 struct Shape {
     static constexpr int R = 8 * NT;                       // query rows of an item
-    static constexpr int KW = D / 32, VW = D / 64, MT = D / 16;
+    static constexpr int MT = D / 16;
     static constexpr int STAGE = T * (D + 16);
     static constexpr int STAGES = D == 256 ? 2 : 3;
     static constexpr int OROW = D + 4;                     // floats of a merged row (padded)
@@ -220,9 +220,11 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                  "l"(src), "r"(bytes), "r"(ptx::smem_addr(bar))
                  : "memory");
 }
-// Row r of an 8-token block of the MMA holds token order(r) of it: neighbours differ in parity and the even rows' tokens do
-// too, which spreads the key reads (rows 2i, 2i + 1 in a phase) and the value reads (rows 0, 2, 4, 6) over the banks.
-__device__ __forceinline__ int order(int r) { return r ^ ((r >> 1) & 1); }
+// Four 8 x 8 matrices of 16-bit units, transposed: lane (r, t) receives unit r of rows 2t and 2t + 1 of each.
+__device__ __forceinline__ void load_units(const uint8_t* p, uint32_t (&x)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(ptx::smem_addr(p)) : "memory");
+}
 
 // The query row of column `r` as B operands; what a unit of the sums made with them stands for, and the row's sum in those units.
 template <typename QT, int D, bool F32>
@@ -269,9 +271,7 @@ __device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi
 
 template <int W>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
-    if constexpr (W == 1) {
-        w[0] = *reinterpret_cast<const uint32_t*>(p);
-    } else if constexpr (W == 2) {
+    if constexpr (W == 2) {
         const uint2 v = *reinterpret_cast<const uint2*>(p);
         w[0] = v.x; w[1] = v.y;
     } else {
@@ -296,19 +296,18 @@ struct State {
 template <int D, int NT, bool F32, bool MASKED>
 __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, const uint8_t* vc, const float2* kp, int first, int len,
                                      uint32_t there, int r, int t) {
-    constexpr int KW = D / 32, VW = D / 64, MT = D / 16;
-    const int rt = order(r);
-    float s[NT][2][4];
+    constexpr int KW = D / 32, MT = D / 16;
+    float s[NT][2][4], s2[NT][2][4];                       // two chains of MMAs each: their latency bounds a warp
     // ---- S^T = K Q^T, 16 tokens at a time
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
         uint32_t w0[KW], w1[KW];
-        load_words<KW>(kc + (b * 16 + rt) * (D / 2) + t * (D / 8), w0);
-        load_words<KW>(kc + (b * 16 + 8 + rt) * (D / 2) + t * (D / 8), w1);
+        load_words<KW>(kc + (b * 16 + r) * (D / 2) + t * (D / 8), w0);
+        load_words<KW>(kc + (b * 16 + 8 + r) * (D / 2) + t * (D / 8), w1);
 #pragma unroll
         for (int a = 0; a < NT; ++a)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[a][b][e] = 0.f;
+            for (int e = 0; e < 4; ++e) s[a][b][e] = s2[a][b][e] = 0.f;
 #pragma unroll
         for (int i = 0; i < KW; ++i) {
             const uint32_t u0 = w0[i] >> 8, u1 = w1[i] >> 8;
@@ -317,10 +316,10 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
 #pragma unroll
             for (int a = 0; a < NT; ++a) {
                 mma_f16(s[a][b], a0, a1, a2, a3, st.qh[a][4 * i], st.qh[a][4 * i + 1]);
-                mma_f16(s[a][b], c0, c1, c2, c3, st.qh[a][4 * i + 2], st.qh[a][4 * i + 3]);
+                mma_f16(s2[a][b], c0, c1, c2, c3, st.qh[a][4 * i + 2], st.qh[a][4 * i + 3]);
                 if (F32) {
                     mma_f16(s[a][b], a0, a1, a2, a3, st.ql[a][4 * i], st.ql[a][4 * i + 1]);
-                    mma_f16(s[a][b], c0, c1, c2, c3, st.ql[a][4 * i + 2], st.ql[a][4 * i + 3]);
+                    mma_f16(s2[a][b], c0, c1, c2, c3, st.ql[a][4 * i + 2], st.ql[a][4 * i + 3]);
                 }
             }
         }
@@ -331,7 +330,7 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
     for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int tok = b * 16 + h * 8 + rt;
+            const int tok = b * 16 + h * 8 + r;
             const float2 kk = kp[tok], vv = kp[T + tok];
             vs[b][h] = vv.x;
             vz[b][h] = vv.y;
@@ -340,10 +339,10 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
 #pragma unroll
             for (int a = 0; a < NT; ++a)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) s[a][b][2 * h + e] = kk.x * fmaf(-kk.y, st.qr[a][e], s[a][b][2 * h + e]);
+                for (int e = 0; e < 2; ++e) s[a][b][2 * h + e] = kk.x * fmaf(-kk.y, st.qr[a][e], s[a][b][2 * h + e] + s2[a][b][2 * h + e]);
         }
     auto hidden = [&](int b, int h, int a, int e) {
-        const int tok = first + b * 16 + h * 8 + rt;
+        const int tok = first + b * 16 + h * 8 + r;
         return MASKED && (tok >= len || tok >= st.limit[a][e] || !((there >> (2 * b + h)) & 1u));
     };
     uint32_t ph[NT][4], pl[NT][F32 ? 4 : 1];               // weights as B operands of the second product
@@ -410,33 +409,29 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
                 }
             }
     }
-    // ---- O^T += V^T P^T: this lane's channels are D/8 r .. D/8 r + D/8 - 1
-    const int ka = order(2 * t), kb = order(2 * t + 1);
+    // ---- O^T += V^T P^T.  The transposing load pairs a 16-bit unit (4 channels) of two tokens in a register: lane (r, t)
+    // gets channels 32 g + 4 r .. + 3 of tokens 2t, 2t + 1; two of them make an m16 tile's rows r and r + 8
+    const int lane = 4 * r + t;
+    const uint8_t* mine = vc + ((lane >> 3 & 1) * 8 + (lane & 7)) * (D / 2) + (lane >> 4) * 16;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        uint32_t v[4][VW];
-        load_words<VW>(vc + (b * 16 + ka) * (D / 2) + r * (D / 16), v[0]);
-        load_words<VW>(vc + (b * 16 + kb) * (D / 2) + r * (D / 16), v[1]);
-        load_words<VW>(vc + (b * 16 + 8 + ka) * (D / 2) + r * (D / 16), v[2]);
-        load_words<VW>(vc + (b * 16 + 8 + kb) * (D / 2) + r * (D / 16), v[3]);
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < VW; ++i)
+        for (int g = 0; g < D / 32; g += 2) {
+            uint32_t x[4];
+            load_units(mine + b * 16 * (D / 2) + g * 16, x);
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                const uint32_t x0 = __byte_perm(v[0][i], v[1][i], y ? 0x7632 : 0x5410);
-                const uint32_t x1 = __byte_perm(v[2][i], v[3][i], y ? 0x7632 : 0x5410);
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
-                    const uint32_t y0 = z ? x0 >> 8 : x0, y1 = z ? x1 >> 8 : x1;
-                    const int m = 4 * i + 2 * y + z;
+                    const uint32_t y0 = z ? x[2 * i] >> 8 : x[2 * i], y1 = z ? x[2 * i + 1] >> 8 : x[2 * i + 1];
+                    const int m = 2 * (g + i) + z;
 #pragma unroll
                     for (int a = 0; a < NT; ++a) {
                         mma_f16(st.o[a][m], y0 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x000F000Fu, y1 & 0x00F000F0u, ph[a][2 * b], ph[a][2 * b + 1]);
                         if (F32) mma_f16(st.o[a][m], y0 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x000F000Fu, y1 & 0x00F000F0u, pl[a][2 * b], pl[a][2 * b + 1]);
                     }
                 }
-            }
-    }
+        }
 }
 
 template <typename QT, int D, int NT>
@@ -600,10 +595,10 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
                     m_top[warp * R + a * 8 + 2 * t + e] = st.top[a][e];
                     m_l[warp * R + a * 8 + 2 * t + e] = st.l[a][e];
                 }
-                float* row = m_o + (warp * R + a * 8 + 2 * t + e) * S::OROW + r * (D / 8);
+                float* row = m_o + (warp * R + a * 8 + 2 * t + e) * S::OROW + 4 * r;
 #pragma unroll
                 for (int m = 0; m < S::MT; m += 2)
-                    *reinterpret_cast<float4*>(row + 2 * m) =
+                    *reinterpret_cast<float4*>(row + 16 * m) =
                         make_float4(fmaf(st.o[a][m][e], 16777216.f, -st.zs[a][e]), fmaf(st.o[a][m][2 + e], 1048576.f, -st.zs[a][e]),
                                     fmaf(st.o[a][m + 1][e], 16777216.f, -st.zs[a][e]), fmaf(st.o[a][m + 1][2 + e], 1048576.f, -st.zs[a][e]));
             }
