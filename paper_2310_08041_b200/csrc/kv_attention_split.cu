@@ -22,7 +22,7 @@
 // Precision: queries are scaled by a power of two per row into fp16's range (a bf16 query's 8 bits stay exact) and float32
 // queries are split in two; weights p_j vs_j are rounded to fp16, 11 bits, for bf16 results (which carry 8) and split in two
 // for float32 ones.  So that no weight leaves fp16's range whatever the value scales are, the running maximum is that of
-// s_j + log2 vs_j (the logarithm cut to +-80), with the largest weight placed at 2^6; it moves only when a weight would pass 2^14,
+// s_j + log2 vs_j (the logarithm cut to +-80; its integer part for float32), with the largest weight placed at 2^6; it moves only when a weight would pass 2^14,
 // which spares most steps the reduction over lanes and the rescaling.  Sums, maxima and zero-point corrections are float32.
 
 #include <cuda_fp16.h>
@@ -325,7 +325,7 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
         }
     }
     // ---- s becomes y, score = qn y in base 2, of tokens (block b, half h) and columns 2t, 2t + 1
-    float vs[2][2], vz[2][2], ve[2][2];
+    float vs[2][2], vz[2][2], ve[2][2], down[2][2];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -334,7 +334,16 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
             const float2 kk = kp[tok], vv = kp[T + tok];
             vs[b][h] = vv.x;
             vz[b][h] = vv.y;
-            ve[b][h] = fminf(fmaxf(lg2(fabsf(vv.x)), -80.f), 80.f) - kPlace;
+            if constexpr (F32) {
+                // the exponent alone, taken out of the weight exactly: the difference that enters the exponential is small
+                // wherever the weight counts, and loses nothing to the size of the logarithm
+                const int eb = min(max(int((__float_as_uint(vv.x) >> 23) & 255u), 127 - 80), 127 + 80);
+                ve[b][h] = __int_as_float(0x4B000000 | eb) - 8388735.f;
+                down[b][h] = __int_as_float((254 - eb) << 23);
+                vs[b][h] = vv.x * down[b][h];
+            } else {
+                ve[b][h] = fminf(fmaxf(lg2(fabsf(vv.x)), -80.f), 80.f);
+            }
             if (MASKED && (first + tok >= len || !((there >> (2 * b + h)) & 1u))) vs[b][h] = vz[b][h] = 0.f;
 #pragma unroll
             for (int a = 0; a < NT; ++a)
@@ -361,7 +370,7 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
                 }
         }
         // the reference moves only when a weight would pass 2^kSlack times its place
-        if (__any_sync(0xffffffffu, m[0] > st.top[a][0] + kSlack || m[1] > st.top[a][1] + kSlack)) {
+        if (__any_sync(0xffffffffu, m[0] > st.top[a][0] + (kPlace + kSlack) || m[1] > st.top[a][1] + (kPlace + kSlack))) {
             float fix[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -369,7 +378,7 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                x = fmaxf(x, st.top[a][e]);
+                x = fmaxf(x - kPlace, st.top[a][e]);
                 fix[e] = x == -INFINITY ? 1.f : ex2(st.top[a][e] - x);
                 st.top[a][e] = x;
                 st.l[a][e] *= fix[e];
@@ -389,9 +398,9 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
                 for (int h = 0; h < 2; ++h) {
                     // a hidden key's parameters may be anything
                     const bool gone = hidden(b, h, a, e);
-                    const float pw = gone ? 0.f : ex2(fmaf(s[a][b][2 * h + e], st.qn[a][e], -at));
+                    const float pw = gone ? 0.f : ex2(fmaf(s[a][b][2 * h + e], st.qn[a][e], F32 ? ve[b][h] - at : -at));
                     const float w = gone ? 0.f : pw * vs[b][h];
-                    st.l[a][e] += pw;
+                    st.l[a][e] = F32 ? fmaf(pw, down[b][h], st.l[a][e]) : st.l[a][e] + pw;
                     st.zs[a][e] = gone ? st.zs[a][e] : fmaf(w, vz[b][h], st.zs[a][e]);
                     s[a][b][2 * h + e] = w;
                 }
@@ -459,7 +468,7 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
     }
-    if (blockIdx.x == 0) p.b.report(status);
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // launched as a dependent: nothing above touched global memory
     int seq;
     int64_t before;
     const int64_t total = locate(p, s_plan, blockIdx.x, gridDim.x, seq, before);
@@ -480,35 +489,39 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
 
     if (warp == kWarps) {
         // ---------------------------------------------------------------- producer: lane = 4 * piece + array
-        const int piece = lane >> 2, array = lane & 3, piece_tokens = 1 << piece_log2, log2p = p.b.page_log2;
+        // The page ids of 32 pieces ahead are held across the lanes, and the 32 behind those are on their way: a load from
+        // the table in front of every tile's copies would cost the tile its latency.
+        const int piece = lane >> 2, array = lane & 3, log2p = p.b.page_log2, per_tile = T >> piece_log2;
+        const uint32_t bytes = uint32_t(array & 1 ? 8 : D / 2) << piece_log2;
+        uint8_t* place = smem + (array == 0 ? 0 : array == 2 ? HALF : array == 1 ? 2 * HALF : 2 * HALF + T * 8) + min(piece, per_tile - 1) * bytes;
+        const uint8_t* source = array == 0 ? c.kc : array == 2 ? c.vc : reinterpret_cast<const uint8_t*>(array == 1 ? c.kp : c.vp);
+        const int row_bytes = array & 1 ? 8 : D / 2;
         int issued = 0;
         bool ok = true;
         while (ok && walk.next(it)) {
             const int32_t* row = p.b.table + int64_t(it.s) * p.b.width;
-            for (int j = it.tile; j < it.tile + it.count; ++j) {
-                const int t0 = j * T + (piece << piece_log2);
-                if (j * T >= it.keys) break;               // nothing there that a row of this item sees
-                const bool mine = (piece << piece_log2) < T && t0 < it.keys;
-                const int page = mine ? row[t0 >> log2p] : 0;
-                const bool good = mine && page >= 0 && page < c.pages;
+            const int pieces = int((unsigned(it.keys) + (1u << piece_log2) - 1) >> piece_log2), stop = min(it.tile + it.count, (pieces + per_tile - 1) / per_tile);
+            auto page_of = [&](int q) { return q < pieces ? row[(int64_t(q) << piece_log2) >> log2p] : 0; };
+            int q0 = it.tile * per_tile, held = page_of(q0 + lane), ahead = page_of(q0 + 32 + lane);
+            for (int j = it.tile; j < stop; ++j) {         // tiles that a row of this item sees
+                const int q = j * per_tile + piece;
+                if (j * per_tile - q0 >= 32) {
+                    q0 += 32;
+                    held = ahead;
+                    ahead = page_of(q0 + 32 + lane);
+                }
+                const int page = __shfl_sync(0xffffffffu, held, q - q0);
+                const bool mine = piece < per_tile && q < pieces, good = mine && page >= 0 && page < c.pages;
                 if (mine && !good) raise_page(status);
-                const uint32_t bytes = uint32_t(piece_tokens) * ((array & 1) ? 8 : D / 2);
                 const uint32_t got = __ballot_sync(0xffffffffu, good), total_bytes = __reduce_add_sync(0xffffffffu, good ? bytes : 0);
+                const int64_t r = c.row(page, it.g, (q << piece_log2) & ((1 << log2p) - 1));
                 if (!wait_bounded(&s_empty[sg], turn ^ 1, ab)) { ok = false; break; }
                 if (lane == 0) {
                     s_pieces[sg] = got;
                     ptx::mbar_arrive_expect_tx(&s_full[sg], total_bytes);
                 }
                 __syncwarp();
-                if (good) {
-                    const int64_t r = c.row(page, it.g, t0 & ((1 << log2p) - 1));
-                    uint8_t* base = smem + sg * S::STAGE;
-                    const int place = piece << piece_log2;
-                    if (array == 0) bulk_load(base + place * (D / 2), c.kc + r * (D / 2), bytes, &s_full[sg]);
-                    else if (array == 2) bulk_load(base + HALF + place * (D / 2), c.vc + r * (D / 2), bytes, &s_full[sg]);
-                    else if (array == 1) bulk_load(base + 2 * HALF + place * 8, c.kp + r, bytes, &s_full[sg]);
-                    else bulk_load(base + 2 * HALF + T * 8 + place * 8, c.vp + r, bytes, &s_full[sg]);
-                }
+                if (good) bulk_load(place + sg * S::STAGE, source + r * row_bytes, bytes, &s_full[sg]);
                 advance();
                 ++issued;
             }
@@ -652,11 +665,12 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
 // the record that share's CTA left.  Its four warps take 8 pieces at a time: a lane looks each up, then all loads are in flight.
 template <typename QT, int D, int R>
 __global__ void __launch_bounds__(kCombineThreads)
-kv_combine_kernel(int group, QT* __restrict__ out, int64_t out_stride, float* __restrict__ lse, int q_heads, const float* __restrict__ part_o,
+kv_combine_kernel(Batch b, int* status, int group, QT* __restrict__ out, int64_t out_stride, float* __restrict__ lse, int q_heads, const float* __restrict__ part_o,
                   const float2* __restrict__ part_ml, const Record* __restrict__ record) {
     constexpr int V = D / 32, W = kCombineThreads / 32;
     __shared__ float s_ml[W][2], s_o[W][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c0 = blockIdx.x, col = blockIdx.y;
+    if (c0 == 0 && col == 0) b.report(status);
     asm volatile("griddepcontrol.wait;" ::: "memory");     // in every CTA: this kernel is not over before the one it depends on
     const Record rec = record[c0];
     if (col >= rec.rows) return;
@@ -732,12 +746,12 @@ int launch(const Cache& c, const Batch& b, const AttnArgs& a, void* workspace, i
     Record* record = reinterpret_cast<Record*>(part_ml + size_t(2) * ctas * S::R);
     auto kern = kv_split_kernel<QT, D, NT>;
     QLLM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
-    kern<<<ctas, kThreads, S::SMEM, st>>>(c, p, static_cast<const QT*>(a.q), a.q_stride, static_cast<QT*>(a.out), a.out_stride, a.scale,
-                                          a.causal, a.lse, part_o, part_ml, record, status);
+    QLLM_CUDA_TRY(launch_dependent(kern, dim3(ctas), dim3(kThreads), S::SMEM, st, c, p, static_cast<const QT*>(a.q), a.q_stride,
+                                   static_cast<QT*>(a.out), a.out_stride, a.scale, a.causal, a.lse, part_o, part_ml, record, status));
     const int rc = after_launch();
     if (rc != QLLM_OK) return rc;
     const int live = int(std::min<int64_t>(S::R, b.rows * a.group));     // rows that an item can have
-    QLLM_CUDA_TRY(launch_dependent(kv_combine_kernel<QT, D, S::R>, dim3(ctas, live), dim3(kCombineThreads), 0, st, a.group,
+    QLLM_CUDA_TRY(launch_dependent(kv_combine_kernel<QT, D, S::R>, dim3(ctas, live), dim3(kCombineThreads), 0, st, b, status, a.group,
                                    static_cast<QT*>(a.out), a.out_stride, a.lse, a.q_heads, static_cast<const float*>(part_o),
                                    static_cast<const float2*>(part_ml), static_cast<const Record*>(record)));
     return after_launch();

@@ -12,6 +12,11 @@ pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 
 
+@pytest.fixture(autouse=True)
+def seeded():
+    torch.manual_seed(7)
+
+
 def host(t):
     return t.float().cpu().numpy().astype(np.float64)
 
@@ -255,13 +260,15 @@ def test_attention_rows_far_from_zero(dtype, news):
     run_case(22, dtype, 64, 64, 2, 4, [300, 200, 65], news, True, scale=1e-8, zeros=(-4000000, 4000000), rounded_codes=True)
 
 
+@pytest.mark.parametrize("seed", range(6))
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("news", [[1, 1], [150, 70]])
-def test_attention_scales_of_every_size(dtype, news):
+def test_attention_scales_of_every_size(dtype, news, seed):
     """Value scales from 1e-12 to 1e12 between tokens, key scales such that weights run over many decades; query rows of very
     different size."""
     lens, page, d, heads, group = [500, 130], 64, 128, 2, 4
     rng = np.random.RandomState(23)
+    torch.manual_seed(seed)
     table = make_table(rng, lens, page, 12)
     cache = random_cache(23, 1, 12, heads, page, d)
     cache.v_param[..., 0] *= 10.0 ** torch.randint(-12, 13, cache.v_param.shape[:-1], device=G.DEV).float()
