@@ -382,7 +382,7 @@ int qllm_layer_workspace(qllm_layer_t* layer, uint8_t** codes, float** a_scale, 
  *   k_codes, v_codes  uint8 [layers][pages][kv_heads][page_size][head_dim / 2], byte i of a row holds channel 2i in its
  *                     low nibble and channel 2i + 1 in its high nibble (the 4-bit layout of qllm_quantize_rows)
  *   k_param, v_param  float [layers][pages][kv_heads][page_size][2]: scale alpha, zero-point; value = alpha (code - zero)
- * page_size is 16, 32, 64, 128 or 256, head_dim 64, 128 or 256 (QLLM_ERR_UNSUPPORTED otherwise); all four arrays are 16-byte
+ * page_size is 16, 32, 64, 128 or 256, head_dim 64, 128 or 256, kv_heads at most 1024 (QLLM_ERR_UNSUPPORTED otherwise); all four arrays are 16-byte
  * aligned.  A token's keys and values take 2 (head_dim / 2 + 8) bytes per head.
  *
  * A BATCH names the sequences that a call works on and their newest tokens:

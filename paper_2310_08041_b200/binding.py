@@ -119,8 +119,14 @@ def _hp(a):
     return None if a is None else a.ctypes.data_as(_vp)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:                      # the handle without a Stream object around it
+            return _raw_stream(_current_device())
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -466,28 +472,32 @@ class KvPool:
                    torch.zeros(seqs, dtype=torch.int32, device=device))
 
 
-def _packed(t, rows, heads, head_dim):
+def _packed(t, shape):
     """Address and row stride of a packed tensor [rows][heads][head_dim]: any row stride, the rest contiguous."""
     assert t.is_cuda, "device arguments must be CUDA tensors"
-    _want(tuple(t.shape) == (rows, heads, head_dim))
-    st = t.stride()
-    _want(st[2] == 1 and (st[1] == head_dim or heads == 1))
-    return t.data_ptr(), st[0] if rows > 1 else max(st[0], heads * head_dim)
+    if t.shape != shape:
+        raise QllmError(QLLM_ERR_SHAPE)
+    row, head, one = t.stride()
+    if one != 1 or (head != shape[2] and shape[1] != 1):
+        raise QllmError(QLLM_ERR_SHAPE)
+    return t.data_ptr(), row if shape[0] > 1 else max(row, shape[1] * shape[2])
 
 
 def qllm_kv_append(cache, layer, k, v, batch, stream=None):
     """k, v [rows][kv_heads][head_dim] (any row stride): the batch's new tokens, quantized into the cache."""
-    kp, ks = _packed(k, batch.rows, cache.kv_heads, cache.head_dim)
-    vp, vs = _packed(v, batch.rows, cache.kv_heads, cache.head_dim)
-    _want(k.dtype == v.dtype)
+    shape = (batch.rows, cache.kv_heads, cache.head_dim)
+    kp, ks = _packed(k, shape)
+    vp, vs = _packed(v, shape)
+    _want(k.dtype is v.dtype)
     _check(_lib.qllm_kv_append(cache._p, layer, kp, ks, vp, vs, _xdtype(k), batch._p, _stream(stream)))
 
 
 def qllm_kv_read(cache, layer, k, v, batch, stream=None):
     """The stored values of the batch's tokens into k, v [rows][kv_heads][head_dim]."""
-    kp, ks = _packed(k, batch.rows, cache.kv_heads, cache.head_dim)
-    vp, vs = _packed(v, batch.rows, cache.kv_heads, cache.head_dim)
-    _want(k.dtype == v.dtype)
+    shape = (batch.rows, cache.kv_heads, cache.head_dim)
+    kp, ks = _packed(k, shape)
+    vp, vs = _packed(v, shape)
+    _want(k.dtype is v.dtype)
     _check(_lib.qllm_kv_read(cache._p, layer, kp, ks, vp, vs, _xdtype(k), batch._p, _stream(stream)))
 
 
@@ -501,10 +511,12 @@ def qllm_kv_attention_workspace(cache, q_heads, q, batch):
 def qllm_kv_attention(cache, layer, q, out, scale, batch, workspace, causal=True, lse=None, stream=None):
     """q, out [rows][q_heads][head_dim] (any row stride); workspace: uint8 tensor of qllm_kv_attention_workspace bytes; lse: None
     or float32 [rows][q_heads]."""
-    heads = q.shape[1] if q.dim() == 3 else 0
-    qp, qs = _packed(q, batch.rows, heads, cache.head_dim)
-    op, os_ = _packed(out, batch.rows, heads, cache.head_dim)
-    _want(q.dtype == out.dtype)
+    _want(q.dim() == 3)
+    heads = q.shape[1]
+    shape = (batch.rows, heads, cache.head_dim)
+    qp, qs = _packed(q, shape)
+    op, os_ = _packed(out, shape)
+    _want(q.dtype is out.dtype)
     if lse is not None:
         _want(lse.dtype == torch.float32 and tuple(lse.shape) == (batch.rows, heads))
     _check(_lib.qllm_kv_attention(cache._p, layer, qp, qs, op, os_, _xdtype(q), heads, scale, 1 if causal else 0, _dp(lse),

@@ -17,9 +17,17 @@ std::atomic<int64_t> g_launch_count{0};
 __device__ int g_status_word = 0;
 
 int* device_status_word() {
+    static std::atomic<int*> cache[64];                    // the address never changes while the library is loaded
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
+    if (dev >= 0 && dev < 64) {
+        int* known = cache[dev].load(std::memory_order_relaxed);
+        if (known) return known;
+    }
     int* p = nullptr;
     cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&p), g_status_word);
     if (e != cudaSuccess) { cuda_fail(e); return nullptr; }
+    if (dev >= 0 && dev < 64) cache[dev].store(p, std::memory_order_relaxed);
     return p;
 }
 

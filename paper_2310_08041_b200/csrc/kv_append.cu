@@ -2,11 +2,13 @@
 //
 // qllm_kv_append is the per-token quantizer of Eq. 2 on rows of one head, written to the row's place in its page:
 // alpha = (max - min) / 15, zero = -round(min / alpha), code = clamp(round(x / alpha) + zero, 0, 15), with the float32
-// arithmetic of qllm_quantize_rows (the same operations in the same order: the codes are the same).  Both directions
-// move bytes: head_dim values of 2 or 4 bytes on one side, head_dim / 2 + 8 bytes on the other.  head_dim / 8 lanes own
-// a row, 8 channels each: one or two 16-byte accesses of the values, one 32-bit word of codes, the range by shuffles
-// inside the group, whole 32-byte sectors on both sides.  A group takes U rows of keys or values at once (their loads
-// are in flight together, and the search for a row's sequence and page runs under them).
+// arithmetic of qllm_quantize_rows' one-pass kernels (the same operations: the codes are the same).  Both directions move
+// bytes: head_dim values of 2 or 4 bytes on one side, head_dim / 2 + 8 bytes on the other.  head_dim / 8 lanes own a row, 8
+// channels each: one or two 16-byte accesses of the values, one 32-bit word of codes, the range by shuffles inside the
+// group, whole 32-byte sectors on both sides.  A CTA takes a run of tokens: where each belongs (sequence, page, place) is
+// found once per token by one thread, for all of its 2 kv_heads rows, and four rows of a group are in flight together.
+
+#include <algorithm>
 
 #include "kv_cache.cuh"
 #include "reassemble_quant_common.cuh"
@@ -45,120 +47,143 @@ __device__ __forceinline__ uint32_t codes8(const float (&f)[8], float lo, float 
     return p;
 }
 
-// Row units are ordered [packed row][keys, values][head].
-template <typename T, int D, int U>
-__global__ void __launch_bounds__(256)
-kv_append_kernel(const T* __restrict__ k, int64_t k_stride, const T* __restrict__ v, int64_t v_stride, Cache c, Batch b, int* status) {
-    constexpr int L = D / 8, G = 256 / L;                  // lanes of a row, rows of a CTA and step
-    if (blockIdx.x == 0) b.report(status);
-    const int lane = threadIdx.x % L, group = threadIdx.x / L;
-    const int64_t units = b.rows * 2 * c.heads, first = int64_t(blockIdx.x) * (G * U) + group;
-    float f[U][8];
-    bool live[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t r = first + u * G;
-        live[u] = r < units;
-        const int64_t t = live[u] ? r / (2 * c.heads) : 0;
-        const int w = live[u] ? int(r - t * (2 * c.heads)) : 0;
-        const T* p = w < c.heads ? k + t * k_stride + int64_t(w) * D : v + t * v_stride + int64_t(w - c.heads) * D;
-        if (live[u]) load8<T>(p + lane * 8, f[u]);
+constexpr int kMostTokens = 32;                            // of a CTA
+
+// A CTA's run of tokens.  Its row units are ordered [token][keys, values][head].
+struct Run {
+    int tokens;                                            // per CTA
+    uint32_t inverse;                                      // ceil(2^32 / (2 heads)): unit -> token, units < 2^16
+};
+
+// (page, place) of the CTA's tokens in shared memory: page < 0 where the token has none (-1: nobody's row, -2: absent)
+__device__ __forceinline__ void find_places(const Cache& c, const Batch& b, int64_t t0, int n, int2* s_place, int* status) {
+    if (threadIdx.x < n) {
+        int s, page, place = 0;
+        const bool ok = find_place(c, b, t0 + threadIdx.x, s, page, place, status);
+        s_place[threadIdx.x] = make_int2(ok ? page : s < 0 ? -1 : -2, place);
     }
+    __syncthreads();
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256)
+kv_append_kernel(const T* __restrict__ k, int64_t k_stride, const T* __restrict__ v, int64_t v_stride, Cache c, Batch b, Run run, int* status) {
+    constexpr int L = D / 8, G = 256 / L, U = 4;           // lanes of a row, rows of a CTA and step, steps in flight
+    __shared__ int2 s_place[kMostTokens];
+    const int lane = threadIdx.x % L, group = threadIdx.x / L, per_token = 2 * c.heads;
+    const int64_t t0 = int64_t(blockIdx.x) * run.tokens;
+    const int tokens = int(min(int64_t(run.tokens), b.rows - t0)), units = tokens * per_token;
+    for (int base = 0; base < units; base += G * U) {
+        float f[U][8];
+        int tok[U], w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        float lo = INFINITY, hi = -INFINITY;
-        if (live[u]) {
+        for (int u = 0; u < U; ++u) {
+            const int r = base + u * G + group;
+            tok[u] = int(__umulhi(uint32_t(r), run.inverse));
+            w[u] = r - tok[u] * per_token;
+            if (r < units) {
+                const int64_t t = t0 + tok[u];
+                load8<T>((w[u] < c.heads ? k + t * k_stride + int64_t(w[u]) * D : v + t * v_stride + int64_t(w[u] - c.heads) * D) + lane * 8, f[u]);
+            } else {
+                tok[u] = -1;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { lo = fminf(lo, f[u][j]); hi = fmaxf(hi, f[u][j]); }
+                for (int j = 0; j < 8; ++j) f[u][j] = 0.f;
+            }
+        }
+        if (base == 0) {                                   // under the first loads
+            if (blockIdx.x == 0) b.report(status);
+            find_places(c, b, t0, tokens, s_place, status);
         }
 #pragma unroll
-        for (int o = L / 2; o > 0; o >>= 1) {
-            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        for (int u = 0; u < U; ++u) {
+            if (base + u * G >= units) break;              // the whole CTA is done
+            float lo = f[u][0], hi = f[u][0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) { lo = fminf(lo, f[u][j]); hi = fmaxf(hi, f[u][j]); }
+#pragma unroll
+            for (int o = L / 2; o > 0; o >>= 1) {
+                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+            }
+            const int2 at = tok[u] < 0 ? make_int2(-1, 0) : s_place[tok[u]];
+            if (at.x >= 0) {
+                float alpha = (hi - lo) / 15.f;
+                if (!(hi > lo)) alpha = lo != 0.f ? fabsf(lo) : 1.f;
+                const float inv = __frcp_rn(alpha), zero = -rintf(lo * inv);
+                const bool keys = w[u] < c.heads;
+                const int64_t row = c.row(at.x, keys ? w[u] : w[u] - c.heads, at.y);
+                reinterpret_cast<uint32_t*>((keys ? c.kc : c.vc) + row * (D / 2))[lane] = codes8(f[u], lo, hi, inv, zero);
+                if (lane == 0) (keys ? c.kp : c.vp)[row] = make_float2(alpha, zero);
+            }
         }
-        if (!live[u]) continue;
-        const int64_t r = first + u * G, t = r / (2 * c.heads);
-        const int w = int(r - t * (2 * c.heads));
-        int s, page, place;
-        if (!find_place(c, b, t, s, page, place, status)) continue;
-        float alpha = (hi - lo) / 15.f;
-        if (!(hi > lo)) alpha = lo != 0.f ? fabsf(lo) : 1.f;
-        const float inv = __frcp_rn(alpha), zero = -rintf(lo * inv);
-        const bool keys = w < c.heads;
-        const int64_t row = c.row(page, keys ? w : w - c.heads, place);
-        reinterpret_cast<uint32_t*>((keys ? c.kc : c.vc) + row * (D / 2))[lane] = codes8(f[u], lo, hi, inv, zero);
-        if (lane == 0) (keys ? c.kp : c.vp)[row] = make_float2(alpha, zero);
     }
 }
 
-template <typename T, int D, int U>
+template <typename T, int D>
 __global__ void __launch_bounds__(256)
-kv_read_kernel(T* __restrict__ k, int64_t k_stride, T* __restrict__ v, int64_t v_stride, Cache c, Batch b, int* status) {
-    constexpr int L = D / 8, G = 256 / L;
+kv_read_kernel(T* __restrict__ k, int64_t k_stride, T* __restrict__ v, int64_t v_stride, Cache c, Batch b, Run run, int* status) {
+    constexpr int L = D / 8, G = 256 / L, U = 4;
+    __shared__ int2 s_place[kMostTokens];
+    const int lane = threadIdx.x % L, group = threadIdx.x / L, per_token = 2 * c.heads;
+    const int64_t t0 = int64_t(blockIdx.x) * run.tokens;
+    const int tokens = int(min(int64_t(run.tokens), b.rows - t0)), units = tokens * per_token;
     if (blockIdx.x == 0) b.report(status);
-    const int lane = threadIdx.x % L, group = threadIdx.x / L;
-    const int64_t units = b.rows * 2 * c.heads, first = int64_t(blockIdx.x) * (G * U) + group;
-    uint32_t word[U];
-    float2 prm[U];
-    bool live[U];
+    find_places(c, b, t0, tokens, s_place, status);
+    for (int base = 0; base < units; base += G * U) {
+        uint32_t word[U];
+        float2 prm[U];
+        int tok[U], w[U], page[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t r = first + u * G, t = r / (2 * c.heads);
-        const int w = int(r - t * (2 * c.heads));
-        int s = -1, page, place;
-        word[u] = 0;
-        prm[u] = make_float2(0.f, 0.f);
-        if (r < units && find_place(c, b, t, s, page, place, status)) {
-            const bool keys = w < c.heads;
-            const int64_t row = c.row(page, keys ? w : w - c.heads, place);
-            word[u] = reinterpret_cast<const uint32_t*>((keys ? c.kc : c.vc) + row * (D / 2))[lane];
-            prm[u] = (keys ? c.kp : c.vp)[row];
+        for (int u = 0; u < U; ++u) {
+            const int r = base + u * G + group;
+            tok[u] = int(__umulhi(uint32_t(r), run.inverse));
+            w[u] = r - tok[u] * per_token;
+            const int2 at = r < units ? s_place[tok[u]] : make_int2(-1, 0);
+            page[u] = at.x;
+            word[u] = 0;
+            prm[u] = make_float2(0.f, 0.f);
+            if (at.x >= 0) {
+                const bool keys = w[u] < c.heads;
+                const int64_t row = c.row(at.x, keys ? w[u] : w[u] - c.heads, at.y);
+                word[u] = reinterpret_cast<const uint32_t*>((keys ? c.kc : c.vc) + row * (D / 2))[lane];
+                prm[u] = (keys ? c.kp : c.vp)[row];
+            }
         }
-        live[u] = s >= 0;
-    }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        if (!live[u]) continue;
-        const int64_t r = first + u * G, t = r / (2 * c.heads);
-        const int w = int(r - t * (2 * c.heads));
-        float f[8];
+        for (int u = 0; u < U; ++u) {
+            if (page[u] == -1) continue;
+            const int64_t t = t0 + tok[u];
+            float f[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = (float((word[u] >> (4 * j)) & 15u) - prm[u].y) * prm[u].x;
-        store8((w < c.heads ? k + t * k_stride + int64_t(w) * D : v + t * v_stride + int64_t(w - c.heads) * D) + lane * 8, f);
+            for (int j = 0; j < 8; ++j) f[j] = (float((word[u] >> (4 * j)) & 15u) - prm[u].y) * prm[u].x;
+            store8((w[u] < c.heads ? k + t * k_stride + int64_t(w[u]) * D : v + t * v_stride + int64_t(w[u] - c.heads) * D) + lane * 8, f);
+        }
     }
 }
 
-// Four rows per group once that still gives every SM two CTAs; single rows below (more CTAs, shorter latency).
-inline bool four_rows(int64_t units, int rows_per_step) {
-    return units >= int64_t(device_sm_count()) * 2 * 4 * rows_per_step;
+// Tokens of a CTA: as many as keep eight CTAs on every SM, at most 1024 rows' worth (unit numbers stay below 2^16) and at least
+// one step's worth where a token has few rows.
+inline Run run_of(const Batch& b, int heads, int rows_per_step) {
+    const int per_token = 2 * heads;
+    int64_t n = b.rows / (int64_t(device_sm_count()) * 8);
+    n = std::min<int64_t>(n, std::max(1, 16 * rows_per_step / per_token));
+    n = std::max<int64_t>(n, std::min(rows_per_step / per_token, 8));
+    n = std::min<int64_t>(std::max<int64_t>(n, 1), kMostTokens);
+    return Run{int(n), uint32_t(((uint64_t(1) << 32) + per_token - 1) / per_token)};
 }
 
 template <typename T, int D>
 int launch_append(const void* k, int64_t ks, const void* v, int64_t vs, const Cache& c, const Batch& b, int* status, cudaStream_t st) {
-    constexpr int G = 256 / (D / 8);
-    const int64_t units = b.rows * 2 * c.heads;
-    const T *kp = static_cast<const T*>(k), *vp = static_cast<const T*>(v);
-    if (four_rows(units, G)) {
-        const int64_t grid = (units + 4 * G - 1) / (4 * G);
-        if (grid > 0x7fffffff) return QLLM_ERR_UNSUPPORTED;
-        kv_append_kernel<T, D, 4><<<unsigned(grid), 256, 0, st>>>(kp, ks, vp, vs, c, b, status);
-    } else {
-        kv_append_kernel<T, D, 1><<<unsigned((units + G - 1) / G), 256, 0, st>>>(kp, ks, vp, vs, c, b, status);
-    }
+    const Run run = run_of(b, c.heads, 256 / (D / 8));
+    kv_append_kernel<T, D><<<unsigned((b.rows + run.tokens - 1) / run.tokens), 256, 0, st>>>(
+        static_cast<const T*>(k), ks, static_cast<const T*>(v), vs, c, b, run, status);
     return after_launch();
 }
 template <typename T, int D>
 int launch_read(void* k, int64_t ks, void* v, int64_t vs, const Cache& c, const Batch& b, int* status, cudaStream_t st) {
-    constexpr int G = 256 / (D / 8);
-    const int64_t units = b.rows * 2 * c.heads;
-    T *kp = static_cast<T*>(k), *vp = static_cast<T*>(v);
-    if (four_rows(units, G)) {
-        const int64_t grid = (units + 4 * G - 1) / (4 * G);
-        if (grid > 0x7fffffff) return QLLM_ERR_UNSUPPORTED;
-        kv_read_kernel<T, D, 4><<<unsigned(grid), 256, 0, st>>>(kp, ks, vp, vs, c, b, status);
-    } else {
-        kv_read_kernel<T, D, 1><<<unsigned((units + G - 1) / G), 256, 0, st>>>(kp, ks, vp, vs, c, b, status);
-    }
+    const Run run = run_of(b, c.heads, 256 / (D / 8));
+    kv_read_kernel<T, D><<<unsigned((b.rows + run.tokens - 1) / run.tokens), 256, 0, st>>>(
+        static_cast<T*>(k), ks, static_cast<T*>(v), vs, c, b, run, status);
     return after_launch();
 }
 

@@ -744,8 +744,8 @@ int launch(const Cache& c, const Batch& b, const AttnArgs& a, void* workspace, i
     float* part_o = static_cast<float*>(workspace);
     float2* part_ml = reinterpret_cast<float2*>(part_o + size_t(2) * ctas * S::R * D);
     Record* record = reinterpret_cast<Record*>(part_ml + size_t(2) * ctas * S::R);
-    auto kern = kv_split_kernel<QT, D, NT>;
-    QLLM_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+    constexpr auto kern = &kv_split_kernel<QT, D, NT>;
+    QLLM_CUDA_TRY(allow_smem<kern>(S::SMEM));
     QLLM_CUDA_TRY(launch_dependent(kern, dim3(ctas), dim3(kThreads), S::SMEM, st, c, p, static_cast<const QT*>(a.q), a.q_stride,
                                    static_cast<QT*>(a.out), a.out_stride, a.scale, a.causal, a.lse, part_o, part_ml, record, status));
     const int rc = after_launch();

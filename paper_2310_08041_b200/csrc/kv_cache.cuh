@@ -104,7 +104,7 @@ inline bool head_dim_ok(int d) { return d == 64 || d == 128 || d == 256; }
 inline int check_cache(const qllm_kv_cache_t* c) {
     if (!c) return QLLM_ERR_NULL;
     if (c->layers <= 0 || c->pages <= 0 || c->kv_heads <= 0 || c->page_size <= 0 || c->head_dim <= 0) return QLLM_ERR_SHAPE;
-    if (page_log2(c->page_size) < 0 || !head_dim_ok(c->head_dim) || c->kv_heads > 65535) return QLLM_ERR_UNSUPPORTED;
+    if (page_log2(c->page_size) < 0 || !head_dim_ok(c->head_dim) || c->kv_heads > 1024) return QLLM_ERR_UNSUPPORTED;
     if (!c->k_codes || !c->k_param || !c->v_codes || !c->v_param) return QLLM_ERR_NULL;
     if (!aligned16(c->k_codes) || !aligned16(c->k_param) || !aligned16(c->v_codes) || !aligned16(c->v_param)) return QLLM_ERR_ALIGN;
     return QLLM_OK;

@@ -384,7 +384,7 @@ extern "C" int qllm_kv_pages_fork(const qllm_kv_cache_t* cache, const qllm_kv_po
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const Pool p = pool_of(pool, kv::page_log2(cache->page_size));
     const size_t smem = (size_t(pool->seqs) + 2 * size_t(n)) * 4;
-    QLLM_CUDA_TRY(cudaFuncSetAttribute(kv_fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kPoolMax * 4));
+    QLLM_CUDA_TRY(allow_smem<&kv_fork_kernel>(3 * kPoolMax * 4));
     kv_fork_kernel<<<1, kThreads, smem, st>>>(p, parent, child, n, fresh, status);
     const int rc1 = after_launch();
     if (rc1 != QLLM_OK) return rc1;

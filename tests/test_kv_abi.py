@@ -42,7 +42,7 @@ def attention(c, b, layer=0, q=ONE, qs=1024, out=ONE, os=1024, dtype=1, heads=8,
 
 
 CACHES = [(dict(layers=0), "SHAPE"), (dict(pages=0), "SHAPE"), (dict(kv_heads=-1), "SHAPE"), (dict(page_size=48), "UNSUPPORTED"),
-          (dict(page_size=8), "UNSUPPORTED"), (dict(page_size=512), "UNSUPPORTED"), (dict(head_dim=96), "UNSUPPORTED"),
+          (dict(page_size=8), "UNSUPPORTED"), (dict(page_size=512), "UNSUPPORTED"), (dict(head_dim=96), "UNSUPPORTED"), (dict(kv_heads=1025), "UNSUPPORTED"),
           (dict(head_dim=0), "SHAPE"), (dict(k_codes=None), "NULL"), (dict(v_param=None), "NULL"), (dict(v_codes=8), "ALIGN"),
           (dict(k_param=4), "ALIGN")]
 BATCHES = [(dict(seqs=-1), "SHAPE"), (dict(table_width=0), "SHAPE"), (dict(rows=-1), "SHAPE"), (dict(max_new=-1), "SHAPE"),
