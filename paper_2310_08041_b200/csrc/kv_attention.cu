@@ -21,9 +21,22 @@ int check_attention(const qllm_kv_cache_t* cache, int q_heads, int dtype, const 
     return QLLM_OK;
 }
 
-// Query rows per key head of the sequence with the most new tokens, as the batch says.
-int rows_hint(const qllm_kv_cache_t* cache, int q_heads, const qllm_kv_batch_t* batch) {
-    return int(std::min<int64_t>(int64_t(batch->max_new) * (q_heads / cache->kv_heads), 0x7fffffff));
+// Which kernels a call launches.  The streaming kernel reads a sequence's keys once per 8 or 16 query rows, the tensor-core kernel
+// once per 256 and unpacks them for 256 whether there are that many or not: kPromptRows is where they meet.  Either serves
+// any count, so what the batch's hint says wrongly costs time only.  A batch with the same number of new tokens in every
+// sequence, as far as the hint goes, needs one of them; others get both, each taking its sequences.
+constexpr int kPromptRows = 64;
+struct Choice {
+    bool split, prompt;
+    int hint, most_rows;                                   // query rows per key head of the largest sequence; the border
+};
+Choice choose(const qllm_kv_cache_t* cache, int q_heads, int dtype, const qllm_kv_batch_t* batch) {
+    Choice c;
+    c.hint = int(std::min<int64_t>(int64_t(batch->max_new) * (q_heads / cache->kv_heads), 0x7fffffff));
+    c.prompt = kv::prompt_serves(cache->head_dim, dtype) && c.hint > kPromptRows;
+    c.split = !c.prompt || (batch->seqs > 1 && batch->rows != int64_t(batch->seqs) * batch->max_new);
+    c.most_rows = !c.prompt ? 0x7fffffff : c.split ? kPromptRows : 0;
+    return c;
 }
 
 }  // namespace
@@ -33,7 +46,10 @@ extern "C" int64_t qllm_kv_attention_workspace(const qllm_kv_cache_t* cache, int
     const int rc = qllm::check_attention(cache, q_heads, dtype, batch);
     if (rc != QLLM_OK) return rc;
     if (batch->rows == 0 || batch->seqs == 0) return 0;
-    return qllm::kv::split_workspace(cache->head_dim, dtype, qllm::rows_hint(cache, q_heads, batch));
+    const qllm::Choice ch = qllm::choose(cache, q_heads, dtype, batch);
+    const int64_t split = ch.split ? qllm::kv::split_workspace(cache->head_dim, dtype, ch.prompt ? qllm::kPromptRows : ch.hint) : 0;
+    const int64_t prompt = ch.prompt ? qllm::kv::prompt_workspace(qllm::kv::view(batch, cache), cache->kv_heads, cache->head_dim, q_heads / cache->kv_heads) : 0;
+    return std::max(split, prompt);                        // one after the other on the stream
 }
 
 extern "C" int qllm_kv_attention(const qllm_kv_cache_t* cache, int layer, const void* q, int64_t q_stride, void* out,
@@ -67,6 +83,9 @@ extern "C" int qllm_kv_attention(const qllm_kv_cache_t* cache, int layer, const 
     a.group = q_heads / cache->kv_heads;
     a.causal = causal;
     a.scale = scale;
-    a.most_rows = 0x7fffffff;
-    return kv::launch_attention_split(c, b, cache->head_dim, a, rows_hint(cache, q_heads, batch), workspace, status, st);
+    const Choice ch = choose(cache, q_heads, dtype, batch);
+    a.most_rows = ch.most_rows;
+    if (ch.prompt) rc = kv::launch_attention_prompt(c, b, cache->head_dim, a, workspace, status, st);
+    if (rc == QLLM_OK && ch.split) rc = kv::launch_attention_split(c, b, cache->head_dim, a, ch.prompt ? kPromptRows : ch.hint, workspace, status, st);
+    return rc;
 }

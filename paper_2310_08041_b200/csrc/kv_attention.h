@@ -13,7 +13,8 @@ struct AttnArgs {
     int64_t q_stride, out_stride;   // elements
     int dtype, q_heads, group, causal;
     float scale;
-    // Sequences with more than this many (new token, grouped query head) rows per key head are another kernel's.
+    // Sequences with more than this many (new token, grouped query head) rows per key head are the prompt kernel's, the others
+    // the streaming kernel's.
     int most_rows;
 };
 
@@ -21,6 +22,11 @@ struct AttnArgs {
 int64_t split_workspace(int head_dim, int dtype, int rows_hint);
 int launch_attention_split(const Cache& c, const Batch& b, int head_dim, const AttnArgs& a, int rows_hint, void* workspace,
                            int* status, cudaStream_t st);
+
+// Tensor-core kernel (kv_attention_prompt.cu): sequences with more than most_rows query rows per key head.
+bool prompt_serves(int head_dim, int dtype);
+int64_t prompt_workspace(const Batch& b, int heads, int head_dim, int group);
+int launch_attention_prompt(const Cache& c, const Batch& b, int head_dim, const AttnArgs& a, void* workspace, int* status, cudaStream_t st);
 
 }  // namespace kv
 }  // namespace qllm

@@ -1,0 +1,725 @@
+// Attention over the 4-bit cache for many query rows per key head (prompts, chunks of prompts): tcgen05 tensor cores.
+//
+// A CTA owns 256 query rows of one key head (query tokens x the heads of the group, two tiles of 128) and walks the keys in
+// tiles of 128 tokens.  Both products run as 128 x 128 tcgen05 MMAs in fp16: S_t = Q_t K^T into tensor memory, softmax by one
+// thread per row, P_t back into tensor memory over S_t, O_t += P_t V.  While one tile's rows are in the softmax, the
+// tensor core works for the other.  The tensor pipe bounds it: 4 * 128 * 128 * head_dim operations a tile pair against
+// about 3.5 issue slots per score and 1.5 per code unpacked, each key tile being unpacked once for 256 rows.
+//
+// Roles (16 warps): 0-3 and 4-7 the softmax of tiles 0 and 1 (a thread per row), 8-11 unpack codes (a thread per token), 12
+// fetches codes and parameters with bulk copies, 13 issues the MMAs.  Registers are shifted to the softmax warps.
+//
+// Operands.  Keys enter as the exact integers (code - zero), the scale multiplies finished scores: a nibble under the
+// exponent of 1024 is the fp16 number 1024 + c (1024 + 16 c from the upper half of a byte), one packed fp16 operation makes
+// it c - zero.  Queries are scaled per row by a power of two into fp16 (a bf16 query's 8 bits are kept).  Values enter as
+// (code - zero) vs 2^-E, E the exponent of the tile's largest value, so that a weight is p 2^E and nothing acts per score and
+// token: rounded to fp16 in the scale and in the product, 11 bits each, where a bf16 result carries 8.  Tiles whose value
+// scales differ by more than 2^10, or pass 2^80, keep bare codes and multiply the weights by vs instead.  Rows far from
+// zero (|zero| > 900) round (code - zero) to 11 bits.  Channels lie in the order 0 4 1 5 2 6 3 7 of each eight, as the
+// masks leave them: the queries are stored alike and the output is put right at the end.
+
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "kv_attention.h"
+#include "ptx_sm100.cuh"
+#include "qgemm_tc_common.cuh"
+
+namespace qllm {
+namespace {
+
+using namespace kv;
+using tc::Abort;
+using tc::wait_bounded;
+
+constexpr int BM = 128, BN = 128;                          // query rows of a tile, tokens of a key tile
+constexpr int kThreads = 512;
+constexpr int kSlots = 3;                                  // key tiles whose parameters are held
+constexpr float kPlace = 6.f, kSlack = 8.f;                // as in kv_attention_split.cu
+
+template <int D>
+struct Shape {
+    static constexpr int ATOM = BN * 128;                  // 128 rows of 64 fp16 in the 128-byte swizzle
+    static constexpr int OP = D / 64 * ATOM;               // one operand tile
+    static constexpr int OPS = 4;                          // operand buffers: keys 0 and 2, values 1 and 3
+    static constexpr int RAW = BN * (D / 2);               // codes as they come
+    static constexpr int RAWS = 3;
+    static constexpr int RAWP = 2 * BN * 8;                // both parameter arrays, fetched with the keys: two of them
+    static constexpr int PRM = BN * 4;                     // one float per token
+    static constexpr int SMEM = 1024 + 2 * OP + OPS * OP + RAWS * RAW + 2 * RAWP + 3 * kSlots * PRM;
+    static constexpr uint32_t TMEM_S = 0, TMEM_O = 256;    // columns: S_0, S_1, O_0, O_1
+};
+
+// ---- instructions ---------------------------------------------------------------------------------------------------------
+// kind::f16: fp16 x fp16, fp32 accumulate; A K-major, B K-major or (b_mn) N-major
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn) {
+    return (1u << 4) | (0u << 7) | (0u << 10) | (uint32_t(b_mn) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
+}
+__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+                 "l"(b), "r"(idesc), "r"(uint32_t(accumulate))
+                 : "memory");
+}
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a),
+                 "l"(b), "r"(idesc), "r"(uint32_t(accumulate))
+                 : "memory");
+}
+// N-major operand: rows (K) of 64 elements, groups of 8 rows 1024 bytes apart, blocks of 64 N-elements `block` bytes apart
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr, uint32_t block) {
+    uint64_t d = ptx::smem_desc_sw128(addr) & ~(uint64_t(0x3FFF) << 16);
+    return d | (uint64_t(block >> 4) << 16);
+}
+__device__ __forceinline__ void tmem_st_x32(uint32_t addr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float lg2(float x) {
+    float r;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }     // -126 <= e <= 127
+__device__ __forceinline__ uint32_t bits(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+__device__ __forceinline__ __half2 halves(uint32_t v) { return *reinterpret_cast<const __half2*>(&v); }
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ptx::smem_addr(dst)),
+                 "l"(src), "r"(bytes), "r"(ptx::smem_addr(bar))
+                 : "memory");
+}
+
+// ---- work -----------------------------------------------------------------------------------------------------------------
+struct Args {
+    Cache c;
+    Batch b;
+    const __nv_bfloat16* q;
+    __nv_bfloat16* out;
+    float* lse;                                            // may be null
+    int64_t q_stride, out_stride;
+    int group, q_heads, causal, most_rows, splits;         // sequences with at most most_rows query rows are another kernel's
+    float scale;
+    float* part_o;                                         // [splits][rows][q_heads][D], unnormalised
+    float2* part_ml;                                       // [splits][rows][q_heads]: reference exponent, sum
+    int* status;
+};
+
+// 256-row blocks of a sequence
+__device__ __forceinline__ unsigned blocks_of(const Args& a, int s) {
+    const unsigned rows = unsigned(a.b.count(s)) * unsigned(a.group);
+    return rows <= unsigned(a.most_rows) ? 0 : (rows + 2 * BM - 1) / (2 * BM);
+}
+
+// One word of codes -> 8 fp16 of (code - zero), times `mul` for values.  far: zero does not fit the fast form.
+template <bool VALUES>
+__device__ __forceinline__ uint4 unpack8(uint32_t w, __half2 sub, __half2 sub16, __half2 mul) {
+    const uint32_t u = w >> 8;
+    const __half2 sixteenth = __floats2half2_rn(0.0625f, 0.0625f);
+    __half2 h0 = __hadd2(halves((w & 0x000F000Fu) | 0x64006400u), sub), h1 = __hfma2(halves((w & 0x00F000F0u) | 0x64006400u), sixteenth, sub16);
+    __half2 h2 = __hadd2(halves((u & 0x000F000Fu) | 0x64006400u), sub), h3 = __hfma2(halves((u & 0x00F000F0u) | 0x64006400u), sixteenth, sub16);
+    if (VALUES) { h0 = __hmul2(h0, mul); h1 = __hmul2(h1, mul); h2 = __hmul2(h2, mul); h3 = __hmul2(h3, mul); }
+    return make_uint4(bits(h0), bits(h1), bits(h2), bits(h3));
+}
+// the same for any zero: (code - zero) factor in float32, rounded once
+__device__ __forceinline__ uint4 unpack8_far(uint32_t w, float zero, float factor) {
+    uint32_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        h[i] = bits(__floats2half2_rn((float((w >> (4 * i)) & 15u) - zero) * factor, (float((w >> (4 * i + 16)) & 15u) - zero) * factor));
+    return make_uint4(h[0], h[1], h[2], h[3]);
+}
+
+// A thread's token: 64 / 32 bytes of codes -> its row of an operand tile.
+template <int D, bool VALUES>
+__device__ __forceinline__ void unpack_row(const uint8_t* raw, uint8_t* op, int tok, float zero, float factor, bool far) {
+    constexpr int CH = D / 32;                             // 16-byte chunks of a row
+    const __half2 sub = __float2half2_rn(-(1024.f + zero)), sub16 = __float2half2_rn(-(64.f + zero)), mul = __float2half2_rn(factor);
+    const uint8_t* src = raw + tok * (D / 2);
+    uint8_t* dst = op + tok * 128;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int ch = (i + (CH == 4 ? tok >> 1 : tok >> 2)) & (CH - 1);     // neighbours read different banks
+        const uint4 w = *reinterpret_cast<const uint4*>(src + 16 * ch);
+        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int u = 4 * ch + k;                      // 16-byte unit: 8 channels
+            const uint4 v = far ? unpack8_far(ww[k], zero, factor) : unpack8<VALUES>(ww[k], sub, sub16, mul);
+            *reinterpret_cast<uint4*>(dst + (u >> 3) * Shape<D>::ATOM + (((u & 7) ^ (tok & 7)) << 4)) = v;
+        }
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
+    using S = Shape<D>;
+    extern __shared__ uint8_t smem_dyn[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
+    uint8_t* s_q = smem;                                   // [2] tiles
+    uint8_t* s_op = s_q + 2 * S::OP;                       // [OPS]
+    uint8_t* s_raw = s_op + S::OPS * S::OP;                // [RAWS]
+    uint8_t* s_rawp = s_raw + S::RAWS * S::RAW;            // [2] (a third tile's keys wait for the first one's values to be unpacked)
+    float* s_ks = reinterpret_cast<float*>(s_rawp + 2 * S::RAWP);            // [kSlots][BN] key scales
+    float* s_vs = s_ks + kSlots * BN;                      // value scales and their logarithms, for tiles of bare codes
+    float* s_lv = s_vs + kSlots * BN;
+    __shared__ uint64_t s_bar[32];
+    __shared__ uint32_t s_tmem, s_pieces[S::RAWS];
+    __shared__ int s_abort, s_find[4], s_exp[2 * 4];
+    __shared__ float s_e[kSlots];                          // exponent of a tile's values
+    __shared__ uint32_t s_flags[kSlots], s_there[kSlots][4];                 // 1: bare codes, 2: some tokens are not there (bits)
+    uint64_t* raw_full = s_bar;                            // [RAWS]
+    uint64_t* raw_empty = raw_full + S::RAWS;              // [RAWS]
+    uint64_t* op_full = raw_empty + S::RAWS;               // [OPS]
+    uint64_t* op_empty = op_full + S::OPS;                 // [OPS]
+    uint64_t* prm_full = op_empty + S::OPS;                // [kSlots]
+    uint64_t* s_full = prm_full + kSlots;                  // [2]
+    uint64_t* p_full = s_full + 2;                         // [2]
+    uint64_t* o_full = p_full + 2;                         // [2]
+    uint64_t* q_full = o_full + 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::RAWS; ++i) { ptx::mbar_init(&raw_full[i], 1); ptx::mbar_init(&raw_empty[i], 4); }
+        for (int i = 0; i < S::OPS; ++i) { ptx::mbar_init(&op_full[i], 4); ptx::mbar_init(&op_empty[i], 1); }
+        for (int i = 0; i < kSlots; ++i) ptx::mbar_init(&prm_full[i], 4);
+        for (int i = 0; i < 2; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 4); ptx::mbar_init(&o_full[i], 1); }
+        ptx::mbar_init(q_full, 8);
+        s_abort = 0;
+        ptx::fence_barrier_init();
+        ptx::fence_proxy_async_smem();
+    }
+    if (warp == 0) {                                       // which sequence, which block of it
+        unsigned x = blockIdx.x;
+        int found = -1;
+        for (int base = 0; base < a.b.seqs; base += 32) {
+            const int s = base + lane;
+            const unsigned n = s < a.b.seqs ? blocks_of(a, s) : 0;
+            unsigned incl = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned y = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += y;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, x < incl);
+            if (hit) {
+                const int l = __ffs(hit) - 1;
+                const unsigned cnt = __shfl_sync(0xffffffffu, n, l), end = __shfl_sync(0xffffffffu, incl, l);
+                found = base + l;
+                x = cnt - 1 - (x - (end - cnt));           // the last block, which sees the most keys, first
+                break;
+            }
+            x -= __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (lane == 0) { s_find[0] = found; s_find[1] = int(x); }
+    }
+    __syncthreads();
+    const int seq = s_find[0];
+    if (seq < 0) return;
+    const int blk = s_find[1], g = blockIdx.y, n = a.b.count(seq), len = a.b.len(seq);
+    const int64_t row0 = a.b.row(seq);
+    const unsigned rows = unsigned(n) * unsigned(a.group);
+    // key tiles of the two query tiles, and those of this split
+    int nt[2], j0, j1;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const unsigned first = (2 * unsigned(blk) + t) * BM, last = min(first + BM, rows) - 1;
+        const int keys = !a.causal ? len : max(len - n + int(last / unsigned(a.group)) + 1, 0);
+        nt[t] = first >= rows ? 0 : int((unsigned(keys) + BN - 1) / BN);
+    }
+    {
+        const int all = max(nt[0], nt[1]);
+        j0 = int(int64_t(all) * blockIdx.z / a.splits);
+        j1 = int(int64_t(all) * (blockIdx.z + 1) / a.splits);
+    }
+    const Abort ab{&s_abort, a.status};
+    if (warp == 13) {
+        ptx::tmem_alloc(&s_tmem, 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = s_tmem;
+
+    if (warp < 8) {
+        // ------------------------------------------------------------------------------------------------ softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        const int t = warp >> 2, local = threadIdx.x & 127;
+        const unsigned rr = (2 * unsigned(blk) + t) * BM + local, i = rr / unsigned(a.group);
+        const bool real = rr < rows;
+        const int head = g * a.group + int(rr - i * a.group);
+        const int limit = !real ? 0x7fffffff : !a.causal ? len : max(len - n + int(i) + 1, 0);
+        // ---- this row's query into the operand tile
+        float qn;
+        {
+            const __nv_bfloat16* src = a.q + (row0 + i) * a.q_stride + int64_t(head) * D;
+            float top = 0.f;
+            if (real)
+#pragma unroll 4
+                for (int k = 0; k < D / 8; ++k) {
+                    float f[8];
+                    load8<__nv_bfloat16>(src + 8 * k, f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
+                }
+            const int e = max(int(__float_as_uint(top) >> 23) - 127, -100);
+            const float up = pow2i(13 - e) * (a.scale < 0.f ? -1.f : 1.f);
+            qn = fmaxf(pow2i(e - 13) * fabsf(a.scale) * 1.4426950408889634f, 1e-37f);      // not 0: it meets the -infinity of masks
+            uint8_t* dst = s_q + t * S::OP + local * 128;
+#pragma unroll 4
+            for (int k = 0; k < D / 8; ++k) {
+                float f[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) f[x] = 0.f;
+                if (real) load8<__nv_bfloat16>(src + 8 * k, f);
+                uint32_t h[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) h[x] = bits(__floats2half2_rn(f[x] * up, f[x + 4] * up));
+                *reinterpret_cast<uint4*>(dst + (k >> 3) * S::ATOM + (((k & 7) ^ (local & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(q_full);
+        }
+        const int low = __reduce_min_sync(0xffffffffu, limit);               // fewest keys of this warp's rows
+        const uint32_t lanes = uint32_t(warp & 3) << 21;                     // TMEM lane offset of this warp's rows
+        const uint32_t t_s = tmem + S::TMEM_S + t * BN + lanes, t_o = tmem + S::TMEM_O + t * D + lanes;
+        const int stop = min(nt[t], j1);
+        float top = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int j = j0; j < stop; ++j) {
+            const int slot = (j - j0) % kSlots;
+            if (!wait_bounded(&prm_full[slot], ((j - j0) / kSlots) & 1, ab) || !wait_bounded(&s_full[t], (j - j0) & 1, ab)) { ok = false; break; }
+            ptx::tc_fence_after_sync();
+            const float* ks = s_ks + slot * BN;
+            const uint32_t flags = s_flags[slot];
+            const int first = j * BN;
+            const bool masked = first + BN > low || (flags & 2);
+            float y[BN];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t r[32];
+                ptx::tmem_ld_32x32b_x32(t_s + 32 * c, r);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) y[32 * c + k] = __uint_as_float(r[k]);
+            }
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < BN; k += 4) {
+                const float4 v = *reinterpret_cast<const float4*>(ks + k);
+                y[k] *= v.x; y[k + 1] *= v.y; y[k + 2] *= v.z; y[k + 3] *= v.w;
+            }
+            if (masked) {
+                uint32_t there[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) there[c] = s_there[slot][c];
+#pragma unroll
+                for (int k = 0; k < BN; ++k)
+                    if (first + k >= limit || !((there[k >> 5] >> (k & 31)) & 1u)) y[k] = -INFINITY;
+            }
+            const float e = s_e[slot];
+            float m;
+            if (!(flags & 1)) {
+                float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int k = 0; k < BN; k += 8) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) m4[x] = fmaxf(m4[x], fmaxf(y[k + x], y[k + 4 + x]));
+                }
+                m = fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), qn, e);
+            } else {
+                m = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < BN; ++k) m = fmaxf(m, fmaf(y[k], qn, s_lv[slot * BN + k]));
+            }
+            if (__any_sync(0xffffffffu, m > top + (kPlace + kSlack))) {
+                const float to = fmaxf(m - kPlace, top), fix = to == -INFINITY ? 1.f : ex2(top - to);
+                top = to;
+                l *= fix;
+                if (j > j0) {
+#pragma unroll 1
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t r[32];
+                        ptx::tmem_ld_32x32b_x32(t_o + 32 * c, r);
+                        ptx::tmem_ld_wait();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * fix);
+                        tmem_st_x32(t_o + 32 * c, r);
+                    }
+                    tmem_st_wait();
+                }
+            }
+            const float at = top == -INFINITY ? 0.f : top;
+            if (!(flags & 1)) {
+                const float sub = e - at;
+                float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        const float p0 = ex2(fmaf(y[64 * h + 2 * k], qn, sub)), p1 = ex2(fmaf(y[64 * h + 2 * k + 1], qn, sub));
+                        l4[2 * (k & 1)] += p0;
+                        l4[2 * (k & 1) + 1] += p1;
+                        p[k] = bits(__floats2half2_rn(p0, p1));
+                    }
+                    tmem_st_x32(t_s + 32 * h, p);
+                }
+                l = fmaf((l4[0] + l4[1]) + (l4[2] + l4[3]), pow2i(-int(e)), l);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        float w[2];
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const int tok = 64 * h + 2 * k + x;
+                            const float v = ex2(fmaf(y[tok], qn, -at));
+                            l += v;
+                            // a hidden key's value scale may be anything
+                            w[x] = y[tok] == -INFINITY ? 0.f : v * s_vs[slot * BN + tok];
+                        }
+                        p[k] = bits(__floats2half2_rn(w[0], w[1]));
+                    }
+                    tmem_st_x32(t_s + 32 * h, p);
+                }
+            }
+            tmem_st_wait();
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&p_full[t]);
+        }
+        // ---- the row's output
+        const int64_t row = row0 + i;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const bool some = stop > j0;
+        if (ok && some) {
+            ok = wait_bounded(&o_full[t], 0, ab);
+            ptx::tc_fence_after_sync();
+        }
+        if (ok) {
+            const int64_t at = (int64_t(blockIdx.z) * a.b.rows + row) * a.q_heads + head;
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t r[32];
+                if (some) {
+                    ptx::tmem_ld_32x32b_x32(t_o + 32 * c, r);
+                    ptx::tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) r[k] = 0;
+                }
+                if (real) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float f[8];
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) f[x] = __uint_as_float(r[8 * k + 2 * (x & 3) + (x >> 2)]);   // 0 4 1 5 2 6 3 7
+                        if (a.splits > 1) {
+                            store8(a.part_o + at * D + 32 * c + 8 * k, f);
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) f[x] *= inv;
+                            store8(a.out + row * a.out_stride + int64_t(head) * D + 32 * c + 8 * k, f);
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+            if (real) {
+                if (a.splits > 1) a.part_ml[at] = make_float2(top, l);
+                else if (a.lse) a.lse[row * a.q_heads + head] = l == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(l)) * 0.6931471805599453f;
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        const int piece_log2 = min(a.b.page_log2, 7), per_tile = BN >> piece_log2;
+        if (warp < 12) {
+            // -------------------------------------------------------------------------------------------- unpack
+            const int tok = threadIdx.x - 256, uw = warp - 8;
+            bool ok = true;
+            uint32_t step = 0;                             // 2 * tile + (0 keys, 1 values)
+            const int top_keys = !a.causal ? len : max(len - n + int((min((2 * unsigned(blk) + 2) * BM, rows) - 1) / unsigned(a.group)) + 1, 0);
+            for (int j = j0; ok && j < j1; ++j) {
+                float kz, kf, vz, vf;
+                bool kfar, vfar;
+                const int slot = (j - j0) % kSlots;
+                // ---- keys, and both parameters
+                {
+                    const int rs = step % S::RAWS, ob = step % S::OPS;
+                    if (!wait_bounded(&raw_full[rs], (step / S::RAWS) & 1, ab)) { ok = false; break; }
+                    const uint8_t* raw = s_raw + rs * S::RAW;
+                    const uint32_t pieces = s_pieces[rs];
+                    const bool good = j * BN + tok < top_keys && ((pieces >> (tok >> piece_log2)) & 1u);
+                    const float2* prm = reinterpret_cast<const float2*>(s_rawp + ((j - j0) & 1) * S::RAWP);
+                    float2 kp = prm[tok], vp = prm[BN + tok];
+                    if (!good) kp = vp = make_float2(0.f, 0.f);
+                    // keys: (code - zero) 2^-k, k = 0 unless the zero-point is far off
+                    kf = 1.f;
+                    // parameters that are no numbers: the operands stay finite, a row that sees the token gets it from the score
+                    if (!(fabsf(vp.x) <= 3e38f && fabsf(vp.y) <= 3e38f)) { kp.x = NAN; vp = make_float2(0.f, 0.f); }
+                    if (!(fabsf(kp.y) <= 3e38f)) { kp.x = NAN; kp.y = 0.f; }
+                    kfar = fabsf(kp.y) > 900.f || kp.y != rintf(kp.y);
+                    if (kfar) {
+                        const int k = min(max(int((__float_as_uint(kp.y) >> 23) & 255u) - 127 - 9, 0), 120);
+                        kf = pow2i(-k);
+                        kp.x *= pow2i(k);
+                    }
+                    kz = kp.y;
+                    s_ks[slot * BN + tok] = kp.x;
+                    // values
+                    vz = vp.y;
+                    vfar = fabsf(vz) > 900.f || vz != rintf(vz);
+                    const float far_value = fabsf(vp.x) * fmaxf(fabsf(vz), fabsf(15.f - vz));    // the largest value of the row
+                    const bool fits = far_value < 1.2e24f;                   // 2^80, as the cut of the logarithm
+                    const int ex = !good || far_value == 0.f ? -1000 : !fits ? 1000 : max(int(__float_as_uint(far_value) >> 23) - 127, -80);
+                    const int hi = __reduce_max_sync(0xffffffffu, ex), lo = __reduce_min_sync(0xffffffffu, good && far_value != 0.f ? ex : 1000);
+                    if (lane == 0) { s_exp[uw] = hi; s_exp[4 + uw] = lo; }
+                    const uint32_t there = __ballot_sync(0xffffffffu, good);
+                    if (lane == 0) s_there[slot][uw] = there;
+                    ptx::named_bar_sync(2, 128);
+                    const int e = max(max(s_exp[0], s_exp[1]), max(s_exp[2], s_exp[3])), f = min(min(s_exp[4], s_exp[5]), min(s_exp[6], s_exp[7]));
+                    const bool bare = e > 900 || (f < 900 && e - f > 10);
+                    const int et = bare || e < -900 ? 0 : e;
+                    if (bare) {
+                        vf = 1.f;
+                        if (vfar) {
+                            const int k = min(max(int((__float_as_uint(vz) >> 23) & 255u) - 127 - 9, 0), 120);
+                            vf = pow2i(-k);
+                            vp.x *= pow2i(k);
+                        }
+                        s_vs[slot * BN + tok] = vp.x;
+                        s_lv[slot * BN + tok] = fminf(fmaxf(lg2(fabsf(vp.x)), -80.f), 80.f);
+                    } else {
+                        vf = vp.x * pow2i(-et);
+                    }
+                    if (!good) vf = 0.f;
+                    if (tok == 0) {
+                        s_e[slot] = float(et);
+                        s_flags[slot] = bare ? 1 : 0;
+                    }
+                    ptx::named_bar_sync(2, 128);           // s_exp is free again; tile-wide flags follow
+                    if (lane == 0 && there != 0xffffffffu) atomicOr(&s_flags[slot], 2u);
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&prm_full[slot]);
+                    if (!wait_bounded(&op_empty[ob], ((step / S::OPS) & 1) ^ 1, ab)) { ok = false; break; }
+                    unpack_row<D, false>(raw, s_op + ob * S::OP, tok, kz, kf, kfar);
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) { ptx::mbar_arrive(&op_full[ob]); ptx::mbar_arrive(&raw_empty[rs]); }
+                    ++step;
+                }
+                // ---- values
+                {
+                    const int rs = step % S::RAWS, ob = step % S::OPS;
+                    if (!wait_bounded(&raw_full[rs], (step / S::RAWS) & 1, ab) || !wait_bounded(&op_empty[ob], ((step / S::OPS) & 1) ^ 1, ab)) { ok = false; break; }
+                    unpack_row<D, true>(s_raw + rs * S::RAW, s_op + ob * S::OP, tok, vz, vf, vfar);
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) { ptx::mbar_arrive(&op_full[ob]); ptx::mbar_arrive(&raw_empty[rs]); }
+                    ++step;
+                }
+            }
+        } else if (warp == 12) {
+            // -------------------------------------------------------------------------------------------- codes in
+            // lane = 4 * piece + array (keys' codes, their parameters, the values' parameters, the values' codes)
+            const int piece = lane >> 2, array = lane & 3, log2p = a.b.page_log2;
+            const int keys = min(len, j1 * BN), pieces = int((unsigned(keys) + (1u << piece_log2) - 1) >> piece_log2);
+            const int32_t* table = a.b.table + int64_t(seq) * a.b.width;
+            auto page_of = [&](int q) { return q < pieces ? table[(int64_t(q) << piece_log2) >> log2p] : 0; };
+            const uint32_t bytes = uint32_t(array == 0 || array == 3 ? D / 2 : 8) << piece_log2;
+            const int offset = (array == 2 ? BN * 8 : 0) + min(piece, per_tile - 1) * int(bytes);
+            const uint8_t* source = array == 0 ? a.c.kc : array == 3 ? a.c.vc : reinterpret_cast<const uint8_t*>(array == 1 ? a.c.kp : a.c.vp);
+            const int row_bytes = array == 0 || array == 3 ? D / 2 : 8;
+            bool ok = true;
+            uint32_t step = 0;
+            int q0 = j0 * per_tile, held = page_of(q0 + lane), ahead = page_of(q0 + 32 + lane);
+            for (int j = j0; ok && j < j1; ++j) {
+                const int q = j * per_tile + piece;
+                if (j * per_tile - q0 >= 32) {
+                    q0 += 32;
+                    held = ahead;
+                    ahead = page_of(q0 + 32 + lane);
+                }
+                const int page = __shfl_sync(0xffffffffu, held, q - q0);
+                const bool mine = piece < per_tile && q < pieces, good = mine && page >= 0 && page < a.c.pages;
+                if (mine && !good) raise_page(a.status);
+                const int64_t r = a.c.row(page, g, (q << piece_log2) & ((1 << log2p) - 1));
+                const uint32_t got = __ballot_sync(0xffffffffu, good && array == 0);
+                uint32_t mask = 0;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) mask |= ((got >> (4 * x)) & 1u) << x;
+#pragma unroll
+                for (int v = 0; v < 2; ++v, ++step) {
+                    const bool now = good && (array == 3) == (v == 1);
+                    const uint32_t total = __reduce_add_sync(0xffffffffu, now ? bytes : 0);
+                    const int rs = step % S::RAWS;
+                    if (!wait_bounded(&raw_empty[rs], ((step / S::RAWS) & 1) ^ 1, ab)) { ok = false; break; }
+                    if (lane == 0) {
+                        s_pieces[rs] = mask;
+                        ptx::mbar_arrive_expect_tx(&raw_full[rs], total);
+                    }
+                    __syncwarp();
+                    uint8_t* target = array == 0 || array == 3 ? s_raw + rs * S::RAW : s_rawp + ((j - j0) & 1) * S::RAWP;
+                    if (now) bulk_load(target + offset, source + r * row_bytes, bytes, &raw_full[rs]);
+                }
+            }
+            if (!ok) {                                     // give copies still in flight a bounded chance to land
+                for (uint32_t k = 0; k < uint32_t(S::RAWS) && k < step; ++k) {
+                    const uint32_t x = step - 1 - k;
+                    const long long t0 = clock64();
+                    while (!ptx::mbar_try_wait(&raw_full[x % S::RAWS], (x / S::RAWS) & 1) && clock64() - t0 < (1ll << 24)) {}
+                }
+            }
+        } else if (warp == 13 && lane == 0) {
+            // -------------------------------------------------------------------------------------------- MMAs
+            constexpr uint32_t id_s = idesc_f16(BM, BN, false), id_o = idesc_f16(BM, D, true);
+            auto score = [&](int t, int ob) {
+                const uint32_t q = ptx::smem_addr(s_q + t * S::OP), k = ptx::smem_addr(s_op + ob * S::OP);
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x)
+                    mma_f16_ss(tmem + S::TMEM_S + t * BN, ptx::smem_desc_sw128(q + (x >> 2) * S::ATOM + (x & 3) * 32),
+                               ptx::smem_desc_sw128(k + (x >> 2) * S::ATOM + (x & 3) * 32), id_s, x != 0);
+                ptx::mma_commit(&s_full[t]);
+            };
+            bool ok = wait_bounded(q_full, 0, ab);
+            if (ok && j0 < j1) {
+                ok = wait_bounded(&op_full[0], 0, ab);
+                if (ok) {
+                    ptx::tc_fence_after_sync();
+                    if (j0 < nt[0]) score(0, 0);
+                    if (j0 < nt[1]) score(1, 0);
+                    ptx::mma_commit(&op_empty[0]);
+                }
+            }
+            for (int j = j0; ok && j < j1; ++j) {
+                const uint32_t sv = 2 * (j - j0) + 1, sk = sv + 1;           // steps of V_j and K_j+1
+                const bool more = j + 1 < j1;
+                if (!wait_bounded(&op_full[sv % S::OPS], (sv / S::OPS) & 1, ab)) break;
+                if (more && !wait_bounded(&op_full[sk % S::OPS], (sk / S::OPS) & 1, ab)) break;
+                const uint32_t v = ptx::smem_addr(s_op + (sv % S::OPS) * S::OP);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (j >= nt[t]) continue;
+                    if (!wait_bounded(&p_full[t], (j - j0) & 1, ab)) { ok = false; break; }
+                    ptx::tc_fence_after_sync();
+#pragma unroll
+                    for (int x = 0; x < BN / 16; ++x)
+                        mma_f16_ts(tmem + S::TMEM_O + t * D, tmem + S::TMEM_S + t * BN + 8 * x, smem_desc_mn(v + x * 2048, S::ATOM), id_o, j > j0 || x > 0);
+                    if (more && j + 1 < nt[t]) score(t, sk % S::OPS);
+                    else ptx::mma_commit(&o_full[t]);
+                }
+                ptx::mma_commit(&op_empty[sv % S::OPS]);
+                if (more) ptx::mma_commit(&op_empty[sk % S::OPS]);
+            }
+        }
+    }
+    __syncwarp();
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 13) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+}
+
+// Joins the splits of a row: a CTA per (packed row, 4 query heads), a warp per head.
+template <int D>
+__global__ void __launch_bounds__(128) kv_prompt_join_kernel(const Args a) {
+    constexpr int V = D / 32;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 5), row = unit / a.q_heads;
+    if (row >= a.b.rows) return;
+    const int s = a.b.seq_of(row);
+    if (s < 0 || blocks_of(a, s) == 0) return;
+    const int64_t step = a.b.rows * a.q_heads;
+    float m = -INFINITY;
+    for (int z = 0; z < a.splits; ++z) m = fmaxf(m, a.part_ml[z * step + unit].x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = 0.f;
+    for (int z = 0; z < a.splits; ++z) {
+        const float2 ml = a.part_ml[z * step + unit];
+        const float f = ml.y == 0.f ? 0.f : ml.x == -INFINITY ? 1.f : ex2(ml.x - ref);       // (a NaN sum goes through)
+        if (f == 0.f) continue;
+        l = fmaf(f, ml.y, l);
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = fmaf(f, a.part_o[(z * step + unit) * D + lane * V + i], o[i]);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int head = int(unit - row * a.q_heads);
+#pragma unroll
+    for (int i = 0; i < V; ++i) a.out[row * a.out_stride + int64_t(head) * D + lane * V + i] = __float2bfloat16(o[i] * inv);
+    if (a.lse && lane == 0) a.lse[unit] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+}
+
+// CTAs of a call at most, per split: every sequence rounds its rows up once.
+inline int64_t blocks_bound(const Batch& b, int group) { return (b.rows * group + 2 * BM - 1) / (2 * BM) + std::min<int64_t>(b.seqs, b.rows); }
+
+// Keys are cut into as many parts as fill the SMs once with the blocks that there are likely to be.
+inline int splits_of(const Batch& b, int heads, int group) {
+    const int64_t ctas = ((b.rows * group + 2 * BM - 1) / (2 * BM)) * heads;
+    return int(std::max<int64_t>(1, std::min<int64_t>(8, device_sm_count() / ctas)));
+}
+
+template <int D>
+int launch(const Args& a, cudaStream_t st) {
+    constexpr auto kern = &kv_prompt_kernel<D>;
+    QLLM_CUDA_TRY(allow_smem<kern>(Shape<D>::SMEM));
+    kern<<<dim3(unsigned(blocks_bound(a.b, a.group)), a.c.heads, a.splits), kThreads, Shape<D>::SMEM, st>>>(a);
+    int rc = after_launch();
+    if (rc != QLLM_OK || a.splits == 1) return rc;
+    QLLM_CUDA_TRY(launch_dependent(kv_prompt_join_kernel<D>, dim3(unsigned((a.b.rows * a.q_heads + 3) / 4)), dim3(128), 0, st, a));
+    return after_launch();
+}
+
+}  // namespace
+
+namespace kv {
+
+bool prompt_serves(int head_dim, int dtype) { return dtype == QLLM_BF16 && (head_dim == 64 || head_dim == 128); }
+
+int64_t prompt_workspace(const Batch& b, int heads, int head_dim, int group) {
+    const int splits = splits_of(b, heads, group);
+    return splits == 1 ? 0 : int64_t(splits) * b.rows * heads * group * (head_dim + 2) * 4;
+}
+
+int launch_attention_prompt(const Cache& c, const Batch& b, int head_dim, const AttnArgs& x, void* workspace, int* status, cudaStream_t st) {
+    Args a;
+    a.c = c;
+    a.b = b;
+    a.q = static_cast<const __nv_bfloat16*>(x.q);
+    a.out = static_cast<__nv_bfloat16*>(x.out);
+    a.lse = x.lse;
+    a.q_stride = x.q_stride;
+    a.out_stride = x.out_stride;
+    a.group = x.group;
+    a.q_heads = x.q_heads;
+    a.causal = x.causal;
+    a.most_rows = x.most_rows;
+    a.scale = x.scale;
+    a.splits = splits_of(b, c.heads, x.group);
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + int64_t(a.splits) * b.rows * x.q_heads * head_dim);
+    a.status = status;
+    return head_dim == 64 ? launch<64>(a, st) : launch<128>(a, st);
+}
+
+}  // namespace kv
+}  // namespace qllm

@@ -73,7 +73,7 @@ def attend(cache, layer, q, batch, scale, causal, fill=7.0, workspace=None):
     return out.t, lse.t
 
 
-def check_attention(got, lse, ref, dtype, rounded_codes=False):
+def check_attention(got, lse, ref, dtype, rounded_codes=False, prompt=False):
     """|error| <= rounding of the output + what the weights' and scores' errors can move.
 
     Weights: a bf16 call rounds each weight p_j vs_j once to 11 bits (fp16, half a step 2^-11 relative, or 2^-25 of the largest
@@ -81,6 +81,8 @@ def check_attention(got, lse, ref, dtype, rounded_codes=False):
     in float32, each of at most |mag| with at most 2^-23 relative error per addition, so (256 + 8) 2^-23 mag < 2^-14.9 mag in the
     worst order; every kernel adds them in groups of 16 at least, whose error is at most (16 + 16) 2^-23 mag = 2^-18 mag.  A
     relative change of every weight by e moves out by at most 2 e spread.  exp and the running rescalings: 2^-20.
+    prompt (bf16, more than 64 query rows per key head): the prompt kernel also rounds the value scale and the value it
+    multiplies to 11 bits, 2^-11 of the value each, which is at most the spread's term of its token.
     rounded_codes: the prompt kernel stores (code - zero) of rows far from zero in 11 bits, moving a score by 2^-11 mag and a
     value by 2^-11 of itself.  Sums over the keys: `seen` terms of one sign (the weights) or of at most the spread in all, added
     in float32 in any order, are off by at most seen 2^-24 of that sum; a logarithm turns a relative error into the same
@@ -88,6 +90,7 @@ def check_attention(got, lse, ref, dtype, rounded_codes=False):
     out, ref_lse, spread, mag, seen = ref
     w = 2.0 ** -11 + seen * 2.0 ** -25 if dtype == torch.bfloat16 else 2.0 ** -22 + seen * 2.0 ** -36
     w = w + 2 * seen * 2.0 ** -24                            # numerator and denominator
+    w = w + (2 * 2.0 ** -11 if prompt else 0)
     e = 2.0 ** -18 * mag + 2.0 ** -20 + (2.0 ** -11 * (mag + 1) if rounded_codes else 0)
     tol = (w + 2 * e)[..., None] * spread + np.abs(out) * torch.finfo(dtype).eps / 2 + 1e-30
     a = host(got)
@@ -111,7 +114,8 @@ def run_case(seed, dtype, d, page, heads, group, lens, news, causal, scale=None,
     scale = d ** -0.5 if scale is None else scale
     got, lse = attend(cache, layers - 1, q, batch, scale, causal)
     ref = kv_ref.attention(store_of(cache, layers - 1), table, lens, start, host(q), scale, causal)
-    check_attention(got, lse, ref, DT[dtype], rounded_codes)
+    hint = (max(news) if max_new is None else max_new) * group
+    check_attention(got, lse, ref, DT[dtype], rounded_codes, prompt=dtype == "bf16" and hint > 64)
     assert B.qllm_poll_status() == B.QLLM_OK
     return got
 
@@ -214,6 +218,8 @@ LENS = {
     "several new": ([9, 200, 64, 1000, 3], [9, 5, 1, 12, 3]),
     "prompt": ([257], [257]),
     "chunk": ([700, 90], [130, 90]),
+    "blocks": ([1000, 3000, 520], [600, 257, 515]),
+    "long chunk": ([9000], [70]),
     "mixed": ([300, 513, 1, 129, 1030], [300, 1, 1, 129, 2]),
 }
 
@@ -279,7 +285,7 @@ def test_attention_scales_of_every_size(dtype, news, seed):
     q = q.to(DT[dtype])
     got, lse = attend(cache, 0, q, batch, 0.09, True)
     ref = kv_ref.attention(store_of(cache, 0), table, lens, start, host(q), 0.09, True)
-    check_attention(got, lse, ref, DT[dtype])
+    check_attention(got, lse, ref, DT[dtype], prompt=dtype == "bf16" and max(news) * group > 64)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -404,7 +410,7 @@ def test_offsets_beyond_32_bits(news):
     got, lse = attend(cache, 1, q, batch, 0.09, True)
     st = kv_ref.Store(*[t[1, pages - 3:].cpu().numpy() for t in (c[0], p[0], c[1], p[1])])
     ref = kv_ref.attention(st, np.array([[2, 1, 0]]), lens, start, host(q), 0.09, True)
-    check_attention(got, lse, ref, torch.bfloat16)
+    check_attention(got, lse, ref, torch.bfloat16, prompt=news[0] > 64)
 
 
 def test_streams_and_graphs():
@@ -597,7 +603,7 @@ def test_behind_a_quantized_layer(out_dtype):
         B.qllm_kv_append(cache, 1, k, v, batch)
         got, lse = attend(cache, 1, q, batch, d ** -0.5, True)
         ref = kv_ref.attention(store_of(cache, 1), batch.table.cpu().numpy(), batch.seq_lens.tolist(), start, host(q), d ** -0.5, True)
-        check_attention(got, lse, ref, DT[out_dtype])
+        check_attention(got, lse, ref, DT[out_dtype], prompt=out_dtype == "bf16" and batch.max_new * group > 64)
 
     B.qllm_kv_pages_extend(cache, pool, ints([41, 0, 0, 0]))
     start = [0, 41, 41, 41, 41]
