@@ -7,7 +7,7 @@
 // about 3.5 issue slots per score and 1.5 per code unpacked, each key tile being unpacked once for 256 rows.
 //
 // Roles (16 warps): 0-3 and 4-7 the softmax of tiles 0 and 1 (a thread per row), 8-11 unpack codes (a thread per token), 12
-// fetches codes and parameters with bulk copies, 13 issues the MMAs.  Registers are shifted to the softmax warps.
+// fetches codes and parameters with bulk copies, 13 issues the MMAs.
 //
 // Operands.  Keys enter as the exact integers (code - zero), the scale multiplies finished scores: a nibble under the
 // exponent of 1024 is the fp16 number 1024 + c (1024 + 16 c from the upper half of a byte), one packed fp16 operation makes
@@ -81,6 +81,25 @@ __device__ __forceinline__ void tmem_st_x32(uint32_t addr, const uint32_t (&r)[3
         "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
         : "memory");
 }
+__device__ __forceinline__ void tmem_st_x16(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// two floats at a time
+struct F2 {
+    uint64_t v;
+    __device__ __forceinline__ F2() {}
+    __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ F2(uint32_t a, uint32_t b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b)); }
+    __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ex2(float x) {
     float r;
@@ -145,21 +164,97 @@ __device__ __forceinline__ uint4 unpack8_far(uint32_t w, float zero, float facto
 template <int D, bool VALUES>
 __device__ __forceinline__ void unpack_row(const uint8_t* raw, uint8_t* op, int tok, float zero, float factor, bool far) {
     constexpr int CH = D / 32;                             // 16-byte chunks of a row
-    const __half2 sub = __float2half2_rn(-(1024.f + zero)), sub16 = __float2half2_rn(-(64.f + zero)), mul = __float2half2_rn(factor);
     const uint8_t* src = raw + tok * (D / 2);
     uint8_t* dst = op + tok * 128;
+    auto unit = [&](int u) { return reinterpret_cast<uint4*>(dst + (u >> 3) * Shape<D>::ATOM + (((u & 7) ^ (tok & 7)) << 4)); };   // 8 channels
+    if (far) {
+#pragma unroll 1
+        for (int u = 0; u < D / 8; ++u) *unit(u) = unpack8_far(reinterpret_cast<const uint32_t*>(src)[u], zero, factor);
+        return;
+    }
+    const __half2 sub = __float2half2_rn(-(1024.f + zero)), sub16 = __float2half2_rn(-(64.f + zero)), mul = __float2half2_rn(factor);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int ch = (i + (CH == 4 ? tok >> 1 : tok >> 2)) & (CH - 1);     // neighbours read different banks
         const uint4 w = *reinterpret_cast<const uint4*>(src + 16 * ch);
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+        *unit(4 * ch) = unpack8<VALUES>(w.x, sub, sub16, mul);
+        *unit(4 * ch + 1) = unpack8<VALUES>(w.y, sub, sub16, mul);
+        *unit(4 * ch + 2) = unpack8<VALUES>(w.z, sub, sub16, mul);
+        *unit(4 * ch + 3) = unpack8<VALUES>(w.w, sub, sub16, mul);
+    }
+}
+
+// 32 scores of a row as they lie in tensor memory, times the keys' scales; MASKED: -infinity where the row does not see the token.
+template <bool MASKED>
+__device__ __forceinline__ void scores32(uint32_t addr, const float* ks, int first, int limit, const uint32_t* there, F2 (&y)[16]) {
+    uint32_t r[32];
+    ptx::tmem_ld_32x32b_x32(addr, r);
+    ptx::tmem_ld_wait();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int u = 4 * ch + k;                      // 16-byte unit: 8 channels
-            const uint4 v = far ? unpack8_far(ww[k], zero, factor) : unpack8<VALUES>(ww[k], sub, sub16, mul);
-            *reinterpret_cast<uint4*>(dst + (u >> 3) * Shape<D>::ATOM + (((u & 7) ^ (tok & 7)) << 4)) = v;
+    for (int k = 0; k < 16; k += 2) {
+        const float4 v = *reinterpret_cast<const float4*>(ks + 2 * k);
+        y[k] = mul2(F2(r[2 * k], r[2 * k + 1]), F2(v.x, v.y));
+        y[k + 1] = mul2(F2(r[2 * k + 2], r[2 * k + 3]), F2(v.z, v.w));
+    }
+    if (MASKED) {
+        const int n = limit - first;                       // tokens of the 32 in front of the limit
+        const uint32_t seen = *there & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            float a, b;
+            y[k].get(a, b);
+            y[k] = F2(seen >> (2 * k) & 1 ? a : -INFINITY, seen >> (2 * k + 1) & 1 ? b : -INFINITY);
         }
     }
+}
+// Largest score of a row in a key tile, in base 2 and times the largest value: the loops over 32 columns stay rolled, which
+// keeps the code of all roles in the instruction cache (unrolled over the tile the kernel took four times as long).
+template <bool MASKED, bool BARE>
+__device__ __forceinline__ float tile_max(uint32_t t_s, const float* ks, const float* lv, int first, int limit, const uint32_t* there, float qn, float e) {
+    float m[2] = {-INFINITY, -INFINITY};
+#pragma unroll 1
+    for (int c = 0; c < BN / 32; ++c) {
+        F2 y[16];
+        scores32<MASKED>(t_s + 32 * c, ks + 32 * c, first + 32 * c, limit, there + c, y);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            float a, b;
+            if (BARE) y[k] = fma2(y[k], F2(qn, qn), *reinterpret_cast<const F2*>(lv + 32 * c + 2 * k));
+            y[k].get(a, b);
+            m[k & 1] = fmaxf(m[k & 1], fmaxf(a, b));
+        }
+    }
+    const float x = fmaxf(m[0], m[1]);
+    return BARE ? x : fmaf(x, qn, e);
+}
+// The row's weights into the place of its scores (16 columns for 32: a chunk overwrites what has been read); returns their sum.
+template <bool MASKED, bool BARE>
+__device__ __forceinline__ float tile_weights(uint32_t t_s, const float* ks, const float* vs, int first, int limit, const uint32_t* there, float qn, float sub) {
+    F2 l[2] = {F2(0.f, 0.f), F2(0.f, 0.f)};
+#pragma unroll 1
+    for (int c = 0; c < BN / 32; ++c) {
+        F2 y[16];
+        scores32<MASKED>(t_s + 32 * c, ks + 32 * c, first + 32 * c, limit, there + c, y);
+        uint32_t p[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            float a, b;
+            fma2(y[k], F2(qn, qn), F2(sub, sub)).get(a, b);
+            float pa = ex2(a), pb = ex2(b);
+            l[k & 1] = add2(l[k & 1], F2(pa, pb));
+            if (BARE) {
+                // a hidden key's value scale may be anything
+                const float2 v = *reinterpret_cast<const float2*>(vs + 32 * c + 2 * k);
+                pa = pa == 0.f ? 0.f : pa * v.x;
+                pb = pb == 0.f ? 0.f : pb * v.y;
+            }
+            p[k] = bits(__floats2half2_rn(pa, pb));
+        }
+        tmem_st_x16(t_s + 16 * c, p);
+    }
+    float a, b;
+    add2(l[0], l[1]).get(a, b);
+    return a + b;
 }
 
 template <int D>
@@ -201,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
         ptx::fence_proxy_async_smem();
     }
     if (warp == 0) {                                       // which sequence, which block of it
-        unsigned x = blockIdx.x;
+        unsigned x = blockIdx.x / a.c.heads;               // heads vary fastest: all of them start with their longest blocks
         int found = -1;
         for (int base = 0; base < a.b.seqs; base += 32) {
             const int s = base + lane;
@@ -227,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
     __syncthreads();
     const int seq = s_find[0];
     if (seq < 0) return;
-    const int blk = s_find[1], g = blockIdx.y, n = a.b.count(seq), len = a.b.len(seq);
+    const int blk = s_find[1], g = blockIdx.x % a.c.heads, n = a.b.count(seq), len = a.b.len(seq);
     const int64_t row0 = a.b.row(seq);
     const unsigned rows = unsigned(n) * unsigned(a.group);
     // key tiles of the two query tiles, and those of this split
@@ -240,8 +335,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
     }
     {
         const int all = max(nt[0], nt[1]);
-        j0 = int(int64_t(all) * blockIdx.z / a.splits);
-        j1 = int(int64_t(all) * (blockIdx.z + 1) / a.splits);
+        j0 = int(int64_t(all) * blockIdx.y / a.splits);
+        j1 = int(int64_t(all) * (blockIdx.y + 1) / a.splits);
     }
     const Abort ab{&s_abort, a.status};
     if (warp == 13) {
@@ -255,7 +350,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
 
     if (warp < 8) {
         // ------------------------------------------------------------------------------------------------ softmax
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         const int t = warp >> 2, local = threadIdx.x & 127;
         const unsigned rr = (2 * unsigned(blk) + t) * BM + local, i = rr / unsigned(a.group);
         const bool real = rr < rows;
@@ -307,43 +401,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
             const uint32_t flags = s_flags[slot];
             const int first = j * BN;
             const bool masked = first + BN > low || (flags & 2);
-            float y[BN];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t r[32];
-                ptx::tmem_ld_32x32b_x32(t_s + 32 * c, r);
-#pragma unroll
-                for (int k = 0; k < 32; ++k) y[32 * c + k] = __uint_as_float(r[k]);
-            }
-            ptx::tmem_ld_wait();
-#pragma unroll
-            for (int k = 0; k < BN; k += 4) {
-                const float4 v = *reinterpret_cast<const float4*>(ks + k);
-                y[k] *= v.x; y[k + 1] *= v.y; y[k + 2] *= v.z; y[k + 3] *= v.w;
-            }
-            if (masked) {
-                uint32_t there[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) there[c] = s_there[slot][c];
-#pragma unroll
-                for (int k = 0; k < BN; ++k)
-                    if (first + k >= limit || !((there[k >> 5] >> (k & 31)) & 1u)) y[k] = -INFINITY;
-            }
-            const float e = s_e[slot];
-            float m;
-            if (!(flags & 1)) {
-                float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int k = 0; k < BN; k += 8) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) m4[x] = fmaxf(m4[x], fmaxf(y[k + x], y[k + 4 + x]));
-                }
-                m = fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), qn, e);
-            } else {
-                m = -INFINITY;
-#pragma unroll
-                for (int k = 0; k < BN; ++k) m = fmaxf(m, fmaf(y[k], qn, s_lv[slot * BN + k]));
-            }
+            const float e = s_e[slot], *vs = s_vs + slot * BN, *lv = s_lv + slot * BN;
+            const uint32_t* there = s_there[slot];
+            const bool bare = flags & 1;
+            const float m = bare     ? tile_max<true, true>(t_s, ks, lv, first, limit, there, qn, e)
+                            : masked ? tile_max<true, false>(t_s, ks, lv, first, limit, there, qn, e)
+                                     : tile_max<false, false>(t_s, ks, lv, first, limit, there, qn, e);
             if (__any_sync(0xffffffffu, m > top + (kPlace + kSlack))) {
                 const float to = fmaxf(m - kPlace, top), fix = to == -INFINITY ? 1.f : ex2(top - to);
                 top = to;
@@ -362,42 +425,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 }
             }
             const float at = top == -INFINITY ? 0.f : top;
-            if (!(flags & 1)) {
-                const float sub = e - at;
-                float l4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t p[32];
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        const float p0 = ex2(fmaf(y[64 * h + 2 * k], qn, sub)), p1 = ex2(fmaf(y[64 * h + 2 * k + 1], qn, sub));
-                        l4[2 * (k & 1)] += p0;
-                        l4[2 * (k & 1) + 1] += p1;
-                        p[k] = bits(__floats2half2_rn(p0, p1));
-                    }
-                    tmem_st_x32(t_s + 32 * h, p);
-                }
-                l = fmaf((l4[0] + l4[1]) + (l4[2] + l4[3]), pow2i(-int(e)), l);
-            } else {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t p[32];
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        float w[2];
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const int tok = 64 * h + 2 * k + x;
-                            const float v = ex2(fmaf(y[tok], qn, -at));
-                            l += v;
-                            // a hidden key's value scale may be anything
-                            w[x] = y[tok] == -INFINITY ? 0.f : v * s_vs[slot * BN + tok];
-                        }
-                        p[k] = bits(__floats2half2_rn(w[0], w[1]));
-                    }
-                    tmem_st_x32(t_s + 32 * h, p);
-                }
-            }
+            if (bare) l += tile_weights<true, true>(t_s, ks, vs, first, limit, there, qn, -at);
+            else l = fmaf(masked ? tile_weights<true, false>(t_s, ks, vs, first, limit, there, qn, e - at)
+                                 : tile_weights<false, false>(t_s, ks, vs, first, limit, there, qn, e - at), pow2i(-int(e)), l);
             tmem_st_wait();
             ptx::tc_fence_before_sync();
             __syncwarp();
@@ -412,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
             ptx::tc_fence_after_sync();
         }
         if (ok) {
-            const int64_t at = (int64_t(blockIdx.z) * a.b.rows + row) * a.q_heads + head;
+            const int64_t at = (int64_t(blockIdx.y) * a.b.rows + row) * a.q_heads + head;
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t r[32];
@@ -446,7 +476,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
             }
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         const int piece_log2 = min(a.b.page_log2, 7), per_tile = BN >> piece_log2;
         if (warp < 12) {
             // -------------------------------------------------------------------------------------------- unpack
@@ -682,7 +711,9 @@ template <int D>
 int launch(const Args& a, cudaStream_t st) {
     constexpr auto kern = &kv_prompt_kernel<D>;
     QLLM_CUDA_TRY(allow_smem<kern>(Shape<D>::SMEM));
-    kern<<<dim3(unsigned(blocks_bound(a.b, a.group)), a.c.heads, a.splits), kThreads, Shape<D>::SMEM, st>>>(a);
+    const int64_t ctas = blocks_bound(a.b, a.group) * a.c.heads;
+    if (ctas > 0x7fffffff) return QLLM_ERR_UNSUPPORTED;
+    kern<<<dim3(unsigned(ctas), a.splits), kThreads, Shape<D>::SMEM, st>>>(a);
     int rc = after_launch();
     if (rc != QLLM_OK || a.splits == 1) return rc;
     QLLM_CUDA_TRY(launch_dependent(kv_prompt_join_kernel<D>, dim3(unsigned((a.b.rows * a.q_heads + 3) / 4)), dim3(128), 0, st, a));
