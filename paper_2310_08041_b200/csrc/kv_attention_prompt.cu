@@ -7,7 +7,8 @@
 // about 3.5 issue slots per score and 1.5 per code unpacked, each key tile being unpacked once for 256 rows.
 //
 // Roles (16 warps): 0-3 and 4-7 the softmax of tiles 0 and 1 (a thread per row), 8-11 unpack codes (a thread per token), 12
-// fetches codes and parameters with bulk copies, 13 issues the MMAs.
+// fetches codes and parameters with bulk copies, 13 issues the MMAs, 14 turns a tile's parameters into what the others need.
+// Registers are shifted to the softmax warps.
 //
 // Operands.  Keys enter as the exact integers (code - zero), the scale multiplies finished scores: a nibble under the
 // exponent of 1024 is the fp16 number 1024 + c (1024 + 16 c from the upper half of a byte), one packed fp16 operation makes
@@ -35,7 +36,7 @@ using tc::wait_bounded;
 
 constexpr int BM = 128, BN = 128;                          // query rows of a tile, tokens of a key tile
 constexpr int kThreads = 512;
-constexpr int kSlots = 3;                                  // key tiles whose parameters are held
+constexpr int kSlots = 4;                                  // key tiles whose parameters are held
 constexpr float kPlace = 6.f, kSlack = 8.f;                // as in kv_attention_split.cu
 
 template <int D>
@@ -47,7 +48,7 @@ struct Shape {
     static constexpr int RAWS = 3;
     static constexpr int RAWP = 2 * BN * 8;                // both parameter arrays, fetched with the keys: two of them
     static constexpr int PRM = BN * 4;                     // one float per token
-    static constexpr int SMEM = 1024 + 2 * OP + OPS * OP + RAWS * RAW + 2 * RAWP + 3 * kSlots * PRM;
+    static constexpr int SMEM = 1024 + 2 * OP + OPS * OP + RAWS * RAW + 2 * RAWP + 2 * kSlots * PRM;
     static constexpr uint32_t TMEM_S = 0, TMEM_O = 256;    // columns: S_0, S_1, O_0, O_1
 };
 
@@ -120,6 +121,26 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                  : "memory");
 }
 
+// Shared memory by 32-bit address: what is reached through pointers handed to functions would be generic accesses.
+__device__ __forceinline__ float4 lds4(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds1(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint4 lds4u(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ void sts4(uint32_t a, uint4 v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
 // ---- work -----------------------------------------------------------------------------------------------------------------
 struct Args {
     Cache c;
@@ -160,45 +181,54 @@ __device__ __forceinline__ uint4 unpack8_far(uint32_t w, float zero, float facto
     return make_uint4(h[0], h[1], h[2], h[3]);
 }
 
-// A thread's token: 64 / 32 bytes of codes -> its row of an operand tile.
+// Zero-points for which 1024 + zero, or code - zero, is no exact fp16 integer.
+__device__ __forceinline__ bool is_far(float zero) { return fabsf(zero) > 900.f || zero != rintf(zero); }
+
+// A thread's token: 64 / 32 bytes of codes -> its row of an operand tile (shared addresses).
 template <int D, bool VALUES>
-__device__ __forceinline__ void unpack_row(const uint8_t* raw, uint8_t* op, int tok, float zero, float factor, bool far) {
+__device__ __forceinline__ void unpack_row(uint32_t raw, uint32_t op, int tok, float zero, float factor, bool far) {
     constexpr int CH = D / 32;                             // 16-byte chunks of a row
-    const uint8_t* src = raw + tok * (D / 2);
-    uint8_t* dst = op + tok * 128;
-    auto unit = [&](int u) { return reinterpret_cast<uint4*>(dst + (u >> 3) * Shape<D>::ATOM + (((u & 7) ^ (tok & 7)) << 4)); };   // 8 channels
+    const uint32_t src = raw + tok * (D / 2), dst = op + tok * 128;
+    auto unit = [&](int u) { return dst + (u >> 3) * Shape<D>::ATOM + (((u & 7) ^ (tok & 7)) << 4); };      // 8 channels
     if (far) {
 #pragma unroll 1
-        for (int u = 0; u < D / 8; ++u) *unit(u) = unpack8_far(reinterpret_cast<const uint32_t*>(src)[u], zero, factor);
+        for (int u = 0; u < D / 8; ++u) sts4(unit(u), unpack8_far(lds1(src + 4 * u), zero, factor));
         return;
     }
     const __half2 sub = __float2half2_rn(-(1024.f + zero)), sub16 = __float2half2_rn(-(64.f + zero)), mul = __float2half2_rn(factor);
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < CH; ++i) {
         const int ch = (i + (CH == 4 ? tok >> 1 : tok >> 2)) & (CH - 1);     // neighbours read different banks
-        const uint4 w = *reinterpret_cast<const uint4*>(src + 16 * ch);
-        *unit(4 * ch) = unpack8<VALUES>(w.x, sub, sub16, mul);
-        *unit(4 * ch + 1) = unpack8<VALUES>(w.y, sub, sub16, mul);
-        *unit(4 * ch + 2) = unpack8<VALUES>(w.z, sub, sub16, mul);
-        *unit(4 * ch + 3) = unpack8<VALUES>(w.w, sub, sub16, mul);
+        const uint4 w = lds4u(src + 16 * ch);
+        sts4(unit(4 * ch), unpack8<VALUES>(w.x, sub, sub16, mul));
+        sts4(unit(4 * ch + 1), unpack8<VALUES>(w.y, sub, sub16, mul));
+        sts4(unit(4 * ch + 2), unpack8<VALUES>(w.z, sub, sub16, mul));
+        sts4(unit(4 * ch + 3), unpack8<VALUES>(w.w, sub, sub16, mul));
     }
 }
 
-// 32 scores of a row as they lie in tensor memory, times the keys' scales; MASKED: -infinity where the row does not see the token.
+// A row's 128 scores as they lie in tensor memory (`addr`) become its weights in their place (16 columns for 32: a chunk
+// overwrites what has been read).  ks, vs, there: shared addresses of the key tile's key scales, value scales, bits of the tokens
+// that exist.  MASKED: some token of the tile is hidden from some row; BARE: the weights carry the value scales.
+//
+// Two passes, maximum and weights, in loops of 32 columns that stay rolled, as the unpacking does: four roles run at once, and
+// what bounds them is fetching instructions.  Unrolled over the tile, with the row held in registers between the passes, a
+// chunk of 1024 tokens behind up to 8191 (64/8 heads) took 453 us instead of 417; in one pass with a second one in the rare
+// case that the reference moved, 515.
 template <bool MASKED>
-__device__ __forceinline__ void scores32(uint32_t addr, const float* ks, int first, int limit, const uint32_t* there, F2 (&y)[16]) {
+__device__ __forceinline__ void scores32(uint32_t addr, uint32_t ks, int first, int limit, uint32_t there, F2 (&y)[16]) {
     uint32_t r[32];
     ptx::tmem_ld_32x32b_x32(addr, r);
     ptx::tmem_ld_wait();
+    const int n = limit - first;                           // tokens of the 32 in front of the limit
+    const uint32_t seen = !MASKED ? 0 : lds1(there) & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1);
 #pragma unroll
     for (int k = 0; k < 16; k += 2) {
-        const float4 v = *reinterpret_cast<const float4*>(ks + 2 * k);
+        const float4 v = lds4(ks + 8 * k);
         y[k] = mul2(F2(r[2 * k], r[2 * k + 1]), F2(v.x, v.y));
         y[k + 1] = mul2(F2(r[2 * k + 2], r[2 * k + 3]), F2(v.z, v.w));
     }
     if (MASKED) {
-        const int n = limit - first;                       // tokens of the 32 in front of the limit
-        const uint32_t seen = *there & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1);
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             float a, b;
@@ -207,53 +237,55 @@ __device__ __forceinline__ void scores32(uint32_t addr, const float* ks, int fir
         }
     }
 }
-// Largest score of a row in a key tile, in base 2 and times the largest value: the loops over 32 columns stay rolled, which
-// keeps the code of all roles in the instruction cache (unrolled over the tile the kernel took four times as long).
+__device__ __forceinline__ float log_scale(float v) { return fminf(fmaxf(lg2(fabsf(v)), -80.f), 80.f); }
 template <bool MASKED, bool BARE>
-__device__ __forceinline__ float tile_max(uint32_t t_s, const float* ks, const float* lv, int first, int limit, const uint32_t* there, float qn, float e) {
-    float m[2] = {-INFINITY, -INFINITY};
+__device__ __forceinline__ float tile_max(uint32_t addr, uint32_t ks, uint32_t vs, int first, int limit, uint32_t there, float qn, float e) {
+    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
     for (int c = 0; c < BN / 32; ++c) {
         F2 y[16];
-        scores32<MASKED>(t_s + 32 * c, ks + 32 * c, first + 32 * c, limit, there + c, y);
+        scores32<MASKED>(addr + 32 * c, ks + 128 * c, first + 32 * c, limit, there + 4 * c, y);
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
+            if (BARE) {                                    // s_j + log2 vs_j, cut to +-80
+                float a, b;
+                F2(lds1(vs + 128 * c + 8 * k), lds1(vs + 128 * c + 8 * k + 4)).get(a, b);
+                y[k] = fma2(y[k], F2(qn, qn), F2(log_scale(a), log_scale(b)));
+            }
             float a, b;
-            if (BARE) y[k] = fma2(y[k], F2(qn, qn), *reinterpret_cast<const F2*>(lv + 32 * c + 2 * k));
             y[k].get(a, b);
-            m[k & 1] = fmaxf(m[k & 1], fmaxf(a, b));
+            m[k & 3] = fmaxf(m[k & 3], fmaxf(a, b));
         }
     }
-    const float x = fmaxf(m[0], m[1]);
+    const float x = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
     return BARE ? x : fmaf(x, qn, e);
 }
-// The row's weights into the place of its scores (16 columns for 32: a chunk overwrites what has been read); returns their sum.
 template <bool MASKED, bool BARE>
-__device__ __forceinline__ float tile_weights(uint32_t t_s, const float* ks, const float* vs, int first, int limit, const uint32_t* there, float qn, float sub) {
-    F2 l[2] = {F2(0.f, 0.f), F2(0.f, 0.f)};
+__device__ __forceinline__ float tile_weights(uint32_t addr, uint32_t ks, uint32_t vs, int first, int limit, uint32_t there, float qn, float sub) {
+    const F2 q2(qn, qn), s2(sub, sub);
+    F2 l[4] = {F2(0.f, 0.f), F2(0.f, 0.f), F2(0.f, 0.f), F2(0.f, 0.f)};
 #pragma unroll 1
     for (int c = 0; c < BN / 32; ++c) {
         F2 y[16];
-        scores32<MASKED>(t_s + 32 * c, ks + 32 * c, first + 32 * c, limit, there + c, y);
+        scores32<MASKED>(addr + 32 * c, ks + 128 * c, first + 32 * c, limit, there + 4 * c, y);
         uint32_t p[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             float a, b;
-            fma2(y[k], F2(qn, qn), F2(sub, sub)).get(a, b);
-            float pa = ex2(a), pb = ex2(b);
-            l[k & 1] = add2(l[k & 1], F2(pa, pb));
-            if (BARE) {
-                // a hidden key's value scale may be anything
-                const float2 v = *reinterpret_cast<const float2*>(vs + 32 * c + 2 * k);
-                pa = pa == 0.f ? 0.f : pa * v.x;
-                pb = pb == 0.f ? 0.f : pb * v.y;
+            fma2(y[k], q2, s2).get(a, b);
+            a = ex2(a);
+            b = ex2(b);
+            l[k & 3] = add2(l[k & 3], F2(a, b));
+            if (BARE) {                                    // (a hidden key's value scale may be anything)
+                a = a == 0.f ? 0.f : a * __uint_as_float(lds1(vs + 128 * c + 8 * k));
+                b = b == 0.f ? 0.f : b * __uint_as_float(lds1(vs + 128 * c + 8 * k + 4));
             }
-            p[k] = bits(__floats2half2_rn(pa, pb));
+            p[k] = bits(__floats2half2_rn(a, b));
         }
-        tmem_st_x16(t_s + 16 * c, p);
+        tmem_st_x16(addr + 16 * c, p);
     }
     float a, b;
-    add2(l[0], l[1]).get(a, b);
+    add2(add2(l[0], l[1]), add2(l[2], l[3])).get(a, b);
     return a + b;
 }
 
@@ -267,11 +299,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
     uint8_t* s_raw = s_op + S::OPS * S::OP;                // [RAWS]
     uint8_t* s_rawp = s_raw + S::RAWS * S::RAW;            // [2] (a third tile's keys wait for the first one's values to be unpacked)
     float* s_ks = reinterpret_cast<float*>(s_rawp + 2 * S::RAWP);            // [kSlots][BN] key scales
-    float* s_vs = s_ks + kSlots * BN;                      // value scales and their logarithms, for tiles of bare codes
-    float* s_lv = s_vs + kSlots * BN;
+    float* s_vs = s_ks + kSlots * BN;                      // value scales, for tiles of bare codes
     __shared__ uint64_t s_bar[32];
     __shared__ uint32_t s_tmem, s_pieces[S::RAWS];
-    __shared__ int s_abort, s_find[4], s_exp[2 * 4];
+    __shared__ int s_abort, s_find[2];
     __shared__ float s_e[kSlots];                          // exponent of a tile's values
     __shared__ uint32_t s_flags[kSlots], s_there[kSlots][4];                 // 1: bare codes, 2: some tokens are not there (bits)
     uint64_t* raw_full = s_bar;                            // [RAWS]
@@ -288,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::RAWS; ++i) { ptx::mbar_init(&raw_full[i], 1); ptx::mbar_init(&raw_empty[i], 4); }
         for (int i = 0; i < S::OPS; ++i) { ptx::mbar_init(&op_full[i], 4); ptx::mbar_init(&op_empty[i], 1); }
-        for (int i = 0; i < kSlots; ++i) ptx::mbar_init(&prm_full[i], 4);
+        for (int i = 0; i < kSlots; ++i) ptx::mbar_init(&prm_full[i], 1);
         for (int i = 0; i < 2; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 4); ptx::mbar_init(&o_full[i], 1); }
         ptx::mbar_init(q_full, 8);
         s_abort = 0;
@@ -350,6 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
 
     if (warp < 8) {
         // ------------------------------------------------------------------------------------------------ softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");                // 256 * 184 + 256 * 72 = 512 * 128
         const int t = warp >> 2, local = threadIdx.x & 127;
         const unsigned rr = (2 * unsigned(blk) + t) * BM + local, i = rr / unsigned(a.group);
         const bool real = rr < rows;
@@ -397,18 +429,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
             const int slot = (j - j0) % kSlots;
             if (!wait_bounded(&prm_full[slot], ((j - j0) / kSlots) & 1, ab) || !wait_bounded(&s_full[t], (j - j0) & 1, ab)) { ok = false; break; }
             ptx::tc_fence_after_sync();
-            const float* ks = s_ks + slot * BN;
+            const uint32_t ks = ptx::smem_addr(s_ks + slot * BN);
             const uint32_t flags = s_flags[slot];
             const int first = j * BN;
             const bool masked = first + BN > low || (flags & 2);
-            const float e = s_e[slot], *vs = s_vs + slot * BN, *lv = s_lv + slot * BN;
-            const uint32_t* there = s_there[slot];
+            const float e = s_e[slot];
+            const uint32_t vs = ks + kSlots * S::PRM, there = ptx::smem_addr(s_there[slot]);
             const bool bare = flags & 1;
-            const float m = bare     ? tile_max<true, true>(t_s, ks, lv, first, limit, there, qn, e)
-                            : masked ? tile_max<true, false>(t_s, ks, lv, first, limit, there, qn, e)
-                                     : tile_max<false, false>(t_s, ks, lv, first, limit, there, qn, e);
+            const float m = bare     ? tile_max<true, true>(t_s, ks, vs, first, limit, there, qn, e)
+                            : masked ? tile_max<true, false>(t_s, ks, vs, first, limit, there, qn, e)
+                                     : tile_max<false, false>(t_s, ks, vs, first, limit, there, qn, e);
+            // the reference moves only when a weight would pass 2^(kPlace + kSlack)
             if (__any_sync(0xffffffffu, m > top + (kPlace + kSlack))) {
-                const float to = fmaxf(m - kPlace, top), fix = to == -INFINITY ? 1.f : ex2(top - to);
+                const float to = m > top + (kPlace + kSlack) ? m - kPlace : top, fix = to == top ? 1.f : ex2(top - to);
                 top = to;
                 l *= fix;
                 if (j > j0) {
@@ -476,92 +509,101 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
             }
         }
     } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         const int piece_log2 = min(a.b.page_log2, 7), per_tile = BN >> piece_log2;
         if (warp < 12) {
             // -------------------------------------------------------------------------------------------- unpack
-            const int tok = threadIdx.x - 256, uw = warp - 8;
+            const int tok = threadIdx.x - 256;
             bool ok = true;
             uint32_t step = 0;                             // 2 * tile + (0 keys, 1 values)
-            const int top_keys = !a.causal ? len : max(len - n + int((min((2 * unsigned(blk) + 2) * BM, rows) - 1) / unsigned(a.group)) + 1, 0);
             for (int j = j0; ok && j < j1; ++j) {
-                float kz, kf, vz, vf;
-                bool kfar, vfar;
                 const int slot = (j - j0) % kSlots;
-                // ---- keys, and both parameters
-                {
+                const uint32_t prm = ptx::smem_addr(s_rawp + ((j - j0) & 1) * S::RAWP) + 8 * tok;
+                if (!wait_bounded(&prm_full[slot], ((j - j0) / kSlots) & 1, ab)) { ok = false; break; }
+#pragma unroll 1
+                for (int v = 0; v < 2; ++v, ++step) {      // keys, values
                     const int rs = step % S::RAWS, ob = step % S::OPS;
+                    const uint32_t raw = ptx::smem_addr(s_raw + rs * S::RAW), op = ptx::smem_addr(s_op + ob * S::OP);
                     if (!wait_bounded(&raw_full[rs], (step / S::RAWS) & 1, ab)) { ok = false; break; }
-                    const uint8_t* raw = s_raw + rs * S::RAW;
-                    const uint32_t pieces = s_pieces[rs];
+                    const float zero = __uint_as_float(lds1(prm + v * (BN * 8))), factor = __uint_as_float(lds1(prm + v * (BN * 8) + 4));
+                    const bool far = is_far(zero);
+                    if (!wait_bounded(&op_empty[ob], ((step / S::OPS) & 1) ^ 1, ab)) { ok = false; break; }
+                    if (v == 0) unpack_row<D, false>(raw, op, tok, zero, factor, far);
+                    else unpack_row<D, true>(raw, op, tok, zero, factor, far);
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) { ptx::mbar_arrive(&op_full[ob]); ptx::mbar_arrive(&raw_empty[rs]); }
+                }
+            }
+        } else if (warp == 14) {
+            // -------------------------------------------------------------------------------------------- parameters
+            // Lane l has tokens l, l + 32, ..  The (zero, factor) that unpacking needs takes the place of (scale, zero).
+            const int top_keys = !a.causal ? len : max(len - n + int((min((2 * unsigned(blk) + 2) * BM, rows) - 1) / unsigned(a.group)) + 1, 0);
+            for (int j = j0; j < j1; ++j) {
+                const int slot = (j - j0) % kSlots, step = 2 * (j - j0), rs = step % S::RAWS;
+                if (!wait_bounded(&raw_full[rs], (step / S::RAWS) & 1, ab)) break;
+                const uint32_t pieces = s_pieces[rs];
+                float2* prm = reinterpret_cast<float2*>(s_rawp + ((j - j0) & 1) * S::RAWP);
+                float vx[4], vz[4];
+                int hi = -1000, lo = 1000;
+                uint32_t goods = 0, everywhere = 0xffffffffu;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int tok = 32 * i + lane;
                     const bool good = j * BN + tok < top_keys && ((pieces >> (tok >> piece_log2)) & 1u);
-                    const float2* prm = reinterpret_cast<const float2*>(s_rawp + ((j - j0) & 1) * S::RAWP);
                     float2 kp = prm[tok], vp = prm[BN + tok];
                     if (!good) kp = vp = make_float2(0.f, 0.f);
-                    // keys: (code - zero) 2^-k, k = 0 unless the zero-point is far off
-                    kf = 1.f;
+                    goods |= uint32_t(good) << i;
                     // parameters that are no numbers: the operands stay finite, a row that sees the token gets it from the score
                     if (!(fabsf(vp.x) <= 3e38f && fabsf(vp.y) <= 3e38f)) { kp.x = NAN; vp = make_float2(0.f, 0.f); }
                     if (!(fabsf(kp.y) <= 3e38f)) { kp.x = NAN; kp.y = 0.f; }
-                    kfar = fabsf(kp.y) > 900.f || kp.y != rintf(kp.y);
-                    if (kfar) {
+                    // keys: (code - zero) 2^-k, k = 0 unless the zero-point is far off
+                    float kf = 1.f;
+                    if (is_far(kp.y)) {
                         const int k = min(max(int((__float_as_uint(kp.y) >> 23) & 255u) - 127 - 9, 0), 120);
                         kf = pow2i(-k);
                         kp.x *= pow2i(k);
                     }
-                    kz = kp.y;
                     s_ks[slot * BN + tok] = kp.x;
-                    // values
-                    vz = vp.y;
-                    vfar = fabsf(vz) > 900.f || vz != rintf(vz);
-                    const float far_value = fabsf(vp.x) * fmaxf(fabsf(vz), fabsf(15.f - vz));    // the largest value of the row
-                    const bool fits = far_value < 1.2e24f;                   // 2^80, as the cut of the logarithm
-                    const int ex = !good || far_value == 0.f ? -1000 : !fits ? 1000 : max(int(__float_as_uint(far_value) >> 23) - 127, -80);
-                    const int hi = __reduce_max_sync(0xffffffffu, ex), lo = __reduce_min_sync(0xffffffffu, good && far_value != 0.f ? ex : 1000);
-                    if (lane == 0) { s_exp[uw] = hi; s_exp[4 + uw] = lo; }
+                    prm[tok] = make_float2(kp.y, kf);
+                    vx[i] = vp.x;
+                    vz[i] = vp.y;
+                    const float largest = fabsf(vp.x) * fmaxf(fabsf(vp.y), fabsf(15.f - vp.y));
+                    if (good && largest != 0.f) {
+                        const int ex = largest < 1.2e24f ? max(int(__float_as_uint(largest) >> 23) - 127, -80) : 1000;   // 2^80: the logarithm's cut
+                        hi = max(hi, ex);
+                        lo = min(lo, ex);
+                    }
                     const uint32_t there = __ballot_sync(0xffffffffu, good);
-                    if (lane == 0) s_there[slot][uw] = there;
-                    ptx::named_bar_sync(2, 128);
-                    const int e = max(max(s_exp[0], s_exp[1]), max(s_exp[2], s_exp[3])), f = min(min(s_exp[4], s_exp[5]), min(s_exp[6], s_exp[7]));
-                    const bool bare = e > 900 || (f < 900 && e - f > 10);
-                    const int et = bare || e < -900 ? 0 : e;
+                    everywhere &= there;
+                    if (lane == 0) s_there[slot][i] = there;
+                }
+                hi = __reduce_max_sync(0xffffffffu, hi);
+                lo = __reduce_min_sync(0xffffffffu, lo);
+                const bool bare = hi > 900 || hi - lo > 10;                  // (no values at all: -1000 and 1000)
+                const int e = bare || hi < -900 ? 0 : hi;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float vf = 1.f;
                     if (bare) {
-                        vf = 1.f;
-                        if (vfar) {
-                            const int k = min(max(int((__float_as_uint(vz) >> 23) & 255u) - 127 - 9, 0), 120);
+                        if (is_far(vz[i])) {
+                            const int k = min(max(int((__float_as_uint(vz[i]) >> 23) & 255u) - 127 - 9, 0), 120);
                             vf = pow2i(-k);
-                            vp.x *= pow2i(k);
+                            vx[i] *= pow2i(k);
                         }
-                        s_vs[slot * BN + tok] = vp.x;
-                        s_lv[slot * BN + tok] = fminf(fmaxf(lg2(fabsf(vp.x)), -80.f), 80.f);
+                        s_vs[slot * BN + 32 * i + lane] = vx[i];
                     } else {
-                        vf = vp.x * pow2i(-et);
+                        vf = vx[i] * pow2i(-e);
                     }
-                    if (!good) vf = 0.f;
-                    if (tok == 0) {
-                        s_e[slot] = float(et);
-                        s_flags[slot] = bare ? 1 : 0;
-                    }
-                    ptx::named_bar_sync(2, 128);           // s_exp is free again; tile-wide flags follow
-                    if (lane == 0 && there != 0xffffffffu) atomicOr(&s_flags[slot], 2u);
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(&prm_full[slot]);
-                    if (!wait_bounded(&op_empty[ob], ((step / S::OPS) & 1) ^ 1, ab)) { ok = false; break; }
-                    unpack_row<D, false>(raw, s_op + ob * S::OP, tok, kz, kf, kfar);
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) { ptx::mbar_arrive(&op_full[ob]); ptx::mbar_arrive(&raw_empty[rs]); }
-                    ++step;
+                    prm[BN + 32 * i + lane] = make_float2(vz[i], goods >> i & 1 ? vf : 0.f);
                 }
-                // ---- values
-                {
-                    const int rs = step % S::RAWS, ob = step % S::OPS;
-                    if (!wait_bounded(&raw_full[rs], (step / S::RAWS) & 1, ab) || !wait_bounded(&op_empty[ob], ((step / S::OPS) & 1) ^ 1, ab)) { ok = false; break; }
-                    unpack_row<D, true>(s_raw + rs * S::RAW, s_op + ob * S::OP, tok, vz, vf, vfar);
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) { ptx::mbar_arrive(&op_full[ob]); ptx::mbar_arrive(&raw_empty[rs]); }
-                    ++step;
+                if (lane == 0) {
+                    s_e[slot] = float(e);
+                    s_flags[slot] = (bare ? 1 : 0) | (everywhere != 0xffffffffu ? 2 : 0);
                 }
+                ptx::fence_proxy_async_smem();             // the next bulk copy into prm comes after these writes
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&prm_full[slot]);
             }
         } else if (warp == 12) {
             // -------------------------------------------------------------------------------------------- codes in
