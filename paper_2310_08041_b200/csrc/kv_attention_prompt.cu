@@ -32,6 +32,7 @@ namespace {
 
 using namespace kv;
 using tc::Abort;
+
 using tc::wait_bounded;
 
 constexpr int BM = 128, BN = 128;                          // query rows of a tile, tokens of a key tile
@@ -57,21 +58,28 @@ struct Shape {
 __host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn) {
     return (1u << 4) | (0u << 7) | (0u << 10) | (uint32_t(b_mn) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
 }
-__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
-                 "l"(b), "r"(idesc), "r"(uint32_t(accumulate))
+// Shared-memory operands are given by the low words of their descriptors (the high word is the same for all): a step along an
+// operand is one addition, and the issuing warp, whose every instruction waits for its turn among 15 others, is not what the
+// tensor core waits for.
+constexpr uint32_t kDescHigh = uint32_t((uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61) >> 32);
+__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
                  : "memory");
 }
-__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a),
-                 "l"(b), "r"(idesc), "r"(uint32_t(accumulate))
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
                  : "memory");
 }
-// N-major operand: rows (K) of 64 elements, groups of 8 rows 1024 bytes apart, blocks of 64 N-elements `block` bytes apart
-__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr, uint32_t block) {
-    uint64_t d = ptx::smem_desc_sw128(addr) & ~(uint64_t(0x3FFF) << 16);
-    return d | (uint64_t(block >> 4) << 16);
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r;
 }
+// Low word of a descriptor in the 128-byte swizzle: address, and (N-major operands: rows of 64 elements along K, groups of 8 rows
+// 1024 bytes apart) the distance between blocks of 64 N-elements.
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t block) { return (addr & 0x3FFFFu) >> 4 | (block >> 4) << 16; }
 __device__ __forceinline__ void tmem_st_x32(uint32_t addr, const uint32_t (&r)[32]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
@@ -216,10 +224,7 @@ __device__ __forceinline__ void unpack_row(uint32_t raw, uint32_t op, int tok, f
 // chunk of 1024 tokens behind up to 8191 (64/8 heads) took 453 us instead of 417; in one pass with a second one in the rare
 // case that the reference moved, 515.
 template <bool MASKED>
-__device__ __forceinline__ void scores32(uint32_t addr, uint32_t ks, int first, int limit, uint32_t there, F2 (&y)[16]) {
-    uint32_t r[32];
-    ptx::tmem_ld_32x32b_x32(addr, r);
-    ptx::tmem_ld_wait();
+__device__ __forceinline__ void scores32(const uint32_t (&r)[32], uint32_t ks, int first, int limit, uint32_t there, F2 (&y)[16]) {
     const int n = limit - first;                           // tokens of the 32 in front of the limit
     const uint32_t seen = !MASKED ? 0 : lds1(there) & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1);
 #pragma unroll
@@ -241,10 +246,14 @@ __device__ __forceinline__ float log_scale(float v) { return fminf(fmaxf(lg2(fab
 template <bool MASKED, bool BARE>
 __device__ __forceinline__ float tile_max(uint32_t addr, uint32_t ks, uint32_t vs, int first, int limit, uint32_t there, float qn, float e) {
     float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    uint32_t next[32];
+    ptx::tmem_ld_32x32b_x32(addr, next);
 #pragma unroll 1
     for (int c = 0; c < BN / 32; ++c) {
+        ptx::tmem_ld_wait();
         F2 y[16];
-        scores32<MASKED>(addr + 32 * c, ks + 128 * c, first + 32 * c, limit, there + 4 * c, y);
+        scores32<MASKED>(next, ks + 128 * c, first + 32 * c, limit, there + 4 * c, y);
+        if (c + 1 < BN / 32) ptx::tmem_ld_32x32b_x32(addr + 32 * (c + 1), next);           // in flight under this chunk
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             if (BARE) {                                    // s_j + log2 vs_j, cut to +-80
@@ -264,10 +273,14 @@ template <bool MASKED, bool BARE>
 __device__ __forceinline__ float tile_weights(uint32_t addr, uint32_t ks, uint32_t vs, int first, int limit, uint32_t there, float qn, float sub) {
     const F2 q2(qn, qn), s2(sub, sub);
     F2 l[4] = {F2(0.f, 0.f), F2(0.f, 0.f), F2(0.f, 0.f), F2(0.f, 0.f)};
+    uint32_t next[32];
+    ptx::tmem_ld_32x32b_x32(addr, next);
 #pragma unroll 1
     for (int c = 0; c < BN / 32; ++c) {
+        ptx::tmem_ld_wait();
         F2 y[16];
-        scores32<MASKED>(addr + 32 * c, ks + 128 * c, first + 32 * c, limit, there + 4 * c, y);
+        scores32<MASKED>(next, ks + 128 * c, first + 32 * c, limit, there + 4 * c, y);
+        if (c + 1 < BN / 32) ptx::tmem_ld_32x32b_x32(addr + 32 * (c + 1), next);
         uint32_t p[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
@@ -656,16 +669,26 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                     while (!ptx::mbar_try_wait(&raw_full[x % S::RAWS], (x / S::RAWS) & 1) && clock64() - t0 < (1ll << 24)) {}
                 }
             }
-        } else if (warp == 13 && lane == 0) {
+        } else if (warp == 13) {
             // -------------------------------------------------------------------------------------------- MMAs
             constexpr uint32_t id_s = idesc_f16(BM, BN, false), id_o = idesc_f16(BM, D, true);
+            const uint32_t leader = elect_one();
+            const uint32_t q_low = desc_low(ptx::smem_addr(s_q), 16), k_low = desc_low(ptx::smem_addr(s_op), 16), v_low = desc_low(ptx::smem_addr(s_op), S::ATOM);
             auto score = [&](int t, int ob) {
-                const uint32_t q = ptx::smem_addr(s_q + t * S::OP), k = ptx::smem_addr(s_op + ob * S::OP);
+                const uint32_t q = q_low + t * (S::OP >> 4), k = k_low + ob * (S::OP >> 4);
+                if (leader) {
 #pragma unroll
-                for (int x = 0; x < D / 16; ++x)
-                    mma_f16_ss(tmem + S::TMEM_S + t * BN, ptx::smem_desc_sw128(q + (x >> 2) * S::ATOM + (x & 3) * 32),
-                               ptx::smem_desc_sw128(k + (x >> 2) * S::ATOM + (x & 3) * 32), id_s, x != 0);
-                ptx::mma_commit(&s_full[t]);
+                    for (int x = 0; x < D / 16; ++x) {
+                        const uint32_t at = ((x >> 2) * S::ATOM + (x & 3) * 32) >> 4;
+                        mma_f16_ss(tmem + S::TMEM_S + t * BN, q + at, k + at, id_s, x != 0);
+                    }
+                    ptx::mma_commit(&s_full[t]);
+                }
+                __syncwarp();
+            };
+            auto commit = [&](uint64_t* bar) {
+                if (leader) ptx::mma_commit(bar);
+                __syncwarp();
             };
             bool ok = wait_bounded(q_full, 0, ab);
             if (ok && j0 < j1) {
@@ -674,7 +697,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                     ptx::tc_fence_after_sync();
                     if (j0 < nt[0]) score(0, 0);
                     if (j0 < nt[1]) score(1, 0);
-                    ptx::mma_commit(&op_empty[0]);
+                    commit(&op_empty[0]);
                 }
             }
             for (int j = j0; ok && j < j1; ++j) {
@@ -682,20 +705,23 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 const bool more = j + 1 < j1;
                 if (!wait_bounded(&op_full[sv % S::OPS], (sv / S::OPS) & 1, ab)) break;
                 if (more && !wait_bounded(&op_full[sk % S::OPS], (sk / S::OPS) & 1, ab)) break;
-                const uint32_t v = ptx::smem_addr(s_op + (sv % S::OPS) * S::OP);
+                const uint32_t v = v_low + (sv % S::OPS) * (S::OP >> 4);
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     if (j >= nt[t]) continue;
                     if (!wait_bounded(&p_full[t], (j - j0) & 1, ab)) { ok = false; break; }
                     ptx::tc_fence_after_sync();
+                    if (leader) {
 #pragma unroll
-                    for (int x = 0; x < BN / 16; ++x)
-                        mma_f16_ts(tmem + S::TMEM_O + t * D, tmem + S::TMEM_S + t * BN + 8 * x, smem_desc_mn(v + x * 2048, S::ATOM), id_o, j > j0 || x > 0);
+                        for (int x = 0; x < BN / 16; ++x)
+                            mma_f16_ts(tmem + S::TMEM_O + t * D, tmem + S::TMEM_S + t * BN + 8 * x, v + x * (2048 >> 4), id_o, x > 0 ? 1u : uint32_t(j > j0));
+                    }
+                    __syncwarp();
                     if (more && j + 1 < nt[t]) score(t, sk % S::OPS);
-                    else ptx::mma_commit(&o_full[t]);
+                    else commit(&o_full[t]);
                 }
-                ptx::mma_commit(&op_empty[sv % S::OPS]);
-                if (more) ptx::mma_commit(&op_empty[sk % S::OPS]);
+                commit(&op_empty[sv % S::OPS]);
+                if (more) commit(&op_empty[sk % S::OPS]);
             }
         }
     }
