@@ -1,23 +1,24 @@
 // Attention over the 4-bit cache for many query rows per key head (prompts, chunks of prompts): tcgen05 tensor cores.
 //
 // A CTA owns 256 query rows of one key head (query tokens x the heads of the group, two tiles of 128) and walks the keys in
-// tiles of 128 tokens.  Both products run as 128 x 128 tcgen05 MMAs in fp16: S_t = Q_t K^T into tensor memory, softmax by one
-// thread per row, P_t back into tensor memory over S_t, O_t += P_t V.  While one tile's rows are in the softmax, the
-// tensor core works for the other.  The tensor pipe bounds it: 4 * 128 * 128 * head_dim operations a tile pair against
-// about 3.5 issue slots per score and 1.5 per code unpacked, each key tile being unpacked once for 256 rows.
+// tiles of 128 tokens.  Both products run as 128 x 128 tcgen05 MMAs in fp16: S_t = Q_t K^T into tensor memory, softmax by two
+// threads per row (64 columns each), P_t back into tensor memory over S_t, O_t += P_t V.  While one tile's rows are in the
+// softmax, the tensor core works for the other.  The tensor pipe's 4 * 256 * 128 * head_dim operations a step and the softmax's
+// issue slots are about equal; each key tile is unpacked once for 256 rows.
 //
-// Roles (16 warps): 0-3 and 4-7 the softmax of tiles 0 and 1 (a thread per row), 8-11 unpack codes (a thread per token), 12
-// fetches codes and parameters with bulk copies, 13 issues the MMAs, 14 turns a tile's parameters into what the others need.
-// Registers are shifted to the softmax warps.
+// Roles (24 warps): 0-7 and 8-15 the softmax of tiles 0 and 1, 16-19 unpack codes (a thread per token), 20 fetches codes and
+// parameters with bulk copies, 21 issues the MMAs, 22 turns a tile's parameters into what the others need.  Registers are
+// shifted to the softmax warps.
 //
-// Operands.  Keys enter as the exact integers (code - zero), the scale multiplies finished scores: a nibble under the
-// exponent of 1024 is the fp16 number 1024 + c (1024 + 16 c from the upper half of a byte), one packed fp16 operation makes
-// it c - zero.  Queries are scaled per row by a power of two into fp16 (a bf16 query's 8 bits are kept).  Values enter as
-// (code - zero) vs 2^-E, E the exponent of the tile's largest value, so that a weight is p 2^E and nothing acts per score and
-// token: rounded to fp16 in the scale and in the product, 11 bits each, where a bf16 result carries 8.  Tiles whose value
-// scales differ by more than 2^10, or pass 2^80, keep bare codes and multiply the weights by vs instead.  Rows far from
-// zero (|zero| > 900) round (code - zero) to 11 bits.  Channels lie in the order 0 4 1 5 2 6 3 7 of each eight, as the
-// masks leave them: the queries are stored alike and the output is put right at the end.
+// Operands.  A nibble under the exponent of 1024 is the fp16 number 1024 + c (1024 + 16 c from the upper half of a byte), one
+// packed fp16 operation makes it the exact integer c - zero, another the operand (c - zero) scale 2^-E, E the exponent of the
+// tile's largest key or value: rounded to fp16 in the scale and in the product, 11 bits each, where keys and values of 16 bits
+// would carry 8.  So nothing acts per score and token: a score's factor is the row's times 2^E, a weight is p 2^E.  Queries are
+// scaled per row by a power of two into fp16 (a bf16 query's 8 bits are kept).  Tiles whose value scales differ by more than
+// 2^10, or pass 2^80, keep the values' bare codes and multiply the weights by vs instead, since a weight of a small value must
+// not lose its bits to a large value that the row hardly looks at.  Rows far from zero (|zero| > 900) are made in float32.
+// Channels lie in the order 0 4 1 5 2 6 3 7 of each eight, as the masks leave them: the queries are stored alike and the output
+// is put right at the end.
 
 #include <cuda_fp16.h>
 
@@ -36,7 +37,7 @@ using tc::Abort;
 using tc::wait_bounded;
 
 constexpr int BM = 128, BN = 128;                          // query rows of a tile, tokens of a key tile
-constexpr int kThreads = 512;
+constexpr int kThreads = 768;
 constexpr int kSlots = 4;                                  // key tiles whose parameters are held
 constexpr float kPlace = 6.f, kSlack = 8.f;                // as in kv_attention_split.cu
 
@@ -49,7 +50,7 @@ struct Shape {
     static constexpr int RAWS = 3;
     static constexpr int RAWP = 2 * BN * 8;                // both parameter arrays, fetched with the keys: two of them
     static constexpr int PRM = BN * 4;                     // one float per token
-    static constexpr int SMEM = 1024 + 2 * OP + OPS * OP + RAWS * RAW + 2 * RAWP + 2 * kSlots * PRM;
+    static constexpr int SMEM = 1024 + 2 * OP + OPS * OP + RAWS * RAW + 2 * RAWP + kSlots * PRM;
     static constexpr uint32_t TMEM_S = 0, TMEM_O = 256;    // columns: S_0, S_1, O_0, O_1
 };
 
@@ -106,7 +107,6 @@ struct F2 {
     __device__ __forceinline__ F2(uint32_t a, uint32_t b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b)); }
     __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
 };
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
 __device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
 __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -130,11 +130,6 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 }
 
 // Shared memory by 32-bit address: what is reached through pointers handed to functions would be generic accesses.
-__device__ __forceinline__ float4 lds4(uint32_t a) {
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
-    return v;
-}
 __device__ __forceinline__ uint32_t lds1(uint32_t a) {
     uint32_t v;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
@@ -170,15 +165,13 @@ __device__ __forceinline__ unsigned blocks_of(const Args& a, int s) {
     return rows <= unsigned(a.most_rows) ? 0 : (rows + 2 * BM - 1) / (2 * BM);
 }
 
-// One word of codes -> 8 fp16 of (code - zero), times `mul` for values.  far: zero does not fit the fast form.
-template <bool VALUES>
+// One word of codes -> 8 fp16 of (code - zero) mul.
 __device__ __forceinline__ uint4 unpack8(uint32_t w, __half2 sub, __half2 sub16, __half2 mul) {
     const uint32_t u = w >> 8;
     const __half2 sixteenth = __floats2half2_rn(0.0625f, 0.0625f);
-    __half2 h0 = __hadd2(halves((w & 0x000F000Fu) | 0x64006400u), sub), h1 = __hfma2(halves((w & 0x00F000F0u) | 0x64006400u), sixteenth, sub16);
-    __half2 h2 = __hadd2(halves((u & 0x000F000Fu) | 0x64006400u), sub), h3 = __hfma2(halves((u & 0x00F000F0u) | 0x64006400u), sixteenth, sub16);
-    if (VALUES) { h0 = __hmul2(h0, mul); h1 = __hmul2(h1, mul); h2 = __hmul2(h2, mul); h3 = __hmul2(h3, mul); }
-    return make_uint4(bits(h0), bits(h1), bits(h2), bits(h3));
+    const __half2 h0 = __hadd2(halves((w & 0x000F000Fu) | 0x64006400u), sub), h1 = __hfma2(halves((w & 0x00F000F0u) | 0x64006400u), sixteenth, sub16);
+    const __half2 h2 = __hadd2(halves((u & 0x000F000Fu) | 0x64006400u), sub), h3 = __hfma2(halves((u & 0x00F000F0u) | 0x64006400u), sixteenth, sub16);
+    return make_uint4(bits(__hmul2(h0, mul)), bits(__hmul2(h1, mul)), bits(__hmul2(h2, mul)), bits(__hmul2(h3, mul)));
 }
 // the same for any zero: (code - zero) factor in float32, rounded once
 __device__ __forceinline__ uint4 unpack8_far(uint32_t w, float zero, float factor) {
@@ -193,7 +186,7 @@ __device__ __forceinline__ uint4 unpack8_far(uint32_t w, float zero, float facto
 __device__ __forceinline__ bool is_far(float zero) { return fabsf(zero) > 900.f || zero != rintf(zero); }
 
 // A thread's token: 64 / 32 bytes of codes -> its row of an operand tile (shared addresses).
-template <int D, bool VALUES>
+template <int D>
 __device__ __forceinline__ void unpack_row(uint32_t raw, uint32_t op, int tok, float zero, float factor, bool far) {
     constexpr int CH = D / 32;                             // 16-byte chunks of a row
     const uint32_t src = raw + tok * (D / 2), dst = op + tok * 128;
@@ -208,84 +201,65 @@ __device__ __forceinline__ void unpack_row(uint32_t raw, uint32_t op, int tok, f
     for (int i = 0; i < CH; ++i) {
         const int ch = (i + (CH == 4 ? tok >> 1 : tok >> 2)) & (CH - 1);     // neighbours read different banks
         const uint4 w = lds4u(src + 16 * ch);
-        sts4(unit(4 * ch), unpack8<VALUES>(w.x, sub, sub16, mul));
-        sts4(unit(4 * ch + 1), unpack8<VALUES>(w.y, sub, sub16, mul));
-        sts4(unit(4 * ch + 2), unpack8<VALUES>(w.z, sub, sub16, mul));
-        sts4(unit(4 * ch + 3), unpack8<VALUES>(w.w, sub, sub16, mul));
+        sts4(unit(4 * ch), unpack8(w.x, sub, sub16, mul));
+        sts4(unit(4 * ch + 1), unpack8(w.y, sub, sub16, mul));
+        sts4(unit(4 * ch + 2), unpack8(w.z, sub, sub16, mul));
+        sts4(unit(4 * ch + 3), unpack8(w.w, sub, sub16, mul));
     }
 }
 
-// A row's 128 scores as they lie in tensor memory (`addr`) become its weights in their place (16 columns for 32: a chunk
-// overwrites what has been read).  ks, vs, there: shared addresses of the key tile's key scales, value scales, bits of the tokens
-// that exist.  MASKED: some token of the tile is hidden from some row; BARE: the weights carry the value scales.
+// Half a row's scores as they lie in tensor memory (64 columns from `addr`) become its weights in their place (16 columns for
+// 32: a chunk overwrites what has been read).  vs, there: shared addresses of the half's value scales and bits of the tokens that
+// exist.  MASKED: some token of the tile is hidden from some row; BARE: the weights carry the value scales.
 //
-// Two passes, maximum and weights, in loops of 32 columns that stay rolled, as the unpacking does: four roles run at once, and
-// what bounds them is fetching instructions.  Unrolled over the tile, with the row held in registers between the passes, a
-// chunk of 1024 tokens behind up to 8191 (64/8 heads) took 453 us instead of 417; in one pass with a second one in the rare
-// case that the reference moved, 515.
+// Two passes, maximum and weights, in loops of 32 columns that stay rolled, as the unpacking does: unrolled over the tile, with
+// the row held in registers between the passes, the roles' code together outran the instruction cache (a chunk of 1024 tokens
+// behind up to 8191, 64/8 heads, one thread per row: 453 us instead of 417).
+constexpr int kCols = 64;
 template <bool MASKED>
-__device__ __forceinline__ void scores32(const uint32_t (&r)[32], uint32_t ks, int first, int limit, uint32_t there, F2 (&y)[16]) {
+__device__ __forceinline__ void hide(uint32_t (&r)[32], int first, int limit, uint32_t there) {
+    if (!MASKED) return;
     const int n = limit - first;                           // tokens of the 32 in front of the limit
-    const uint32_t seen = !MASKED ? 0 : lds1(there) & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1);
+    const uint32_t seen = lds1(there) & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1);
 #pragma unroll
-    for (int k = 0; k < 16; k += 2) {
-        const float4 v = lds4(ks + 8 * k);
-        y[k] = mul2(F2(r[2 * k], r[2 * k + 1]), F2(v.x, v.y));
-        y[k + 1] = mul2(F2(r[2 * k + 2], r[2 * k + 3]), F2(v.z, v.w));
-    }
-    if (MASKED) {
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            float a, b;
-            y[k].get(a, b);
-            y[k] = F2(seen >> (2 * k) & 1 ? a : -INFINITY, seen >> (2 * k + 1) & 1 ? b : -INFINITY);
-        }
-    }
+    for (int k = 0; k < 32; ++k) r[k] = seen >> k & 1 ? r[k] : 0xFF800000u;
 }
-__device__ __forceinline__ float log_scale(float v) { return fminf(fmaxf(lg2(fabsf(v)), -80.f), 80.f); }
+__device__ __forceinline__ float log_scale(uint32_t v) { return fminf(fmaxf(lg2(fabsf(__uint_as_float(v))), -80.f), 80.f); }
 template <bool MASKED, bool BARE>
-__device__ __forceinline__ float tile_max(uint32_t addr, uint32_t ks, uint32_t vs, int first, int limit, uint32_t there, float qn, float e) {
+__device__ __forceinline__ float half_max(uint32_t addr, uint32_t vs, int first, int limit, uint32_t there, float qn) {
     float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    uint32_t next[32];
-    ptx::tmem_ld_32x32b_x32(addr, next);
 #pragma unroll 1
-    for (int c = 0; c < BN / 32; ++c) {
+    for (int c = 0; c < kCols / 32; ++c) {
+        uint32_t r[32];
+        ptx::tmem_ld_32x32b_x32(addr + 32 * c, r);
         ptx::tmem_ld_wait();
-        F2 y[16];
-        scores32<MASKED>(next, ks + 128 * c, first + 32 * c, limit, there + 4 * c, y);
-        if (c + 1 < BN / 32) ptx::tmem_ld_32x32b_x32(addr + 32 * (c + 1), next);           // in flight under this chunk
+        hide<MASKED>(r, first + 32 * c, limit, there + 4 * c);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
+        for (int k = 0; k < 32; k += 2) {
+            float a = __uint_as_float(r[k]), b = __uint_as_float(r[k + 1]);
             if (BARE) {                                    // s_j + log2 vs_j, cut to +-80
-                float a, b;
-                F2(lds1(vs + 128 * c + 8 * k), lds1(vs + 128 * c + 8 * k + 4)).get(a, b);
-                y[k] = fma2(y[k], F2(qn, qn), F2(log_scale(a), log_scale(b)));
+                a = fmaf(a, qn, log_scale(lds1(vs + 128 * c + 4 * k)));
+                b = fmaf(b, qn, log_scale(lds1(vs + 128 * c + 4 * k + 4)));
             }
-            float a, b;
-            y[k].get(a, b);
-            m[k & 3] = fmaxf(m[k & 3], fmaxf(a, b));
+            m[k >> 1 & 3] = fmaxf(m[k >> 1 & 3], fmaxf(a, b));
         }
     }
-    const float x = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-    return BARE ? x : fmaf(x, qn, e);
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 template <bool MASKED, bool BARE>
-__device__ __forceinline__ float tile_weights(uint32_t addr, uint32_t ks, uint32_t vs, int first, int limit, uint32_t there, float qn, float sub) {
+__device__ __forceinline__ float half_weights(uint32_t addr, uint32_t vs, int first, int limit, uint32_t there, float qn, float sub) {
     const F2 q2(qn, qn), s2(sub, sub);
     F2 l[4] = {F2(0.f, 0.f), F2(0.f, 0.f), F2(0.f, 0.f), F2(0.f, 0.f)};
-    uint32_t next[32];
-    ptx::tmem_ld_32x32b_x32(addr, next);
 #pragma unroll 1
-    for (int c = 0; c < BN / 32; ++c) {
+    for (int c = 0; c < kCols / 32; ++c) {
+        uint32_t r[32], p[16];
+        ptx::tmem_ld_32x32b_x32(addr + 32 * c, r);
         ptx::tmem_ld_wait();
-        F2 y[16];
-        scores32<MASKED>(next, ks + 128 * c, first + 32 * c, limit, there + 4 * c, y);
-        if (c + 1 < BN / 32) ptx::tmem_ld_32x32b_x32(addr + 32 * (c + 1), next);
-        uint32_t p[16];
+        hide<MASKED>(r, first + 32 * c, limit, there + 4 * c);
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             float a, b;
-            fma2(y[k], q2, s2).get(a, b);
+            fma2(F2(r[2 * k], r[2 * k + 1]), q2, s2).get(a, b);
             a = ex2(a);
             b = ex2(b);
             l[k & 3] = add2(l[k & 3], F2(a, b));
@@ -311,12 +285,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
     uint8_t* s_op = s_q + 2 * S::OP;                       // [OPS]
     uint8_t* s_raw = s_op + S::OPS * S::OP;                // [RAWS]
     uint8_t* s_rawp = s_raw + S::RAWS * S::RAW;            // [2] (a third tile's keys wait for the first one's values to be unpacked)
-    float* s_ks = reinterpret_cast<float*>(s_rawp + 2 * S::RAWP);            // [kSlots][BN] key scales
-    float* s_vs = s_ks + kSlots * BN;                      // value scales, for tiles of bare codes
+    float* s_vs = reinterpret_cast<float*>(s_rawp + 2 * S::RAWP);            // [kSlots][BN] value scales, for tiles of bare codes
     __shared__ uint64_t s_bar[32];
     __shared__ uint32_t s_tmem, s_pieces[S::RAWS];
     __shared__ int s_abort, s_find[2];
-    __shared__ float s_e[kSlots];                          // exponent of a tile's values
+    __shared__ float s_ek[kSlots], s_e[kSlots];            // 2^exponent of a tile's keys, exponent of its values
+    __shared__ float s_half[2][2][BM];                     // what the two threads of a row tell each other
     __shared__ uint32_t s_flags[kSlots], s_there[kSlots][4];                 // 1: bare codes, 2: some tokens are not there (bits)
     uint64_t* raw_full = s_bar;                            // [RAWS]
     uint64_t* raw_empty = raw_full + S::RAWS;              // [RAWS]
@@ -333,8 +307,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
         for (int i = 0; i < S::RAWS; ++i) { ptx::mbar_init(&raw_full[i], 1); ptx::mbar_init(&raw_empty[i], 4); }
         for (int i = 0; i < S::OPS; ++i) { ptx::mbar_init(&op_full[i], 4); ptx::mbar_init(&op_empty[i], 1); }
         for (int i = 0; i < kSlots; ++i) ptx::mbar_init(&prm_full[i], 1);
-        for (int i = 0; i < 2; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 4); ptx::mbar_init(&o_full[i], 1); }
-        ptx::mbar_init(q_full, 8);
+        for (int i = 0; i < 2; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 8); ptx::mbar_init(&o_full[i], 1); }
+        ptx::mbar_init(q_full, 16);
         s_abort = 0;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
@@ -383,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
         j1 = int(int64_t(all) * (blockIdx.y + 1) / a.splits);
     }
     const Abort ab{&s_abort, a.status};
-    if (warp == 13) {
+    if (warp == 21) {
         ptx::tmem_alloc(&s_tmem, 512);
         ptx::tmem_relinquish();
     }
@@ -392,15 +366,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
     ptx::tc_fence_after_sync();
     const uint32_t tmem = s_tmem;
 
-    if (warp < 8) {
+    if (warp < 16) {
         // ------------------------------------------------------------------------------------------------ softmax
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");                // 256 * 184 + 256 * 72 = 512 * 128
-        const int t = warp >> 2, local = threadIdx.x & 127;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");                 // 512 * 96 + 256 * 48 = 768 * 80
+        const int t = warp >> 3, half = warp >> 2 & 1, local = threadIdx.x & 127;            // tile, half of the columns, row
+        const int pair = 1 + (t * 4 + (warp & 3));         // barrier of the two warps that share 32 rows
         const unsigned rr = (2 * unsigned(blk) + t) * BM + local, i = rr / unsigned(a.group);
         const bool real = rr < rows;
         const int head = g * a.group + int(rr - i * a.group);
         const int limit = !real ? 0x7fffffff : !a.causal ? len : max(len - n + int(i) + 1, 0);
-        // ---- this row's query into the operand tile
+        float* mine = &s_half[t][half][local];
+        const float* other = &s_half[t][half ^ 1][local];
+        // ---- this row's query into the operand tile, half of the channels each
         float qn;
         {
             const __nv_bfloat16* src = a.q + (row0 + i) * a.q_stride + int64_t(head) * D;
@@ -416,9 +393,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
             const int e = max(int(__float_as_uint(top) >> 23) - 127, -100);
             const float up = pow2i(13 - e) * (a.scale < 0.f ? -1.f : 1.f);
             qn = fmaxf(pow2i(e - 13) * fabsf(a.scale) * 1.4426950408889634f, 1e-37f);      // not 0: it meets the -infinity of masks
-            uint8_t* dst = s_q + t * S::OP + local * 128;
-#pragma unroll 4
-            for (int k = 0; k < D / 8; ++k) {
+            const uint32_t dst = ptx::smem_addr(s_q) + t * S::OP + local * 128;
+#pragma unroll 2
+            for (int k = half * (D / 16); k < (half + 1) * (D / 16); ++k) {
                 float f[8];
 #pragma unroll
                 for (int x = 0; x < 8; ++x) f[x] = 0.f;
@@ -426,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 uint32_t h[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) h[x] = bits(__floats2half2_rn(f[x] * up, f[x + 4] * up));
-                *reinterpret_cast<uint4*>(dst + (k >> 3) * S::ATOM + (((k & 7) ^ (local & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                sts4(dst + (k >> 3) * S::ATOM + (((k & 7) ^ (local & 7)) << 4), make_uint4(h[0], h[1], h[2], h[3]));
             }
             ptx::fence_proxy_async_smem();
             __syncwarp();
@@ -434,24 +411,27 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
         }
         const int low = __reduce_min_sync(0xffffffffu, limit);               // fewest keys of this warp's rows
         const uint32_t lanes = uint32_t(warp & 3) << 21;                     // TMEM lane offset of this warp's rows
-        const uint32_t t_s = tmem + S::TMEM_S + t * BN + lanes, t_o = tmem + S::TMEM_O + t * D + lanes;
+        const uint32_t t_s = tmem + S::TMEM_S + t * BN + half * kCols + lanes, t_o = tmem + S::TMEM_O + t * D + half * (D / 2) + lanes;
         const int stop = min(nt[t], j1);
         float top = -INFINITY, l = 0.f;
         bool ok = true;
         for (int j = j0; j < stop; ++j) {
             const int slot = (j - j0) % kSlots;
-            if (!wait_bounded(&prm_full[slot], ((j - j0) / kSlots) & 1, ab) || !wait_bounded(&s_full[t], (j - j0) & 1, ab)) { ok = false; break; }
+            if (ok && (!wait_bounded(&prm_full[slot], ((j - j0) / kSlots) & 1, ab) || !wait_bounded(&s_full[t], (j - j0) & 1, ab))) ok = false;
+            // (after a wait ran out the loop goes on without waiting: the two warps of a row still meet)
             ptx::tc_fence_after_sync();
-            const uint32_t ks = ptx::smem_addr(s_ks + slot * BN);
             const uint32_t flags = s_flags[slot];
-            const int first = j * BN;
-            const bool masked = first + BN > low || (flags & 2);
-            const float e = s_e[slot];
-            const uint32_t vs = ks + kSlots * S::PRM, there = ptx::smem_addr(s_there[slot]);
-            const bool bare = flags & 1;
-            const float m = bare     ? tile_max<true, true>(t_s, ks, vs, first, limit, there, qn, e)
-                            : masked ? tile_max<true, false>(t_s, ks, vs, first, limit, there, qn, e)
-                                     : tile_max<false, false>(t_s, ks, vs, first, limit, there, qn, e);
+            const int first = j * BN + half * kCols;
+            const bool masked = j * BN + BN > low || (flags & 2), bare = flags & 1;
+            const float e = s_e[slot], qk = fminf(fmaxf(qn * s_ek[slot], 1e-37f), 3e38f);
+            const uint32_t vs = ptx::smem_addr(s_vs + slot * BN + half * kCols), there = ptx::smem_addr(&s_there[slot][2 * half]);
+            float m = bare     ? half_max<true, true>(t_s, vs, first, limit, there, qk)
+                      : masked ? half_max<true, false>(t_s, vs, first, limit, there, qk)
+                               : half_max<false, false>(t_s, vs, first, limit, there, qk);
+            *mine = m;
+            ptx::named_bar_sync(pair, 64);
+            m = fmaxf(m, *other);
+            if (!bare) m = fmaf(m, qk, e);
             // the reference moves only when a weight would pass 2^(kPlace + kSlack)
             if (__any_sync(0xffffffffu, m > top + (kPlace + kSlack))) {
                 const float to = m > top + (kPlace + kSlack) ? m - kPlace : top, fix = to == top ? 1.f : ex2(top - to);
@@ -459,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 l *= fix;
                 if (j > j0) {
 #pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
+                    for (int c = 0; c < D / 64; ++c) {
                         uint32_t r[32];
                         ptx::tmem_ld_32x32b_x32(t_o + 32 * c, r);
                         ptx::tmem_ld_wait();
@@ -471,15 +451,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 }
             }
             const float at = top == -INFINITY ? 0.f : top;
-            if (bare) l += tile_weights<true, true>(t_s, ks, vs, first, limit, there, qn, -at);
-            else l = fmaf(masked ? tile_weights<true, false>(t_s, ks, vs, first, limit, there, qn, e - at)
-                                 : tile_weights<false, false>(t_s, ks, vs, first, limit, there, qn, e - at), pow2i(-int(e)), l);
+            if (bare) l += half_weights<true, true>(t_s, vs, first, limit, there, qk, -at);
+            else l = fmaf(masked ? half_weights<true, false>(t_s, vs, first, limit, there, qk, e - at)
+                                 : half_weights<false, false>(t_s, vs, first, limit, there, qk, e - at), pow2i(-int(e)), l);
             tmem_st_wait();
             ptx::tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&p_full[t]);
         }
-        // ---- the row's output
+        // ---- the row's output, half of the channels each
+        ptx::named_bar_sync(pair, 64);                     // `mine` has been read
+        *mine = l;
+        ptx::named_bar_sync(pair, 64);
+        l += *other;
         const int64_t row = row0 + i;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const bool some = stop > j0;
@@ -490,7 +474,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
         if (ok) {
             const int64_t at = (int64_t(blockIdx.y) * a.b.rows + row) * a.q_heads + head;
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = 0; c < D / 64; ++c) {
+                const int ch = half * (D / 2) + 32 * c;
                 uint32_t r[32];
                 if (some) {
                     ptx::tmem_ld_32x32b_x32(t_o + 32 * c, r);
@@ -506,27 +491,27 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
 #pragma unroll
                         for (int x = 0; x < 8; ++x) f[x] = __uint_as_float(r[8 * k + 2 * (x & 3) + (x >> 2)]);   // 0 4 1 5 2 6 3 7
                         if (a.splits > 1) {
-                            store8(a.part_o + at * D + 32 * c + 8 * k, f);
+                            store8(a.part_o + at * D + ch + 8 * k, f);
                         } else {
 #pragma unroll
                             for (int x = 0; x < 8; ++x) f[x] *= inv;
-                            store8(a.out + row * a.out_stride + int64_t(head) * D + 32 * c + 8 * k, f);
+                            store8(a.out + row * a.out_stride + int64_t(head) * D + ch + 8 * k, f);
                         }
                     }
                 }
                 __syncwarp();
             }
-            if (real) {
+            if (real && half == 0) {
                 if (a.splits > 1) a.part_ml[at] = make_float2(top, l);
                 else if (a.lse) a.lse[row * a.q_heads + head] = l == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(l)) * 0.6931471805599453f;
             }
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         const int piece_log2 = min(a.b.page_log2, 7), per_tile = BN >> piece_log2;
-        if (warp < 12) {
+        if (warp < 20) {
             // -------------------------------------------------------------------------------------------- unpack
-            const int tok = threadIdx.x - 256;
+            const int tok = threadIdx.x - 512;
             bool ok = true;
             uint32_t step = 0;                             // 2 * tile + (0 keys, 1 values)
             for (int j = j0; ok && j < j1; ++j) {
@@ -541,14 +526,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                     const float zero = __uint_as_float(lds1(prm + v * (BN * 8))), factor = __uint_as_float(lds1(prm + v * (BN * 8) + 4));
                     const bool far = is_far(zero);
                     if (!wait_bounded(&op_empty[ob], ((step / S::OPS) & 1) ^ 1, ab)) { ok = false; break; }
-                    if (v == 0) unpack_row<D, false>(raw, op, tok, zero, factor, far);
-                    else unpack_row<D, true>(raw, op, tok, zero, factor, far);
+                    unpack_row<D>(raw, op, tok, zero, factor, far);
                     ptx::fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) { ptx::mbar_arrive(&op_full[ob]); ptx::mbar_arrive(&raw_empty[rs]); }
                 }
             }
-        } else if (warp == 14) {
+        } else if (warp == 22) {
             // -------------------------------------------------------------------------------------------- parameters
             // Lane l has tokens l, l + 32, ..  The (zero, factor) that unpacking needs takes the place of (scale, zero).
             const int top_keys = !a.causal ? len : max(len - n + int((min((2 * unsigned(blk) + 2) * BM, rows) - 1) / unsigned(a.group)) + 1, 0);
@@ -557,32 +541,24 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 if (!wait_bounded(&raw_full[rs], (step / S::RAWS) & 1, ab)) break;
                 const uint32_t pieces = s_pieces[rs];
                 float2* prm = reinterpret_cast<float2*>(s_rawp + ((j - j0) & 1) * S::RAWP);
-                float vx[4], vz[4];
-                int hi = -1000, lo = 1000;
+                float2 kp[4], vp[4];
+                int hi = -1000, lo = 1000, khi = -1000;
                 uint32_t goods = 0, everywhere = 0xffffffffu;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int tok = 32 * i + lane;
                     const bool good = j * BN + tok < top_keys && ((pieces >> (tok >> piece_log2)) & 1u);
-                    float2 kp = prm[tok], vp = prm[BN + tok];
-                    if (!good) kp = vp = make_float2(0.f, 0.f);
+                    kp[i] = prm[tok];
+                    vp[i] = prm[BN + tok];
+                    if (!good) kp[i] = vp[i] = make_float2(0.f, 0.f);
                     goods |= uint32_t(good) << i;
-                    // parameters that are no numbers: the operands stay finite, a row that sees the token gets it from the score
-                    if (!(fabsf(vp.x) <= 3e38f && fabsf(vp.y) <= 3e38f)) { kp.x = NAN; vp = make_float2(0.f, 0.f); }
-                    if (!(fabsf(kp.y) <= 3e38f)) { kp.x = NAN; kp.y = 0.f; }
-                    // keys: (code - zero) 2^-k, k = 0 unless the zero-point is far off
-                    float kf = 1.f;
-                    if (is_far(kp.y)) {
-                        const int k = min(max(int((__float_as_uint(kp.y) >> 23) & 255u) - 127 - 9, 0), 120);
-                        kf = pow2i(-k);
-                        kp.x *= pow2i(k);
-                    }
-                    s_ks[slot * BN + tok] = kp.x;
-                    prm[tok] = make_float2(kp.y, kf);
-                    vx[i] = vp.x;
-                    vz[i] = vp.y;
-                    const float largest = fabsf(vp.x) * fmaxf(fabsf(vp.y), fabsf(15.f - vp.y));
-                    if (good && largest != 0.f) {
+                    // parameters that are no numbers: the values stay finite, a row that sees the token gets it from the score
+                    if (!(fabsf(vp[i].x) <= 3e38f && fabsf(vp[i].y) <= 3e38f)) { kp[i].x = NAN; vp[i] = make_float2(0.f, 0.f); }
+                    if (!(fabsf(kp[i].y) <= 3e38f)) { kp[i].x = NAN; kp[i].y = 0.f; }
+                    const float klargest = fabsf(kp[i].x) * fmaxf(fabsf(kp[i].y), fabsf(15.f - kp[i].y));
+                    if (klargest > 0.f && klargest <= 3e38f) khi = max(khi, int(__float_as_uint(klargest) >> 23) - 127);
+                    const float largest = fabsf(vp[i].x) * fmaxf(fabsf(vp[i].y), fabsf(15.f - vp[i].y));
+                    if (largest != 0.f) {
                         const int ex = largest < 1.2e24f ? max(int(__float_as_uint(largest) >> 23) - 127, -80) : 1000;   // 2^80: the logarithm's cut
                         hi = max(hi, ex);
                         lo = min(lo, ex);
@@ -593,24 +569,27 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 }
                 hi = __reduce_max_sync(0xffffffffu, hi);
                 lo = __reduce_min_sync(0xffffffffu, lo);
+                khi = __reduce_max_sync(0xffffffffu, khi);
                 const bool bare = hi > 900 || hi - lo > 10;                  // (no values at all: -1000 and 1000)
-                const int e = bare || hi < -900 ? 0 : hi;
+                const int e = bare || hi < -900 ? 0 : hi, ek = khi < -900 ? 0 : min(max(khi, -120), 120);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
+                    prm[32 * i + lane] = make_float2(kp[i].y, kp[i].x * pow2i(-ek));
                     float vf = 1.f;
                     if (bare) {
-                        if (is_far(vz[i])) {
-                            const int k = min(max(int((__float_as_uint(vz[i]) >> 23) & 255u) - 127 - 9, 0), 120);
+                        if (is_far(vp[i].y)) {
+                            const int k = min(max(int((__float_as_uint(vp[i].y) >> 23) & 255u) - 127 - 9, 0), 120);
                             vf = pow2i(-k);
-                            vx[i] *= pow2i(k);
+                            vp[i].x *= pow2i(k);
                         }
-                        s_vs[slot * BN + 32 * i + lane] = vx[i];
+                        s_vs[slot * BN + 32 * i + lane] = vp[i].x;
                     } else {
-                        vf = vx[i] * pow2i(-e);
+                        vf = vp[i].x * pow2i(-e);
                     }
-                    prm[BN + 32 * i + lane] = make_float2(vz[i], goods >> i & 1 ? vf : 0.f);
+                    prm[BN + 32 * i + lane] = make_float2(vp[i].y, goods >> i & 1 ? vf : 0.f);
                 }
                 if (lane == 0) {
+                    s_ek[slot] = pow2i(ek);
                     s_e[slot] = float(e);
                     s_flags[slot] = (bare ? 1 : 0) | (everywhere != 0xffffffffu ? 2 : 0);
                 }
@@ -618,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&prm_full[slot]);
             }
-        } else if (warp == 12) {
+        } else if (warp == 20) {
             // -------------------------------------------------------------------------------------------- codes in
             // lane = 4 * piece + array (keys' codes, their parameters, the values' parameters, the values' codes)
             const int piece = lane >> 2, array = lane & 3, log2p = a.b.page_log2;
@@ -669,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                     while (!ptx::mbar_try_wait(&raw_full[x % S::RAWS], (x / S::RAWS) & 1) && clock64() - t0 < (1ll << 24)) {}
                 }
             }
-        } else if (warp == 13) {
+        } else if (warp == 21) {
             // -------------------------------------------------------------------------------------------- MMAs
             constexpr uint32_t id_s = idesc_f16(BM, BN, false), id_o = idesc_f16(BM, D, true);
             const uint32_t leader = elect_one();
@@ -714,7 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                     if (leader) {
 #pragma unroll
                         for (int x = 0; x < BN / 16; ++x)
-                            mma_f16_ts(tmem + S::TMEM_O + t * D, tmem + S::TMEM_S + t * BN + 8 * x, v + x * (2048 >> 4), id_o, x > 0 ? 1u : uint32_t(j > j0));
+                            mma_f16_ts(tmem + S::TMEM_O + t * D, tmem + S::TMEM_S + t * BN + (x >> 2) * kCols + 8 * (x & 3), v + x * (2048 >> 4), id_o, x > 0 ? 1u : uint32_t(j > j0));
                     }
                     __syncwarp();
                     if (more && j + 1 < nt[t]) score(t, sk % S::OPS);
@@ -728,7 +707,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
     __syncwarp();
     ptx::tc_fence_before_sync();
     __syncthreads();
-    if (warp == 13) {
+    if (warp == 21) {
         ptx::tc_fence_after_sync();
         ptx::tmem_dealloc(tmem, 512);
     }

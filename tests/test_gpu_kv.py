@@ -82,7 +82,8 @@ def check_attention(got, lse, ref, dtype, rounded_codes=False, prompt=False):
     worst order; every kernel adds them in groups of 16 at least, whose error is at most (16 + 16) 2^-23 mag = 2^-18 mag.  A
     relative change of every weight by e moves out by at most 2 e spread.  exp and the running rescalings: 2^-20.
     prompt (bf16, more than 64 query rows per key head): the prompt kernel also rounds the value scale and the value it
-    multiplies to 11 bits, 2^-11 of the value each, which is at most the spread's term of its token.
+    multiplies to 11 bits, 2^-11 of the value each, which is at most the spread's term of its token; and likewise the key's scale
+    and product, 2^-11 of |key| each, which moves a score by at most 2^-10 scale sum |q| |key| <= 2^-10 mag.
     rounded_codes: the prompt kernel stores (code - zero) of rows far from zero in 11 bits, moving a score by 2^-11 mag and a
     value by 2^-11 of itself.  Sums over the keys: `seen` terms of one sign (the weights) or of at most the spread in all, added
     in float32 in any order, are off by at most seen 2^-24 of that sum; a logarithm turns a relative error into the same
@@ -91,7 +92,7 @@ def check_attention(got, lse, ref, dtype, rounded_codes=False, prompt=False):
     w = 2.0 ** -11 + seen * 2.0 ** -25 if dtype == torch.bfloat16 else 2.0 ** -22 + seen * 2.0 ** -36
     w = w + 2 * seen * 2.0 ** -24                            # numerator and denominator
     w = w + (2 * 2.0 ** -11 if prompt else 0)
-    e = 2.0 ** -18 * mag + 2.0 ** -20 + (2.0 ** -11 * (mag + 1) if rounded_codes else 0)
+    e = 2.0 ** -18 * mag + 2.0 ** -20 + (2.0 ** -10 * mag if prompt else 0) + (2.0 ** -11 * (mag + 1) if rounded_codes else 0)
     tol = (w + 2 * e)[..., None] * spread + np.abs(out) * torch.finfo(dtype).eps / 2 + 1e-30
     a = host(got)
     bad = ~(np.abs(a - out) <= tol)
