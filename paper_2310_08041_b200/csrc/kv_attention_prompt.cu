@@ -377,38 +377,46 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
         const int limit = !real ? 0x7fffffff : !a.causal ? len : max(len - n + int(i) + 1, 0);
         float* mine = &s_half[t][half][local];
         const float* other = &s_half[t][half ^ 1][local];
-        // ---- this row's query into the operand tile, half of the channels each
-        float qn;
+        // ---- the queries into their operand tiles: D / 8 lanes to a row, all of a warp's loads in flight together
         {
-            const __nv_bfloat16* src = a.q + (row0 + i) * a.q_stride + int64_t(head) * D;
-            float top = 0.f;
-            if (real)
-#pragma unroll 4
-                for (int k = 0; k < D / 8; ++k) {
-                    float f[8];
-                    load8<__nv_bfloat16>(src + 8 * k, f);
+            constexpr int L = D / 8, PER = 32 / L, IT = 2 * BM / (16 * PER);
+            const int c = lane % L;
+            uint4 raw[IT];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
+            for (int x = 0; x < IT; ++x) {
+                const unsigned r = 2 * unsigned(blk) * BM + (x * 16 + warp) * PER + lane / L, ri = r / unsigned(a.group);
+                raw[x] = make_uint4(0, 0, 0, 0);
+                if (r < rows) raw[x] = __ldg(reinterpret_cast<const uint4*>(a.q + (row0 + ri) * a.q_stride + int64_t(g * a.group + int(r - ri * a.group)) * D) + c);
+            }
+#pragma unroll
+            for (int x = 0; x < IT; ++x) {
+                const int r = (x * 16 + warp) * PER + lane / L;              // row of the block
+                const uint32_t w[4] = {raw[x].x, raw[x].y, raw[x].z, raw[x].w};
+                float f[8], m = 0.f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    f[2 * k] = __uint_as_float(w[k] << 16);
+                    f[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+                    m = fmaxf(m, fmaxf(fabsf(f[2 * k]), fabsf(f[2 * k + 1])));
                 }
-            const int e = max(int(__float_as_uint(top) >> 23) - 127, -100);
-            const float up = pow2i(13 - e) * (a.scale < 0.f ? -1.f : 1.f);
-            qn = fmaxf(pow2i(e - 13) * fabsf(a.scale) * 1.4426950408889634f, 1e-37f);      // not 0: it meets the -infinity of masks
-            const uint32_t dst = ptx::smem_addr(s_q) + t * S::OP + local * 128;
-#pragma unroll 2
-            for (int k = half * (D / 16); k < (half + 1) * (D / 16); ++k) {
-                float f[8];
 #pragma unroll
-                for (int x = 0; x < 8; ++x) f[x] = 0.f;
-                if (real) load8<__nv_bfloat16>(src + 8 * k, f);
+                for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                const int e = max(int(__float_as_uint(m) >> 23) - 127, -100);
+                const float up = pow2i(13 - e) * (a.scale < 0.f ? -1.f : 1.f);
                 uint32_t h[4];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) h[x] = bits(__floats2half2_rn(f[x] * up, f[x + 4] * up));
-                sts4(dst + (k >> 3) * S::ATOM + (((k & 7) ^ (local & 7)) << 4), make_uint4(h[0], h[1], h[2], h[3]));
+                for (int k = 0; k < 4; ++k) h[k] = bits(__floats2half2_rn(f[k] * up, f[k + 4] * up));
+                const int rl = r & (BM - 1);
+                sts4(ptx::smem_addr(s_q) + (r / BM) * S::OP + rl * 128 + (c >> 3) * S::ATOM + (((c & 7) ^ (rl & 7)) << 4), make_uint4(h[0], h[1], h[2], h[3]));
+                if (c == 0) s_half[r / BM][0][rl] = fmaxf(pow2i(e - 13) * fabsf(a.scale) * 1.4426950408889634f, 1e-37f);   // not 0: it meets the -infinity of masks
             }
             ptx::fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(q_full);
         }
+        ptx::named_bar_sync(9, 512);
+        const float qn = s_half[t][0][local];              // factor of the row's sums, into base 2
+        ptx::named_bar_sync(9, 512);
         const int low = __reduce_min_sync(0xffffffffu, limit);               // fewest keys of this warp's rows
         const uint32_t lanes = uint32_t(warp & 3) << 21;                     // TMEM lane offset of this warp's rows
         const uint32_t t_s = tmem + S::TMEM_S + t * BN + half * kCols + lanes, t_o = tmem + S::TMEM_O + t * D + half * (D / 2) + lanes;
