@@ -387,12 +387,12 @@ int qllm_layer_workspace(qllm_layer_t* layer, uint8_t** codes, float** a_scale, 
  *
  * A BATCH names the sequences that a call works on and their newest tokens:
  *   table     device int32 [seqs][table_width]: table[s][j] is the page of positions j page_size .. of sequence s.  Only the
- *             entries that seq_lens reaches are read.
+ *             entries that seq_lens reaches are read.  table_width * page_size <= 2^30 (QLLM_ERR_UNSUPPORTED).
  *   seq_lens  device int32 [seqs]: tokens of the sequence in the cache, the new ones included
  *   q_start   device int32 [seqs + 1], not decreasing: rows q_start[s] .. q_start[s+1] - 1 of the call's packed tensors are the
  *             new tokens of sequence s, its last positions in order.  A sequence may have none.
- *   rows      rows of the packed tensors, at least q_start[seqs]; rows in front of q_start[0] and from q_start[seqs] on are
- *             left as they are
+ *   rows      rows of the packed tensors (rows * q_heads < 2^31 for the attention), at least q_start[seqs]; rows in front of
+ *             q_start[0] and from q_start[seqs] on are left as they are
  *   max_new   the most new tokens of one sequence.  A hint: it selects kernels and sizes the workspace of the attention,
  *             results do not depend on its being right.
  * Where a sequence has more new tokens than length, the first of them have no position: qllm_kv_append skips them,

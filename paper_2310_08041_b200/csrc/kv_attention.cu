@@ -13,8 +13,7 @@ using namespace kv;
 
 int check_attention(const qllm_kv_cache_t* cache, int q_heads, int dtype, const qllm_kv_batch_t* batch) {
     if (!dtype_ok(dtype)) return QLLM_ERR_DTYPE;
-    int rc = check_cache(cache);
-    if (rc == QLLM_OK) rc = check_batch(batch);
+    const int rc = check_cache_batch(cache, batch);
     if (rc != QLLM_OK) return rc;
     if (q_heads <= 0 || q_heads % cache->kv_heads) return QLLM_ERR_SHAPE;
     if (q_heads > 65535 || batch->rows * q_heads > 0x7fffffff) return QLLM_ERR_UNSUPPORTED;   // query rows are counted in 31 bits
@@ -22,10 +21,12 @@ int check_attention(const qllm_kv_cache_t* cache, int q_heads, int dtype, const 
 }
 
 // Which kernels a call launches.  The streaming kernel reads a sequence's keys once per 8 or 16 query rows, the tensor-core kernel
-// once per 256 and unpacks them for 256 whether there are that many or not: kPromptRows is where they meet.  Either serves
-// any count, so what the batch's hint says wrongly costs time only.  A batch with the same number of new tokens in every
+// once per 256 and unpacks them for 256 whether there are that many or not: kPromptRows is where they meet (us, streaming against
+// tensor-core kernel, heads of 128 in bf16, at 64 / 96 / 128 rows: 4 sequences of 4096 tokens on 8 heads 37 : 43, 49 : 45,
+// 60 : 48; 1 of 32768 on 8 heads 53 : 88, 73 : 89, 92 : 90; 4 of 2048 on 32 heads 64 : 76, 88 : 65, 111 : 68).  Either serves any
+// count, so what the batch's hint says wrongly costs time only.  A batch with the same number of new tokens in every
 // sequence, as far as the hint goes, needs one of them; others get both, each taking its sequences.
-constexpr int kPromptRows = 64;
+constexpr int kPromptRows = 96;
 struct Choice {
     bool split, prompt;
     int hint, most_rows;                                   // query rows per key head of the largest sequence; the border
@@ -48,7 +49,7 @@ extern "C" int64_t qllm_kv_attention_workspace(const qllm_kv_cache_t* cache, int
     if (batch->rows == 0 || batch->seqs == 0) return 0;
     const qllm::Choice ch = qllm::choose(cache, q_heads, dtype, batch);
     const int64_t split = ch.split ? qllm::kv::split_workspace(cache->head_dim, dtype, ch.prompt ? qllm::kPromptRows : ch.hint) : 0;
-    const int64_t prompt = ch.prompt ? qllm::kv::prompt_workspace(qllm::kv::view(batch, cache), cache->kv_heads, cache->head_dim, q_heads / cache->kv_heads) : 0;
+    const int64_t prompt = ch.prompt ? qllm::kv::prompt_workspace(qllm::kv::view(batch, cache), cache->kv_heads, cache->head_dim, q_heads / cache->kv_heads, batch->max_new) : 0;
     return std::max(split, prompt);                        // one after the other on the stream
 }
 
@@ -85,7 +86,7 @@ extern "C" int qllm_kv_attention(const qllm_kv_cache_t* cache, int layer, const 
     a.scale = scale;
     const Choice ch = choose(cache, q_heads, dtype, batch);
     a.most_rows = ch.most_rows;
-    if (ch.prompt) rc = kv::launch_attention_prompt(c, b, cache->head_dim, a, workspace, status, st);
+    if (ch.prompt) rc = kv::launch_attention_prompt(c, b, cache->head_dim, a, batch->max_new, workspace, status, st);
     if (rc == QLLM_OK && ch.split) rc = kv::launch_attention_split(c, b, cache->head_dim, a, ch.prompt ? kPromptRows : ch.hint, workspace, status, st);
     return rc;
 }

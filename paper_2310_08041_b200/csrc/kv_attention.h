@@ -25,8 +25,9 @@ int launch_attention_split(const Cache& c, const Batch& b, int head_dim, const A
 
 // Tensor-core kernel (kv_attention_prompt.cu): sequences with more than most_rows query rows per key head.
 bool prompt_serves(int head_dim, int dtype);
-int64_t prompt_workspace(const Batch& b, int heads, int head_dim, int group);
-int launch_attention_prompt(const Cache& c, const Batch& b, int head_dim, const AttnArgs& a, void* workspace, int* status, cudaStream_t st);
+int64_t prompt_workspace(const Batch& b, int heads, int head_dim, int group, int max_new);
+int launch_attention_prompt(const Cache& c, const Batch& b, int head_dim, const AttnArgs& a, int max_new, void* workspace, int* status,
+                            cudaStream_t st);
 
 }  // namespace kv
 }  // namespace qllm

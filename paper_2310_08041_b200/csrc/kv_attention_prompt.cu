@@ -313,6 +313,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
     }
+    if (warp == 1 && blockIdx.x == 0 && blockIdx.y == 0) a.b.report(a.status, lane, 32);
     if (warp == 0) {                                       // which sequence, which block of it
         unsigned x = blockIdx.x / a.c.heads;               // heads vary fastest: all of them start with their longest blocks
         int found = -1;
@@ -756,9 +757,10 @@ __global__ void __launch_bounds__(128) kv_prompt_join_kernel(const Args a) {
 // CTAs of a call at most, per split: every sequence rounds its rows up once.
 inline int64_t blocks_bound(const Batch& b, int group) { return (b.rows * group + 2 * BM - 1) / (2 * BM) + std::min<int64_t>(b.seqs, b.rows); }
 
-// Keys are cut into as many parts as fill the SMs once with the blocks that there are likely to be.
-inline int splits_of(const Batch& b, int heads, int group) {
-    const int64_t ctas = ((b.rows * group + 2 * BM - 1) / (2 * BM)) * heads;
+// Keys are cut into as many parts as fill the SMs once with the blocks that there are likely to be: all new tokens in sequences
+// of max_new.
+inline int splits_of(const Batch& b, int heads, int group, int max_new) {
+    const int64_t seqs = (b.rows + max_new - 1) / max_new, ctas = seqs * ((int64_t(max_new) * group + 2 * BM - 1) / (2 * BM)) * heads;
     return int(std::max<int64_t>(1, std::min<int64_t>(8, device_sm_count() / ctas)));
 }
 
@@ -781,12 +783,13 @@ namespace kv {
 
 bool prompt_serves(int head_dim, int dtype) { return dtype == QLLM_BF16 && (head_dim == 64 || head_dim == 128); }
 
-int64_t prompt_workspace(const Batch& b, int heads, int head_dim, int group) {
-    const int splits = splits_of(b, heads, group);
+int64_t prompt_workspace(const Batch& b, int heads, int head_dim, int group, int max_new) {
+    const int splits = splits_of(b, heads, group, max_new);
     return splits == 1 ? 0 : int64_t(splits) * b.rows * heads * group * (head_dim + 2) * 4;
 }
 
-int launch_attention_prompt(const Cache& c, const Batch& b, int head_dim, const AttnArgs& x, void* workspace, int* status, cudaStream_t st) {
+int launch_attention_prompt(const Cache& c, const Batch& b, int head_dim, const AttnArgs& x, int max_new, void* workspace, int* status,
+                            cudaStream_t st) {
     Args a;
     a.c = c;
     a.b = b;
@@ -800,7 +803,7 @@ int launch_attention_prompt(const Cache& c, const Batch& b, int head_dim, const 
     a.causal = x.causal;
     a.most_rows = x.most_rows;
     a.scale = x.scale;
-    a.splits = splits_of(b, c.heads, x.group);
+    a.splits = splits_of(b, c.heads, x.group, max_new);
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + int64_t(a.splits) * b.rows * x.q_heads * head_dim);
     a.status = status;

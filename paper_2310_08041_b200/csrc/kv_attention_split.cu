@@ -670,8 +670,8 @@ kv_combine_kernel(Batch b, int* status, int group, QT* __restrict__ out, int64_t
     constexpr int V = D / 32, W = kCombineThreads / 32;
     __shared__ float s_ml[W][2], s_o[W][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c0 = blockIdx.x, col = blockIdx.y;
-    if (c0 == 0 && col == 0) b.report(status);
     asm volatile("griddepcontrol.wait;" ::: "memory");     // in every CTA: this kernel is not over before the one it depends on
+    if (blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1) b.report(status, threadIdx.x, kCombineThreads);
     const Record rec = record[c0];
     if (col >= rec.rows) return;
     float m = -INFINITY, l = 0.f, o[V];

@@ -52,9 +52,9 @@ struct Batch {
         }
         return lo > 0 && t - row(lo - 1) < count(lo - 1) ? lo - 1 : -1;
     }
-    // Called by one whole CTA: raises the status word for lengths and row ranges that had to be cut.
-    __device__ __forceinline__ void report(int* status) const {
-        for (int s = threadIdx.x; s < seqs; s += blockDim.x) {
+    // Raises the status word for lengths and row ranges that had to be cut: `n` threads of one CTA, this is number `i`.
+    __device__ __forceinline__ void report(int* status, int i, int n) const {
+        for (int s = i; s < seqs; s += n) {
             const int a = start[s], b = start[s + 1];
             if (lens[s] != len(s) || a < 0 || b < a || b > rows) raise_page(status);
         }
@@ -116,6 +116,13 @@ inline int check_batch(const qllm_kv_batch_t* b) {
     if (b->rows > (int64_t(1) << 30) || b->seqs > (1 << 20) || b->table_width > (1 << 23)) return QLLM_ERR_UNSUPPORTED;
     if (b->seqs > 0 && b->rows > 0 && (!b->table || !b->seq_lens || !b->q_start)) return QLLM_ERR_NULL;
     return QLLM_OK;
+}
+// Both at once; positions are counted in 30 bits.
+inline int check_cache_batch(const qllm_kv_cache_t* c, const qllm_kv_batch_t* b) {
+    int rc = check_cache(c);
+    if (rc == QLLM_OK) rc = check_batch(b);
+    if (rc != QLLM_OK) return rc;
+    return int64_t(b->table_width) * c->page_size > (int64_t(1) << 30) ? QLLM_ERR_UNSUPPORTED : QLLM_OK;
 }
 // A packed tensor of `heads` heads; dtype has been checked.
 inline int check_packed(const void* p, int64_t stride, int heads, int head_dim, int dtype) {

@@ -195,6 +195,7 @@ kv_fork_kernel(Pool p, const int32_t* __restrict__ parent, const int32_t* __rest
             const int page = from[j];
             to[j] = page;
             if (page >= 0 && page < p.pages) atomicAdd(&p.refs[page], 1);
+            else raise_page(status);
         }
         if (lane == 0) {
             if (len & (P - 1)) to[full] = s_page[r];
@@ -350,6 +351,7 @@ int check_both(const qllm_kv_cache_t* c, const qllm_kv_pool_t* p) {
     if (rc == QLLM_OK) rc = check_pool(p);
     if (rc != QLLM_OK) return rc;
     if (c->pages != p->pages) return QLLM_ERR_SHAPE;
+    if (int64_t(p->table_width) * c->page_size > (int64_t(1) << 30)) return QLLM_ERR_UNSUPPORTED;
     return c->layers > kMaxLayers ? QLLM_ERR_UNSUPPORTED : QLLM_OK;
 }
 Pool pool_of(const qllm_kv_pool_t* p, int log2) {

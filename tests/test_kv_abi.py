@@ -76,6 +76,16 @@ def test_batches_refused(kw, e):
     assert L.qllm_kv_attention_workspace(p(cache()), 8, 1, p(b)) == err(e)
 
 
+def test_positions_counted_in_30_bits():
+    b = batch(table_width=(1 << 22) + 1)
+    c = cache(page_size=256)
+    for fn in (L.qllm_kv_append, L.qllm_kv_read):
+        assert tokens(fn, c, b) == B.QLLM_ERR_UNSUPPORTED
+    assert attention(c, b) == B.QLLM_ERR_UNSUPPORTED
+    assert L.qllm_kv_pages_extend(p(c), p(pool(table_width=(1 << 22) + 1)), ONE, None) == B.QLLM_ERR_UNSUPPORTED
+    assert attention(cache(), batch(rows=1 << 29)) == B.QLLM_ERR_UNSUPPORTED          # query rows in 31 bits
+
+
 def test_tensors_refused():
     for fn in (L.qllm_kv_append, L.qllm_kv_read):
         assert tokens(fn, cache(), batch(), dtype=2) == B.QLLM_ERR_DTYPE
