@@ -21,9 +21,11 @@
 //
 // Precision: queries are scaled by a power of two per row into fp16's range (a bf16 query's 8 bits stay exact) and float32
 // queries are split in two; weights p_j vs_j are rounded to fp16, 11 bits, for bf16 results (which carry 8) and split in two
-// for float32 ones.  So that no weight leaves fp16's range whatever the value scales are, the running maximum is that of
-// s_j + log2 vs_j (the logarithm cut to +-80; its integer part for float32), with the largest weight placed at 2^6; it moves only when a weight would pass 2^14,
-// which spares most steps the reduction over lanes and the rescaling.  Sums, maxima and zero-point corrections are float32.
+// for float32 ones, whose codes also enter as normal numbers and whose sums over more than 16 or 32 terms are float32 additions.
+// So that no weight leaves fp16's range whatever the value scales are, the running maximum is that of s_j + log2 vs_j (the
+// logarithm cut to +-80; its integer part for float32), with the largest weight placed at 2^6; it moves only when a weight would
+// pass 2^14, which spares most steps the reduction over lanes and the rescaling.  Sums, maxima and zero-point corrections are
+// float32.
 
 #include <cuda_fp16.h>
 
@@ -226,6 +228,19 @@ __device__ __forceinline__ void load_units(const uint8_t* p, uint32_t (&x)[4]) {
                  : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(ptx::smem_addr(p)) : "memory");
 }
 
+// Codes as A operands: two nibbles of a word (`upper`: those of bits 4-7 and 20-23, else 0-3 and 16-19).  bf16 calls take them as
+// they are masked, denormal numbers c 2^-24 and 16 c 2^-24.  The MMA aligns its sums to the operands' nominal exponents, which for
+// denormals lie up to 10 bits above their values, and cuts what falls off: 2^-16 of a sum is lost, nothing to 8 or 11 bits.  float32
+// calls take c - 8 as normal numbers (1024 + c and 1024 + 16 c are fp16 numbers, one packed operation makes the difference).
+template <bool F32>
+__device__ __forceinline__ uint32_t codes2(uint32_t w, bool upper) {
+    if constexpr (!F32) return w & (upper ? 0x00F000F0u : 0x000F000Fu);
+    const uint32_t h = (w & (upper ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;
+    const __half2 v = *reinterpret_cast<const __half2*>(&h);
+    const __half2 r = upper ? __hfma2(v, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hadd2(v, __float2half2_rn(-1032.f));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+
 // The query row of column `r` as B operands; what a unit of the sums made with them stands for, and the row's sum in those units.
 template <typename QT, int D, bool F32>
 __device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi)[D / 8], uint32_t (&lo)[F32 ? D / 8 : 1], float& unit, float& ratio) {
@@ -246,8 +261,9 @@ __device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     const int e = max(int(__float_as_uint(top) >> 23) - 127, -100);      // 2^e <= top < 2^(e+1); infinities: 128
     const float up = pow2i(min(13 - e, 126));
-    unit = e > 115 ? INFINITY : pow2i(e + 11);             // 2^24 / 2^(13 - e): what one unit of an MMA sum stands for
-    ratio = e > 115 ? NAN : sum * pow2i(-e - 11);
+    constexpr int kUnit = F32 ? -13 : 11;                  // what one unit of an MMA sum stands for: 2^(e - 13), times 2^24
+    unit = e > 115 ? INFINITY : pow2i(e + kUnit);
+    ratio = e > 115 ? NAN : sum * pow2i(-e - kUnit);
 #pragma unroll
     for (int i = 0; i < N / 8; ++i) {
         float f[8];
@@ -255,7 +271,7 @@ __device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi
         for (int j = 0; j < 8; ++j) f[j] = 0.f;
         if (row) load8<QT>(row + t * N + 8 * i, f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] *= (j & 1) ? up * 0.0625f : up;
+        for (int j = 0; j < 8; ++j) f[j] *= (j & 1) && !F32 ? up * 0.0625f : up;
         // word 8i of the codes gives the pairs (0, 4), (1, 5) x 16, (2, 6), (3, 7) x 16
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -297,6 +313,7 @@ template <int D, int NT, bool F32, bool MASKED>
 __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, const uint8_t* vc, const float2* kp, int first, int len,
                                      uint32_t there, int r, int t) {
     constexpr int KW = D / 32, MT = D / 16;
+    constexpr float kCentre = F32 ? 8.f : 0.f;             // what the operands have taken off the codes
     float s[NT][2][4], s2[NT][2][4];                       // two chains of MMAs each: their latency bounds a warp
     // ---- S^T = K Q^T, 16 tokens at a time
 #pragma unroll
@@ -311,15 +328,23 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
 #pragma unroll
         for (int i = 0; i < KW; ++i) {
             const uint32_t u0 = w0[i] >> 8, u1 = w1[i] >> 8;
-            const uint32_t a0 = w0[i] & 0x000F000Fu, a1 = w1[i] & 0x000F000Fu, a2 = w0[i] & 0x00F000F0u, a3 = w1[i] & 0x00F000F0u;
-            const uint32_t c0 = u0 & 0x000F000Fu, c1 = u1 & 0x000F000Fu, c2 = u0 & 0x00F000F0u, c3 = u1 & 0x00F000F0u;
+            const uint32_t a0 = codes2<F32>(w0[i], false), a1 = codes2<F32>(w1[i], false), a2 = codes2<F32>(w0[i], true), a3 = codes2<F32>(w1[i], true);
+            const uint32_t c0 = codes2<F32>(u0, false), c1 = codes2<F32>(u1, false), c2 = codes2<F32>(u0, true), c3 = codes2<F32>(u1, true);
 #pragma unroll
             for (int a = 0; a < NT; ++a) {
-                mma_f16(s[a][b], a0, a1, a2, a3, st.qh[a][4 * i], st.qh[a][4 * i + 1]);
-                mma_f16(s2[a][b], c0, c1, c2, c3, st.qh[a][4 * i + 2], st.qh[a][4 * i + 3]);
-                if (F32) {
-                    mma_f16(s[a][b], a0, a1, a2, a3, st.ql[a][4 * i], st.ql[a][4 * i + 1]);
-                    mma_f16(s2[a][b], c0, c1, c2, c3, st.ql[a][4 * i + 2], st.ql[a][4 * i + 3]);
+                if constexpr (F32) {
+                    // the MMA cuts its sums instead of rounding them: 16 channels at a time, joined by additions that round
+                    float d[4] = {0.f, 0.f, 0.f, 0.f};
+                    mma_f16(d, a0, a1, a2, a3, st.ql[a][4 * i], st.ql[a][4 * i + 1]);
+                    mma_f16(d, a0, a1, a2, a3, st.qh[a][4 * i], st.qh[a][4 * i + 1]);
+                    float d2[4] = {0.f, 0.f, 0.f, 0.f};
+                    mma_f16(d2, c0, c1, c2, c3, st.ql[a][4 * i + 2], st.ql[a][4 * i + 3]);
+                    mma_f16(d2, c0, c1, c2, c3, st.qh[a][4 * i + 2], st.qh[a][4 * i + 3]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { s[a][b][e] += d[e]; s2[a][b][e] += d2[e]; }
+                } else {
+                    mma_f16(s[a][b], a0, a1, a2, a3, st.qh[a][4 * i], st.qh[a][4 * i + 1]);
+                    mma_f16(s2[a][b], c0, c1, c2, c3, st.qh[a][4 * i + 2], st.qh[a][4 * i + 3]);
                 }
             }
         }
@@ -333,7 +358,7 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
             const int tok = b * 16 + h * 8 + r;
             const float2 kk = kp[tok], vv = kp[T + tok];
             vs[b][h] = vv.x;
-            vz[b][h] = vv.y;
+            vz[b][h] = vv.y - kCentre;
             if constexpr (F32) {
                 // the exponent alone, taken out of the weight exactly: the difference that enters the exponential is small
                 // wherever the weight counts, and loses nothing to the size of the logarithm
@@ -348,7 +373,7 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
 #pragma unroll
             for (int a = 0; a < NT; ++a)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) s[a][b][2 * h + e] = kk.x * fmaf(-kk.y, st.qr[a][e], s[a][b][2 * h + e] + s2[a][b][2 * h + e]);
+                for (int e = 0; e < 2; ++e) s[a][b][2 * h + e] = kk.x * fmaf(kCentre - kk.y, st.qr[a][e], s[a][b][2 * h + e] + s2[a][b][2 * h + e]);
         }
     auto hidden = [&](int b, int h, int a, int e) {
         const int tok = first + b * 16 + h * 8 + r;
@@ -423,24 +448,42 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
     const int lane = 4 * r + t;
     const uint8_t* mine = vc + ((lane >> 3 & 1) * 8 + (lane & 7)) * (D / 2) + (lane >> 4) * 16;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int g = 0; g < D / 32; g += 2) {
+        uint32_t x[2][4];
+        load_units(mine + g * 16, x[0]);
+        load_units(mine + 16 * (D / 2) + g * 16, x[1]);
 #pragma unroll
-        for (int g = 0; g < D / 32; g += 2) {
-            uint32_t x[4];
-            load_units(mine + b * 16 * (D / 2) + g * 16, x);
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int z = 0; z < 2; ++z) {
+                const int m = 2 * (g + i) + z;
+                float sum[NT][4];                          // float32: the step's share by itself, added to the rest with rounding
+                if (F32)
 #pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    const uint32_t y0 = z ? x[2 * i] >> 8 : x[2 * i], y1 = z ? x[2 * i + 1] >> 8 : x[2 * i + 1];
-                    const int m = 2 * (g + i) + z;
+                    for (int a = 0; a < NT; ++a)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[a][e] = 0.f;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const uint32_t y0 = z ? x[b][2 * i] >> 8 : x[b][2 * i], y1 = z ? x[b][2 * i + 1] >> 8 : x[b][2 * i + 1];
+                    const uint32_t v0 = codes2<F32>(y0, false), v1 = codes2<F32>(y0, true), v2 = codes2<F32>(y1, false), v3 = codes2<F32>(y1, true);
 #pragma unroll
                     for (int a = 0; a < NT; ++a) {
-                        mma_f16(st.o[a][m], y0 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x000F000Fu, y1 & 0x00F000F0u, ph[a][2 * b], ph[a][2 * b + 1]);
-                        if (F32) mma_f16(st.o[a][m], y0 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x000F000Fu, y1 & 0x00F000F0u, pl[a][2 * b], pl[a][2 * b + 1]);
+                        if constexpr (F32) {
+                            mma_f16(sum[a], v0, v1, v2, v3, pl[a][2 * b], pl[a][2 * b + 1]);
+                            mma_f16(sum[a], v0, v1, v2, v3, ph[a][2 * b], ph[a][2 * b + 1]);
+                        } else {
+                            mma_f16(st.o[a][m], v0, v1, v2, v3, ph[a][2 * b], ph[a][2 * b + 1]);
+                        }
                     }
                 }
-        }
+                if (F32)
+#pragma unroll
+                    for (int a = 0; a < NT; ++a)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) st.o[a][m][e] += sum[a][e];
+            }
+    }
 }
 
 template <typename QT, int D, int NT>
@@ -594,6 +637,7 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
         // ---- the four warps' states meet
         float* m_top = reinterpret_cast<float*>(merge);    // [warps][R], then [warps][R] sums, [warps][R][OROW] outputs
         float* m_l = m_top + kWarps * R;
+        constexpr float kLow = F32 ? 1.f : 16777216.f, kHigh = F32 ? 1.f : 1048576.f;          // what codes2 has them in
         float* m_o = m_l + kWarps * R;
 #pragma unroll
         for (int a = 0; a < NT; ++a)
@@ -612,8 +656,8 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
 #pragma unroll
                 for (int m = 0; m < S::MT; m += 2)
                     *reinterpret_cast<float4*>(row + 16 * m) =
-                        make_float4(fmaf(st.o[a][m][e], 16777216.f, -st.zs[a][e]), fmaf(st.o[a][m][2 + e], 1048576.f, -st.zs[a][e]),
-                                    fmaf(st.o[a][m + 1][e], 16777216.f, -st.zs[a][e]), fmaf(st.o[a][m + 1][2 + e], 1048576.f, -st.zs[a][e]));
+                        make_float4(fmaf(st.o[a][m][e], kLow, -st.zs[a][e]), fmaf(st.o[a][m][2 + e], kHigh, -st.zs[a][e]),
+                                    fmaf(st.o[a][m + 1][e], kLow, -st.zs[a][e]), fmaf(st.o[a][m + 1][2 + e], kHigh, -st.zs[a][e]));
             }
         ptx::named_bar_sync(1, 32 * kWarps);
         const bool whole = it.count == it.tiles;
