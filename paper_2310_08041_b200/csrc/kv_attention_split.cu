@@ -13,15 +13,15 @@
 // In a CTA: one warp fetches a tile's codes and parameters with bulk copies, one per page and array, several tiles ahead; four
 // warps own 32 of its tokens each, with a softmax state of their own that meets at the item's end.  Both products run
 // transposed (S^T = K Q^T, O^T = V^T P^T) so that 16 tokens or channels fill the 16 rows of the warp-level MMA and the 8
-// query rows its 8 columns: a decode step's few rows waste nothing.  A nibble masked in place is a denormal fp16 number
-// (c 2^-24, or c 2^-20 from the upper half of a byte), which the MMA takes exactly: five logical instructions turn 8 key codes
-// (eight of 16-bit units that a transposing load has paired, 16 value codes) into operands.  Channel and token order inside an operand is free as long as both sides agree, so the codes of one 16-byte
-// read are used where they lie, and the factor 16 of the upper nibbles is taken out of the queries, or of the output's odd
-// channels at the end.
+// query rows its 8 columns: a decode step's few rows waste nothing.  A nibble masked in place is a denormal fp16 number (c 2^-24,
+// or c 2^-20 from the upper half of a byte), which the MMA takes: five logical instructions turn 8 key codes into operands, and as
+// many and four packed subtractions the value codes of 16-bit units that a transposing load has paired.  Channel order inside an
+// operand is free as long as both sides agree, so the key codes of one 16-byte read are used where they lie, and the factor 16 of
+// the upper nibbles is taken out of the queries.
 //
 // Precision: queries are scaled by a power of two per row into fp16's range (a bf16 query's 8 bits stay exact) and float32
 // queries are split in two; weights p_j vs_j are rounded to fp16, 11 bits, for bf16 results (which carry 8) and split in two
-// for float32 ones, whose codes also enter as normal numbers and whose sums over more than 16 or 32 terms are float32 additions.
+// for float32 ones, whose keys also enter as normal numbers and whose sums over more than 16 or 32 terms are float32 additions.
 // So that no weight leaves fp16's range whatever the value scales are, the running maximum is that of s_j + log2 vs_j (the
 // logarithm cut to +-80; its integer part for float32), with the largest weight placed at 2^6; it moves only when a weight would
 // pass 2^14, which spares most steps the reduction over lanes and the rescaling.  Sums, maxima and zero-point corrections are
@@ -228,13 +228,14 @@ __device__ __forceinline__ void load_units(const uint8_t* p, uint32_t (&x)[4]) {
                  : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(ptx::smem_addr(p)) : "memory");
 }
 
-// Codes as A operands: two nibbles of a word (`upper`: those of bits 4-7 and 20-23, else 0-3 and 16-19).  bf16 calls take them as
-// they are masked, denormal numbers c 2^-24 and 16 c 2^-24.  The MMA aligns its sums to the operands' nominal exponents, which for
-// denormals lie up to 10 bits above their values, and cuts what falls off: 2^-16 of a sum is lost, nothing to 8 or 11 bits.  float32
-// calls take c - 8 as normal numbers (1024 + c and 1024 + 16 c are fp16 numbers, one packed operation makes the difference).
-template <bool F32>
+// Codes as A operands: two nibbles of a word (`upper`: those of bits 4-7 and 20-23, else 0-3 and 16-19).  The keys of a bf16 call
+// are taken as they are masked, denormal numbers c 2^-24 and 16 c 2^-24.  The MMA aligns its sums to the operands' nominal
+// exponents, which for denormals lie up to 10 bits above their values, and cuts what falls off: 2^-16 of a score's terms is lost.
+// NORMAL (values, whose sums run over the whole context, and everything in float32): c - 8 as normal numbers; 1024 + c and
+// 1024 + 16 c are fp16 numbers, one packed operation makes the difference.
+template <bool NORMAL>
 __device__ __forceinline__ uint32_t codes2(uint32_t w, bool upper) {
-    if constexpr (!F32) return w & (upper ? 0x00F000F0u : 0x000F000Fu);
+    if constexpr (!NORMAL) return w & (upper ? 0x00F000F0u : 0x000F000Fu);
     const uint32_t h = (w & (upper ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;
     const __half2 v = *reinterpret_cast<const __half2*>(&h);
     const __half2 r = upper ? __hfma2(v, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hadd2(v, __float2half2_rn(-1032.f));
@@ -313,7 +314,7 @@ template <int D, int NT, bool F32, bool MASKED>
 __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, const uint8_t* vc, const float2* kp, int first, int len,
                                      uint32_t there, int r, int t) {
     constexpr int KW = D / 32, MT = D / 16;
-    constexpr float kCentre = F32 ? 8.f : 0.f;             // what the operands have taken off the codes
+    constexpr float kCentre = F32 ? 8.f : 0.f;             // what the operands have taken off the keys' codes
     float s[NT][2][4], s2[NT][2][4];                       // two chains of MMAs each: their latency bounds a warp
     // ---- S^T = K Q^T, 16 tokens at a time
 #pragma unroll
@@ -358,7 +359,7 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
             const int tok = b * 16 + h * 8 + r;
             const float2 kk = kp[tok], vv = kp[T + tok];
             vs[b][h] = vv.x;
-            vz[b][h] = vv.y - kCentre;
+            vz[b][h] = vv.y - 8.f;
             if constexpr (F32) {
                 // the exponent alone, taken out of the weight exactly: the difference that enters the exponential is small
                 // wherever the weight counts, and loses nothing to the size of the logarithm
@@ -466,7 +467,7 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     const uint32_t y0 = z ? x[b][2 * i] >> 8 : x[b][2 * i], y1 = z ? x[b][2 * i + 1] >> 8 : x[b][2 * i + 1];
-                    const uint32_t v0 = codes2<F32>(y0, false), v1 = codes2<F32>(y0, true), v2 = codes2<F32>(y1, false), v3 = codes2<F32>(y1, true);
+                    const uint32_t v0 = codes2<true>(y0, false), v1 = codes2<true>(y0, true), v2 = codes2<true>(y1, false), v3 = codes2<true>(y1, true);
 #pragma unroll
                     for (int a = 0; a < NT; ++a) {
                         if constexpr (F32) {
@@ -637,7 +638,6 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
         // ---- the four warps' states meet
         float* m_top = reinterpret_cast<float*>(merge);    // [warps][R], then [warps][R] sums, [warps][R][OROW] outputs
         float* m_l = m_top + kWarps * R;
-        constexpr float kLow = F32 ? 1.f : 16777216.f, kHigh = F32 ? 1.f : 1048576.f;          // what codes2 has them in
         float* m_o = m_l + kWarps * R;
 #pragma unroll
         for (int a = 0; a < NT; ++a)
@@ -656,8 +656,8 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
 #pragma unroll
                 for (int m = 0; m < S::MT; m += 2)
                     *reinterpret_cast<float4*>(row + 16 * m) =
-                        make_float4(fmaf(st.o[a][m][e], kLow, -st.zs[a][e]), fmaf(st.o[a][m][2 + e], kHigh, -st.zs[a][e]),
-                                    fmaf(st.o[a][m + 1][e], kLow, -st.zs[a][e]), fmaf(st.o[a][m + 1][2 + e], kHigh, -st.zs[a][e]));
+                        make_float4(st.o[a][m][e] - st.zs[a][e], st.o[a][m][2 + e] - st.zs[a][e], st.o[a][m + 1][e] - st.zs[a][e],
+                                    st.o[a][m + 1][2 + e] - st.zs[a][e]);
             }
         ptx::named_bar_sync(1, 32 * kWarps);
         const bool whole = it.count == it.tiles;
