@@ -33,7 +33,6 @@ namespace {
 
 using namespace kv;
 using tc::Abort;
-
 using tc::wait_bounded;
 
 constexpr int BM = 128, BN = 128;                          // query rows of a tile, tokens of a key tile
@@ -212,9 +211,10 @@ __device__ __forceinline__ void unpack_row(uint32_t raw, uint32_t op, int tok, f
 // 32: a chunk overwrites what has been read).  vs, there: shared addresses of the half's value scales and bits of the tokens that
 // exist.  MASKED: some token of the tile is hidden from some row; BARE: the weights carry the value scales.
 //
-// Two passes, maximum and weights, in loops of 32 columns that stay rolled, as the unpacking does: unrolled over the tile, with
-// the row held in registers between the passes, the roles' code together outran the instruction cache (a chunk of 1024 tokens
-// behind up to 8191, 64/8 heads, one thread per row: 453 us instead of 417).
+// Two passes over tensor memory, maximum and weights, of 32 columns at a time.  Holding the half row in registers between them
+// spills; with one thread per row, where it did not, the code of all roles together outran the instruction cache (chunks of 1024
+// tokens behind up to 8191, 64/8 heads: 453 us instead of 417), as unrolled unpacking does.  Taking every second, third or
+// fourth exponential by a polynomial, off the special-function unit, gained nothing (357, 341, 343 us against 330).
 constexpr int kCols = 64;
 template <bool MASKED>
 __device__ __forceinline__ void hide(uint32_t (&r)[32], int first, int limit, uint32_t there) {
@@ -228,7 +228,7 @@ __device__ __forceinline__ float log_scale(uint32_t v) { return fminf(fmaxf(lg2(
 template <bool MASKED, bool BARE>
 __device__ __forceinline__ float half_max(uint32_t addr, uint32_t vs, int first, int limit, uint32_t there, float qn) {
     float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
+#pragma unroll
     for (int c = 0; c < kCols / 32; ++c) {
         uint32_t r[32];
         ptx::tmem_ld_32x32b_x32(addr + 32 * c, r);
@@ -250,7 +250,7 @@ template <bool MASKED, bool BARE>
 __device__ __forceinline__ float half_weights(uint32_t addr, uint32_t vs, int first, int limit, uint32_t there, float qn, float sub) {
     const F2 q2(qn, qn), s2(sub, sub);
     F2 l[4] = {F2(0.f, 0.f), F2(0.f, 0.f), F2(0.f, 0.f), F2(0.f, 0.f)};
-#pragma unroll 1
+#pragma unroll
     for (int c = 0; c < kCols / 32; ++c) {
         uint32_t r[32], p[16];
         ptx::tmem_ld_32x32b_x32(addr + 32 * c, r);
