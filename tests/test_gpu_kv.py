@@ -459,6 +459,27 @@ def test_streams_and_graphs():
     assert B.qllm_poll_status() == B.QLLM_OK
 
 
+@pytest.mark.parametrize("seed", range(40))
+def test_attention_random_shapes(seed):
+    rng = np.random.RandomState(1000 + seed)
+    d, page, dtype = int(rng.choice([64, 128, 256])), int(rng.choice([16, 32, 64, 128, 256])), ["bf16", "f32"][rng.randint(2)]
+    heads, group, seqs = rng.randint(1, 4), rng.randint(1, 12), rng.randint(1, 7)
+    lens = [int(x) for x in np.exp(rng.uniform(0, np.log(1500), seqs))]
+    news = [int(min(n, max(0, rng.choice([0, 1, 1, 3, 17, n // 2, n])))) for n in lens]
+    if sum(news) == 0:
+        news[0] = 1
+    run_case(seed, dtype, d, page, heads, group, lens, news, bool(rng.rand() < 0.8), stride_pad=8 * rng.randint(0, 3),
+             max_new=int(rng.choice([max(news), max(news), 1, 4000])))
+
+
+def test_read_of_a_page_that_does_not_exist_is_zero():
+    cache = random_cache(40, 1, 4, 2, 16, 64)
+    k, v = torch.full((40, 2, 64), 5.0, device=G.DEV), torch.full((40, 2, 64), 5.0, device=G.DEV)
+    B.qllm_kv_read(cache, 0, k, v, B.KvBatch(ints([[1, 9, 2]]), ints([40]), ints([0, 40]), 40, 40))
+    assert (k[16:32] == 0).all() and (v[16:32] == 0).all() and (k[:16] != 0).any() and (k[32:] != 0).any()
+    assert B.qllm_poll_status() == B.QLLM_ERR_PAGE
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_more_sequences_than_threads(dtype):
     """The kernels share out the work of all sequences: more of them than a CTA has threads, many without new tokens, a few with

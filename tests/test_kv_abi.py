@@ -116,6 +116,21 @@ def test_tensors_refused():
     assert attention(None, batch()) == B.QLLM_ERR_NULL
 
 
+def test_workspace():
+    """The size depends on the arguments only (148 SMs are assumed without a device); smaller, missing and unaligned ones are refused."""
+    for dtype, b in ((0, batch()), (1, batch()), (1, batch(rows=4000, max_new=2000)), (1, batch(seqs=1, rows=300, max_new=300))):
+        n = L.qllm_kv_attention_workspace(p(cache()), 8, dtype, p(b))
+        assert n >= 0 and n == L.qllm_kv_attention_workspace(p(cache()), 8, dtype, p(b))
+        if n:
+            kw = dict(dtype=dtype)
+            assert attention(cache(), b, ws=None, **kw) == B.QLLM_ERR_NULL
+            assert attention(cache(), b, bytes_=n - 1, **kw) == B.QLLM_ERR_SHAPE
+            assert attention(cache(), b, ws=8, **kw) == B.QLLM_ERR_ALIGN
+    assert L.qllm_kv_attention_workspace(p(cache()), 8, 1, p(batch(rows=0))) == 0
+    assert L.qllm_kv_attention_workspace(p(cache()), 6, 1, p(batch())) == B.QLLM_ERR_SHAPE
+    assert B.qllm_status_string(B.QLLM_ERR_PAGE) not in ("ok", "unknown status")
+
+
 def test_pools_refused():
     for kw, e in [(dict(pages=0), "SHAPE"), (dict(seqs=0), "SHAPE"), (dict(table_width=0), "SHAPE"), (dict(seqs=8193), "UNSUPPORTED"),
                   (dict(refs=None), "NULL"), (dict(table=None), "NULL"), (dict(seq_lens=None), "NULL")]:
