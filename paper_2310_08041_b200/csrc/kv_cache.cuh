@@ -50,7 +50,7 @@ struct Batch {
             const int mid = (lo + hi) >> 1;
             if (start[mid] <= t) lo = mid + 1; else hi = mid;
         }
-        return lo > 0 && t - row(lo - 1) < count(lo - 1) ? lo - 1 : -1;
+        return lo > 0 && t >= row(lo - 1) && t - row(lo - 1) < count(lo - 1) ? lo - 1 : -1;
     }
     // Raises the status word for lengths and row ranges that had to be cut: `n` threads of one CTA, this is number `i`.
     __device__ __forceinline__ void report(int* status, int i, int n) const {
