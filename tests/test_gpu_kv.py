@@ -459,6 +459,66 @@ def test_streams_and_graphs():
     assert B.qllm_poll_status() == B.QLLM_OK
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news", [[1, 2], [120, 1], [130, 130]])
+def test_attention_leaves_other_rows_and_the_gaps_of_strided_outputs(dtype, news):
+    heads, group, page, d = 2, 4, 32, 64
+    rng = np.random.RandomState(41)
+    lens = [150, 400]
+    table = make_table(rng, lens, page, 20)
+    cache = random_cache(41, 1, 20, heads, page, d)
+    start = [6, 6 + news[0], 6 + sum(news)]
+    rows = start[-1] + 9
+    batch = B.KvBatch(ints(table), ints(lens), ints(start), rows, max(news))
+    q = torch.randn(rows, heads * group, d, device=G.DEV).to(DT[dtype])
+    wide = torch.full((rows, heads * group * d + 32), 5.0, device=G.DEV, dtype=DT[dtype])
+    out = wide[:, 16:-16].unflatten(1, (heads * group, d))
+    lse = torch.full((rows, heads * group), 5.0, device=G.DEV)
+    ws = torch.empty(max(16, B.qllm_kv_attention_workspace(cache, heads * group, q, batch)), dtype=torch.uint8, device=G.DEV)
+    B.qllm_kv_attention(cache, 0, q, out, 0.1, batch, ws, lse=lse)
+    assert (wide[:, :16] == 5).all() and (wide[:, -16:] == 5).all()
+    for a, b in ((0, 6), (start[-1], rows)):
+        assert (wide[a:b] == 5).all() and (lse[a:b] == 5).all()
+    ref = kv_ref.attention(store_of(cache, 0), table, lens, start, host(q), 0.1, True)
+    cut = tuple(r[6:start[-1]] for r in ref)
+    check_attention(out[6:start[-1]], lse[6:start[-1]], cut, DT[dtype], prompt=dtype == "bf16" and max(news) * group > 96)
+    assert B.qllm_poll_status() == B.QLLM_OK
+
+
+@pytest.mark.parametrize("news", [[200], [130, 1, 0]])
+def test_prompt_kernels_in_a_graph(news):
+    """The tensor-core kernel with its keys cut into parts (few rows), alone and together with the streaming one, captured on a
+    stream of its own and replayed while lengths and pages change."""
+    heads, group, page, d = 1, 4, 16, 128
+    rng = np.random.RandomState(42)
+    top = [1500] * len(news)
+    table = make_table(rng, top, page, 300)
+    cache = random_cache(42, 1, 300, heads, page, d)
+    batch, start = batch_of(table, top, news)
+    q = torch.randn(batch.rows, heads * group, d, device=G.DEV).bfloat16()
+    out, st = torch.empty_like(q), torch.cuda.Stream()
+    ws = torch.full((B.qllm_kv_attention_workspace(cache, heads * group, q, batch),), 0xFF, dtype=torch.uint8, device=G.DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        B.qllm_kv_attention(cache, 0, q, out, 0.09, batch, ws, stream=st)
+    st.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        B.qllm_kv_attention(cache, 0, q, out, 0.09, batch, ws, stream=st)
+    for lens in ([1500] * len(news), [200, 17, 0][:len(news)], [911, 1, 64][:len(news)]):
+        other = make_table(np.random.RandomState(lens[0]), top, page, 300)
+        batch.seq_lens.copy_(ints(lens))
+        batch.table.copy_(ints(other))
+        q.normal_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            g.replay()
+        torch.cuda.synchronize()
+        ref = kv_ref.attention(store_of(cache, 0), other, lens, start, host(q), 0.09, True)
+        check_attention(out, torch.from_numpy(ref[1]).float(), ref, torch.bfloat16, prompt=True)
+    assert B.qllm_poll_status() == B.QLLM_OK
+
+
 @pytest.mark.parametrize("seed", range(40))
 def test_attention_random_shapes(seed):
     rng = np.random.RandomState(1000 + seed)
