@@ -30,7 +30,7 @@
 // Measured (us a call, both kernels; the bytes of the cache at the measured copy rate in brackets): one sequence of 131071
 // tokens, 64 query on 8 key heads of 128, bf16: 44 (23), of which the main kernel streams 24 at that rate, starts for 6 (plan, table,
 // first tiles) and spreads over 8 at the end, and joining takes 5; 32 sequences of 176 to 9001 tokens: 37 (16); 6 sequences, up to
-// 5 new tokens, 40 heads, float32: 24 (4).  Without its arithmetic the kernel took 2 us less: latency at both ends, not the
+// 5 new tokens, 40 heads, float32: 23 (4).  Without its arithmetic the kernel took 2 us less: latency at both ends, not the
 // instruction rate, is what is left.  Tried and dropped: four CTAs per SM in 96 registers (spills, 60 instead of 48), two or three
 // times as many shares as CTAs that fit (60, 80), reading page ids tile by tile (no difference).
 
@@ -70,8 +70,9 @@ struct Shape {
 // ---- the line of work ----------------------------------------------------------------------------------------------------
 // An item costs kItemCost tiles for its queries, its first loads and its end, then one for each tile of keys: a share that
 // ends in front of the first tile takes none of the item.  (Counting tiles alone gave the CTAs that got the short sequences of
-// a ragged batch half as much work again.)
-constexpr int kItemCost = 3;
+// a ragged batch half as much work again: 46 us instead of 40 for 32 sequences of 176 to 9001 tokens.  2, 3 and 5 tiles: 36.6,
+// 36.6, 38.0 us there, 22.7, 24.2, 25.5 for 6 sequences of up to 1999 tokens, 40 heads, float32.)
+constexpr int kItemCost = 2;
 
 struct Plan {
     Batch b;
