@@ -16,7 +16,9 @@
 // would carry 8.  So nothing acts per score and token: a score's factor is the row's times 2^E, a weight is p 2^E.  Queries are
 // scaled per row by a power of two into fp16 (a bf16 query's 8 bits are kept).  Tiles whose value scales differ by more than
 // 2^10, or pass 2^80, keep the values' bare codes and multiply the weights by vs instead, since a weight of a small value must
-// not lose its bits to a large value that the row hardly looks at.  Rows far from zero (|zero| > 900) are made in float32.
+// not lose its bits to a large value that the row hardly looks at.  So do tiles in which a key's scale 2^-E is no normal fp16 number: a
+// key must not lose its bits to a louder one that the row does not see, or turns away from.  There each key's own power of two acts on its
+// score.  Rows far from zero (|zero| > 900) are made in float32.
 // Channels lie in the order 0 4 1 5 2 6 3 7 of each eight, as the masks leave them: the queries are stored alike and the output
 // is put right at the end.
 
@@ -54,7 +56,7 @@ struct Shape {
     static constexpr int RAW = BN * (D / 2);               // codes as they come
     static constexpr int RAWS = 3;
     static constexpr int RAWP = 2 * BN * 8;                // both parameter arrays, fetched with the keys: two of them
-    static constexpr int PRM = BN * 4;                     // one float per token
+    static constexpr int PRM = BN * 6;                     // per token: a value scale, the upper half of a power of two
     static constexpr int SMEM = 1024 + 2 * OP + OPS * OP + RAWS * RAW + 2 * RAWP + kSlots * PRM;
     static constexpr uint32_t TMEM_S = 0, TMEM_O = 256;    // columns: S_0, S_1, O_0, O_1
 };
@@ -214,8 +216,9 @@ __device__ __forceinline__ void unpack_row(uint32_t raw, uint32_t op, int tok, f
 }
 
 // Half a row's scores as they lie in tensor memory (64 columns from `addr`) become its weights in their place (16 columns for
-// 32: a chunk overwrites what has been read).  vs, there: shared addresses of the half's value scales and bits of the tokens that
-// exist.  MASKED: some token of the tile is hidden from some row; BARE: the weights carry the value scales.
+// 32: a chunk overwrites what has been read).  vs, kx, there: shared addresses of the half's value scales, of its keys' powers of two
+// and of the bits of the tokens that exist.  MASKED: some token of the tile is hidden from some row; BARE: the scores take the keys'
+// powers of two, the weights the value scales.
 //
 // Two passes over tensor memory, maximum and weights, of 32 columns at a time.  Holding the half row in registers between them
 // spills; with one thread per row, where it did not, the code of all roles together outran the instruction cache (chunks of 1024
@@ -230,15 +233,27 @@ __device__ __forceinline__ void hide(uint32_t (&r)[32], int first, int limit, ui
 #pragma unroll
     for (int k = 0; k < 32; ++k) r[k] = seen >> k & 1 ? r[k] : 0xFF800000u;
 }
+// (in front of the masks: a hidden key's power of two would turn their infinity into NaN if it were no number)
+template <bool BARE>
+__device__ __forceinline__ void scale_keys(uint32_t (&r)[32], uint32_t kx) {
+    if (!BARE) return;
+#pragma unroll
+    for (int k = 0; k < 32; k += 2) {
+        const uint32_t x = lds1(kx + 2 * k);
+        r[k] = __float_as_uint(__uint_as_float(r[k]) * __uint_as_float(x << 16));
+        r[k + 1] = __float_as_uint(__uint_as_float(r[k + 1]) * __uint_as_float(x & 0xFFFF0000u));
+    }
+}
 __device__ __forceinline__ float log_scale(uint32_t v) { return fminf(fmaxf(lg2(fabsf(__uint_as_float(v))), -80.f), 80.f); }
 template <bool MASKED, bool BARE>
-__device__ __forceinline__ float half_max(uint32_t addr, uint32_t vs, int first, int limit, uint32_t there, float qn) {
+__device__ __forceinline__ float half_max(uint32_t addr, uint32_t vs, uint32_t kx, int first, int limit, uint32_t there, float qn) {
     float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
     for (int c = 0; c < kCols / 32; ++c) {
         uint32_t r[32];
         ptx::tmem_ld_32x32b_x32(addr + 32 * c, r);
         ptx::tmem_ld_wait();
+        scale_keys<BARE>(r, kx + 64 * c);
         hide<MASKED>(r, first + 32 * c, limit, there + 4 * c);
 #pragma unroll
         for (int k = 0; k < 32; k += 2) {
@@ -253,7 +268,7 @@ __device__ __forceinline__ float half_max(uint32_t addr, uint32_t vs, int first,
     return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 template <bool MASKED, bool BARE>
-__device__ __forceinline__ float half_weights(uint32_t addr, uint32_t vs, int first, int limit, uint32_t there, float qn, float sub) {
+__device__ __forceinline__ float half_weights(uint32_t addr, uint32_t vs, uint32_t kx, int first, int limit, uint32_t there, float qn, float sub) {
     const F2 q2(qn, qn), s2(sub, sub);
     F2 l[4] = {F2(0.f, 0.f), F2(0.f, 0.f), F2(0.f, 0.f), F2(0.f, 0.f)};
 #pragma unroll
@@ -261,6 +276,7 @@ __device__ __forceinline__ float half_weights(uint32_t addr, uint32_t vs, int fi
         uint32_t r[32], p[16];
         ptx::tmem_ld_32x32b_x32(addr + 32 * c, r);
         ptx::tmem_ld_wait();
+        scale_keys<BARE>(r, kx + 64 * c);
         hide<MASKED>(r, first + 32 * c, limit, there + 4 * c);
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
@@ -292,6 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
     uint8_t* s_raw = s_op + S::OPS * S::OP;                // [RAWS]
     uint8_t* s_rawp = s_raw + S::RAWS * S::RAW;            // [2] (a third tile's keys wait for the first one's values to be unpacked)
     float* s_vs = reinterpret_cast<float*>(s_rawp + 2 * S::RAWP);            // [kSlots][BN] value scales, for tiles of bare codes
+    uint16_t* s_kx = reinterpret_cast<uint16_t*>(s_vs + kSlots * BN);        // [kSlots][BN] powers of two (upper halves of floats), likewise
     __shared__ uint64_t s_bar[32];
     __shared__ uint32_t s_tmem, s_pieces[S::RAWS];
     __shared__ int s_abort, s_find[2];
@@ -439,10 +456,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
             const int first = j * BN + half * kCols;
             const bool masked = j * BN + BN > low || (flags & 2), bare = flags & 1;
             const float e = s_e[slot], qk = fminf(fmaxf(qn * s_ek[slot], 1e-37f), 3e38f);
-            const uint32_t vs = ptx::smem_addr(s_vs + slot * BN + half * kCols), there = ptx::smem_addr(&s_there[slot][2 * half]);
-            float m = bare     ? half_max<true, true>(t_s, vs, first, limit, there, qk)
-                      : masked ? half_max<true, false>(t_s, vs, first, limit, there, qk)
-                               : half_max<false, false>(t_s, vs, first, limit, there, qk);
+            const uint32_t vs = ptx::smem_addr(s_vs + slot * BN + half * kCols), kx = ptx::smem_addr(s_kx + slot * BN + half * kCols), there = ptx::smem_addr(&s_there[slot][2 * half]);
+            float m = bare     ? half_max<true, true>(t_s, vs, kx, first, limit, there, qk)
+                      : masked ? half_max<true, false>(t_s, vs, kx, first, limit, there, qk)
+                               : half_max<false, false>(t_s, vs, kx, first, limit, there, qk);
             *mine = m;
             ptx::named_bar_sync(pair, 64);
             m = fmaxf(m, *other);
@@ -466,9 +483,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 }
             }
             const float at = top == -INFINITY ? 0.f : top;
-            if (bare) l += half_weights<true, true>(t_s, vs, first, limit, there, qk, -at);
-            else l = fmaf(masked ? half_weights<true, false>(t_s, vs, first, limit, there, qk, e - at)
-                                 : half_weights<false, false>(t_s, vs, first, limit, there, qk, e - at), pow2i(-int(e)), l);
+            if (bare) l += half_weights<true, true>(t_s, vs, kx, first, limit, there, qk, -at);
+            else l = fmaf(masked ? half_weights<true, false>(t_s, vs, kx, first, limit, there, qk, e - at)
+                                 : half_weights<false, false>(t_s, vs, kx, first, limit, there, qk, e - at), pow2i(-int(e)), l);
             tmem_st_wait();
             ptx::tc_fence_before_sync();
             __syncwarp();
@@ -557,7 +574,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 const uint32_t pieces = s_pieces[rs];
                 float2* prm = reinterpret_cast<float2*>(s_rawp + ((j - j0) & 1) * S::RAWP);
                 float2 kp[4], vp[4];
-                int hi = -1000, lo = 1000, khi = -1000;
+                int hi = -1000, lo = 1000, khi = -1000, klo = 1000;
+                float kround[4];                           // what of a key is rounded to fp16: its scale, or (far from zero) its values
                 uint32_t goods = 0, everywhere = 0xffffffffu;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -571,7 +589,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                     if (!(fabsf(vp[i].x) <= 3e38f && fabsf(vp[i].y) <= 3e38f)) { kp[i].x = NAN; vp[i] = make_float2(0.f, 0.f); }
                     if (!(fabsf(kp[i].y) <= 3e38f)) { kp[i].x = NAN; kp[i].y = 0.f; }
                     const float klargest = fabsf(kp[i].x) * fmaxf(fabsf(kp[i].y), fabsf(15.f - kp[i].y));
-                    if (klargest > 0.f && klargest <= 3e38f) khi = max(khi, int(__float_as_uint(klargest) >> 23) - 127);
+                    kround[i] = klargest > 0.f && klargest <= 3e38f ? (is_far(kp[i].y) ? klargest : fabsf(kp[i].x)) : 0.f;
+                    if (kround[i] != 0.f) {
+                        khi = max(khi, int(__float_as_uint(klargest) >> 23) - 127);
+                        klo = min(klo, int(__float_as_uint(kround[i]) >> 23) - 127);
+                    }
                     const float largest = fabsf(vp[i].x) * fmaxf(fabsf(vp[i].y), fabsf(15.f - vp[i].y));
                     if (largest != 0.f) {
                         const int ex = largest < 1.2e24f ? max(int(__float_as_uint(largest) >> 23) - 127, -80) : 1000;   // 2^80: the logarithm's cut
@@ -585,13 +607,20 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 hi = __reduce_max_sync(0xffffffffu, hi);
                 lo = __reduce_min_sync(0xffffffffu, lo);
                 khi = __reduce_max_sync(0xffffffffu, khi);
-                const bool bare = hi > 900 || hi - lo > 10;                  // (no values at all: -1000 and 1000)
-                const int e = bare || hi < -900 ? 0 : hi, ek = khi < -900 ? 0 : min(max(khi, -120), 120);
+                klo = __reduce_min_sync(0xffffffffu, klo);
+                const int ek = khi < -900 ? 0 : min(max(khi, -120), 120);
+                const bool bare = hi > 900 || hi - lo > 10 || klo < ek - 14;                  // (none at all: -1000 and 1000)
+                const int e = bare || hi < -900 ? 0 : hi;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    prm[32 * i + lane] = make_float2(kp[i].y, kp[i].x * pow2i(-ek));
-                    float vf = 1.f;
+                    float vf = 1.f, kf = kp[i].x * pow2i(-ek);
                     if (bare) {
+                        int x = ek;                        // (a scale that is 0 or no number stays what it is)
+                        if (kround[i] != 0.f) {
+                            x = int(__float_as_uint(kround[i]) >> 23) - 127;
+                            kf = kp[i].x * pow2i(-x);
+                        }
+                        s_kx[slot * BN + 32 * i + lane] = uint16_t(__float_as_uint(pow2i(max(x - ek, -126))) >> 16);
                         if (is_far(vp[i].y)) {
                             const int k = min(max(int((__float_as_uint(vp[i].y) >> 23) & 255u) - 127 - 9, 0), 120);
                             vf = pow2i(-k);
@@ -601,6 +630,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                     } else {
                         vf = vp[i].x * pow2i(-e);
                     }
+                    prm[32 * i + lane] = make_float2(kp[i].y, kf);
                     prm[BN + 32 * i + lane] = make_float2(vp[i].y, goods >> i & 1 ? vf : 0.f);
                 }
                 if (lane == 0) {

@@ -1,0 +1,70 @@
+"""The 4-bit cache where its numbers lie far apart: keys and values of very different size in one tile, rows without a range, rows
+that are no numbers, queries near the end of their type."""
+import numpy as np
+import pytest
+import torch
+
+import gpu_util as G
+import kv_bounds
+import kv_ref
+from paper_2310_08041_b200 import binding as B
+from test_gpu_kv import DT, attend, batch_of, check_attention, host, ints, make_table, random_cache, store_of
+from test_gpu_kv_prompt import layer_of, queries
+
+pytestmark = pytest.mark.gpu
+
+
+def place(table, s, position, page):
+    return int(table[s, position // page]), position % page
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("power", [8, 12, 14, 16, 20, 24, 33, 60])
+@pytest.mark.parametrize("where", ["behind the rows", "seen and turned away from", "far from zero"])
+def test_a_loud_key_leaves_the_others_their_bits(where, power, d):
+    """One key 2^power times the others, in a tile of the tensor-core kernel: behind the rows that are looked at (causal), or in front of
+    them with a score so low that it has no weight.  The others' scores decide every row and keep their precision; so they do where all
+    keys lie far from zero."""
+    lens, news, page, heads, group = [300, 150], [150, 100], 64, 2, 4
+    table = make_table(np.random.RandomState(61), lens, page, 9)
+    cache = random_cache(61, 1, 9, heads, page, d)
+    batch, start = batch_of(table, lens, news)
+    q, scale = queries(62, batch.rows, heads * group, d), d ** -0.5
+    if where == "far from zero":
+        cache.k_param[..., 1] = torch.randint(-4000, 4000, cache.k_param.shape[:-1], device=G.DEV).float()
+        scale /= 300
+    for s, n in enumerate(lens):
+        at = n - 1 if where != "seen and turned away from" else 70 + s
+        p, i = place(table, s, at, page)
+        cache.k_param[0, p, :, i, 0] *= 2.0 ** power
+        if where == "seen and turned away from":
+            cache.k_param[0, p, :, i, 1] = 16.0              # code - zero < 0 in every channel
+            q = q.abs()
+    want = kv_bounds.expect(layer_of(cache), table, lens, start, q, scale, True)
+    got, lse = attend(cache, 0, q, batch, scale, True)
+    rows = [r for r in range(batch.rows) if r + 1 not in start] if where != "seen and turned away from" else None
+    kv_bounds.check(got, lse, want, rows)
+    assert B.qllm_poll_status() == B.QLLM_OK
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_keys_of_every_size(causal, d):
+    """Key scales spread evenly over 2^-40 .. 1 in every tile, and queries large enough for the small ones to matter too."""
+    lens, news, page, heads, group = [500, 130], [200, 130], 32, 2, 2
+    table = make_table(np.random.RandomState(63), lens, page, 25)
+    cache = random_cache(63, 1, 25, heads, page, d)
+    g = torch.Generator(device=G.DEV); g.manual_seed(63)
+    cache.k_param[..., 0] = 2.0 ** (torch.rand(cache.k_param.shape[:-1], generator=g, device=G.DEV) * -40)
+    cache.k_param[..., 1] = 16.0                             # with queries above zero every score is negative: the small ones lead
+    batch, start = batch_of(table, lens, news)
+    q = queries(64, batch.rows, heads * group, d).abs() * 2.0 ** torch.randint(0, 30, (batch.rows, heads * group, 1), generator=g, device=G.DEV)
+    q = q.bfloat16()
+    want = kv_bounds.expect(layer_of(cache), table, lens, start, q, d ** -0.5, causal)
+    got, lse = attend(cache, 0, q, batch, d ** -0.5, causal)
+    kv_bounds.check(got, lse, want)
+    # a key without a scale, as in a cache that was never written, scores zero
+    cache.k_param[:, ::2, :, ::3, 0] = 0.0
+    want = kv_bounds.expect(layer_of(cache), table, lens, start, q, d ** -0.5, causal)
+    got, lse = attend(cache, 0, q, batch, d ** -0.5, causal)
+    kv_bounds.check(got, lse, want)
