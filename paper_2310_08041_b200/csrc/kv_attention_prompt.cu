@@ -16,9 +16,9 @@
 // would carry 8.  So nothing acts per score and token: a score's factor is the row's times 2^E, a weight is p 2^E.  Queries are
 // scaled per row by a power of two into fp16 (a bf16 query's 8 bits are kept).  Tiles whose value scales differ by more than
 // 2^10, or pass 2^80, keep the values' bare codes and multiply the weights by vs instead, since a weight of a small value must
-// not lose its bits to a large value that the row hardly looks at.  So do tiles in which a key's scale 2^-E is no normal fp16 number: a
-// key must not lose its bits to a louder one that the row does not see, or turns away from.  There each key's own power of two acts on its
-// score.  Rows far from zero (|zero| > 900) are made in float32.
+// not lose its bits to a large value that the row hardly looks at.  So do tiles in which some scale 2^-E is no normal fp16 number (values
+// far from zero have scales far below them): a key or value must not lose its bits to a louder one that the row does not see, or turns
+// away from.  There each key's own power of two acts on its score.  Rows far from zero (|zero| > 900) are made in float32.
 // Channels lie in the order 0 4 1 5 2 6 3 7 of each eight, as the masks leave them: the queries are stored alike and the output
 // is put right at the end.
 
@@ -574,7 +574,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 const uint32_t pieces = s_pieces[rs];
                 float2* prm = reinterpret_cast<float2*>(s_rawp + ((j - j0) & 1) * S::RAWP);
                 float2 kp[4], vp[4];
-                int hi = -1000, lo = 1000, khi = -1000, klo = 1000;
+                int hi = -1000, lo = 1000, vlo = 1000, khi = -1000, klo = 1000;
                 float kround[4];                           // what of a key is rounded to fp16: its scale, or (far from zero) its values
                 uint32_t goods = 0, everywhere = 0xffffffffu;
 #pragma unroll
@@ -599,6 +599,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                         const int ex = largest < 1.2e24f ? max(int(__float_as_uint(largest) >> 23) - 127, -80) : 1000;   // 2^80: the logarithm's cut
                         hi = max(hi, ex);
                         lo = min(lo, ex);
+                        if (ex > -80 && !is_far(vp[i].y)) vlo = min(vlo, int(__float_as_uint(fabsf(vp[i].x)) >> 23) - 127);
                     }
                     const uint32_t there = __ballot_sync(0xffffffffu, good);
                     everywhere &= there;
@@ -606,10 +607,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 }
                 hi = __reduce_max_sync(0xffffffffu, hi);
                 lo = __reduce_min_sync(0xffffffffu, lo);
+                vlo = __reduce_min_sync(0xffffffffu, vlo);
                 khi = __reduce_max_sync(0xffffffffu, khi);
                 klo = __reduce_min_sync(0xffffffffu, klo);
                 const int ek = khi < -900 ? 0 : min(max(khi, -120), 120);
-                const bool bare = hi > 900 || hi - lo > 10 || klo < ek - 14;                  // (none at all: -1000 and 1000)
+                const bool bare = hi > 900 || hi - lo > 10 || vlo < hi - 14 || klo < ek - 14;      // (none at all: -1000 and 1000)
                 const int e = bare || hi < -900 ? 0 : hi;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {

@@ -68,3 +68,27 @@ def test_keys_of_every_size(causal, d):
     want = kv_bounds.expect(layer_of(cache), table, lens, start, q, d ** -0.5, causal)
     got, lse = attend(cache, 0, q, batch, d ** -0.5, causal)
     kv_bounds.check(got, lse, want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("zero", [3, 60, 200, 400, 800, 899])
+@pytest.mark.parametrize("apart", [1.02, 1.9, 8.0, 100.0])
+def test_quiet_values_far_from_zero_beside_loud_ones(apart, zero, d):
+    """Values up to nearly 2^11 apart in one tile of the tensor-core kernel, zero-points up to where it takes them as they are: rows whose
+    weight lies on quiet tokens have their values with the bits that a scale has in fp16.  The quiet scale lies between two
+    subnormal fp16 numbers when it is counted in the loud values' power of two."""
+    lens, news, page, heads, group = [400, 150], [150, 100], 64, 2, 4
+    table = make_table(np.random.RandomState(65), lens, page, 11)
+    cache = random_cache(65, 1, 11, heads, page, d)
+    batch, start = batch_of(table, lens, news)
+    g = torch.Generator(device=G.DEV); g.manual_seed(65)
+    cache.v_param[..., 1] = -zero
+    loud = torch.rand(cache.v_param.shape[:-1], generator=g, device=G.DEV) < 0.2
+    power = int(np.floor(np.log2(zero + 15)))                # of the loudest value: their scale is 1
+    quiet = (np.floor(apart * 16384 / (zero + 15)) + 0.45) * 2.0 ** (power - 24)
+    cache.v_param[..., 0] = torch.where(loud, 1.0, quiet)
+    cache.k_param[..., 1] = torch.where(loud, 20.0, cache.k_param[..., 1])   # queries above zero turn away from the loud tokens
+    q = queries(66, batch.rows, heads * group, d).abs()
+    want = kv_bounds.expect(layer_of(cache), table, lens, start, q, d ** -0.5, True)
+    got, lse = attend(cache, 0, q, batch, d ** -0.5, True)
+    kv_bounds.check(got, lse, want)
