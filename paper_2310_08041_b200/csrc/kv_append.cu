@@ -36,6 +36,13 @@ __device__ __forceinline__ uint32_t codes8(const float (&f)[8], float lo, float 
     return p;
 }
 
+// The smaller one, NaN if either is: a row's NaN reaches its scale and zero-point through its minimum, and the row reads back as NaN.
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 constexpr int kMostTokens = 32;                            // of a CTA
 
 // A CTA's run of tokens.  Its row units are ordered [token][keys, values][head].
@@ -126,10 +133,10 @@ kv_append_kernel(const T* __restrict__ k, int64_t k_stride, const T* __restrict_
             if (base + u * G >= units) break;              // the whole CTA is done
             float lo = f[u][0][0], hi = lo;
 #pragma unroll
-            for (int j = 1; j < 16; ++j) { lo = fminf(lo, f[u][j >> 3][j & 7]); hi = fmaxf(hi, f[u][j >> 3][j & 7]); }
+            for (int j = 1; j < 16; ++j) { lo = min_nan(lo, f[u][j >> 3][j & 7]); hi = fmaxf(hi, f[u][j >> 3][j & 7]); }
 #pragma unroll
             for (int o = L / 2; o > 0; o >>= 1) {
-                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+                lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
                 hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
             }
             const int2 at = tok[u] < 0 ? make_int2(-1, 0) : s_place[tok[u]];

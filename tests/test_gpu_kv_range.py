@@ -92,3 +92,32 @@ def test_quiet_values_far_from_zero_beside_loud_ones(apart, zero, d):
     want = kv_bounds.expect(layer_of(cache), table, lens, start, q, d ** -0.5, True)
     got, lse = attend(cache, 0, q, batch, d ** -0.5, True)
     kv_bounds.check(got, lse, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_a_row_with_nan_reads_back_as_nan(dtype, d):
+    """One NaN anywhere in a key or value row, and the row is NaN when it is read and in the attention of every token that sees it; rows
+    beside it, of the same token too, are as without it."""
+    heads, page, n = 2, 16, 40
+    cache = B.KvCache.empty(1, 4, heads, page, d)
+    batch, start = batch_of(np.array([[2, 0, 3]]), [n], [n])
+    g = torch.Generator(device=G.DEV); g.manual_seed(71)
+    x = torch.randn(n, 2, heads, d, generator=g, device=G.DEV).to(DT[dtype])
+    B.qllm_kv_append(cache, 0, x[:, 0], x[:, 1], batch)
+    clean = torch.empty_like(x)
+    B.qllm_kv_read(cache, 0, clean[:, 0], clean[:, 1], batch)
+    bad = torch.zeros(n, 2, heads, dtype=torch.bool, device=G.DEV)
+    for i, (t, kv, h) in enumerate([(0, 0, 0), (7, 1, 1), (21, 0, 1), (21, 1, 0), (39, 1, 0)]):
+        x[t, kv, h, (17 * i + d - 1) % d] = float("nan") if i % 2 else -float("nan")
+        bad[t, kv, h] = True
+    B.qllm_kv_append(cache, 0, x[:, 0], x[:, 1], batch)
+    back = torch.empty_like(x)
+    B.qllm_kv_read(cache, 0, back[:, 0], back[:, 1], batch)
+    assert torch.isnan(back[bad]).all() and torch.equal(back[~bad], clean[~bad])
+    q = torch.randn(n, 2 * heads, d, generator=g, device=G.DEV).to(DT[dtype])
+    got, lse = attend(cache, 0, q, batch, 0.1, True)
+    first = torch.where(bad.any(1), torch.arange(n, device=G.DEV)[:, None], n).amin(0)          # per key head
+    sees = torch.arange(n, device=G.DEV)[:, None] >= first[None]
+    sees = sees.repeat_interleave(2, 1)
+    assert torch.isnan(got[sees].float()).all() and torch.isfinite(got[~sees].float()).all()
