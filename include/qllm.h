@@ -428,7 +428,8 @@ typedef struct qllm_kv_batch {
 /* Quantizes the new tokens' keys and values and stores them at their positions.  A row is quantized as by
  * qllm_quantize_rows(bits = 4) on its head_dim channels, x / alpha taken as the exact product of x with the float32 reciprocal
  * of alpha and rounded once (as that call's one-pass kernels do; its kernel for other channel counts rounds the product to
- * float32 first, which can differ where a quotient lies within a float32 rounding of a tie).  k, v: device, QLLM_F32 or
+ * float32 first, which can differ where a quotient lies within a float32 rounding of a tie).  Scales are 2^-127 at
+ * least, whose reciprocal float32 still holds (qllm_quantize_rows has no such limit).  k, v: device, QLLM_F32 or
  * QLLM_BF16 (dtype).  A row holding an infinity has no finite scale and reads back as infinities and NaN; a row holding a NaN
  * reads back as NaN (qllm_quantize_rows ignores NaN when it takes a row's range).  Pages that receive tokens must belong to one
  * position of one sequence. */

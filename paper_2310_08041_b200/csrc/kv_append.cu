@@ -43,6 +43,9 @@ __device__ __forceinline__ float min_nan(float a, float b) {
     return r;
 }
 
+// The least scale: its reciprocal is still a float32 number, that of 2^-128 is infinite.
+constexpr float kLeastScale = 0x1p-127f;
+
 constexpr int kMostTokens = 32;                            // of a CTA
 
 // A CTA's run of tokens.  Its row units are ordered [token][keys, values][head].
@@ -143,6 +146,7 @@ kv_append_kernel(const T* __restrict__ k, int64_t k_stride, const T* __restrict_
             if (at.x >= 0) {
                 float alpha = fifteenth(hi - lo);
                 if (!(hi > lo)) alpha = lo != 0.f ? fabsf(lo) : 1.f;
+                if (alpha < kLeastScale) alpha = kLeastScale;                // (not for NaN)
                 const float inv = __frcp_rn(alpha), zero = -rintf(lo * inv);
                 const bool keys = w[u] < c.heads;
                 const int64_t row = c.row(at.x, keys ? w[u] : w[u] - c.heads, at.y);

@@ -121,3 +121,43 @@ def test_a_row_with_nan_reads_back_as_nan(dtype, d):
     sees = torch.arange(n, device=G.DEV)[:, None] >= first[None]
     sees = sees.repeat_interleave(2, 1)
     assert torch.isnan(got[sees].float()).all() and torch.isfinite(got[~sees].float()).all()
+
+
+TINY = 2.0 ** -127
+
+
+def tiny_rows(d):
+    """Rows whose range, or whose only value, is too small for a float32 reciprocal; some far from zero for it, some at its border."""
+    g = torch.Generator().manual_seed(72)
+    u = torch.rand(16, d, generator=g, dtype=torch.float64)
+    rows = [u[0] * 1e-39, u[1] * 1e-39 - 5e-40, -u[2] * 1e-39, torch.full((d,), 1e-40), torch.full((d,), -1e-40), torch.full((d,), 2.0 ** -149),
+            (u[3] < 0.5) * 2.0 ** -149, 1e-37 + u[4] * 2e-38, 1e-33 + (u[5] < 0.1) * 1e-40, -1e-31 - (u[6] < 0.1) * 1e-38, u[7] * 15 * TINY,
+            u[8] * 14.9 * 2 * TINY, u[9] * 1e-30, torch.zeros(d), torch.full((d,), 2.0 ** -126), torch.full((d,), -3e-38)]
+    return torch.stack([r.double() for r in rows]).float()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_rows_whose_range_has_no_reciprocal(dtype, d):
+    """Underflowed rows are finite data: they read back within half a step, a step being a fifteenth of the range or 2^-127 where that
+    is larger, and attention over them is finite."""
+    x = tiny_rows(d).to(DT[dtype]).to(G.DEV)
+    n, heads, page = x.shape[0], 1, 16
+    cache = B.KvCache.empty(1, 3, heads, page, d)
+    batch, start = batch_of(np.array([[1]]), [n], [n])
+    rows = x[:, None].contiguous()
+    B.qllm_kv_append(cache, 0, rows, rows.flip(0).contiguous(), batch)
+    k, v = torch.empty_like(rows, dtype=torch.float32), torch.empty_like(rows, dtype=torch.float32)
+    B.qllm_kv_read(cache, 0, k, v, batch)
+    x64 = x.double()
+    # half a step; the zero-point and the quotient are float32 numbers, off by 2^-23 of a row far from zero each, as is the range's step
+    step = ((x64.amax(-1) - x64.amin(-1)) / 15).clamp(min=TINY)[:, None]
+    step = torch.where((x64.amax(-1) == x64.amin(-1))[:, None], TINY, step)                     # a constant row is its own scale
+    tol = step * (0.5 + 2.0 ** -20) + 2.0 ** -21 * x64.abs() + 2.0 ** -148
+    assert torch.isfinite(k).all() and ((k[:, 0].double() - x64).abs() <= tol).all()
+    assert torch.equal(v, k.flip(0))
+    q = torch.randn(n, 4 * heads, d, device=G.DEV).to(DT[dtype])
+    got, lse = attend(cache, 0, q, batch, 0.1, True)
+    ref = kv_ref.attention(store_of(cache, 0), np.array([[1]]), [n], start, host(q), 0.1, True)
+    # all values lie below 2e-31, and weights of values so far below the row of zeros, whose scale is 1, may count as nothing
+    assert (np.abs(host(got) - ref[0]) <= 1e-30).all() and np.abs(host(lse) - ref[1]).max() < 1e-4
