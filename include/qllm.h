@@ -425,14 +425,17 @@ typedef struct qllm_kv_batch {
     int     max_new;
 } qllm_kv_batch_t;
 
-/* Quantizes the new tokens' keys and values and stores them at their positions.  A row is quantized as by
- * qllm_quantize_rows(bits = 4) on its head_dim channels, x / alpha taken as the exact product of x with the float32 reciprocal
- * of alpha and rounded once (as that call's one-pass kernels do; its kernel for other channel counts rounds the product to
- * float32 first, which can differ where a quotient lies within a float32 rounding of a tie).  Scales are 2^-127 at
- * least, whose reciprocal float32 still holds (qllm_quantize_rows has no such limit).  k, v: device, QLLM_F32 or
- * QLLM_BF16 (dtype).  A row holding an infinity has no finite scale and reads back as infinities and NaN; a row holding a NaN
- * reads back as NaN (qllm_quantize_rows ignores NaN when it takes a row's range).  Pages that receive tokens must belong to one
- * position of one sequence. */
+/* Quantizes the new tokens' keys and values and stores them at their positions.  k, v: device, QLLM_F32 or QLLM_BF16 (dtype).
+ * A row is quantized as by qllm_quantize_rows(bits = 4) on its head_dim channels, x / alpha taken as the exact product of x with
+ * the float32 reciprocal of alpha and rounded once (as that call's one-pass kernels do; its kernel for other channel counts
+ * rounds the product to float32 first, which can differ where a quotient lies within a float32 rounding of a tie), but for rows
+ * that it has no good answer for:
+ *   - scales are 2^-127 at least, whose reciprocal float32 still holds;
+ *   - a finite row has a finite scale, also where its range passes float32, and where a rounded zero-point would put one of its
+ *     values beyond the type, the zero-point is the quotient itself;
+ *   - a row holding a NaN reads back as NaN.
+ * A row holding an infinity has no finite scale and reads back as infinities and NaN.  Pages that receive tokens must belong to
+ * one position of one sequence. */
 int qllm_kv_append(const qllm_kv_cache_t* cache, int layer, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                    int dtype, const qllm_kv_batch_t* batch, void* stream);
 

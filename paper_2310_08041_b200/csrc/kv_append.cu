@@ -100,6 +100,20 @@ __device__ __forceinline__ float fifteenth(float x) {
     return x > 1e-30f && x < 1e38f ? fmaf(fmaf(-15.f, q, x), 1.f / 15.f, q) : x / 15.f;
 }
 
+// A finite row with values near the end of its type: where a rounded zero-point would put the row's first or last value beyond the type,
+// the zero-point is the quotient itself, both ends a little inside the row's (2^-20: float32 roundings cannot take them out again).
+// The row is moved by the zero-point's fraction instead, at half its size, so that its codes follow as from a rounded one.
+__device__ __forceinline__ void fit_range(float (&f)[2][8], float lo, float hi, float& alpha, float& inv, float& zero) {
+    if (alpha == INFINITY || fmaxf(zero, rintf(hi * inv)) * alpha <= 3.38953139e38f) return;     // bf16's largest number
+    alpha *= 1.f - 0x1p-20f;
+    inv = __frcp_rn(alpha);
+    zero = -lo * inv * (1.f - 0x1p-21f);
+    const float by = 0.5f * (zero - truncf(zero)) * alpha;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) f[j >> 3][j & 7] = fmaf(0.5f, f[j >> 3][j & 7], by);
+    inv *= 2.f;
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
 kv_append_kernel(const T* __restrict__ k, int64_t k_stride, const T* __restrict__ v, int64_t v_stride, Cache c, Batch b, Run run, int* status) {
@@ -144,10 +158,12 @@ kv_append_kernel(const T* __restrict__ k, int64_t k_stride, const T* __restrict_
             }
             const int2 at = tok[u] < 0 ? make_int2(-1, 0) : s_place[tok[u]];
             if (at.x >= 0) {
-                float alpha = fifteenth(hi - lo);
+                const bool wide = hi - lo == INFINITY;     // a finite row's scale is finite all the same
+                float alpha = fifteenth(wide ? 0.5f * hi - 0.5f * lo : hi - lo) * (wide ? 2.f : 1.f);
                 if (!(hi > lo)) alpha = lo != 0.f ? fabsf(lo) : 1.f;
                 if (alpha < kLeastScale) alpha = kLeastScale;                // (not for NaN)
-                const float inv = __frcp_rn(alpha), zero = -rintf(lo * inv);
+                float inv = __frcp_rn(alpha), zero = -rintf(lo * inv);
+                if (alpha > 0x1p120f) fit_range(f[u], lo, hi, alpha, inv, zero);
                 const bool keys = w[u] < c.heads;
                 const int64_t row = c.row(at.x, keys ? w[u] : w[u] - c.heads, at.y);
                 reinterpret_cast<uint2*>((keys ? c.kc : c.vc) + row * (D / 2))[lane] =

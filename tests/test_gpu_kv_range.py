@@ -161,3 +161,56 @@ def test_rows_whose_range_has_no_reciprocal(dtype, d):
     ref = kv_ref.attention(store_of(cache, 0), np.array([[1]]), [n], start, host(q), 0.1, True)
     # all values lie below 2e-31, and weights of values so far below the row of zeros, whose scale is 1, may count as nothing
     assert (np.abs(host(got) - ref[0]) <= 1e-30).all() and np.abs(host(lse) - ref[1]).max() < 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_rows_whose_range_passes_the_largest_float(dtype, d):
+    """hi - lo beyond float32 is still finite data: its fifteenth is a float32 number, and the row reads back within half of it."""
+    g = torch.Generator(device=G.DEV); g.manual_seed(73)
+    n, page = 12, 16
+    x = (torch.rand(n, 1, d, generator=g, device=G.DEV) * 2 - 1) * 3.3e38
+    x[:, 0, 0], x[:, 0, d - 1] = 3.3e38, -3.3e38
+    x[1] = x[1].sign() * 3.3e38
+    x[2, 0, 0] = 1e38                                        # -3.3e38 .. 3.3e38 at one end only
+    x[3, 0] = torch.where(x[3, 0] < 0, -3.38e38, 0.5e38)
+    x = x.to(DT[dtype])
+    cache = B.KvCache.empty(1, 3, 1, page, d)
+    batch, start = batch_of(np.array([[2]]), [n], [n])
+    B.qllm_kv_append(cache, 0, x, x, batch)
+    k, v = torch.empty(n, 1, d, device=G.DEV), torch.empty(n, 1, d, device=G.DEV)
+    B.qllm_kv_read(cache, 0, k, v, batch)
+    x64 = x.double()
+    step = (x64.amax(-1, keepdim=True) - x64.amin(-1, keepdim=True)) / 15
+    # the values themselves may pass the largest float32 by the rounding of their step: no infinity may come out of that
+    assert torch.isfinite(k).all() and torch.equal(k, v)
+    assert ((k.double() - x64).abs() <= step * (0.5 + 2.0 ** -20) + 2.0 ** -21 * x64.abs()).all()
+    # an infinity still has no finite scale
+    x[5, 0, 3] = float("inf")
+    B.qllm_kv_append(cache, 0, x, x, batch)
+    B.qllm_kv_read(cache, 0, k, v, batch)
+    assert not torch.isfinite(k[5]).any() and torch.isfinite(k[4]).all() and torch.isfinite(k[6]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_beside_the_largest_float(dtype):
+    """Rows that lie at one end of float32, far from zero for their range or not: finite, within half a step."""
+    g = torch.Generator(device=G.DEV); g.manual_seed(74)
+    ends = [(3.0e38, 3.38e38), (-3.38e38, -3.0e38), (2.0e38, 3.38e38), (-3.38e38, 1e30), (-1e38, 3.38e38), (3.3e38, 3.38e38), (-3.38e38, 3.1e38), (0.0, 3.38e38)]
+    n, d = len(ends), 128
+    x = torch.rand(n, 1, d, generator=g, device=G.DEV)
+    for i, (lo, hi) in enumerate(ends):
+        x[i] = lo * (1 - x[i]) + hi * x[i]
+        x[i, 0, 5], x[i, 0, 77] = lo, hi
+    x = x.to(DT[dtype])
+    cache = B.KvCache.empty(1, 3, 1, 16, d)
+    batch, start = batch_of(np.array([[1]]), [n], [n])
+    B.qllm_kv_append(cache, 0, x, x, batch)
+    k, v = torch.empty_like(x), torch.empty_like(x)
+    B.qllm_kv_read(cache, 0, k, v, batch)
+    x64 = x.double()
+    step = (x64.amax(-1, keepdim=True) - x64.amin(-1, keepdim=True)) / 15
+    assert torch.isfinite(k).all() and torch.equal(k, v)
+    # half a step, float32 roundings of scale, zero-point and value, and the value's rounding to the type
+    tol = step * (0.5 + 2.0 ** -20) + x64.abs() * (2.0 ** -20 + torch.finfo(x.dtype).eps) + step * torch.finfo(x.dtype).eps
+    assert ((k.double() - x64).abs() <= tol).all()
