@@ -470,8 +470,10 @@ int qllm_kv_attention(const qllm_kv_cache_t* cache, int layer, const void* q, in
  *   seq_lens  device int32 [seqs]; 0 = the sequence is unused
  * pool->pages equals cache->pages (QLLM_ERR_SHAPE).  A program starts from refs = 0, table = -1, seq_lens = 0.  Pages are taken lowest free index first, in list order, so results
  * do not depend on timing.  seqs <= 8192 and lists of at most 8192 entries (QLLM_ERR_UNSUPPORTED).  The calls change the pool
- * on the device; an entry that cannot be served (an index out of range, too few free pages, no room in the table) changes
- * nothing, the others are served, and the status word becomes QLLM_ERR_PAGE.  Calls on one pool must be ordered (one stream). */
+ * on the device; an entry that cannot be served (an index out of range, too few free pages, no room in the table, for a fork a parent's
+ * page that does not exist) changes nothing, the others are served, and the status word becomes QLLM_ERR_PAGE.  Freeing and
+ * compacting report a page that does not exist in a table they walk: the first forgets it with its sequence, the second leaves
+ * it in its place.  Calls on one pool must be ordered (one stream). */
 typedef struct qllm_kv_pool {
     int32_t* refs;
     int32_t* table;
