@@ -225,6 +225,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 }
 __device__ __forceinline__ float2 unpack2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 __device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }     // -126 <= e <= 127
+// 2^e for any e
+__device__ __forceinline__ float pow2(int e) { return pow2i(min(max(e, -126), 127)) * (e < -126 ? pow2i(max(e + 126, -126)) : 1.f); }
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ptx::smem_addr(dst)),
                  "l"(src), "r"(bytes), "r"(ptx::smem_addr(bar))
@@ -250,9 +252,12 @@ __device__ __forceinline__ uint32_t codes2(uint32_t w, bool upper) {
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// The query row of column `r` as B operands; what a unit of the sums made with them stands for, and the row's sum in those units.
+// The query row of column `r` as B operands.  2^(e + kUnit) is what a unit of the sums made with them stands for, `ratio` the row's sum
+// in those units (NaN for a row that is not finite).
+template <bool F32>
+constexpr int kUnit = F32 ? -13 : 11;                      // 2^(e - 13), times 2^24 for the codes of a bf16 call
 template <typename QT, int D, bool F32>
-__device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi)[D / 8], uint32_t (&lo)[F32 ? D / 8 : 1], float& unit, float& ratio) {
+__device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi)[D / 8], uint32_t (&lo)[F32 ? D / 8 : 1], int& e, float& ratio) {
     constexpr int N = D / 4;                               // channels of this lane: N t .. N t + N - 1
     float top = 0.f, sum = 0.f;
     if (row) {
@@ -261,18 +266,13 @@ __device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi
             float f[8];
             load8<QT>(row + t * N + 8 * i, f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { top = fmaxf(top, fabsf(f[j])); sum += f[j]; }
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[j]));
         }
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    const int e = max(int(__float_as_uint(top) >> 23) - 127, -100);      // 2^e <= top < 2^(e+1); infinities: 128
-    const float up = pow2i(min(13 - e, 126));
-    constexpr int kUnit = F32 ? -13 : 11;                  // what one unit of an MMA sum stands for: 2^(e - 13), times 2^24
-    unit = e > 115 ? INFINITY : pow2i(e + kUnit);
-    ratio = e > 115 ? NAN : sum * pow2i(-e - kUnit);
+    e = max(int(__float_as_uint(top) >> 23) - 127, -100);                // 2^e <= top < 2^(e+1); infinities: 128
+    const float up = pow2i(13 - e);
 #pragma unroll
     for (int i = 0; i < N / 8; ++i) {
         float f[8];
@@ -280,7 +280,11 @@ __device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi
         for (int j = 0; j < 8; ++j) f[j] = 0.f;
         if (row) load8<QT>(row + t * N + 8 * i, f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] *= (j & 1) && !F32 ? up * 0.0625f : up;
+        for (int j = 0; j < 8; ++j) {
+            f[j] *= up;                                    // (summed at this size: the sum of large queries may pass float32)
+            sum += f[j];
+            if ((j & 1) && !F32) f[j] *= 0.0625f;
+        }
         // word 8i of the codes gives the pairs (0, 4), (1, 5) x 16, (2, 6), (3, 7) x 16
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -292,6 +296,9 @@ __device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi
             }
         }
     }
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    ratio = e > 127 ? NAN : sum * pow2i(-13 - kUnit<F32>);
 }
 
 template <int W>
@@ -312,15 +319,16 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
 template <int D, int NT, bool F32>
 struct State {
     uint32_t qh[NT][D / 8], ql[NT][F32 ? D / 8 : 1];       // queries of column r as B operands
-    float qn[NT][2], qr[NT][2];                            // factor of the key sums (into base 2), sum of the query in their units
+    float qn[NT][2], qr[NT][2];                            // factor of the scores (into base 2), sum of the query in the units of its key sums
     int limit[NT][2];                                      // keys that the column sees
     float o[NT][D / 16][4], top[NT][2], l[NT][2], zs[NT][2];
 };
 
-// 32 tokens, from `first` on.  MASKED: some are hidden from some column, or not there.
+// 32 tokens, from `first` on.  key_unit: what the key scales are multiplied by, the part of the columns' factors that float32 would not
+// hold in qn.  MASKED: some tokens are hidden from some column, or not there.
 template <int D, int NT, bool F32, bool MASKED>
-__device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, const uint8_t* vc, const float2* kp, int first, int len,
-                                     uint32_t there, int r, int t) {
+__device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, const uint8_t* vc, const float2* kp, float key_unit,
+                                     int first, int len, uint32_t there, int r, int t) {
     constexpr int KW = D / 32, MT = D / 16;
     constexpr float kCentre = F32 ? 8.f : 0.f;             // what the operands have taken off the keys' codes
     float s[NT][2][4], s2[NT][2][4];                       // two chains of MMAs each: their latency bounds a warp
@@ -365,7 +373,9 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int tok = b * 16 + h * 8 + r;
-            const float2 kk = kp[tok], vv = kp[T + tok];
+            float2 kk = kp[tok];
+            const float2 vv = kp[T + tok];
+            kk.x *= key_unit;
             vs[b][h] = vv.x;
             vz[b][h] = vv.y - 8.f;
             if constexpr (F32) {
@@ -590,28 +600,38 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
 
     // -------------------------------------------------------------------- consumers
     const int r = lane >> 2, t = lane & 3;
+    const int scale_e = int(__float_as_uint(scale) >> 23 & 255u) - 126;      // |scale| log2 e < 2^(scale_e + 1)
     bool ok = true;                                        // false: a wait ran out; go through the motions without waiting
     while (walk.next(it)) {
         State<D, NT, F32> st;
-        int low = 0x7fffffff;                              // the fewest keys that a column sees
+        int low = 0x7fffffff, top_e = -100, e[NT];         // the fewest keys that a column sees, the largest query's exponent
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
             const unsigned rr = unsigned(it.qt) * R + a * 8 + r, i = rr / unsigned(p.group);
             const bool real = int(i) < it.n;
             const QT* row = real ? q + (it.row0 + i) * q_stride + (int64_t(it.g) * p.group + (rr - i * p.group)) * D : nullptr;
-            float unit, ratio;
-            load_queries<QT, D, F32>(row, t, st.qh[a], st.ql[a], unit, ratio);
+            float ratio;
+            load_queries<QT, D, F32>(row, t, st.qh[a], st.ql[a], e[a], ratio);
+            if (e[a] <= 127) top_e = max(top_e, e[a]);
             const int lim = !real ? 0x7fffffff : !causal ? it.len : max(it.len - it.n + int(i) + 1, 0);
             low = min(low, lim);
-            unit *= scale * 1.4426950408889634f;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {                  // column 2t + e is lane group 2t + e
-                st.qn[a][e] = __shfl_sync(0xffffffffu, unit, (2 * t + e) * 4);
                 st.qr[a][e] = __shfl_sync(0xffffffffu, ratio, (2 * t + e) * 4);
                 st.limit[a][e] = __shfl_sync(0xffffffffu, lim, (2 * t + e) * 4);
             }
         }
         low = __reduce_min_sync(0xffffffffu, low);
+        // the largest query's factor stays below 2^65, what is above goes to the keys (nothing but for queries of 2^50 and more): left
+        // in qn it would pass float32 for the largest queries, and the keys that such queries can have would make subnormal scores
+        const int lift = min(max(__reduce_max_sync(0xffffffffu, top_e) + kUnit<F32> + scale_e - 64, 0), 126);
+        const float key_unit = pow2i(lift);
+#pragma unroll
+        for (int a = 0; a < NT; ++a) {
+            const float unit = pow2(e[a] + kUnit<F32> - lift) * (scale * 1.4426950408889634f);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) st.qn[a][x] = __shfl_sync(0xffffffffu, unit, (2 * t + x) * 4);
+        }
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
 #pragma unroll
@@ -632,12 +652,12 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
             const int first = j * T + warp * 32;           // token of this warp's row 0
             const uint32_t pieces = s_pieces[sg];
             if (first + 32 <= low && pieces == all_pieces) {
-                step<D, NT, F32, false>(st, kc, vc, kp, first, it.len, 15u, r, t);
+                step<D, NT, F32, false>(st, kc, vc, kp, key_unit, first, it.len, 15u, r, t);
             } else if (first < it.keys) {
                 uint32_t there = 0;                        // which 8-token blocks of the 32 tokens lie in pages that exist
 #pragma unroll
                 for (int b8 = 0; b8 < 4; ++b8) there |= ((pieces >> (4 * ((warp * 32 + b8 * 8) >> piece_log2))) & 1u) << b8;
-                step<D, NT, F32, true>(st, kc, vc, kp, first, it.len, there, r, t);
+                step<D, NT, F32, true>(st, kc, vc, kp, key_unit, first, it.len, there, r, t);
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&s_empty[sg]);

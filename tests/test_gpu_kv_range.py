@@ -214,3 +214,23 @@ def test_rows_beside_the_largest_float(dtype):
     # half a step, float32 roundings of scale, zero-point and value, and the value's rounding to the type
     tol = step * (0.5 + 2.0 ** -20) + x64.abs() * (2.0 ** -20 + torch.finfo(x.dtype).eps) + step * torch.finfo(x.dtype).eps
     assert ((k.double() - x64).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news", [[1, 1], [5, 2], [70, 130]])
+@pytest.mark.parametrize("power", [100, 114, 115, 116, 117, 120, 125, 127])
+def test_queries_near_the_end_of_their_type(power, news, dtype):
+    """Finite queries of up to 2^128 against keys so small that the scores are ordinary; beside them, in the same calls, rows of ordinary
+    size, whose scores vanish."""
+    lens, page, heads, group, d = [300, 140], 64, 2, 4, 128
+    table = make_table(np.random.RandomState(75), lens, page, 9)
+    cache = random_cache(75, 1, 9, heads, page, d)
+    cache.k_param[..., 0] *= 2.0 ** -(power - 1)
+    batch, start = batch_of(table, lens, news)
+    q = torch.randn(batch.rows, heads * group, d, device=G.DEV).clamp(-3.9, 3.9)
+    q[:, 1::2] *= 2.0 ** (power - 2)
+    q = q.to(DT[dtype])
+    got, lse = attend(cache, 0, q, batch, 0.09, True)
+    ref = kv_ref.attention(store_of(cache, 0), table, lens, start, host(q), 0.09, True)
+    check_attention(got, lse, ref, DT[dtype], prompt=dtype == "bf16" and max(news) * group > 96)
+    assert B.qllm_poll_status() == B.QLLM_OK
