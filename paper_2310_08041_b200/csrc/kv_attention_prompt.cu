@@ -14,7 +14,8 @@
 // packed fp16 operation makes it the exact integer c - zero, another the operand (c - zero) scale 2^-E, E the exponent of the
 // tile's largest key or value: rounded to fp16 in the scale and in the product, 11 bits each, where keys and values of 16 bits
 // would carry 8.  So nothing acts per score and token: a score's factor is the row's times 2^E, a weight is p 2^E.  Queries are
-// scaled per row by a power of two into fp16 (a bf16 query's 8 bits are kept).  Tiles whose value scales differ by more than
+// scaled per row by a power of two into fp16 (a bf16 query's 8 bits are kept); the scale's mantissa goes to the
+// keys (split_scale).  Tiles whose value scales differ by more than
 // 2^10, or pass 2^80, keep the values' bare codes and multiply the weights by vs instead, since a weight of a small value must
 // not lose its bits to a large value that the row hardly looks at.  So do tiles in which some scale 2^-E is no normal fp16 number (values
 // far from zero have scales far below them): a key or value must not lose its bits to a louder one that the row does not see, or turns
@@ -380,6 +381,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
         j0 = int(int64_t(all) * blockIdx.y / a.splits);
         j1 = int(int64_t(all) * (blockIdx.y + 1) / a.splits);
     }
+    int scale_e;
+    const float scale_m = split_scale(a.scale, scale_e);
     const Abort ab{&s_abort, a.status};
     if (warp == 21) {
         ptx::tmem_alloc(&s_tmem, 512);
@@ -426,13 +429,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
 #pragma unroll
                 for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
                 const int e = max(int(__float_as_uint(m) >> 23) - 127, -100);
-                const float up = pow2i(13 - e) * (a.scale < 0.f ? -1.f : 1.f);
+                const float up = pow2i(13 - e) * (scale_m < 0.f ? -1.f : 1.f);
                 uint32_t h[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) h[k] = bits(__floats2half2_rn(f[k] * up, f[k + 4] * up));
                 const int rl = r & (BM - 1);
                 sts4(ptx::smem_addr(s_q) + (r / BM) * S::OP + rl * 128 + (c >> 3) * S::ATOM + (((c & 7) ^ (rl & 7)) << 4), make_uint4(h[0], h[1], h[2], h[3]));
-                if (c == 0) s_half[r / BM][0][rl] = fmaxf(pow2i(e - 13) * fabsf(a.scale) * 1.4426950408889634f, 1e-37f);   // not 0: it meets the -infinity of masks
+                if (c == 0) s_half[r / BM][0][rl] = pow2i(min(max(e - 13 + scale_e, -122), 127));          // not 0: it meets the -infinity of masks
             }
             ptx::fence_proxy_async_smem();
             __syncwarp();
@@ -445,8 +448,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
         const uint32_t lanes = uint32_t(warp & 3) << 21;                     // TMEM lane offset of this warp's rows
         const uint32_t t_s = tmem + S::TMEM_S + t * BN + half * kCols + lanes, t_o = tmem + S::TMEM_O + t * D + half * (D / 2) + lanes;
         const int stop = min(nt[t], j1);
-        float top = -INFINITY, l = 0.f;
-        bool ok = true;
+        float top = -INFINITY, over = -INFINITY, l = 0.f;                    // the reference, what a score may reach under it, the weights' sum
+        bool ok = true, larges = false;                    // some row's reference is a large score
         for (int j = j0; j < stop; ++j) {
             const int slot = (j - j0) % kSlots;
             if (ok && (!wait_bounded(&prm_full[slot], ((j - j0) / kSlots) & 1, ab) || !wait_bounded(&s_full[t], (j - j0) & 1, ab))) ok = false;
@@ -455,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
             const uint32_t flags = s_flags[slot];
             const int first = j * BN + half * kCols;
             const bool masked = j * BN + BN > low || (flags & 2), bare = flags & 1;
-            const float e = s_e[slot], qk = fminf(fmaxf(qn * s_ek[slot], 1e-37f), 3e38f);
+            const float e = s_e[slot], qk = fminf(fmaxf(qn * s_ek[slot], 0x1p-122f), 0x1p127f);
             const uint32_t vs = ptx::smem_addr(s_vs + slot * BN + half * kCols), kx = ptx::smem_addr(s_kx + slot * BN + half * kCols), there = ptx::smem_addr(&s_there[slot][2 * half]);
             float m = bare     ? half_max<true, true>(t_s, vs, kx, first, limit, there, qk)
                       : masked ? half_max<true, false>(t_s, vs, kx, first, limit, there, qk)
@@ -465,9 +468,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
             m = fmaxf(m, *other);
             if (!bare) m = fmaf(m, qk, e);
             // the reference moves only when a weight would pass 2^(kPlace + kSlack)
-            if (__any_sync(0xffffffffu, m > top + (kPlace + kSlack))) {
-                const float to = m > top + (kPlace + kSlack) ? m - kPlace : top, fix = to == top ? 1.f : ex2(top - to);
+            if (__any_sync(0xffffffffu, m > over)) {
+                const float to = m > over ? m - kPlace : top, fix = to == top ? 1.f : ex2(top - to);
                 top = to;
+                over = to + (fabsf(to) < kLargeScore ? kPlace + kSlack : kPlace);
+                larges = __any_sync(0xffffffffu, fabsf(to) >= kLargeScore && to != -INFINITY);
                 l *= fix;
                 if (j > j0) {
 #pragma unroll 1
@@ -483,9 +488,26 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                 }
             }
             const float at = top == -INFINITY ? 0.f : top;
-            if (bare) l += half_weights<true, true>(t_s, vs, kx, first, limit, there, qk, -at);
-            else l = fmaf(masked ? half_weights<true, false>(t_s, vs, kx, first, limit, there, qk, e - at)
-                                 : half_weights<false, false>(t_s, vs, kx, first, limit, there, qk, e - at), pow2i(-int(e)), l);
+            float factor = qk, sub = e - at;
+            if (larges && e != 0.f) {
+                const bool large = fabsf(at) >= kLargeScore;
+                // large scores swallow an e that is added to the reference, and with it what tiles differ in: there it comes last, in
+                // a pass of its own (in the loops of all scores it cost 4 to 8 %)
+#pragma unroll 1
+                for (int c = 0; c < kCols / 32; ++c) {
+                    uint32_t r[32];
+                    ptx::tmem_ld_32x32b_x32(t_s + 32 * c, r);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) r[k] = large ? __float_as_uint(fmaf(__uint_as_float(r[k]), qk, -at) + e) : r[k];
+                    tmem_st_x32(t_s + 32 * c, r);
+                }
+                tmem_st_wait();
+                if (large) factor = 1.f, sub = 0.f;
+            }
+            if (bare) l += half_weights<true, true>(t_s, vs, kx, first, limit, there, factor, sub);
+            else l = fmaf(masked ? half_weights<true, false>(t_s, vs, kx, first, limit, there, factor, sub)
+                                 : half_weights<false, false>(t_s, vs, kx, first, limit, there, factor, sub), pow2i(-int(e)), l);
             tmem_st_wait();
             ptx::tc_fence_before_sync();
             __syncwarp();
@@ -582,6 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const Args a) {
                     const int tok = 32 * i + lane;
                     const bool good = j * BN + tok < top_keys && ((pieces >> (tok >> piece_log2)) & 1u);
                     kp[i] = prm[tok];
+                    kp[i].x *= fabsf(scale_m);                   // (its sign is the queries')
                     vp[i] = prm[BN + tok];
                     if (!good) kp[i] = vp[i] = make_float2(0.f, 0.f);
                     goods |= uint32_t(good) << i;

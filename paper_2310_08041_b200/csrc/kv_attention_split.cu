@@ -25,7 +25,7 @@
 // So that no weight leaves fp16's range whatever the value scales are, the running maximum is that of s_j + log2 vs_j (the
 // logarithm cut to +-80; its integer part for float32), with the largest weight placed at 2^6; it moves only when a weight would
 // pass 2^14, which spares most steps the reduction over lanes and the rescaling.  Sums, maxima and zero-point corrections are
-// float32.
+// float32.  A row's factor of its scores is a power of two (split_scale).
 
 // Measured (us a call, both kernels; the bytes of the cache at the measured copy rate in brackets): one sequence of 131071
 // tokens, 64 query on 8 key heads of 128, bf16: 44 (23), of which the main kernel streams 24 at that rate, starts for 6 (plan, table,
@@ -301,6 +301,8 @@ __device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi
     ratio = e > 127 ? NAN : sum * pow2i(-13 - kUnit<F32>);
 }
 
+__device__ __forceinline__ float room(float m) { return fabsf(m) < kLargeScore ? kPlace + kSlack : kPlace; }
+
 template <int W>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
     if constexpr (W == 2) {
@@ -319,13 +321,13 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
 template <int D, int NT, bool F32>
 struct State {
     uint32_t qh[NT][D / 8], ql[NT][F32 ? D / 8 : 1];       // queries of column r as B operands
-    float qn[NT][2], qr[NT][2];                            // factor of the scores (into base 2), sum of the query in the units of its key sums
+    float qn[NT][2], qr[NT][2];                            // factor of the scores (into base 2; a power of two), sum of the query in the units of its key sums
     int limit[NT][2];                                      // keys that the column sees
     float o[NT][D / 16][4], top[NT][2], l[NT][2], zs[NT][2];
 };
 
-// 32 tokens, from `first` on.  key_unit: what the key scales are multiplied by, the part of the columns' factors that float32 would not
-// hold in qn.  MASKED: some tokens are hidden from some column, or not there.
+// 32 tokens, from `first` on.  key_unit: what the key scales are multiplied by, the mantissa of the scale and the part of the columns'
+// factors that float32 would not hold in qn.  MASKED: some tokens are hidden from some column, or not there.
 template <int D, int NT, bool F32, bool MASKED>
 __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, const uint8_t* vc, const float2* kp, float key_unit,
                                      int first, int len, uint32_t there, int r, int t) {
@@ -414,7 +416,7 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
                 }
         }
         // the reference moves only when a weight would pass 2^kSlack times its place
-        if (__any_sync(0xffffffffu, m[0] > st.top[a][0] + (kPlace + kSlack) || m[1] > st.top[a][1] + (kPlace + kSlack))) {
+        if (__any_sync(0xffffffffu, m[0] > st.top[a][0] + room(m[0]) || m[1] > st.top[a][1] + room(m[1]))) {
             float fix[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -442,7 +444,8 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
                 for (int h = 0; h < 2; ++h) {
                     // a hidden key's parameters may be anything
                     const bool gone = hidden(b, h, a, e);
-                    const float pw = gone ? 0.f : ex2(fmaf(s[a][b][2 * h + e], st.qn[a][e], F32 ? ve[b][h] - at : -at));
+                    const float x = fmaf(s[a][b][2 * h + e], st.qn[a][e], -at);
+                    const float pw = gone ? 0.f : ex2(F32 ? x + ve[b][h] : x);       // (large scores would swallow ve beside the reference)
                     const float w = gone ? 0.f : pw * vs[b][h];
                     st.l[a][e] = F32 ? fmaf(pw, down[b][h], st.l[a][e]) : st.l[a][e] + pw;
                     st.zs[a][e] = gone ? st.zs[a][e] : fmaf(w, vz[b][h], st.zs[a][e]);
@@ -600,7 +603,8 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
 
     // -------------------------------------------------------------------- consumers
     const int r = lane >> 2, t = lane & 3;
-    const int scale_e = int(__float_as_uint(scale) >> 23 & 255u) - 126;      // |scale| log2 e < 2^(scale_e + 1)
+    int scale_e;
+    const float scale_m = split_scale(scale, scale_e);
     bool ok = true;                                        // false: a wait ran out; go through the motions without waiting
     while (walk.next(it)) {
         State<D, NT, F32> st;
@@ -625,10 +629,10 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
         // the largest query's factor stays below 2^65, what is above goes to the keys (nothing but for queries of 2^50 and more): left
         // in qn it would pass float32 for the largest queries, and the keys that such queries can have would make subnormal scores
         const int lift = min(max(__reduce_max_sync(0xffffffffu, top_e) + kUnit<F32> + scale_e - 64, 0), 126);
-        const float key_unit = pow2i(lift);
+        const float key_unit = scale_m * pow2i(lift);
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
-            const float unit = pow2(e[a] + kUnit<F32> - lift) * (scale * 1.4426950408889634f);
+            const float unit = pow2(e[a] + kUnit<F32> + scale_e - lift);
 #pragma unroll
             for (int x = 0; x < 2; ++x) st.qn[a][x] = __shfl_sync(0xffffffffu, unit, (2 * t + x) * 4);
         }

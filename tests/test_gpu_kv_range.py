@@ -234,3 +234,57 @@ def test_queries_near_the_end_of_their_type(power, news, dtype):
     ref = kv_ref.attention(store_of(cache, 0), table, lens, start, host(q), 0.09, True)
     check_attention(got, lse, ref, DT[dtype], prompt=dtype == "bf16" and max(news) * group > 96)
     assert B.qllm_poll_status() == B.QLLM_OK
+
+
+def one_in_front(power, sign, page, lens, table, cache, at):
+    """Keys of one sequence all alike and one of twice their size: scores sign 2^power and, at position `at`, twice (a half, when they
+    are negative) that, for queries of ones."""
+    heads, d = cache.kv_heads, cache.head_dim
+    for s, n in enumerate(lens):
+        cache.k_codes[0] = 0x11                              # every code 1: code - zero = 1 - zero = +-1
+        cache.k_param[0, ..., 1] = 0.0 if sign > 0 else 2.0
+        cache.k_param[0, ..., 0] = 2.0 ** power / d
+        for s, n in enumerate(lens):
+            p, i = place(table, s, at % n, page)
+            cache.k_param[0, p, :, i, 0] *= 2.0 if sign > 0 else 0.5
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news", [[1, 1], [9, 3], [70, 130]])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("power", [6, 14, 20, 22, 24, 25, 26, 27, 28, 30, 36, 60, 90])
+def test_scores_of_every_size(power, sign, news, dtype):
+    """Scores whose float32 numbers lie far apart: with one key in front of the others its value comes out, with all keys alike the mean
+    of all values.  The scale's mantissa is no power of two, so no product of it is exact."""
+    lens, page, heads, group, d, scale = [700, 400], 64, 2, 4, 128, 0.7
+    table = make_table(np.random.RandomState(77), lens, page, 20)
+    cache = random_cache(77, 1, 20, heads, page, d)
+    batch, start = batch_of(table, lens, news)
+    q = torch.ones(batch.rows, heads * group, d, device=G.DEV, dtype=DT[dtype])
+    st = store_of(cache, 0)
+    eps = torch.finfo(DT[dtype]).eps
+    for at in (0, 133, 299):                                 # in front of every causal row's limit
+        one_in_front(power, sign, page, lens, table, cache, at)
+        got, lse = attend(cache, 0, q, batch, scale, False)
+        best = scale * sign * 2.0 ** power * (2 if sign > 0 else 0.5)
+        for s, n in enumerate(lens):
+            kc, kp, vc, vp = st.rows(table[s], at % n, at % n + 1)
+            v = np.repeat((vc[0] - vp[0, :, 1:2]) * vp[0, :, 0:1], group, 0)
+            rows = slice(int(start[s]), int(start[s + 1]))
+            a = host(got[rows])
+            # the weights beside it are below 2^-21 together; the value's scale and products carry 11 bits at least
+            assert np.abs(a - v[None]).max() <= (eps + 2 * 2.0 ** -11 if dtype == "bf16" else 2.0 ** -20) * np.abs(v).max(), (at, s)
+            assert np.abs(host(lse[rows]) / best - 1).max() < (2.0 ** -9 if dtype == "bf16" else 2.0 ** -20)
+    cache.k_param[0, ..., 0] = 2.0 ** power / d
+    for causal in (True, False):
+        got, lse = attend(cache, 0, q, batch, scale, causal)
+        st = store_of(cache, 0)
+        for s, n in enumerate(lens):
+            kc, kp, vc, vp = st.rows(table[s], 0, n)
+            v = np.repeat((vc - vp[..., 1:2]) * vp[..., 0:1], group, 1)
+            for i in range(news[s]):
+                m = n - news[s] + i + 1 if causal else n
+                a, want = host(got[int(start[s]) + i]), v[:m].mean(0)
+                spread = np.abs(v[:m]).mean(0)
+                assert (np.abs(a - want) <= np.abs(want) * eps + spread * (2.0 ** -9 if dtype == "bf16" else 2.0 ** -18)).all(), (causal, s, i)
+    assert B.qllm_poll_status() == B.QLLM_OK
