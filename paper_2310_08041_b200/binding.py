@@ -119,7 +119,7 @@ def _hp(a):
     return None if a is None else a.ctypes.data_as(_vp)
 
 
-_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -414,11 +414,22 @@ def _want(cond):
         raise QllmError(QLLM_ERR_SHAPE)
 
 
-def _ints(*ts):
+def _ints(device, *ts):
     for t in ts:
         if t.dtype != torch.int32:
             raise QllmError(QLLM_ERR_DTYPE)
         _dp(t)
+        _on(device, t)
+
+
+def _on(device, t):
+    assert t.get_device() == device, "device arguments must be CUDA tensors of one device"
+
+
+def _kv_stream(stream, device, other):
+    """The stream of a call whose handles (their devices are given) lie on the current device, where the library launches its kernels."""
+    assert _current_device() == device == other, "the arguments must lie on the current device"
+    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 class KvCache:
@@ -433,6 +444,9 @@ class KvCache:
         _want(tuple(k_param.shape) == tuple(v_param.shape) == (layers, pages, heads, page, 2))
         self.k_codes, self.k_param, self.v_codes, self.v_param = k_codes, k_param, v_codes, v_param
         self.layers, self.pages, self.kv_heads, self.page_size, self.head_dim = layers, pages, heads, page, 2 * half
+        self.device = k_codes.get_device()
+        for t in (k_param, v_codes, v_param):
+            _on(self.device, t)
         self._s = _KvCacheStruct(_dp(k_codes), _dp(k_param), _dp(v_codes), _dp(v_param), layers, pages, heads, page, 2 * half)
         self._p = ctypes.addressof(self._s)
 
@@ -448,9 +462,10 @@ class KvBatch:
     their contents may change between calls), rows of the packed tensors, most new tokens of a sequence."""
 
     def __init__(self, table, seq_lens, q_start, rows, max_new):
-        _ints(table, seq_lens, q_start)
+        _ints(table.get_device(), table, seq_lens, q_start)
         _want(table.dim() == 2 and seq_lens.numel() == table.shape[0] and q_start.numel() == table.shape[0] + 1)
         self.table, self.seq_lens, self.q_start, self.rows, self.max_new = table, seq_lens, q_start, rows, max_new
+        self.device = table.get_device()
         self._s = _KvBatchStruct(_dp(table), _dp(seq_lens), _dp(q_start), table.shape[0], table.shape[1], rows, max_new)
         self._p = ctypes.addressof(self._s)
 
@@ -459,9 +474,10 @@ class KvPool:
     """qllm_kv_pool_t: refs int32 [pages], table int32 [seqs][table_width], seq_lens int32 [seqs] (device tensors, kept)."""
 
     def __init__(self, refs, table, seq_lens):
-        _ints(refs, table, seq_lens)
+        _ints(refs.get_device(), refs, table, seq_lens)
         _want(table.dim() == 2 and seq_lens.numel() == table.shape[0])
         self.refs, self.table, self.seq_lens = refs, table, seq_lens
+        self.device = refs.get_device()
         self._s = _KvPoolStruct(_dp(refs), _dp(table), _dp(seq_lens), refs.numel(), table.shape[0], table.shape[1])
         self._p = ctypes.addressof(self._s)
 
@@ -472,9 +488,9 @@ class KvPool:
                    torch.zeros(seqs, dtype=torch.int32, device=device))
 
 
-def _packed(t, shape):
+def _packed(t, shape, device):
     """Address and row stride of a packed tensor [rows][heads][head_dim]: any row stride, the rest contiguous."""
-    assert t.is_cuda, "device arguments must be CUDA tensors"
+    assert t.get_device() == device, "device arguments must be CUDA tensors of one device"
     if t.shape != shape:
         raise QllmError(QLLM_ERR_SHAPE)
     row, head, one = t.stride()
@@ -486,19 +502,19 @@ def _packed(t, shape):
 def qllm_kv_append(cache, layer, k, v, batch, stream=None):
     """k, v [rows][kv_heads][head_dim] (any row stride): the batch's new tokens, quantized into the cache."""
     shape = (batch.rows, cache.kv_heads, cache.head_dim)
-    kp, ks = _packed(k, shape)
-    vp, vs = _packed(v, shape)
+    kp, ks = _packed(k, shape, cache.device)
+    vp, vs = _packed(v, shape, cache.device)
     _want(k.dtype is v.dtype)
-    _check(_lib.qllm_kv_append(cache._p, layer, kp, ks, vp, vs, _xdtype(k), batch._p, _stream(stream)))
+    _check(_lib.qllm_kv_append(cache._p, layer, kp, ks, vp, vs, _xdtype(k), batch._p, _kv_stream(stream, cache.device, batch.device)))
 
 
 def qllm_kv_read(cache, layer, k, v, batch, stream=None):
     """The stored values of the batch's tokens into k, v [rows][kv_heads][head_dim]."""
     shape = (batch.rows, cache.kv_heads, cache.head_dim)
-    kp, ks = _packed(k, shape)
-    vp, vs = _packed(v, shape)
+    kp, ks = _packed(k, shape, cache.device)
+    vp, vs = _packed(v, shape, cache.device)
     _want(k.dtype is v.dtype)
-    _check(_lib.qllm_kv_read(cache._p, layer, kp, ks, vp, vs, _xdtype(k), batch._p, _stream(stream)))
+    _check(_lib.qllm_kv_read(cache._p, layer, kp, ks, vp, vs, _xdtype(k), batch._p, _kv_stream(stream, cache.device, batch.device)))
 
 
 def qllm_kv_attention_workspace(cache, q_heads, q, batch):
@@ -514,51 +530,54 @@ def qllm_kv_attention(cache, layer, q, out, scale, batch, workspace, causal=True
     _want(q.dim() == 3)
     heads = q.shape[1]
     shape = (batch.rows, heads, cache.head_dim)
-    qp, qs = _packed(q, shape)
-    op, os_ = _packed(out, shape)
+    qp, qs = _packed(q, shape, cache.device)
+    op, os_ = _packed(out, shape, cache.device)
     _want(q.dtype is out.dtype)
     if lse is not None:
         _want(lse.dtype == torch.float32 and tuple(lse.shape) == (batch.rows, heads))
+    assert (workspace is None or workspace.get_device() == cache.device) and (lse is None or lse.get_device() == cache.device), \
+        "device arguments must be CUDA tensors of one device"
     _check(_lib.qllm_kv_attention(cache._p, layer, qp, qs, op, os_, _xdtype(q), heads, scale, 1 if causal else 0, _dp(lse),
                                   batch._p, _dp(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                  _stream(stream)))
+                                  _kv_stream(stream, cache.device, batch.device)))
 
 
 def qllm_kv_pages_extend(cache, pool, add, stream=None):
     """add: int32 [seqs], tokens to make room for."""
-    _ints(add)
+    _ints(pool.device, add)
     _want(add.numel() == pool.seq_lens.numel())
-    _check(_lib.qllm_kv_pages_extend(cache._p, pool._p, _dp(add), _stream(stream)))
+    _check(_lib.qllm_kv_pages_extend(cache._p, pool._p, _dp(add), _kv_stream(stream, cache.device, pool.device)))
 
 
 def qllm_kv_pages_fork(cache, pool, parent, child, fresh=None, stream=None):
     """parent, child: int32 [n].  Returns fresh, int32 [n] (made here when not given, which goes with the current stream only)."""
-    _ints(parent, child)
+    _ints(pool.device, parent, child)
     _want(parent.numel() == child.numel())
     if fresh is None:
         _want(stream is None)
         fresh = torch.empty_like(parent)
-    _ints(fresh)
+    _ints(pool.device, fresh)
     _want(fresh.numel() == parent.numel())
-    _check(_lib.qllm_kv_pages_fork(cache._p, pool._p, _dp(parent), _dp(child), parent.numel(), _dp(fresh), _stream(stream)))
+    _check(_lib.qllm_kv_pages_fork(cache._p, pool._p, _dp(parent), _dp(child), parent.numel(), _dp(fresh),
+                                     _kv_stream(stream, cache.device, pool.device)))
     return fresh
 
 
 def qllm_kv_pages_free(pool, seqs, stream=None):
     """seqs: int32 [n], the sequences that have ended."""
-    _ints(seqs)
-    _check(_lib.qllm_kv_pages_free(pool._p, _dp(seqs), seqs.numel(), _stream(stream)))
+    _ints(pool.device, seqs)
+    _check(_lib.qllm_kv_pages_free(pool._p, _dp(seqs), seqs.numel(), _kv_stream(stream, pool.device, pool.device)))
 
 
 def qllm_kv_pages_compact(cache, pool, remap, stream=None):
     """remap: int32 [pages], receives every page's new index (-1: free)."""
-    _ints(remap)
+    _ints(pool.device, remap)
     _want(remap.numel() == pool.refs.numel())
-    _check(_lib.qllm_kv_pages_compact(cache._p, pool._p, _dp(remap), _stream(stream)))
+    _check(_lib.qllm_kv_pages_compact(cache._p, pool._p, _dp(remap), _kv_stream(stream, cache.device, pool.device)))
 
 
 def qllm_kv_pages_copy(cache, src, dst, stream=None):
     """src, dst: int32 [n]."""
-    _ints(src, dst)
+    _ints(cache.device, src, dst)
     _want(src.numel() == dst.numel())
-    _check(_lib.qllm_kv_pages_copy(cache._p, _dp(src), _dp(dst), src.numel(), _stream(stream)))
+    _check(_lib.qllm_kv_pages_copy(cache._p, _dp(src), _dp(dst), src.numel(), _kv_stream(stream, cache.device, cache.device)))
