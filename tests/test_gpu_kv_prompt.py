@@ -65,3 +65,34 @@ def test_a_graph_writes_logarithms_and_outputs_within_the_bounds(news):
         torch.cuda.synchronize()
         kv_bounds.check(out, lse, kv_bounds.expect(layer_of(cache), table, lens, start, q, 0.09, True))
     assert B.qllm_poll_status() == B.QLLM_OK
+
+
+@pytest.mark.parametrize("seed", range(30))
+def test_random_shapes_and_ranges(seed):
+    """Calls of every shape that the tensor-core kernel takes, keys cut into parts or not, over scales that spread by up to 2^36 and
+    zero-points up to +-1200, so that its tiles take every path."""
+    rng, g = np.random.RandomState(900 + seed), torch.Generator(device=G.DEV)
+    g.manual_seed(seed)
+    d, page = int(rng.choice([64, 128])), int(rng.choice([16, 32, 64, 128, 256]))
+    heads, group, seqs = int(rng.choice([1, 2, 8])), int(rng.choice([1, 2, 3, 5, 8])), int(rng.randint(1, 4))
+    first = 96 // group + 1 + int(rng.randint(0, 200))
+    news = [first] + [int(rng.randint(1, first + 1)) for _ in range(seqs - 1)]
+    lens = [n + int(rng.choice([0, 1, 130, 700])) for n in news]
+    table = make_table(rng, lens, page, sum(-(-n // page) for n in lens) + 2)
+    cache = random_cache(seed, 1, sum(-(-n // page) for n in lens) + 2, heads, page, d)
+    spread = lambda t, by: t * 2.0 ** (by * (torch.rand(t.shape, generator=g, device=G.DEV) - 1))  # noqa: E731
+    keys, vals, far = rng.choice([0, 8, 16, 36], 3)
+    cache.k_param[..., 0] = spread(cache.k_param[..., 0], float(keys))
+    cache.v_param[..., 0] = spread(cache.v_param[..., 0], float(vals))
+    if far >= 16:
+        cache.v_param[..., 1] = torch.randint(-1200, 1201, cache.v_param.shape[:-1], generator=g, device=G.DEV).float()
+    if far == 36:
+        cache.k_param[..., 1] = torch.randint(-1200, 1201, cache.k_param.shape[:-1], generator=g, device=G.DEV).float()
+    batch, start = batch_of(table, lens, news, max_new=first)
+    q, scale, causal = queries(seed, batch.rows, heads * group, d), float(rng.choice([0.001, 0.09, -0.3])), bool(rng.rand() < 0.7)
+    want = kv_bounds.expect(layer_of(cache), table, lens, start, q, scale, causal)
+    got, lse = attend(cache, 0, q, batch, scale, causal)
+    took = [s for s in range(seqs) if news[s] * group > 96]   # shorter ones are the streaming kernel's
+    rows = torch.cat([torch.arange(int(start[s]), int(start[s + 1])) for s in took]).to(G.DEV)
+    kv_bounds.check(got, lse, want, rows)
+    assert torch.isfinite(got.float()).all() and B.qllm_poll_status() == B.QLLM_OK
