@@ -243,13 +243,13 @@ __global__ void __launch_bounds__(256) kv_free_kernel(Pool p, const int32_t* __r
 }
 
 // ---- copies --------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void copy_page(const Store& s, int src, int dst, int layer, int part, int parts) {
+__device__ __forceinline__ void copy_page(const Store& s, int src, int dst, int layer) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const uint4* from = s.a[k] + (int64_t(layer) * s.pages + src) * s.n[k];
         uint4* to = s.a[k] + (int64_t(layer) * s.pages + dst) * s.n[k];
-        const int64_t step = int64_t(parts) * blockDim.x;
-        for (int64_t i = int64_t(part) * blockDim.x + threadIdx.x; i < s.n[k]; i += 4 * step) {
+        const int64_t step = blockDim.x;
+        for (int64_t i = threadIdx.x; i < s.n[k]; i += 4 * step) {
             uint4 v[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -269,7 +269,7 @@ kv_copy_kernel(Store st, const int32_t* __restrict__ src, const int32_t* __restr
         if (threadIdx.x == 0) raise_page(status);
         return;
     }
-    if (a != b) copy_page(st, a, b, blockIdx.y, 0, 1);
+    if (a != b) copy_page(st, a, b, blockIdx.y);
 }
 
 // The last pages of forked sequences: the parent's partly filled one into the fresh one of entry i's child.
@@ -279,7 +279,7 @@ kv_fork_copy_kernel(Store st, Pool p, const int32_t* __restrict__ parent, const 
     if (to < 0) return;                                    // nothing to copy, or the entry was not served
     const int a = parent[blockIdx.x];
     const int from = p.table[int64_t(a) * p.width + (p.lens[a] >> p.page_log2)];
-    if (from >= 0 && from < st.pages) copy_page(st, from, to, blockIdx.y, 0, 1);
+    if (from >= 0 && from < st.pages) copy_page(st, from, to, blockIdx.y);
 }
 
 // ---- compact -------------------------------------------------------------------------------------------------------
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(256) kv_compact_move_kernel(Store st, Pool p, 
     if (int(blockIdx.y) < st.layers) {
         for (int page = blockIdx.x; page < st.pages; page += gridDim.x) {
             const int to = remap[page];
-            if (to >= 0 && to != page) copy_page(st, page, to, blockIdx.y, 0, 1);
+            if (to >= 0 && to != page) copy_page(st, page, to, blockIdx.y);
         }
         return;
     }
