@@ -147,28 +147,30 @@ kv_fork_kernel(Pool p, const int32_t* __restrict__ parent, const int32_t* __rest
     extern __shared__ int s_dyn[];
     int* s_first = s_dyn;                                  // [seqs] first entry that names the sequence as a child, or one of:
     constexpr int kNobody = 0x7fffffff, kParent = 0x7ffffffe, kBroken = 0x7ffffffd;      // no child; a parent; one that cannot be copied
-    int* s_rank = s_dyn + p.seqs;                          // [n] pages asked for by the entries in front; -1: not served
+    int* s_rank = s_dyn + p.seqs;                          // [n] the parents, then pages asked for by the entries in front; -1: not served
     __shared__ int s_warp[32];
     const int P = 1 << p.page_log2;
     for (int s = threadIdx.x; s < p.seqs; s += kThreads) s_first[s] = kNobody;
     __syncthreads();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int early = warp + 32 * lane < p.seqs ? p.lens[warp + 32 * lane] : 0;      // under the loads below
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const int c = child[i];
+        s_rank[i] = parent[i];
         if (c >= 0 && c < p.seqs) atomicMin(&s_first[c], i);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kThreads) {
-        const int a = parent[i];
+        const int a = s_rank[i];
         if (a >= 0 && a < p.seqs && s_first[a] >= kParent) s_first[a] = kParent;
     }
     __syncthreads();
     // each parent's pages are looked at once, however many children it gets (7000 entries of 1000 parents: entry by entry 376 us), and
     // neighbours by different warps
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int base = warp; base < p.seqs; base += kThreads) {
         const int mine = base + 32 * lane;
         const bool marked = mine < p.seqs && s_first[mine] == kParent;
-        const int length = marked ? p.lens[mine] : 0;
+        const int length = base == warp ? early : marked ? p.lens[mine] : 0;
         for (unsigned left = __ballot_sync(0xffffffffu, marked); left; left &= left - 1) {
             const int l = __ffs(left) - 1, s = base + 32 * l, len = __shfl_sync(0xffffffffu, length, l);
             bool ok = len >= 0 && int64_t(len) <= int64_t(p.width) << p.page_log2;
@@ -186,7 +188,7 @@ kv_fork_kernel(Pool p, const int32_t* __restrict__ parent, const int32_t* __rest
         const int i = base + threadIdx.x;
         int need = 0, ok = 0;
         if (i < n) {
-            const int a = parent[i], c = child[i];
+            const int a = s_rank[i], c = child[i];
             ok = a >= 0 && a < p.seqs && c >= 0 && c < p.seqs && s_first[c] == i && s_first[a] == kParent && p.lens[c] == 0;
             need = ok && (p.lens[a] & (P - 1)) != 0;
             if (!ok) raise_page(status);
