@@ -301,8 +301,6 @@ __device__ __forceinline__ void load_queries(const QT* row, int t, uint32_t (&hi
     ratio = e > 127 ? NAN : sum * pow2i(-13 - kUnit<F32>);
 }
 
-__device__ __forceinline__ float room(float m) { return fabsf(m) < kLargeScore ? kPlace + kSlack : kPlace; }
-
 template <int W>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[W]) {
     if constexpr (W == 2) {
@@ -324,6 +322,7 @@ struct State {
     float qn[NT][2], qr[NT][2];                            // factor of the scores (into base 2; a power of two), sum of the query in the units of its key sums
     int limit[NT][2];                                      // keys that the column sees
     float o[NT][D / 16][4], top[NT][2], l[NT][2], zs[NT][2];
+    float room;                                            // how far scores may lie above `top`: no slack once some were large
 };
 
 // 32 tokens, from `first` on.  key_unit: what the key scales are multiplied by, the mantissa of the scale and the part of the columns'
@@ -416,7 +415,7 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
                 }
         }
         // the reference moves only when a weight would pass 2^kSlack times its place
-        if (__any_sync(0xffffffffu, m[0] > st.top[a][0] + room(m[0]) || m[1] > st.top[a][1] + room(m[1]))) {
+        if (__any_sync(0xffffffffu, m[0] > st.top[a][0] + st.room || m[1] > st.top[a][1] + st.room)) {
             float fix[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -430,6 +429,8 @@ __device__ __forceinline__ void step(State<D, NT, F32>& st, const uint8_t* kc, c
                 st.l[a][e] *= fix[e];
                 st.zs[a][e] *= fix[e];
             }
+            auto large = [](float x) { return fabsf(x) >= kLargeScore && x != -INFINITY; };
+            if (__any_sync(0xffffffffu, large(st.top[a][0]) || large(st.top[a][1]))) st.room = kPlace;
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -626,6 +627,7 @@ kv_split_kernel(Cache c, Plan p, const QT* __restrict__ q, int64_t q_stride, QT*
             }
         }
         low = __reduce_min_sync(0xffffffffu, low);
+        st.room = kPlace + kSlack;
         // the largest query's factor stays below 2^65, what is above goes to the keys (nothing but for queries of 2^50 and more): left
         // in qn it would pass float32 for the largest queries, and the keys that such queries can have would make subnormal scores
         const int lift = min(max(__reduce_max_sync(0xffffffffu, top_e) + kUnit<F32> + scale_e - 64, 0), 126);
