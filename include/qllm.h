@@ -376,7 +376,8 @@ int qllm_layer_workspace(qllm_layer_t* layer, uint8_t** codes, float** a_scale, 
  * 6. Key/value cache in 4 bits                    (device, asynchronous)
  * ==========================================================================
  * What follows the QKV projection: its keys and values are stored with the per-token quantizer of Eq. 2, one scale
- * and zero-point for each token and head, and attention reads them in that form.
+ * and zero-point for each token and head, and attention reads them in that form.  Positions enter none of these calls: models with
+ * rotary embeddings (LLaMA) apply them to the keys before qllm_kv_append and to the queries before the attention.
  *
  * THE CACHE is four caller-owned device arrays over `layers` layers and `pages` pages of page_size tokens:
  *   k_codes, v_codes  uint8 [layers][pages][kv_heads][page_size][head_dim / 2], byte i of a row holds channel 2i in its
@@ -393,8 +394,8 @@ int qllm_layer_workspace(qllm_layer_t* layer, uint8_t** codes, float** a_scale, 
  *             new tokens of sequence s, its last positions in order.  A sequence may have none.
  *   rows      rows of the packed tensors (rows * q_heads < 2^31 for the attention), at least q_start[seqs]; rows in front of
  *             q_start[0] and from q_start[seqs] on are left as they are
- *   max_new   the most new tokens of one sequence.  A hint: it selects kernels and sizes the workspace of the attention,
- *             results do not depend on its being right.
+ *   max_new   the most new tokens of one sequence.  A hint: it selects kernels and sizes the workspace of the attention.  Any
+ *             value gives the same result up to what the kernels round (below); a wrong one costs time.
  * Where a sequence has more new tokens than length, the first of them have no position: qllm_kv_append skips them,
  * qllm_kv_read writes zeros, and causal attention rows see no key.
  *
@@ -457,6 +458,13 @@ int qllm_kv_read(const qllm_kv_cache_t* cache, int layer, void* k, int64_t k_str
  *  workspace  device, 16-byte aligned, qllm_kv_attention_workspace(...) bytes for the same arguments (QLLM_ERR_SHAPE when
  *             smaller), written before it is read: calls that may run at the same time need one each
  *  scale      finite (QLLM_ERR_SHAPE)
+ * Precision: sums, maxima and the softmax's statistics are float32.  QLLM_F32 calls carry 22 bits and more in every product.
+ * QLLM_BF16 calls round each weight to 11 bits; their tensor-core kernel (heads of 64 and 128, more than 96 query rows, i.e. new
+ * tokens x q_heads / kv_heads, in a sequence) also rounds the scales and the products alpha (code - zero) of keys and values to
+ * 11 bits each.  Against 64-bit arithmetic that makes 1.7e-3 to 1.9e-3 of the result, 1.65e-3 of it by its rounding to bf16.
+ * Finite inputs give finite results while scores and results fit float32 and the value scales lie within 2^-80 .. 2^80: beyond,
+ * weights pass fp16 (infinities and NaN), and values of smaller scales may count as 0.
+ *
  * The workspace size depends on the device, the cache's shape, q_heads, dtype and the batch's seqs, rows and max_new; it is
  * negative (a status) for arguments that the call itself would refuse. */
 int64_t qllm_kv_attention_workspace(const qllm_kv_cache_t* cache, int q_heads, int dtype, const qllm_kv_batch_t* batch);

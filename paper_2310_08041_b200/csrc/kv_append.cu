@@ -6,8 +6,10 @@
 // bytes: head_dim values of 2 or 4 bytes on one side, head_dim / 2 + 8 bytes on the other.  head_dim / 16 lanes own a row, 16
 // channels each: 16-byte accesses of the values, 8 bytes of codes, the range by shuffles inside the group.  (With 8 channels a
 // lane, the instructions that a row costs whatever its length were most of them: 94 us instead of 64 to store 9708 bf16 tokens
-// of 2 x 32 rows of 128, 50 instead of 46 to read them; 31 is what the bytes take at the copy rate.)  A CTA takes a run of tokens: where each belongs (sequence, page, place) is found once per token by one
-// thread, for all of its 2 kv_heads rows, and two rows of a group are in flight together.
+// of 2 x 32 rows of 128, 50 instead of 46 to read them; 31 is what the bytes take at the copy rate.  What is left is latency:
+// storing keeps DRAM a third and the issue slots 60 % busy, and its warps, 32 to an SM of 64 registers, wait for their loads.)
+// A CTA takes a run of tokens: where each belongs (sequence, page, place) is found once per token by one thread, for all of its
+// 2 kv_heads rows, and two rows of a group are in flight together.
 
 #include <algorithm>
 

@@ -23,8 +23,10 @@ int check_attention(const qllm_kv_cache_t* cache, int q_heads, int dtype, const 
 // Which kernels a call launches.  The streaming kernel reads a sequence's keys once per 8 or 16 query rows, the tensor-core kernel
 // once per 256 and unpacks them for 256 whether there are that many or not: kPromptRows is where they meet (us, streaming against
 // tensor-core kernel, heads of 128 in bf16, at 64 / 96 / 128 rows: 4 sequences of 4096 tokens on 8 heads 37 : 43, 49 : 45,
-// 60 : 48; 1 of 32768 on 8 heads 53 : 88, 73 : 89, 92 : 90; 4 of 2048 on 32 heads 64 : 76, 88 : 65, 111 : 68).  Either serves any
-// count, so what the batch's hint says wrongly costs time only.  A batch with the same number of new tokens in every
+// 60 : 48; 1 of 32768 on 8 heads 53 : 88, 73 : 89, 92 : 90; 4 of 2048 on 32 heads 64 : 76, 88 : 65, 111 : 68; with a flushed L2 50 : 38,
+// 63 : 40, 77 : 42; 69 : 93, 93 : 93, 116 : 93; 83 : 52, 112 : 52, 138 : 54, and heads of 64 then 36 : 34, 44 : 34, 52 : 34; 48 : 77,
+// 63 : 77, 77 : 77; 56 : 44, 73 : 44, 87 : 44: the border could lie lower for batches, and would have to lie higher for one long
+// context).  Either serves any count, so what the batch's hint says wrongly costs time only.  A batch with the same number of new tokens in every
 // sequence, as far as the hint goes, needs one of them; others get both, each taking its sequences.
 constexpr int kPromptRows = 96;
 struct Choice {

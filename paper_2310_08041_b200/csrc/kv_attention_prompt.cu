@@ -23,8 +23,8 @@
 // Channels lie in the order 0 4 1 5 2 6 3 7 of each eight, as the masks leave them: the queries are stored alike and the output
 // is put right at the end.
 
-// Measured: a prompt of 2048 tokens, 32 heads of 128, causal: 65 us, 0.53 PFLOP/s; 1024 and 17 new tokens behind up to 8191, 64 query
-// on 8 key heads: 322 us, 0.80 PFLOP/s = 0.49 of the measured cuBLAS bf16 rate.  A step of two tiles takes about 5300 cycles where
+// Measured: a prompt of 2048 tokens, 32 heads of 128, causal: 66 us, 0.52 PFLOP/s; 1024 and 17 new tokens behind up to 8191, 64 query
+// on 8 key heads: 320 us, 0.81 PFLOP/s = 0.49 of the measured cuBLAS bf16 rate.  A step of two tiles takes about 5300 cycles where
 // its MMAs need 2048 and its exponentials as many: what is left is the chain through one tile (maximum, exchange, weights,
 // store, product, next scores), which two tiles in flight do not fill.  Tried and dropped, besides what stands at the functions
 // below: waiting warps asleep in their barriers or polling in four instructions (both 2 % slower).

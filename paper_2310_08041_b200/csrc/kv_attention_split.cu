@@ -2,7 +2,8 @@
 //
 // s_j = scale q . k_j, k_j = ks_j (ck_j - kz_j), so s_j = ks_j (scale q . ck_j - kz_j scale sum q): the keys enter the
 // tensor cores as bare codes, scale and zero-point act on finished sums.  Likewise sum_j p_j v_j = sum_j (p_j vs_j) cv_j -
-// sum_j (p_j vs_j) vz_j.  HBM bounds it: a token's keys and values are D + 16 bytes a head, read once per 8 NT query rows.
+// sum_j (p_j vs_j) vz_j.  A token's keys and values are D + 16 bytes a head, read once per 8 NT query rows; in the middle of a long
+// call they come at the copy rate, at its ends latency is what bounds it (measured below).
 //
 // Work split: an item is (sequence, key head, tile of 8 NT query rows); its keys are tiles of T tokens.  All items' tiles form
 // one line, which the CTAs of one resident wave cut into equal shares, each working out its own from the lengths on the
@@ -30,9 +31,12 @@
 // Measured (us a call, both kernels; the bytes of the cache at the measured copy rate in brackets): one sequence of 131071
 // tokens, 64 query on 8 key heads of 128, bf16: 44 (23), of which the main kernel streams 24 at that rate, starts for 6 (plan, table,
 // first tiles) and spreads over 8 at the end, and joining takes 5; 32 sequences of 176 to 9001 tokens: 37 (16); 6 sequences, up to
-// 5 new tokens, 40 heads, float32: 23 (4).  Without its arithmetic the kernel took 2 us less: latency at both ends, not the
-// instruction rate, is what is left.  Tried and dropped: four CTAs per SM in 96 registers (spills, 60 instead of 48), two or three
-// times as many shares as CTAs that fit (60, 80), reading page ids tile by tile (no difference).
+// 5 new tokens, 40 heads, float32: 23 (4).  By events with a flushed L2: 16 sequences of 8192 tokens, 32 query on 8 key heads of 256,
+// 85 (43), in float32 157.  Prompts of float32 calls and of heads of 256 come here too, whose keys are read and decoded again for
+// every 8 rows: 1024 tokens, the same heads, 343 in bf16 and 652 in float32, 269 in float32 at heads of 128 (where the tensor-core
+// kernel takes 38 in bf16).  Without its arithmetic the kernel took 2 us less: latency at both ends, not the instruction rate, is
+// what is left.  Tried and dropped: four CTAs per SM in 96 registers (spills, 60 instead of 48), two or three times as many shares as
+// CTAs that fit (60, 80), reading page ids tile by tile (no difference).
 
 #include <cuda_fp16.h>
 
@@ -811,7 +815,9 @@ kv_combine_kernel(Batch b, int* status, int group, QT* __restrict__ out, int64_t
 }
 
 // Query rows of an item: 16 when a key head has more than 8 of them, which halves the passes over its keys; float32 and
-// 256-channel items of 16 would not leave their accumulators in registers.
+// 256-channel items of 16 would leave most of their accumulators in local memory.  As it is, bytes spilled and read back per thread: 248 / 364
+// and 168 / 280 with 16 rows (heads of 128, 64), 32 / 48 with 8 at heads of 128, 92 / 152 at 256; float32 8 / 12, 12 / 16 and 768 / 852 at
+// heads of 64, 128, 256.  The fifth warp of a CTA is what caps the registers at 168 and 128.
 inline int rows_of_item(int head_dim, int dtype, int rows_hint) { return rows_hint > 8 && head_dim <= 128 && dtype == QLLM_BF16 ? 16 : 8; }
 
 template <typename QT, int D, int NT>

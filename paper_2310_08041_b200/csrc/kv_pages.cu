@@ -5,7 +5,9 @@
 // prefix sums, duplicates are settled by an atomic minimum over list positions or an exchange), which costs a pass over refs; the page
 // contents then move in a second kernel over (page, layer) that reads the bookkeeping's result.  Contents: 2 * page_size * kv_heads * (head_dim / 2 + 8) bytes a page and layer, read and written
 // once in 16-byte accesses, four in flight per thread.  Measured: 43 pages of 32 layers (100 MB copied) 29 us, 6.9 TB/s; 1.25 GB moved
-// by a compaction of 40 layers in 184 us, 6.8 TB/s; the bookkeeping 4 to 8 us.
+// by a compaction of 40 layers in 184 us, 6.8 TB/s; the bookkeeping 4 to 8 us.  Making room: 7 us for one more token of 64 sequences, 8
+// of 512, 12 of 4096; 10 for a prompt of 2048 tokens in pages of 64, 240 for one of 131072 in pages of 16, whose 8192 counts one
+// thread sets.
 
 #include "device_utils.cuh"
 #include "kv_cache.cuh"
