@@ -18,15 +18,15 @@ struct AttnArgs {
     int most_rows;
 };
 
-// scale log2 e = the result 2^e: a row's factor of its scores takes the power of two, the keys the rest (1 to 2 in size, or 0).  A
+// scale log2 e = the result 2^e: a row's factor of its scores takes the power of two, the keys the rest (1 to 2 in size; 0, and less for subnormal scales).  A
 // product with the factor is then exact, and the score that is compared with a maximum is the very one that enters the exponential.
 // (A factor that rounds leaves in the fused difference what the compared product lost, 2^-24 of the score: from scores of 10^8 on
 // weights became infinite.)
 __device__ __forceinline__ float split_scale(float scale, int& e) {
     const float x = fminf(fmaxf(scale * 1.4426950408889634f, -3e38f), 3e38f);
     const uint32_t bits = __float_as_uint(x);
-    e = int(bits >> 23 & 255u) - 127;
-    return e > -127 ? __uint_as_float((bits & 0x807FFFFFu) | 0x3F800000u) : 0.f;         // (subnormal ones count as 0)
+    e = max(int(bits >> 23 & 255u) - 127, -126);
+    return fabsf(x) >= 0x1p-126f ? __uint_as_float((bits & 0x807FFFFFu) | 0x3F800000u) : x * 0x1p126f;
 }
 // Scores from here on: the exponent of a weight is off by the roundings of the reference, none of the slack is left to later tiles.
 constexpr float kLargeScore = 0x1p20f;

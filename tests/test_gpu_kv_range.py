@@ -288,3 +288,43 @@ def test_scores_of_every_size(power, sign, news, dtype):
                 spread = np.abs(v[:m]).mean(0)
                 assert (np.abs(a - want) <= np.abs(want) * eps + spread * (2.0 ** -9 if dtype == "bf16" else 2.0 ** -18)).all(), (causal, s, i)
     assert B.qllm_poll_status() == B.QLLM_OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news", [[1, 1], [70, 130]])
+@pytest.mark.parametrize("power", [-135, -127, -126, -100, 60, 120])
+def test_scales_near_the_ends_of_float32(power, news, dtype):
+    """Scales of 2^power times 0.7, subnormal ones among them, against queries and keys that make ordinary scores of them."""
+    lens, page, heads, group, d = [300, 140], 64, 2, 4, 128
+    table = make_table(np.random.RandomState(79), lens, page, 9)
+    cache = random_cache(79, 1, 9, heads, page, d)
+    there = -power // 2 - 2                                  # half of it on the keys, half on the queries
+    cache.k_param[..., 0] *= 2.0 ** there
+    batch, start = batch_of(table, lens, news)
+    q = (torch.randn(batch.rows, heads * group, d, device=G.DEV) * 2.0 ** (-power - there - 3)).to(DT[dtype])
+    scale = 0.7 * 2.0 ** power
+    got, lse = attend(cache, 0, q, batch, scale, True)
+    ref = kv_ref.attention(store_of(cache, 0), table, lens, start, host(q), float(np.float32(scale)), True)
+    check_attention(got, lse, ref, DT[dtype], prompt=dtype == "bf16" and max(news) * group > 96)
+    assert B.qllm_poll_status() == B.QLLM_OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news", [[1, 3], [70, 130]])
+def test_zero_points_that_are_no_integers(news, dtype):
+    """As append stores them for rows near the end of float32, here at ordinary scales."""
+    lens, page, heads, group, d = [300, 140], 64, 2, 4, 128
+    table = make_table(np.random.RandomState(80), lens, page, 9)
+    cache = random_cache(80, 1, 9, heads, page, d)
+    g = torch.Generator(device=G.DEV); g.manual_seed(80)
+    for p in (cache.k_param, cache.v_param):
+        some = torch.rand(p.shape[:-1], generator=g, device=G.DEV) < 0.5
+        p[..., 1] += torch.where(some, torch.rand(p.shape[:-1], generator=g, device=G.DEV), 0.0)
+    batch, start = batch_of(table, lens, news)
+    q = torch.randn(batch.rows, heads * group, d, device=G.DEV).to(DT[dtype])
+    got, lse = attend(cache, 0, q, batch, 0.09, True)
+    ref = kv_ref.attention(store_of(cache, 0), table, lens, start, host(q), 0.09, True)
+    prompt = dtype == "bf16" and max(news) * group > 96
+    check_attention(got, lse, ref, DT[dtype], prompt=prompt)
+    if prompt:
+        kv_bounds.check(got, lse, kv_bounds.expect(layer_of(cache), table, lens, start, q, 0.09, True))
