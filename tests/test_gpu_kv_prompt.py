@@ -6,8 +6,9 @@ import torch
 
 import gpu_util as G
 import kv_bounds
+import kv_ref
 from paper_2310_08041_b200 import binding as B
-from test_gpu_kv import attend, batch_of, ints, make_table, random_cache
+from test_gpu_kv import DT, attend, batch_of, check_attention, host, ints, make_table, random_cache, store_of
 
 pytestmark = pytest.mark.gpu
 
@@ -19,6 +20,37 @@ def layer_of(cache, layer=0):
 def queries(seed, *shape):
     g = torch.Generator(device=G.DEV); g.manual_seed(seed)
     return torch.randn(*shape, generator=g, device=G.DEV).bfloat16()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_graph_of_the_streaming_kernel_writes_logarithms(dtype):
+    """Few new tokens: captured, replayed while lengths, pages and queries change, against 64-bit logarithms."""
+    heads, group, page, d, news = 2, 4, 16, 128, [1, 3, 0, 2]
+    top = [1500] * len(news)
+    cache = random_cache(55, 1, 400, heads, page, d)
+    batch, start = batch_of(make_table(np.random.RandomState(55), top, page, 400), top, news)
+    q = queries(56, batch.rows, heads * group, d).to(DT[dtype])
+    out, lse, st = torch.empty_like(q), torch.empty(batch.rows, heads * group, device=G.DEV), torch.cuda.Stream()
+    ws = torch.full((B.qllm_kv_attention_workspace(cache, heads * group, q, batch),), 0xFF, dtype=torch.uint8, device=G.DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        B.qllm_kv_attention(cache, 0, q, out, 0.09, batch, ws, lse=lse, stream=st)
+    st.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        B.qllm_kv_attention(cache, 0, q, out, 0.09, batch, ws, lse=lse, stream=st)
+    for lens in ([1500] * 4, [1, 2, 0, 17], [911, 151, 64, 1]):
+        table = make_table(np.random.RandomState(lens[1]), top, page, 400)
+        batch.seq_lens.copy_(ints(lens))
+        batch.table.copy_(ints(table))
+        q.copy_(queries(lens[0], *q.shape))
+        lse.fill_(7.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            g.replay()
+        torch.cuda.synchronize()
+        check_attention(out, lse, kv_ref.attention(store_of(cache, 0), table, lens, start, host(q), 0.09, True), DT[dtype])
+    assert B.qllm_poll_status() == B.QLLM_OK
 
 
 @pytest.mark.parametrize("causal", [True, False])
