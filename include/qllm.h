@@ -27,6 +27,7 @@
  *
  * DEVICE MEMORY.  Which calls may call cudaMalloc / cudaFree:
  *   never      qllm_qgemm_noalloc, qllm_quantize_rows, qllm_calib_absmax, qllm_layernorm_rows, qllm_kv_*,
+ *              qllm_rmsnorm_quant, qllm_dequantize_rows, qllm_adapters_add, qllm_rotary_table,
  *              qllm_channel_distance, qllm_layer_forward / _reassemble_quant / _qgemm / _forward_host (everything a
  *              layer needs is taken in qllm_layer_create and returned in qllm_layer_destroy);
  *   grow-only  qllm_reassemble_quant (compiled-map scratch per (device, stream): grown on the first call
@@ -134,6 +135,36 @@ int qllm_reassemble_quant(const void* x, int x_dtype, int64_t M, int C,
 int qllm_quantize_rows(const void* x, int x_dtype, int64_t M, int C, int bits,
                        uint8_t* codes, float* a_scale, float* a_zero, int32_t* a_rowsum, void* stream);
 
+/* The pre-GEMM stage of blocks with a root-mean-square norm and a residual stream (LLaMA; device, asynchronous):
+ *
+ *   h = x + residual,   y = gamma h / sqrt(mean_k h_k^2 + eps),   x'_c = sum_j coef_j y[src_j],   Eq. 2 on x' per token
+ *
+ *  x         device [M][C], QLLM_F32 or QLLM_BF16 (x_dtype); residual: the same, or NULL (h = x)
+ *  gamma     device float[C];  eps >= 0, finite (QLLM_ERR_SHAPE otherwise)
+ *  map_*     as in qllm_reassemble_quant, or all NULL (x' = y; the arrays are not validated on the device)
+ *  h, y      device out [M][C] of x_dtype, or NULL: the new residual stream and the normalised rows before the map (what adapters,
+ *            routers and heads beside a quantized layer read).  h may be x or residual in place; no other operands may overlap.
+ *  codes, a_scale, a_zero, a_rowsum   as in qllm_reassemble_quant (a_rowsum may be NULL).  codes = NULL: only h and y (at least one
+ *            of them) are made, bits and the other three are ignored, and a map is refused (QLLM_ERR_NULL).
+ *  M = 0 is a successful no-op.  C <= 49152 (QLLM_ERR_UNSUPPORTED), even for 4-bit codes.
+ *
+ * The norm's factor r is common to a token's channels, so codes and zero-point are those of u' = map(gamma h) and a_scale is r times
+ * u's alpha (1 for a row of zeros).  Which code a value gets is thus decided by float32 operations that do not depend on an order: the sum x + residual
+ * (not rounded to x_dtype before it is normalised), the product with gamma, the map's coefficient (rows with several members: summed
+ * in 64 bits, rounded once), and Eq. 2 as in qllm_quantize_rows.  Finite rows whose squares pass float32, or fall below 2^-80, are
+ * scaled by a power of two on the way; gamma's entries are expected within 2^-60 .. 2^60.  A row with a NaN has a NaN
+ * as a_scale; a row with an infinity has the factor 0, as the formula says, and a_scale 0 or NaN.
+ * Multiples of 8 channels up to 16384 (with a map: 8192) stay in registers between reading and writing; others go through shared memory. */
+int qllm_rmsnorm_quant(const void* x, const void* residual, int x_dtype, int64_t M, int C, const float* gamma, float eps,
+                       const int32_t* map_ptr, const int32_t* map_src, const float* map_coef, int bits, void* h, void* y,
+                       uint8_t* codes, float* a_scale, float* a_zero, int32_t* a_rowsum, void* stream);
+
+/* The inverse of the three quantizers above (device, asynchronous): out[m][c] = a_scale[m] (code - a_zero[m]) as QLLM_F32 or QLLM_BF16,
+ * for what reads a row beside the integer GEMM where only its codes exist (a folded or reassembled layer's input).  C even for
+ * 4-bit codes. */
+int qllm_dequantize_rows(const uint8_t* codes, const float* a_scale, const float* a_zero, int64_t M, int C, int bits,
+                         void* out, int out_dtype, void* stream);
+
 /* ==========================================================================
  * 2. Low-bit integer GEMM with dequantizing epilogue   (device, asynchronous)
  * ==========================================================================
@@ -195,6 +226,37 @@ int qllm_qgemm_noalloc(const uint8_t* codes, const float* a_scale, const float* 
  * for bit with a reference. */
 int qllm_qgemm_acc(const uint8_t* codes, const uint8_t* w_codes, int32_t* acc,
                    int64_t M, int N, int K, int a_bits, int w_bits, void* stream);
+
+/* ---- low-rank adapters beside a shared projection     (device, asynchronous) ----
+ * Requests of one batch that were trained with different low-rank adapters share the quantized projection above; what differs is
+ *
+ *   out[m] = base[m] + scale[a] B_a (A_a x[m])       for the rows m of sequence s, a = adapter[s]
+ *
+ * ADAPTERS are caller-owned device arrays over `slots` slots:
+ *   A      bf16 [slots][max_rank][K],  B  bf16 [slots][N][max_rank], 16-byte aligned
+ *   rank   int32 [slots] or NULL (all max_rank): what A holds behind row rank[a] and B behind column rank[a] counts for nothing
+ *   scale  float [slots]
+ * max_rank is a multiple of 8 up to 128, K and N are multiples of 8, slots <= 8192 (QLLM_ERR_UNSUPPORTED).
+ *  x          device [rows][K], base, out device [rows][N], all of dtype (QLLM_F32 or QLLM_BF16); *_stride: distance between rows in
+ *             elements, so that one call can serve a part of a fused projection's columns.  Addresses and strides are multiples of 16 bytes.
+ *             base may be out (with the same stride, QLLM_ERR_SHAPE otherwise), or NULL (zeros); x must not overlap out.
+ *  q_start    device int32 [seqs + 1], the row ranges of the sequences, as in section 6.  Rows of no sequence are left as they are.
+ *  adapter    device int32 [seqs]: the sequence's slot; negative: none (its rows of out become those of base)
+ * Read on the device when the kernel runs, so a captured graph follows their contents.  Row ranges that decrease or leave the
+ * tensors are cut, slots out of range count as none, ranks are cut to 0 .. max_rank, and the status word becomes QLLM_ERR_PAGE
+ * (qllm_poll_status).  seqs <= 2^20, rows <= 2^30.
+ * Precision: sums in float32; of A_a x, 16 bits (QLLM_BF16) or 24 bits (QLLM_F32) enter the second product.  QLLM_F32 rows with an
+ * infinity give NaN. */
+typedef struct qllm_adapters {
+    const void*    A;
+    const void*    B;
+    const float*   scale;
+    const int32_t* rank;
+    int slots, max_rank, K, N;
+} qllm_adapters_t;
+int qllm_adapters_add(const qllm_adapters_t* ad, const void* x, int64_t x_stride, const void* base, int64_t base_stride, void* out,
+                      int64_t out_stride, int dtype, const int32_t* q_start, const int32_t* adapter, int seqs, int64_t rows,
+                      void* stream);
 
 /* ==========================================================================
  * 3. Calibration statistic                        (device, asynchronous)
@@ -376,8 +438,9 @@ int qllm_layer_workspace(qllm_layer_t* layer, uint8_t** codes, float** a_scale, 
  * 6. Key/value cache in 4 bits                    (device, asynchronous)
  * ==========================================================================
  * What follows the QKV projection: its keys and values are stored with the per-token quantizer of Eq. 2, one scale
- * and zero-point for each token and head, and attention reads them in that form.  Positions enter none of these calls: models with
- * rotary embeddings (LLaMA) apply them to the keys before qllm_kv_append and to the queries before the attention.
+ * and zero-point for each token and head, and attention reads them in that form.  Positions enter only
+ * qllm_kv_rotate_append, which turns queries and keys (LLaMA's rotary embeddings) and appends in one go; with the other calls they are
+ * applied to the keys before qllm_kv_append and to the queries before the attention.
  *
  * THE CACHE is four caller-owned device arrays over `layers` layers and `pages` pages of page_size tokens:
  *   k_codes, v_codes  uint8 [layers][pages][kv_heads][page_size][head_dim / 2], byte i of a row holds channel 2i in its
@@ -439,6 +502,27 @@ typedef struct qllm_kv_batch {
  * one position of one sequence. */
 int qllm_kv_append(const qllm_kv_cache_t* cache, int layer, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                    int dtype, const qllm_kv_batch_t* batch, void* stream);
+
+/* THE ANGLES of rotary embeddings: table device float [positions][rot_dim / 2][2], cosine and sine of the angle of pair p at each
+ * position, 16-byte aligned.  rot_dim is a multiple of 16 up to head_dim; channels from rot_dim on are not turned.  interleaved = 0: pair p is
+ * channels (p, p + rot_dim / 2); else (2p, 2p + 1). */
+typedef struct qllm_rotary {
+    const float* table;
+    int positions, rot_dim, interleaved;
+} qllm_rotary_t;
+/* Fills such a table with the angles position / divisor * base^(-2 p / rot_dim), taken in 64 bits.  (Other scalings of the angles: the caller
+ * makes the table.)  base, divisor > 0. */
+int qllm_rotary_table(float* table, int positions, int rot_dim, double base, double divisor, void* stream);
+
+/* qllm_kv_append with the rotation of the new tokens' queries and keys on the way: pair (a, b) of a token at position t becomes
+ * (a cos - b sin, b cos + a sin) with the angles of t, every product and sum rounded to float32.  q [rows][q_heads][head_dim] goes to q_out
+ * (which may be q, with the same stride), rounded once to dtype; k is turned and then quantized, unrounded, and v quantized, as by
+ * qllm_kv_append.  q_heads = 0: no queries.  Tokens without a position (more new tokens than length) and tokens beyond the
+ * table (QLLM_ERR_PAGE) are not stored, and their queries become zeros; where a token's page does not exist (QLLM_ERR_PAGE) its queries are
+ * turned.  Rows of no sequence are left as they are.  q_heads <= 8192 (QLLM_ERR_UNSUPPORTED). */
+int qllm_kv_rotate_append(const qllm_kv_cache_t* cache, int layer, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                          int q_heads, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype,
+                          const qllm_rotary_t* rotary, const qllm_kv_batch_t* batch, void* stream);
 
 /* The inverse: the stored values alpha (code - zero) of the batch's tokens as packed rows (rounded to nearest even for
  * QLLM_BF16).  With q_start counting every token of a sequence it reads the whole sequence back. */

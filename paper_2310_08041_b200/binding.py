@@ -31,6 +31,7 @@ EXPORTS = [
     "qllm_layer_create", "qllm_layer_destroy", "qllm_layer_forward", "qllm_layer_forward_host",
     "qllm_layer_reassemble_quant", "qllm_layer_qgemm",
     "qllm_layer_workspace", "qllm_layer_keep_byte_weights",
+    "qllm_rmsnorm_quant", "qllm_dequantize_rows", "qllm_adapters_add", "qllm_rotary_table", "qllm_kv_rotate_append",
     "qllm_kv_append", "qllm_kv_read", "qllm_kv_attention", "qllm_kv_attention_workspace",
     "qllm_kv_pages_extend", "qllm_kv_pages_fork", "qllm_kv_pages_free", "qllm_kv_pages_compact", "qllm_kv_pages_copy",
     "qllm_status_string", "qllm_last_cuda_error", "qllm_poll_status", "qllm_launch_count", "qllm_debug_wait_expiry",
@@ -81,6 +82,11 @@ _lib.qllm_status_string.argtypes = [_i]
 _lib.qllm_status_string.restype = ctypes.c_char_p
 _lib.qllm_launch_count.restype = _i64
 _lib.qllm_debug_wait_expiry.argtypes = [_vp, _vp]
+_lib.qllm_rmsnorm_quant.argtypes = [_vp, _vp, _i, _i64, _i, _vp, _f, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.qllm_dequantize_rows.argtypes = [_vp, _vp, _vp, _i64, _i, _i, _vp, _i, _vp]
+_lib.qllm_adapters_add.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _i, _vp, _vp, _i, _i64, _vp]
+_lib.qllm_rotary_table.argtypes = [_vp, _i, _i, _d, _d, _vp]
+_lib.qllm_kv_rotate_append.argtypes = [_vp, _i, _vp, _i64, _vp, _i64, _i, _vp, _i64, _vp, _i64, _i, _vp, _vp, _vp]
 _lib.qllm_kv_append.argtypes = [_vp, _i, _vp, _i64, _vp, _i64, _i, _vp, _vp]
 _lib.qllm_kv_read.argtypes = [_vp, _i, _vp, _i64, _vp, _i64, _i, _vp, _vp]
 _lib.qllm_kv_attention.argtypes = [_vp, _i, _vp, _i64, _vp, _i64, _i, _i, _f, _i, _vp, _vp, _vp, _i64, _vp]
@@ -153,6 +159,108 @@ def qllm_quantize_rows(x, bits, codes, a_scale, a_zero, a_rowsum=None, stream=No
     M, C = x.shape
     _check(_lib.qllm_quantize_rows(_dp(x), _xdtype(x), M, C, bits, _dp(codes), _dp(a_scale), _dp(a_zero), _dp(a_rowsum),
                                    _stream(stream)))
+
+
+def qllm_rmsnorm_quant(x, gamma, bits, codes, a_scale, a_zero, a_rowsum=None, residual=None, h=None, y=None, map=None, eps=1e-5, stream=None):
+    """x, residual, h, y [M][C] of one dtype (the last three may be None); gamma float32 [C]; map: None or (ptr, src, coef) device
+    tensors as for qllm_reassemble_quant.  codes = None (then a_scale = a_zero = None too): only h and y."""
+    _want(x.dim() == 2)
+    M, C = x.shape
+    dev = x.get_device()
+    for t in (residual, h, y):
+        if t is not None:
+            _want(t.shape == x.shape)
+            if t.dtype is not x.dtype:
+                raise QllmError(QLLM_ERR_DTYPE)
+            _on(dev, t)
+    _f32(dev, (C,), gamma)
+    if codes is None:
+        _want(a_scale is None and a_zero is None and a_rowsum is None)
+    else:
+        _codes(dev, codes, M, C, bits)
+        _f32(dev, (M,), a_scale, a_zero)
+        if a_rowsum is not None:
+            _ints(dev, a_rowsum)
+            _want(a_rowsum.numel() == M)
+    ptr, src, coef = map if map is not None else (None, None, None)
+    if map is not None:
+        _ints(dev, ptr, src)
+        _want(ptr.numel() == C + 1 and src.numel() == coef.numel())
+        _f32(dev, (src.numel(),), coef)
+    _check(_lib.qllm_rmsnorm_quant(_dp(x), _dp(residual), _xdtype(x), M, C, _dp(gamma), eps, _dp(ptr), _dp(src), _dp(coef), bits, _dp(h), _dp(y),
+                                   _dp(codes), _dp(a_scale), _dp(a_zero), _dp(a_rowsum), _kv_stream(stream, dev, dev)))
+
+
+def qllm_dequantize_rows(codes, a_scale, a_zero, bits, out, stream=None):
+    """out [M][C] (float32 or bf16): the values that codes stand for, a_scale (code - a_zero)."""
+    _want(out.dim() == 2)
+    M, C = out.shape
+    dev = out.get_device()
+    _codes(dev, codes, M, C, bits)
+    _f32(dev, (M,), a_scale, a_zero)
+    _check(_lib.qllm_dequantize_rows(_dp(codes), _dp(a_scale), _dp(a_zero), M, C, bits, _dp(out), _xdtype(out), _kv_stream(stream, dev, dev)))
+
+
+def _codes(device, codes, M, C, bits):
+    if codes.dtype != torch.uint8:
+        raise QllmError(QLLM_ERR_DTYPE)
+    _want(tuple(codes.shape) == (M, C // 2 if bits == 4 else C))
+    _on(device, codes)
+
+
+def _f32(device, shape, *ts):
+    for t in ts:
+        if t.dtype != torch.float32:
+            raise QllmError(QLLM_ERR_DTYPE)
+        _want(tuple(t.shape) == shape)
+        _on(device, t)
+
+
+class _AdaptersStruct(ctypes.Structure):
+    _fields_ = [("A", _vp), ("B", _vp), ("scale", _vp), ("rank", _vp), ("slots", _i), ("max_rank", _i), ("K", _i), ("N", _i)]
+
+
+class Adapters:
+    """qllm_adapters_t over tensors that it keeps: A bf16 [slots][max_rank][K], B bf16 [slots][N][max_rank], scale float32 [slots], rank
+    int32 [slots] or None (all of max_rank).  Their contents may change between calls."""
+
+    def __init__(self, A, B, scale, rank=None):
+        if A.dtype != torch.bfloat16 or B.dtype != torch.bfloat16:
+            raise QllmError(QLLM_ERR_DTYPE)
+        _want(A.dim() == 3 and B.dim() == 3)
+        slots, top, K = A.shape
+        N = B.shape[1]
+        _want(tuple(B.shape) == (slots, N, top))
+        self.device = A.get_device()
+        _on(self.device, B)
+        _f32(self.device, (slots,), scale)
+        if rank is not None:
+            _ints(self.device, rank)
+            _want(rank.numel() == slots)
+        self.A, self.B, self.scale, self.rank, self.slots, self.max_rank, self.K, self.N = A, B, scale, rank, slots, top, K, N
+        self._s = _AdaptersStruct(_dp(A), _dp(B), _dp(scale), _dp(rank), slots, top, K, N)
+        self._p = ctypes.addressof(self._s)
+
+
+def _rows(t, rows, width, device):
+    """Address and row stride of [rows][width] with any row stride."""
+    assert t.get_device() == device, "device arguments must be CUDA tensors of one device"
+    _want(t.shape == (rows, width) and t.stride(1) == 1)
+    return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), width)
+
+
+def qllm_adapters_add(adapters, x, base, out, q_start, adapter, stream=None):
+    """out [rows][N] = base (None: zeros; may be out) + scale B (A x) for the rows q_start[s] .. q_start[s + 1] - 1 of each sequence s with
+    adapter[s] (negative: none); x [rows][K]; q_start int32 [seqs + 1], adapter int32 [seqs]."""
+    rows, dev = x.shape[0], adapters.device
+    xp, xs = _rows(x, rows, adapters.K, dev)
+    op, os_ = _rows(out, rows, adapters.N, dev)
+    bp, bs = (None, 0) if base is None else _rows(base, rows, adapters.N, dev)
+    _want(x.dtype is out.dtype and (base is None or base.dtype is out.dtype))
+    _ints(dev, q_start, adapter)
+    _want(q_start.numel() == adapter.numel() + 1)
+    _check(_lib.qllm_adapters_add(adapters._p, xp, xs, bp, bs, op, os_, _xdtype(x), _dp(q_start), _dp(adapter), adapter.numel(), rows,
+                                  _kv_stream(stream, dev, dev)))
 
 
 def qllm_qgemm(codes, a_scale, a_zero, w_codes, w_scale, w_zero, w_colsum, bias, out, M, N, K, a_bits, w_bits,
@@ -506,6 +614,57 @@ def qllm_kv_append(cache, layer, k, v, batch, stream=None):
     vp, vs = _packed(v, shape, cache.device)
     _want(k.dtype is v.dtype)
     _check(_lib.qllm_kv_append(cache._p, layer, kp, ks, vp, vs, _xdtype(k), batch._p, _kv_stream(stream, cache.device, batch.device)))
+
+
+class _RotaryStruct(ctypes.Structure):
+    _fields_ = [("table", _vp), ("positions", _i), ("rot_dim", _i), ("interleaved", _i)]
+
+
+class Rotary:
+    """qllm_rotary_t over a tensor that it keeps: float32 [positions][rot_dim / 2][2], cosine and sine of every pair's angle
+    (qllm_rotary_table fills one).  Pairs are channels (p, p + rot_dim / 2), or (2p, 2p + 1) where interleaved."""
+
+    def __init__(self, table, interleaved=False):
+        if table.dtype != torch.float32:
+            raise QllmError(QLLM_ERR_DTYPE)
+        _want(table.dim() == 3 and table.shape[2] == 2)
+        self.table, self.positions, self.rot_dim, self.interleaved = table, table.shape[0], 2 * table.shape[1], bool(interleaved)
+        self.device = table.get_device()
+        self._s = _RotaryStruct(_dp(table), self.positions, self.rot_dim, 1 if interleaved else 0)
+        self._p = ctypes.addressof(self._s)
+
+    @classmethod
+    def make(cls, positions, rot_dim, base=10000.0, divisor=1.0, interleaved=False, device="cuda"):
+        r = cls(torch.empty(positions, rot_dim // 2, 2, dtype=torch.float32, device=device), interleaved)
+        qllm_rotary_table(r.table, base, divisor)
+        return r
+
+
+def qllm_rotary_table(table, base=10000.0, divisor=1.0, stream=None):
+    """Fills table float32 [positions][rot_dim / 2][2] with cos, sin of position / divisor * base^(-2 p / rot_dim)."""
+    if table.dtype != torch.float32:
+        raise QllmError(QLLM_ERR_DTYPE)
+    _want(table.dim() == 3 and table.shape[2] == 2)
+    dev = table.get_device()
+    _check(_lib.qllm_rotary_table(_dp(table), table.shape[0], 2 * table.shape[1], base, divisor, _kv_stream(stream, dev, dev)))
+
+
+def qllm_kv_rotate_append(cache, layer, q, q_out, k, v, rotary, batch, stream=None):
+    """qllm_kv_append of k, v with q [rows][q_heads][head_dim] and k turned by their positions' angles; q_out receives the queries (may be
+    q; both None: keys and values only).  Any row strides."""
+    rows, d = batch.rows, cache.head_dim
+    assert rotary.device == cache.device, "device arguments must be CUDA tensors of one device"
+    kp, ks = _packed(k, (rows, cache.kv_heads, d), cache.device)
+    vp, vs = _packed(v, (rows, cache.kv_heads, d), cache.device)
+    _want(k.dtype is v.dtype and (q is None) == (q_out is None))
+    qp = qs = op = os_ = heads = 0
+    if q is not None:
+        _want(q.dim() == 3 and q.dtype is k.dtype and q_out.dtype is k.dtype)
+        heads = q.shape[1]
+        qp, qs = _packed(q, (rows, heads, d), cache.device)
+        op, os_ = _packed(q_out, (rows, heads, d), cache.device)
+    _check(_lib.qllm_kv_rotate_append(cache._p, layer, qp or None, qs, op or None, os_, heads, kp, ks, vp, vs, _xdtype(k), rotary._p, batch._p,
+                                      _kv_stream(stream, cache.device, batch.device)))
 
 
 def qllm_kv_read(cache, layer, k, v, batch, stream=None):
