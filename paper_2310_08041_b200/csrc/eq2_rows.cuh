@@ -54,10 +54,11 @@ __device__ __forceinline__ int store_codes8(const float (&f)[8], const RowQuant&
         return int(__dp4a(nib, 0x01010101u, 0u));
     }
     // saturating packs clamp to 0 .. 255; 6-bit codes are cut at 63 first
-    uint32_t p0 = pack_sat_u8(min(n[3], q.top), min(n[2], q.top), 0u);
-    p0 = pack_sat_u8(min(n[1], q.top), min(n[0], q.top), p0);
-    uint32_t p1 = pack_sat_u8(min(n[7], q.top), min(n[6], q.top), 0u);
-    p1 = pack_sat_u8(min(n[5], q.top), min(n[4], q.top), p1);
+    if (bits == 6) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) n[j] = min(n[j], q.top);
+    }
+    const uint32_t p0 = pack_sat_u8(n[1], n[0], pack_sat_u8(n[3], n[2], 0u)), p1 = pack_sat_u8(n[5], n[4], pack_sat_u8(n[7], n[6], 0u));
     reinterpret_cast<uint2*>(out_row)[g] = make_uint2(p0, p1);
     return int(__dp4a(p1, 0x01010101u, __dp4a(p0, 0x01010101u, 0u)));
 }

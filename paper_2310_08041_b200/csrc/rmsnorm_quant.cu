@@ -12,11 +12,12 @@
 // trees; C terms of one sign are off by at most (8 NV + 12) 2^-24.
 //
 // What bounds it: HBM.  A row is read once, kept in registers, and written once.  The CTAs stay and walk the rows (gamma stays in
-// registers, the next row is requested before the present one's exchange); the code sum of a row leaves with the next row's exchange.
+// registers, the next rows are on their way); the code sum of a row leaves with the next row's exchange.
 
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "common.h"
 #include "device_utils.cuh"
@@ -38,6 +39,7 @@ struct NormArgs {
     uint8_t* codes;                                        // may be null: only h and y
     float *a_scale, *a_zero;
     int32_t* a_rowsum;                                     // may be null
+    float inv_c, inv_levels;                               // 1 / C, 1 / (2^bits - 1)
 };
 
 // 8 channels as they lie in memory.  Loads are plain ones: h may be the residual or x in place.
@@ -81,16 +83,27 @@ struct Raw<float> {
     }
 };
 
+// x / d correctly rounded for d = 15, 63, 255 and inv = 1 / d: the product corrected by its exact residual (Markstein), checked for
+// every mantissa; where something might underflow, the division.
+__device__ __forceinline__ float by_levels(float x, float d, float inv) {
+    const float q = x * inv;
+    return x > 1e-30f && x < 1e38f ? fmaf(fmaf(-d, q, x), inv, q) : x / d;
+}
 // Eq. 2's parameters of u' and the row's factor.  ok = false: the row's numbers are too large or too small for float32 squares or
 // for a reciprocal of the scale (2^-120: its reciprocal and the products with it stay finite).
 struct RowStats {
     float alpha, inv, zero, r;
     bool ok;
-    __device__ __forceinline__ RowStats(float ssq, float lo, float hi, int C, float eps, float qmax) {
-        const float ms = ssq / float(C) + eps;
-        eq2_params(lo, hi, qmax, alpha, inv, zero);
-        r = 1.f / sqrtf(ms);
-        ok = ms < INFINITY && ms >= 0x1p-80f && hi - lo < INFINITY && (alpha >= 0x1p-120f);
+    RowStats() = default;
+    __device__ __forceinline__ RowStats(float ssq, float lo, float hi, const NormArgs& a, float qmax) {
+        const float ms = fmaf(ssq, a.inv_c, a.eps);
+        alpha = by_levels(hi - lo, qmax, a.inv_levels);
+        if (!(hi > lo)) alpha = lo != 0.f ? fabsf(lo) : 1.f;
+        inv = __frcp_rn(alpha);
+        zero = -rintf(lo * inv);
+        r = rsqrtf(ms);                                    // two steps of float32 off at most; corrected once
+        r = fmaf(0.5f * r, fmaf(-ms * r, r, 1.f), r);
+        ok = ms < INFINITY && ms >= 0x1p-80f && hi - lo < INFINITY && alpha >= 0x1p-120f;
     }
 };
 // The factor of a row whose channels have been multiplied by `by` (a power of two), in 64 bits.  0 for a row of zeros with eps = 0 and
@@ -105,271 +118,312 @@ __device__ __forceinline__ float scale_of(float top) {
     return exp2f(float(-min(max(e, -126), 126)));
 }
 
-// MAP: a thread's 8 output channels beside its 8 source channels; u goes through shared memory at word (k % 8) C / 8 + k / 8, where
-// neighbouring threads' neighbouring channels lie side by side.  Rows of the map with one entry (all but the merged ones) are held
-// in registers for the whole launch: word and coefficient; merged rows are walked in the caller's arrays.
-template <typename XT, int NV, int R, bool MAP, int MAXT>
-__global__ void __launch_bounds__(MAXT)
+// Shared memory of the kernel below: S rows as they arrive, each thread's pieces side by side; with a map u (8 words for each of the
+// CTA's vector places), behind it the values of merged outputs, then the merged outputs' entries as (address of u's word, coefficient)
+// and where each one's entries begin and end.
+constexpr int merged_cap(int places) { return 2 * places; }                 // of 8 * places outputs
+constexpr int entry_cap(int places) { return 4 * places; }
+constexpr int map_smem(int places) { return (8 * places + merged_cap(places)) * 4 + entry_cap(places) * 8 + merged_cap(places) * 4; }
+
+__device__ __forceinline__ float shared_at(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// A thread's NV vectors of 8 channels: its own pieces of the next S - 1 rows are on their way into shared memory (asynchronous copies of
+// 16 bytes that only the thread itself reads again: no barrier) while it works on the present one.
+//
+// MAP: a thread also owns 8 NV output channels.  u goes through shared memory at word (k % 8) P + k / 8 (P = NV MAXT places), where
+// neighbouring threads' neighbouring channels lie side by side.  An output with one entry (all but the merged ones) is an address and a
+// coefficient, held in registers for the whole launch.  Merged outputs are dealt out evenly: thread i sums the i-th one and leaves it behind
+// u, from where its owner takes it like any other word.  What a map has beyond the room for these lists is summed by its owner from the
+// caller's arrays.
+template <typename XT, int NV, bool MAP, int MAXT, int MINB, int S>
+__global__ void __launch_bounds__(MAXT, MINB)
 rmsnorm_quant_kernel(const NormArgs a) {
-    extern __shared__ float s_u[];                         // MAP: R rows of u
-    __shared__ float s_red[2][3 * R][32];
-    __shared__ int s_sum[2][R][32];
-    __shared__ float s_top[R][32];
+    constexpr int VB = 8 * int(sizeof(XT)), VQ = VB / 16;  // bytes and 16-byte pieces of a vector
+    constexpr int P = NV * MAXT;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ float s_red[2][3][32];
+    __shared__ int s_sum[2][32], s_count[2];
+    __shared__ float s_top[32];
     const int t = threadIdx.x, T = blockDim.x, lane = t & 31, warp = t >> 5, nw = T >> 5, C = a.C, nvec = C / 8;
     const XT* x = static_cast<const XT*>(a.x);
     const XT* res = static_cast<const XT*>(a.residual);
-    XT* h = static_cast<XT*>(a.h);
-    XT* y = static_cast<XT*>(a.y);
     const float qmax = float((1 << a.bits) - 1);
     const bool quant = a.codes != nullptr;
-    const int64_t step = int64_t(gridDim.x) * R;
+    const int stage = (res ? 2 : 1) * NV * T * VB;
+    const int64_t step = gridDim.x;
     asm volatile("griddepcontrol.wait;" ::: "memory");     // launched as a dependent
 
-    Raw<XT> rx[R][NV], rr[R][NV];
-    const auto request = [&](int64_t m0) {
+    // piece q of vector i of x (or, n = 1, the residual) in a stage
+    const auto piece = [&](int st, int n, int i, int q) { return smem + st * stage + (((n * NV + i) * VQ + q) * T + t) * 16; };
+    const auto request = [&](int st, int64_t m) {
+        if (m < a.M) {
+            const uint8_t* px = reinterpret_cast<const uint8_t*>(x + m * C + 8 * t);
+            const uint8_t* pr = reinterpret_cast<const uint8_t*>(res + m * C + 8 * t);
 #pragma unroll
-        for (int q = 0; q < R; ++q)
+            for (int i = 0; i < NV; ++i)
+                if (t + i * T < nvec) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int g = t + i * T;
-                if (m0 + q < a.M && g < nvec) {
-                    const int64_t at = (m0 + q) * C + 8 * g;
-                    rx[q][i].load(x + at);
-                    if (res) rr[q][i].load(res + at);
+                    for (int q = 0; q < VQ; ++q) {
+                        cp_async16(piece(st, 0, i, q), px + i * T * VB + 16 * q);
+                        if (res) cp_async16(piece(st, 1, i, q), pr + i * T * VB + 16 * q);
+                    }
                 }
-            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    const auto flush = [&](const int (&part)[R][32], int64_t first) {      // by the first warp
-        if (!a.a_rowsum) return;
+    const auto arrived = [&](int st, int n, int i, float (&f)[8]) {
+        Raw<XT> r;
+        if constexpr (VQ == 1) {
+            r.v = *reinterpret_cast<const uint4*>(piece(st, n, i, 0));
+        } else {
+            r.a = *reinterpret_cast<const float4*>(piece(st, n, i, 0));
+            r.b = *reinterpret_cast<const float4*>(piece(st, n, i, 1));
+        }
+        r.get(f);
+    };
+    // h of the thread's i-th vector, times a power of two
+    const auto sum_at = [&](int st, int i, float by, float (&f)[8]) {
+        arrived(st, 0, i, f);
+        if (res) {
+            float o[8];
+            arrived(st, 1, i, o);
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            const int s = warp_sum_int(lane < nw ? part[q][lane] : 0);
-            if (lane == 0 && first + q < a.M) a.a_rowsum[first + q] = s;
+            for (int j = 0; j < 8; ++j) f[j] += o[j];
+        }
+        if (by != 1.f) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] *= by;
         }
     };
-    int64_t m0 = int64_t(blockIdx.x) * R;
-    request(m0);
+    int64_t m = blockIdx.x;
+#pragma unroll
+    for (int i = 0; i + 1 < S; ++i) request(i, m + i * step);
+
     float gamma[NV][8];
-    uint32_t word[MAP ? NV : 1][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) gamma[i][j] = t + i * T < nvec ? __ldg(a.gamma + 8 * (t + i * T) + j) : 0.f;
+
+    float* s_u = reinterpret_cast<float*>(smem + S * stage);
+    uint2* s_entry = reinterpret_cast<uint2*>(s_u + 8 * P + merged_cap(P));
+    uint32_t* s_list = reinterpret_cast<uint32_t*>(s_entry + entry_cap(P));
+    const uint32_t u_addr = uint32_t(__cvta_generic_to_shared(s_u));
+    uint32_t addr[MAP ? NV : 1][8], walked[MAP ? NV : 1];
     float coef[MAP ? NV : 1][8];
-    uint32_t merged[MAP ? NV : 1];
+    const auto addr_of = [&](int k) { return u_addr + 4u * ((uint32_t(k) & 7u) * P + (uint32_t(k) >> 3)); };
+    int merged = 0;
+    if (MAP) {
+        if (t < 2) s_count[t] = 0;
+        __syncthreads();
+        uint32_t several[NV];                              // outputs with several entries
+        int rows = 0, entries = 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int g = t + i * T;
+        for (int i = 0; i < NV; ++i) {
+            const int g = t + i * T;
+            int from[9];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) gamma[i][j] = g < nvec ? a.gamma[8 * g + j] : 0.f;
-        if (MAP) {
-            merged[i] = 0;
+            for (int j = 0; j < 9; ++j) from[j] = g < nvec ? __ldg(a.ptr + 8 * g + j) : j;
+            several[i] = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                word[i][j] = 0;
-                coef[i][j] = 0.f;
-                if (g < nvec) {
-                    const int b = a.ptr[8 * g + j], e = a.ptr[8 * g + j + 1];
-                    if (e - b == 1) {
-                        const uint32_t k = uint32_t(a.src[b]);
-                        word[i][j] = (k & 7u) * uint32_t(nvec) + (k >> 3);
-                        coef[i][j] = a.coef[b];
-                    } else {
-                        merged[i] |= 1u << j;
-                    }
+                addr[i][j] = g < nvec ? addr_of(__ldg(a.src + from[j])) : u_addr;
+                coef[i][j] = g < nvec ? __ldg(a.coef + from[j]) : 0.f;
+                const int n = from[j + 1] - from[j];
+                if (n > 1) {
+                    several[i] |= 1u << j;
+                    ++rows;
+                    entries += min(n, entry_cap(P) + 1);
                 }
             }
+            walked[i] = 0;
         }
-    }
-
-    int parity = 0, turn = 0;
-    int64_t before = -1;                                   // first row of the pass whose code sums wait in s_sum[turn ^ 1]
-    for (; m0 < a.M; m0 += step) {
-        const int live = int(min(int64_t(R), a.M - m0));
-        float f[R][NV][8], v[MAP ? R : 1][MAP ? NV : 1][8], by[R];
+        int slot = merged_cap(P), at = 0;
+        if (rows) {
+            slot = atomicAdd(s_count, rows);
+            at = atomicAdd(s_count + 1, min(entries, entry_cap(P) + 1));
+        }
+        const bool room = slot + rows <= merged_cap(P) && at + entries <= entry_cap(P);
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            by[q] = 1.f;
+        for (int i = 0; i < NV; ++i) {
+            walked[i] = room ? 0 : several[i];
+            const uint32_t own = room ? several[i] : 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (own >> j & 1) {
+                    addr[i][j] = u_addr + 4u * uint32_t(8 * P + slot + __popc(own & ((1u << j) - 1)));
+                    coef[i][j] = 1.f;
+                }
+#pragma unroll 1
+            for (uint32_t left = own; left; left &= left - 1) {
+                const int c = 8 * (t + i * T) + __ffs(left) - 1, b = __ldg(a.ptr + c), e = __ldg(a.ptr + c + 1);
+                s_list[slot++] = uint32_t(at) | uint32_t(at + e - b) << 16;
+#pragma unroll 1
+                for (int k = b; k < e; ++k) s_entry[at++] = make_uint2(addr_of(__ldg(a.src + k)), __float_as_uint(__ldg(a.coef + k)));
+            }
+        }
+        if (!room)
+            for (int k = 0; k < rows; ++k)
+                if (slot + k < merged_cap(P)) s_list[slot + k] = 0;          // no entries
+        __syncthreads();
+        merged = min(s_count[0], merged_cap(P));
+    }
+    const auto flush = [&](const int (&part)[32], int64_t row) {           // by the first warp
+        const int s = warp_sum_int(lane < nw ? part[lane] : 0);
+        if (lane == 0 && a.a_rowsum) a.a_rowsum[row] = s;
+    };
+
+    int parity = 0, turn = 0, st = 0;
+    int64_t before = -1;                                   // the row whose code sums wait in s_sum[turn ^ 1]
+    for (; m < a.M; m += step) {
+        request(st == 0 ? S - 1 : st - 1, m + (S - 1) * step);             // into what the last row was taken from
+        asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+        float f[MAP ? 1 : NV][8], v[MAP ? NV : 1][8], by = 1.f;
+        float ssq, lo, hi;
+        RowStats rs;
+        for (int pass = 0;; ++pass) {
+            ssq = 0.f;
+            lo = INFINITY;
+            hi = -INFINITY;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int g = t + i * T;
-                if (q < live && g < nvec) {
-                    rx[q][i].get(f[q][i]);
-                    if (res) {
-                        float o[8];
-                        rr[q][i].get(o);
+                float (&e)[8] = f[MAP ? 0 : i];
+                if (g < nvec) {
+                    sum_at(st, i, by, e);
+                    if (a.h && pass == 0) Raw<XT>::store(static_cast<XT*>(a.h) + m * C + 8 * g, e);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) f[q][i][j] += o[j];
-                    }
-                    if (h) Raw<XT>::store(h + (m0 + q) * C + 8 * g, f[q][i]);
-                } else {
+                    for (int j = 0; j < 8; ++j) ssq = fmaf(e[j], e[j], ssq);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) f[q][i][j] = 0.f;
-                }
-            }
-        }
-        request(m0 + step);
-
-        float ssq[R], lo[R], hi[R];
-        for (int pass = 0;; ++pass) {
-#pragma unroll
-            for (int q = 0; q < R; ++q) {
-                ssq[q] = 0.f;
-                lo[q] = INFINITY;
-                hi[q] = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int g = t + i * T;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) ssq[q] = fmaf(f[q][i][j], f[q][i][j], ssq[q]);
-                    if (g < nvec) {
-#pragma unroll
-                        for (int j = 0; j < 8; j += 2) {
-                            const float u0 = f[q][i][j] * gamma[i][j], u1 = f[q][i][j + 1] * gamma[i][j + 1];
-                            if (MAP) {
-                                s_u[q * C + j * nvec + g] = u0;
-                                s_u[q * C + (j + 1) * nvec + g] = u1;
-                            } else {
-                                lo[q] = min3(lo[q], u0, u1);
-                                hi[q] = max3(hi[q], u0, u1);
-                            }
+                    for (int j = 0; j < 8; j += 2) {
+                        const float u0 = e[j] * gamma[i][j], u1 = e[j + 1] * gamma[i][j + 1];
+                        if (MAP) {
+                            s_u[j * P + g] = u0;
+                            s_u[(j + 1) * P + g] = u1;
+                        } else {
+                            lo = min3(lo, u0, u1);
+                            hi = max3(hi, u0, u1);
                         }
                     }
                 }
             }
             if (MAP) {
                 __syncthreads();
+                for (int i = t; i < merged; i += T) {
+                    const uint32_t range = s_list[i];
+                    double s = 0.0;
+                    for (uint32_t k = range & 0xFFFFu; k < range >> 16; ++k) {
+                        const uint2 e = s_entry[k];
+                        s = fma(double(__uint_as_float(e.y)), double(shared_at(e.x)), s);
+                    }
+                    s_u[8 * P + i] = float(s);
+                }
+                __syncthreads();
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int g = t + i * T;
                     if (g < nvec) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-#pragma unroll
-                            for (int q = 0; q < R; ++q) v[q][i][j] = coef[i][j] * s_u[q * C + word[i][j]];
-                        if (merged[i]) {
+                        for (int j = 0; j < 8; ++j) v[i][j] = coef[i][j] * shared_at(addr[i][j]);
+                        if (walked[i]) {
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
-                                if (merged[i] >> j & 1) {
+                                if (walked[i] >> j & 1) {
                                     const int e = a.ptr[8 * g + j + 1];
-                                    double s[R];
-#pragma unroll
-                                    for (int q = 0; q < R; ++q) s[q] = 0.0;
-                                    for (int k = a.ptr[8 * g + j]; k < e; ++k) {
-                                        const uint32_t from = uint32_t(a.src[k]), w = (from & 7u) * uint32_t(nvec) + (from >> 3);
-                                        const double c = double(a.coef[k]);
-#pragma unroll
-                                        for (int q = 0; q < R; ++q) s[q] = fma(c, double(s_u[q * C + w]), s[q]);
-                                    }
-#pragma unroll
-                                    for (int q = 0; q < R; ++q) v[q][i][j] = float(s[q]);
+                                    double s = 0.0;
+#pragma unroll 1
+                                    for (int k = a.ptr[8 * g + j]; k < e; ++k) s = fma(double(a.coef[k]), double(shared_at(addr_of(a.src[k]))), s);
+                                    v[i][j] = float(s);
                                 }
                         }
 #pragma unroll
-                        for (int q = 0; q < R; ++q)
-#pragma unroll
-                            for (int j = 0; j < 8; j += 2) {
-                                lo[q] = min3(lo[q], v[q][i][j], v[q][i][j + 1]);
-                                hi[q] = max3(hi[q], v[q][i][j], v[q][i][j + 1]);
-                            }
+                        for (int j = 0; j < 8; j += 2) {
+                            lo = min3(lo, v[i][j], v[i][j + 1]);
+                            hi = max3(hi, v[i][j], v[i][j + 1]);
+                        }
                     }
                 }
             }
             parity ^= 1;
-#pragma unroll
-            for (int q = 0; q < R; ++q) {
-                const float s = warp_sum(ssq[q]), l = redux_min(lo[q]), u = redux_max(hi[q]);
-                if (lane == 0) {
-                    s_red[parity][3 * q][warp] = s;
-                    s_red[parity][3 * q + 1][warp] = l;
-                    s_red[parity][3 * q + 2][warp] = u;
-                }
+            const float s = warp_sum(ssq), l = redux_min(lo), u = redux_max(hi);
+            if (lane == 0) {
+                s_red[parity][0][warp] = s;
+                s_red[parity][1][warp] = l;
+                s_red[parity][2][warp] = u;
             }
             __syncthreads();
-            bool good = true;
-#pragma unroll
-            for (int q = 0; q < R; ++q) {
-                ssq[q] = warp_sum(lane < nw ? s_red[parity][3 * q][lane] : 0.f);
-                lo[q] = redux_min(lane < nw ? s_red[parity][3 * q + 1][lane] : INFINITY);
-                hi[q] = redux_max(lane < nw ? s_red[parity][3 * q + 2][lane] : -INFINITY);
-                if (q < live) good = good && RowStats(ssq[q], lo[q], hi[q], C, a.eps, qmax).ok;
-            }
-            if (good || pass) break;                       // the same in every thread
+            ssq = warp_sum(lane < nw ? s_red[parity][0][lane] : 0.f);
+            lo = redux_min(lane < nw ? s_red[parity][1][lane] : INFINITY);
+            hi = redux_max(lane < nw ? s_red[parity][2][lane] : -INFINITY);
+            rs = RowStats(ssq, lo, hi, a, qmax);
+            if (pass || rs.ok) break;                      // the same in every thread
             // a row with very large or very small numbers: all of it by a power of two, exactly, and once more
+            float top = 0.f;
+#pragma unroll 1
+            for (int i = 0; i < NV; ++i)
+                if (t + i * T < nvec) {
+                    float e[8];
+                    sum_at(st, i, 1.f, e);
 #pragma unroll
-            for (int q = 0; q < R; ++q) {
-                float top = 0.f;
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[q][i][j]));
-                top = redux_max(top);
-                if (lane == 0) s_top[q][warp] = top;
-            }
+                    for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(e[j]));
+                }
+            top = redux_max(top);
+            if (lane == 0) s_top[warp] = top;
             __syncthreads();
-#pragma unroll
-            for (int q = 0; q < R; ++q) {
-                const float top = redux_max(lane < nw ? s_top[q][lane] : 0.f);
-                if (q < live && !RowStats(ssq[q], lo[q], hi[q], C, a.eps, qmax).ok && top > 0.f && top < INFINITY) {
-                    by[q] = scale_of(top);
-#pragma unroll
-                    for (int i = 0; i < NV; ++i)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) f[q][i][j] *= by[q];
-                }
-            }
+            top = redux_max(lane < nw ? s_top[lane] : 0.f);
+            if (top > 0.f && top < INFINITY) by = scale_of(top);
         }
-        // code sums of the rows before: their warps' parts were written in front of this exchange
+        // the code sum of the row before: its warps' parts were written in front of this exchange
         if (quant && before >= 0 && warp == 0) flush(s_sum[turn ^ 1], before);
+        float r = rs.r, scale = rs.alpha * rs.r;
+        if (!rs.ok || by != 1.f) {
+            const double wide = scaled_factor(ssq, C, a.eps, by);
+            r = float(wide);
+            scale = float(wide * double(rs.alpha));
+        }
+        if (lo == 0.f && hi == 0.f) scale = 1.f;           // Eq. 2's choice for a row of zeros
+        const RowQuant rq(lo, hi, rs.inv, rs.zero, qmax);
+        uint8_t* row = a.codes + m * (a.bits == 4 ? C / 2 : C);
+        int sum = 0;
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            if (q >= live) break;
-            const RowStats st(ssq[q], lo[q], hi[q], C, a.eps, qmax);
-            float r = st.r, scale = st.alpha * st.r;
-            if (!st.ok || by[q] != 1.f) {
-                const double wide = scaled_factor(ssq[q], C, a.eps, by[q]);
-                r = float(wide);
-                scale = float(wide * double(st.alpha));
-            }
-            if (lo[q] == 0.f && hi[q] == 0.f) scale = 1.f; // Eq. 2's choice for a row of zeros
-            if (y) {
+        for (int i = 0; i < NV; ++i) {
+            const int g = t + i * T;
+            if (g < nvec) {
+                if (!MAP || a.y) {
+                    float e[8];
+                    if constexpr (MAP) {
+                        sum_at(st, i, by, e);
+                    } else {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int g = t + i * T;
-                    if (g < nvec) {
-                        float o[8];
+                        for (int j = 0; j < 8; ++j) e[j] = f[i][j];
+                    }
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) o[j] = f[q][i][j] * gamma[i][j] * r;
-                        Raw<XT>::store(y + (m0 + q) * C + 8 * g, o);
+                    for (int j = 0; j < 8; ++j) e[j] *= gamma[i][j];
+                    if (!MAP && quant) sum += store_codes8(e, rq, a.bits, row, g);
+                    if (a.y) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) e[j] *= r;
+                        Raw<XT>::store(static_cast<XT*>(a.y) + m * C + 8 * g, e);
                     }
                 }
-            }
-            if (quant) {
-                const RowQuant rq(lo[q], hi[q], st.inv, st.zero, qmax);
-                uint8_t* row = a.codes + (m0 + q) * (a.bits == 4 ? C / 2 : C);
-                int sum = 0;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int g = t + i * T;
-                    if (g < nvec) {
-                        if (MAP) {
-                            sum += store_codes8(v[q][i], rq, a.bits, row, g);
-                        } else {
-                            float u[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) u[j] = f[q][i][j] * gamma[i][j];
-                            sum += store_codes8(u, rq, a.bits, row, g);
-                        }
-                    }
-                }
-                if (a.a_rowsum) {
-                    sum = warp_sum_int(sum);
-                    if (lane == 0) s_sum[turn][q][warp] = sum;
-                }
-                if (t == 0) {
-                    a.a_scale[m0 + q] = scale;
-                    a.a_zero[m0 + q] = st.zero;
-                }
+                if (MAP) sum += store_codes8(v[i], rq, a.bits, row, g);
             }
         }
-        before = m0;
+        if (quant) {
+            sum = warp_sum_int(sum);
+            if (lane == 0) s_sum[turn][warp] = sum;
+            if (t == 0) {
+                a.a_scale[m] = scale;
+                a.a_zero[m] = rs.zero;
+            }
+        }
+        before = m;
         turn ^= 1;
+        st = st + 1 == S ? 0 : st + 1;
     }
     if (quant && before >= 0) {
         __syncthreads();
@@ -418,12 +472,12 @@ rmsnorm_quant_any(const NormArgs a) {
             }
             ssq = block_sum(ssq, red);
             block_minmax(lo, hi, red);
-            if (pass || RowStats(ssq, lo, hi, C, a.eps, qmax).ok) break;
+            if (pass || RowStats(ssq, lo, hi, a, qmax).ok) break;
             float none = 0.f;
             block_minmax(none, top, red);
             if (top > 0.f && top < INFINITY) by = scale_of(top);
         }
-        const RowStats st(ssq, lo, hi, C, a.eps, qmax);
+        const RowStats st(ssq, lo, hi, a, qmax);
         float r = st.r, scale = st.alpha * st.r;
         if (!st.ok || by != 1.f) {
             const double wide = scaled_factor(ssq, C, a.eps, by);
@@ -460,12 +514,23 @@ rmsnorm_quant_any(const NormArgs a) {
     }
 }
 
-template <typename XT, int NV, int R, bool MAP, int MAXT>
+template <typename XT, int NV, bool MAP, int MAXT, int MINB, int S>
 int launch_norm_rows(const NormArgs& a, cudaStream_t st) {
+    constexpr auto kern = rmsnorm_quant_kernel<XT, NV, MAP, MAXT, MINB, S>;
     const int nvec = a.C / 8, T = ((nvec + NV - 1) / NV + 31) / 32 * 32;
-    const int64_t grid = std::min((a.M + R - 1) / R, int64_t(device_sm_count()) * std::max(1, 1024 / T));
-    QLLM_CUDA_TRY(launch_dependent(rmsnorm_quant_kernel<XT, NV, R, MAP, MAXT>, dim3(unsigned(grid)), dim3(unsigned(T)),
-                                   MAP ? size_t(R) * a.C * 4 : 0, st, a));
+    const int smem = S * (a.residual ? 2 : 1) * NV * T * 8 * int(sizeof(XT)) + (MAP ? map_smem(NV * MAXT) : 0);
+    QLLM_CUDA_TRY(allow_smem<kern>(kSmemBudget - 2048));
+    static std::atomic<int> known{0};
+    int regs = known.load(std::memory_order_relaxed);
+    if (!regs) {
+        cudaFuncAttributes fa;
+        QLLM_CUDA_TRY(cudaFuncGetAttributes(&fa, kern));
+        known.store(regs = (fa.numRegs + 7) / 8 * 8, std::memory_order_relaxed);
+    }
+    // the CTAs that an SM holds at once: they stay and walk the rows
+    const int per_sm = std::max(1, std::min({32, 2048 / T, 65536 / (regs * T), kSmemBudget / (smem + 2048)}));
+    const int64_t grid = std::min(a.M, int64_t(device_sm_count()) * per_sm);
+    QLLM_CUDA_TRY(launch_dependent(kern, dim3(unsigned(grid)), dim3(unsigned(T)), size_t(smem), st, a));
     return after_launch();
 }
 
@@ -473,13 +538,15 @@ template <typename XT>
 int launch_norm(const NormArgs& a, cudaStream_t st) {
     const int64_t sms = device_sm_count();
     if (a.C % 8 == 0) {
+        constexpr bool half = sizeof(XT) == 2;
         if (a.ptr) {
-            if (a.C <= 4096) return a.M > 2 * sms ? launch_norm_rows<XT, 1, 2, true, 512>(a, st) : launch_norm_rows<XT, 1, 1, true, 512>(a, st);
-            if (a.C <= 8192) return launch_norm_rows<XT, 2, 1, true, 512>(a, st);
+            if (a.C <= 8192 && a.M <= 2 * sms) return launch_norm_rows<XT, 1, true, 1024, 1, 1>(a, st);
+            if (a.C <= 4096) return launch_norm_rows<XT, 2, true, 256, 2, 3>(a, st);
+            if (a.C <= 8192) return launch_norm_rows<XT, 2, true, 512, 1, half ? 2 : 1>(a, st);
         } else {
-            if (a.C <= 8192 && a.M <= 2 * sms) return launch_norm_rows<XT, 1, 1, false, 1024>(a, st);
-            if (a.C <= 8192) return launch_norm_rows<XT, 2, 1, false, 512>(a, st);
-            if (a.C <= 16384) return launch_norm_rows<XT, 4, 1, false, 512>(a, st);
+            if (a.C <= 8192 && a.M <= 2 * sms) return launch_norm_rows<XT, 1, false, 1024, 1, 1>(a, st);
+            if (a.C <= 8192) return launch_norm_rows<XT, 2, false, 512, 2, 3>(a, st);
+            if (a.C <= 16384) return launch_norm_rows<XT, 4, false, 512, 1, half ? 3 : 1>(a, st);
         }
     }
     const auto kern = rmsnorm_quant_any<XT>;
@@ -562,7 +629,8 @@ extern "C" int qllm_rmsnorm_quant(const void* x, const void* residual, int x_dty
     if (!x || !gamma || (!codes && !y && !h) || (codes && (!a_scale || !a_zero))) return QLLM_ERR_NULL;
     if ((map_ptr || map_src || map_coef) && (!map_ptr || !map_src || !map_coef || !codes)) return QLLM_ERR_NULL;
     if (!aligned16(x) || !aligned16(residual) || !aligned16(h) || !aligned16(y) || !aligned16(codes)) return QLLM_ERR_ALIGN;
-    const NormArgs a{x, residual, M, C, gamma, eps, map_ptr, map_src, map_coef, codes ? bits : 8, h, y, codes, a_scale, a_zero, a_rowsum};
+    const int b = codes ? bits : 8;
+    const NormArgs a{x, residual, M, C, gamma, eps, map_ptr, map_src, map_coef, b, h, y, codes, a_scale, a_zero, a_rowsum, 1.f / float(C), 1.f / float((1 << b) - 1)};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return x_dtype == QLLM_BF16 ? launch_norm<__nv_bfloat16>(a, st) : launch_norm<float>(a, st);
 }
