@@ -137,12 +137,14 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+_DTYPES = {torch.float32: QLLM_F32, torch.bfloat16: QLLM_BF16}
+
+
 def _xdtype(t):
-    if t.dtype == torch.float32:
-        return QLLM_F32
-    if t.dtype == torch.bfloat16:
-        return QLLM_BF16
-    raise QllmError(QLLM_ERR_DTYPE)
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise QllmError(QLLM_ERR_DTYPE)
+    return d
 
 
 # --------------------------------------------------------------------------- device calls
@@ -161,59 +163,52 @@ def qllm_quantize_rows(x, bits, codes, a_scale, a_zero, a_rowsum=None, stream=No
                                    _stream(stream)))
 
 
+def _flat(t, dtype, numel, device):
+    """Address of a contiguous tensor of this type, size and device."""
+    if t.dtype is not dtype:
+        raise QllmError(QLLM_ERR_DTYPE)
+    if t.numel() != numel:
+        raise QllmError(QLLM_ERR_SHAPE)
+    assert t.get_device() == device and t.is_contiguous(), "device arguments must be contiguous CUDA tensors of one device"
+    return t.data_ptr()
+
+
 def qllm_rmsnorm_quant(x, gamma, bits, codes, a_scale, a_zero, a_rowsum=None, residual=None, h=None, y=None, map=None, eps=1e-5, stream=None):
     """x, residual, h, y [M][C] of one dtype (the last three may be None); gamma float32 [C]; map: None or (ptr, src, coef) device
-    tensors as for qllm_reassemble_quant.  codes = None (then a_scale = a_zero = None too): only h and y."""
-    _want(x.dim() == 2)
+    tensors as for qllm_reassemble_quant.  codes = None (then a_scale = a_zero = a_rowsum = None too): only h and y."""
     M, C = x.shape
-    dev = x.get_device()
-    for t in (residual, h, y):
-        if t is not None:
-            _want(t.shape == x.shape)
-            if t.dtype is not x.dtype:
-                raise QllmError(QLLM_ERR_DTYPE)
-            _on(dev, t)
-    _f32(dev, (C,), gamma)
-    if codes is None:
-        _want(a_scale is None and a_zero is None and a_rowsum is None)
-    else:
-        _codes(dev, codes, M, C, bits)
-        _f32(dev, (M,), a_scale, a_zero)
+    n, dev, dtype = M * C, x.get_device(), x.dtype
+    st = _kv_stream(stream, dev, dev)
+    xp, gp = _flat(x, dtype, n, dev), _flat(gamma, torch.float32, C, dev)
+    rp = None if residual is None else _flat(residual, dtype, n, dev)
+    hp = None if h is None else _flat(h, dtype, n, dev)
+    yp = None if y is None else _flat(y, dtype, n, dev)
+    cp = sp = zp = tp = mp = ms = mc = None
+    if codes is not None:
+        cp = _flat(codes, torch.uint8, n // 2 if bits == 4 else n, dev)
+        sp, zp = _flat(a_scale, torch.float32, M, dev), _flat(a_zero, torch.float32, M, dev)
         if a_rowsum is not None:
-            _ints(dev, a_rowsum)
-            _want(a_rowsum.numel() == M)
-    ptr, src, coef = map if map is not None else (None, None, None)
+            tp = _flat(a_rowsum, torch.int32, M, dev)
+    else:
+        _want(a_scale is None and a_zero is None and a_rowsum is None)
     if map is not None:
-        _ints(dev, ptr, src)
-        _want(ptr.numel() == C + 1 and src.numel() == coef.numel())
-        _f32(dev, (src.numel(),), coef)
-    _check(_lib.qllm_rmsnorm_quant(_dp(x), _dp(residual), _xdtype(x), M, C, _dp(gamma), eps, _dp(ptr), _dp(src), _dp(coef), bits, _dp(h), _dp(y),
-                                   _dp(codes), _dp(a_scale), _dp(a_zero), _dp(a_rowsum), _kv_stream(stream, dev, dev)))
+        ptr, src, coef = map
+        nnz = src.numel()
+        mp, ms, mc = _flat(ptr, torch.int32, C + 1, dev), _flat(src, torch.int32, nnz, dev), _flat(coef, torch.float32, nnz, dev)
+    rc = _lib.qllm_rmsnorm_quant(xp, rp, _xdtype(x), M, C, gp, eps, mp, ms, mc, bits, hp, yp, cp, sp, zp, tp, st)
+    if rc:
+        raise QllmError(rc)
 
 
 def qllm_dequantize_rows(codes, a_scale, a_zero, bits, out, stream=None):
     """out [M][C] (float32 or bf16): the values that codes stand for, a_scale (code - a_zero)."""
-    _want(out.dim() == 2)
     M, C = out.shape
-    dev = out.get_device()
-    _codes(dev, codes, M, C, bits)
-    _f32(dev, (M,), a_scale, a_zero)
-    _check(_lib.qllm_dequantize_rows(_dp(codes), _dp(a_scale), _dp(a_zero), M, C, bits, _dp(out), _xdtype(out), _kv_stream(stream, dev, dev)))
-
-
-def _codes(device, codes, M, C, bits):
-    if codes.dtype != torch.uint8:
-        raise QllmError(QLLM_ERR_DTYPE)
-    _want(tuple(codes.shape) == (M, C // 2 if bits == 4 else C))
-    _on(device, codes)
-
-
-def _f32(device, shape, *ts):
-    for t in ts:
-        if t.dtype != torch.float32:
-            raise QllmError(QLLM_ERR_DTYPE)
-        _want(tuple(t.shape) == shape)
-        _on(device, t)
+    n, dev = M * C, out.get_device()
+    rc = _lib.qllm_dequantize_rows(_flat(codes, torch.uint8, n // 2 if bits == 4 else n, dev), _flat(a_scale, torch.float32, M, dev),
+                                   _flat(a_zero, torch.float32, M, dev), M, C, bits, _flat(out, out.dtype, n, dev), _xdtype(out),
+                                   _kv_stream(stream, dev, dev))
+    if rc:
+        raise QllmError(rc)
 
 
 class _AdaptersStruct(ctypes.Structure):
@@ -233,34 +228,36 @@ class Adapters:
         _want(tuple(B.shape) == (slots, N, top))
         self.device = A.get_device()
         _on(self.device, B)
-        _f32(self.device, (slots,), scale)
+        _flat(scale, torch.float32, slots, self.device)
         if rank is not None:
-            _ints(self.device, rank)
-            _want(rank.numel() == slots)
+            _flat(rank, torch.int32, slots, self.device)
         self.A, self.B, self.scale, self.rank, self.slots, self.max_rank, self.K, self.N = A, B, scale, rank, slots, top, K, N
         self._s = _AdaptersStruct(_dp(A), _dp(B), _dp(scale), _dp(rank), slots, top, K, N)
         self._p = ctypes.addressof(self._s)
 
 
-def _rows(t, rows, width, device):
+def _rows(t, shape, dtype, device):
     """Address and row stride of [rows][width] with any row stride."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise QllmError(QLLM_ERR_SHAPE)
     assert t.get_device() == device, "device arguments must be CUDA tensors of one device"
-    _want(t.shape == (rows, width) and t.stride(1) == 1)
-    return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), width)
+    row, one = t.stride()
+    _want(one == 1 or shape[1] == 1)
+    return t.data_ptr(), row if shape[0] > 1 else max(row, shape[1])
 
 
 def qllm_adapters_add(adapters, x, base, out, q_start, adapter, stream=None):
     """out [rows][N] = base (None: zeros; may be out) + scale B (A x) for the rows q_start[s] .. q_start[s + 1] - 1 of each sequence s with
     adapter[s] (negative: none); x [rows][K]; q_start int32 [seqs + 1], adapter int32 [seqs]."""
-    rows, dev = x.shape[0], adapters.device
-    xp, xs = _rows(x, rows, adapters.K, dev)
-    op, os_ = _rows(out, rows, adapters.N, dev)
-    bp, bs = (None, 0) if base is None else _rows(base, rows, adapters.N, dev)
-    _want(x.dtype is out.dtype and (base is None or base.dtype is out.dtype))
-    _ints(dev, q_start, adapter)
-    _want(q_start.numel() == adapter.numel() + 1)
-    _check(_lib.qllm_adapters_add(adapters._p, xp, xs, bp, bs, op, os_, _xdtype(x), _dp(q_start), _dp(adapter), adapter.numel(), rows,
-                                  _kv_stream(stream, dev, dev)))
+    rows, dev, dtype, seqs = x.shape[0], adapters.device, x.dtype, adapter.numel()
+    wide = (rows, adapters.N)
+    xp, xs = _rows(x, (rows, adapters.K), dtype, dev)
+    op, os_ = _rows(out, wide, dtype, dev)
+    bp, bs = (None, 0) if base is None else _rows(base, wide, dtype, dev)
+    rc = _lib.qllm_adapters_add(adapters._p, xp, xs, bp, bs, op, os_, _xdtype(x), _flat(q_start, torch.int32, seqs + 1, dev),
+                                _flat(adapter, torch.int32, seqs, dev), seqs, rows, _kv_stream(stream, dev, dev))
+    if rc:
+        raise QllmError(rc)
 
 
 def qllm_qgemm(codes, a_scale, a_zero, w_codes, w_scale, w_zero, w_colsum, bias, out, M, N, K, a_bits, w_bits,
@@ -652,19 +649,26 @@ def qllm_rotary_table(table, base=10000.0, divisor=1.0, stream=None):
 def qllm_kv_rotate_append(cache, layer, q, q_out, k, v, rotary, batch, stream=None):
     """qllm_kv_append of k, v with q [rows][q_heads][head_dim] and k turned by their positions' angles; q_out receives the queries (may be
     q; both None: keys and values only).  Any row strides."""
-    rows, d = batch.rows, cache.head_dim
-    assert rotary.device == cache.device, "device arguments must be CUDA tensors of one device"
-    kp, ks = _packed(k, (rows, cache.kv_heads, d), cache.device)
-    vp, vs = _packed(v, (rows, cache.kv_heads, d), cache.device)
-    _want(k.dtype is v.dtype and (q is None) == (q_out is None))
-    qp = qs = op = os_ = heads = 0
+    rows, d, dev, dtype = batch.rows, cache.head_dim, cache.device, k.dtype
+    assert rotary.device == dev, "device arguments must be CUDA tensors of one device"
+    shape = (rows, cache.kv_heads, d)
+    kp, ks = _packed(k, shape, dev)
+    vp, vs = _packed(v, shape, dev)
+    if v.dtype is not dtype or (q is None) != (q_out is None):
+        raise QllmError(QLLM_ERR_SHAPE)
+    qp = op = None
+    qs = os_ = heads = 0
     if q is not None:
-        _want(q.dim() == 3 and q.dtype is k.dtype and q_out.dtype is k.dtype)
+        if q.dtype is not dtype or q_out.dtype is not dtype or q.dim() != 3:
+            raise QllmError(QLLM_ERR_SHAPE)
         heads = q.shape[1]
-        qp, qs = _packed(q, (rows, heads, d), cache.device)
-        op, os_ = _packed(q_out, (rows, heads, d), cache.device)
-    _check(_lib.qllm_kv_rotate_append(cache._p, layer, qp or None, qs, op or None, os_, heads, kp, ks, vp, vs, _xdtype(k), rotary._p, batch._p,
-                                      _kv_stream(stream, cache.device, batch.device)))
+        shape = (rows, heads, d)
+        qp, qs = _packed(q, shape, dev)
+        op, os_ = _packed(q_out, shape, dev)
+    rc = _lib.qllm_kv_rotate_append(cache._p, layer, qp, qs, op, os_, heads, kp, ks, vp, vs, _xdtype(k), rotary._p, batch._p,
+                                    _kv_stream(stream, dev, batch.device))
+    if rc:
+        raise QllmError(rc)
 
 
 def qllm_kv_read(cache, layer, k, v, batch, stream=None):

@@ -19,6 +19,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "common.h"
 #include "kv_cache.cuh"
@@ -33,7 +34,7 @@ struct AdapterArgs {
     const int32_t* rank;                                   // null: max_rank
     int slots, max_rank, K, N;
     const int32_t *start, *adapter;
-    int seqs, cluster;
+    int seqs, cluster_log2;                                // CTAs of a tile: 1, 2, 4, 8 or 16
     int64_t rows;
     const void *x, *base;
     void* out;
@@ -42,17 +43,14 @@ struct AdapterArgs {
     // row ranges, cut to what exists
     __device__ __forceinline__ int first(int s) const { return int(min(max(int64_t(start[s]), int64_t(0)), rows)); }
     __device__ __forceinline__ int count(int s) const { return max(first(s + 1) - first(s), 0); }
-    // the group a sequence's rows belong to: its adapter, `slots` for none, -1 for rows that stay as they are
-    __device__ __forceinline__ int group(int s) const {
-        const int a = adapter[s];
-        return a >= 0 && a < slots ? a : base == out ? -1 : slots;
-    }
-    __device__ __forceinline__ int rank_of(int a) const { return a >= slots ? 0 : rank ? min(max(rank[a], 0), max_rank) : max_rank; }
+    // the group that rows with adapter[s] = a belong to: the adapter, `slots` for none, -1 for rows that stay as they are
+    __device__ __forceinline__ int group_of(int a) const { return a >= 0 && a < slots ? a : base == out ? -1 : slots; }
+    __device__ __forceinline__ int raw_rank(int a) const { return rank ? rank[a] : max_rank; }
+    __device__ __forceinline__ int cut_rank(int r) const { return min(max(r, 0), max_rank); }
 };
 
-constexpr int kThreads = 256, kWarps = 8;
-
-// exclusive prefix sum over the CTA's threads; total for everyone.  red: 8 ints
+// exclusive prefix sum over the CTA's threads; total for everyone.  red: an int for each warp
+template <int THREADS>
 __device__ __forceinline__ int block_scan(int v, int* red, int& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int p = v;
@@ -67,7 +65,7 @@ __device__ __forceinline__ int block_scan(int v, int* red, int& total) {
     int before = 0;
     total = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
+    for (int w = 0; w < THREADS / 32; ++w) {
         if (w < warp) before += red[w];
         total += red[w];
     }
@@ -151,93 +149,259 @@ struct Cells<float> {
     }
 };
 
-__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_line(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+__device__ __forceinline__ void st_cluster4(uint32_t addr, float4 v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 __device__ __forceinline__ void st_cluster2(uint32_t addr, uint32_t a, uint32_t b) {
     asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
 }
 
-template <typename T, int MT, int RN>
-struct Layout {
-    static constexpr int kTokens = 16 * MT, kRank = 8 * RN;
+constexpr int kFew = 256;                                  // sequences, and adapters, that find_item's short way takes
+// bytes of shared memory that find_item uses
+__host__ __device__ constexpr int find_bytes(int slots) { return (slots + 2) / 2 * 16 + 3 * kFew * 4; }
+
+// Eight groups of warps split K in the first product and N in the second; HM warps of a group take MT tiles of 16 rows each.
+constexpr int kGroups = 8;
+
+template <typename T, int MT, int HM, int RN>
+struct Shape {
+    static constexpr int kThreads = 32 * kGroups * HM, kTokens = 16 * MT * HM, kRank = 8 * RN;
     static constexpr int kStride = kRank + 8;              // floats / bf16 of a row: rows of a fragment in different banks
     static constexpr int kParts = sizeof(T) == 2 ? 2 : 3;  // of the sums over K
-    static constexpr int kPart = kTokens * kStride * 4;    // one warp's sums; the first is reused for the CTA's
+    static constexpr int kPart = kTokens * kStride * 4;    // one group's sums; the CTA's
     static constexpr int kInner = kTokens * kStride * 2;   // one part of the tile's sums
-    // the counts of all adapters, later the warps' sums
-    static __host__ __device__ constexpr int first_area(int slots) { return kWarps * kPart > (slots + 4) / 4 * 16 ? kWarps * kPart : (slots + 4) / 4 * 16; }
-    static constexpr int bytes(int slots) { return first_area(slots) + kPart + kParts * kInner; }
+    // the counts and ranks of all adapters, later the groups' sums
+    static __host__ __device__ constexpr int first_area(int slots) { return kGroups * kPart > find_bytes(slots) ? kGroups * kPart : find_bytes(slots); }
+    static constexpr bool kAll = MT * HM == 1;             // every CTA adds up all parts of the sums
+    static constexpr int kMostLog2 = kAll && RN <= 4 ? 4 : 3;          // CTAs of a cluster: what shared memory holds twice over
+    static constexpr int kSum = kPart * (kAll ? 1 << kMostLog2 : 1);
+    static constexpr int bytes(int slots) { return first_area(slots) + kSum + kParts * kInner; }
+    // pieces of 32 columns that a warp loads before it multiplies: what its registers hold
+    static constexpr int kWide = sizeof(T) / 2;
+    static constexpr int fit(int regs, int each) { return regs / each >= 4 ? 4 : regs / each >= 1 ? regs / each : 1; }
+    static constexpr int kLoadK = fit(RN >= 8 && MT * HM > 1 ? 48 : 72, 8 * MT * kWide + 4 * RN);
+    static constexpr int kLoadN = fit(72, 8 * MT * kWide + (RN >= 4 ? 4 * RN : 8));
 };
 
-template <typename T, int MT, int RN>
-__global__ void __launch_bounds__(kThreads)
+// rows f .. f + n - 1 at place `to` of the tile's list, as far as they fall into it
+template <int T>
+__device__ __forceinline__ void list_rows(int* s_rows, int to, int n, int f) {
+    for (int i = max(0, -to); i < n && to + i < T; ++i) s_rows[to + i] = f + i;
+}
+struct Item {
+    int slot, cnt, rank;                                   // adapter, rows of the tile, the adapter's rank
+};
+// The tile's item and its rows (packed row numbers in s_rows, -1 behind the last).  false: there is no such tile.  Ends with the CTA
+// synchronised.  Groups of rows are ordered by adapter, the rows of one by sequence.  Up to kFew sequences and adapters take one round of
+// loads, after which every warp finds the item for itself from the counts and the first one lists the rows.
+template <int THREADS, int T>
+__device__ __forceinline__ bool find_item(const AdapterArgs& p, int tile, uint8_t* area, int* s_red, int* s_item, int* s_rows, Item& item) {
+    const int t = threadIdx.x, lane = t & 31, groups = p.slots + 1;
+    int* counts = reinterpret_cast<int*>(area);
+    int* ranks = counts + groups;
+    int* seq_first = reinterpret_cast<int*>(area + (p.slots + 2) / 2 * 16);
+    int* seq_rows = seq_first + kFew;
+    int* seq_group = seq_rows + kFew;
+    for (int i = t; i < groups; i += THREADS) counts[i] = 0;
+    if (t < T) s_rows[t] = -1;
+    __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // launched as a dependent: nothing above touched global memory
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (p.seqs <= kFew && groups <= kFew) {
+        const bool on = t < p.seqs;
+        const int s = on ? t : 0;
+        const int b0 = p.start[s], b1 = p.start[s + 1], ad = p.adapter[s], raw = t < p.slots ? p.raw_rank(t) : 0;
+        const int f = int(min(max(int64_t(b0), int64_t(0)), p.rows)), n = on ? max(int(min(max(int64_t(b1), int64_t(0)), p.rows)) - f, 0) : 0;
+        const int a = n > 0 ? p.group_of(ad) : -1;
+        if (a >= 0) atomicAdd(counts + a, n);
+        if (t < groups) ranks[t] = p.cut_rank(raw);
+        if (blockIdx.x == 0 && on && (b0 < 0 || b1 < b0 || b1 > p.rows || ad >= p.slots)) kv::raise_page(p.status);
+        if (t < kFew) { seq_first[t] = f; seq_rows[t] = n; seq_group[t] = a; }
+        __syncthreads();
+        if (blockIdx.x == 0 && t < p.slots && counts[t] > 0 && raw != ranks[t]) kv::raise_page(p.status);
+        const int eachg = (groups + 31) / 32, eachs = (p.seqs + 31) / 32;       // of a lane
+        int tiles = 0;
+        for (int k = lane * eachg; k < min((lane + 1) * eachg, groups); ++k) tiles += (counts[k] + T - 1) / T;
+        int at = tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, at, o);
+            if (lane >= o) at += v;
+        }
+        if (tile >= __shfl_sync(0xffffffffu, at, 31)) return false;
+        at -= tiles;
+        const bool mine = tile >= at && tile < at + tiles;
+        int slot = 0, from = 0;
+        if (mine)
+            for (int k = lane * eachg; k < min((lane + 1) * eachg, groups); ++k) {
+                const int c = (counts[k] + T - 1) / T;
+                if (tile >= at && tile < at + c) { slot = k; from = (tile - at) * T; }
+                at += c;
+            }
+        const int who = __ffs(__ballot_sync(0xffffffffu, mine)) - 1;
+        slot = __shfl_sync(0xffffffffu, slot, who);
+        from = __shfl_sync(0xffffffffu, from, who);
+        item.slot = slot;
+        item.cnt = min(counts[slot] - from, T);
+        item.rank = ranks[slot];
+        if (t < 32) {
+            const int k0 = lane * eachs, k1 = min(k0 + eachs, p.seqs);
+            int have = 0;
+            for (int k = k0; k < k1; ++k) have += seq_group[k] == slot ? seq_rows[k] : 0;
+            int to = have;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, to, o);
+                if (lane >= o) to += v;
+            }
+            to -= have + from;                             // of the tile's first row
+            if (have > 0 && to < T && to + have > 0)
+                for (int k = k0; k < k1; ++k) {
+                    if (seq_group[k] != slot) continue;
+                    list_rows<T>(s_rows, to, seq_rows[k], seq_first[k]);
+                    to += seq_rows[k];
+                }
+        }
+    } else {
+        // a thread's run of sequences, and of adapters
+        const int per = (p.seqs + THREADS - 1) / THREADS, s0 = min(t * per, p.seqs), s1 = min(s0 + per, p.seqs);
+        for (int i = t; i < groups; i += THREADS) ranks[i] = i < p.slots ? p.cut_rank(p.raw_rank(i)) : 0;
+        for (int s = s0; s < s1; ++s) {
+            const int n = p.count(s), b0 = p.start[s], b1 = p.start[s + 1], ad = p.adapter[s], a = p.group_of(ad);
+            if (n > 0 && a >= 0) atomicAdd(counts + a, n);
+            if (blockIdx.x == 0 && (b0 < 0 || b1 < b0 || b1 > p.rows || ad >= p.slots)) kv::raise_page(p.status);
+        }
+        __syncthreads();
+        if (blockIdx.x == 0)
+            for (int i = t; i < p.slots; i += THREADS)
+                if (counts[i] > 0 && p.raw_rank(i) != ranks[i]) kv::raise_page(p.status);
+        const int each = (groups + THREADS - 1) / THREADS, g0 = min(t * each, groups), g1 = min(g0 + each, groups);
+        int tiles = 0, total, have = 0, all;
+        for (int i = g0; i < g1; ++i) tiles += (counts[i] + T - 1) / T;
+        int at = block_scan<THREADS>(tiles, s_red, total);
+        if (tile >= total) return false;
+        if (tile >= at && tile < at + tiles)
+            for (int i = g0; i < g1; ++i) {
+                const int n = (counts[i] + T - 1) / T;
+                if (tile >= at && tile < at + n) { s_item[0] = i; s_item[1] = (tile - at) * T; }
+                at += n;
+            }
+        __syncthreads();
+        const int slot = s_item[0], from = s_item[1];
+        item.slot = slot;
+        item.cnt = min(counts[slot] - from, T);
+        item.rank = ranks[slot];
+        for (int s = s0; s < s1; ++s) have += p.group_of(p.adapter[s]) == slot ? p.count(s) : 0;
+        int to = block_scan<THREADS>(have, s_red, all) - from;
+        if (have > 0 && to < T && to + have > 0)
+            for (int s = s0; s < s1; ++s) {
+                if (p.group_of(p.adapter[s]) != slot) continue;
+                const int n = p.count(s);
+                list_rows<T>(s_rows, to, n, p.first(s));
+                to += n;
+            }
+    }
+    __syncthreads();
+    return true;
+}
+
+template <typename T, int MT, int HM, int RN>
+__global__ void __launch_bounds__(32 * kGroups * HM, HM == 1 && RN <= 8 ? 2 : 1)
 adapters_add_kernel(const AdapterArgs p) {
-    using Lay = Layout<T, MT, RN>;
-    constexpr int kT = Lay::kTokens, kR = Lay::kRank, kS = Lay::kStride, kParts = Lay::kParts;
+    using S = Shape<T, MT, HM, RN>;
+    constexpr int kThreads = S::kThreads, kT = S::kTokens, kR = S::kRank, kS = S::kStride, kParts = S::kParts;
     constexpr int kQ = kR >= 32 ? 4 : 2;                   // words of a lane's piece of k in the second product
     constexpr int kSteps = kR >= 32 ? kR / 32 : 1;
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ int s_red[kWarps], s_item[3], s_rows[kT];
-    const int t = threadIdx.x, lane = t & 31, warp = t >> 5, g = lane >> 2, q = lane & 3;
-    const int cl = p.cluster, part = int(blockIdx.x) % cl, tile = int(blockIdx.x) / cl;
-    asm volatile("griddepcontrol.wait;" ::: "memory");     // launched as a dependent
+    __shared__ int s_red[kThreads / 32], s_item[4], s_rows[kT];
+    const int t = threadIdx.x, lane = t & 31, group = (t >> 5) / HM, m0 = (t >> 5) % HM * MT, g = lane >> 2, q = lane & 3;
+    const int cl = 1 << p.cluster_log2, part = int(blockIdx.x) & (cl - 1), tile = int(blockIdx.x) >> p.cluster_log2;
+    if (cl > 1) cluster_arrive();                          // waited for before the first write to another CTA's memory: all have started
 
     // ---- the tile's adapter and rows
-    int* counts = reinterpret_cast<int*>(smem);
-    for (int i = t; i <= p.slots; i += kThreads) counts[i] = 0;
-    if (t < kT) s_rows[t] = -1;
-    __syncthreads();
-    for (int s = t; s < p.seqs; s += kThreads) {
-        const int n = p.count(s), a = p.group(s);
-        if (n > 0 && a >= 0) atomicAdd(counts + a, n);
-        if (blockIdx.x == 0) {
-            const int b0 = p.start[s], b1 = p.start[s + 1], ad = p.adapter[s];
-            if (b0 < 0 || b1 < b0 || b1 > p.rows || ad >= p.slots || (ad >= 0 && p.rank && (p.rank[ad] < 0 || p.rank[ad] > p.max_rank)))
-                kv::raise_page(p.status);
-        }
-    }
-    __syncthreads();
-    int total;
-    {
-        const int per = (p.slots + kThreads) / kThreads, g0 = t * per, g1 = min(g0 + per, p.slots + 1);
-        int tiles = 0;
-        for (int i = g0; i < g1; ++i) tiles += (counts[i] + kT - 1) / kT;
-        int at = block_scan(tiles, s_red, total);
-        if (tile >= at && tile < at + tiles)
-            for (int i = g0; i < g1; ++i) {
-                const int n = (counts[i] + kT - 1) / kT;
-                if (tile >= at && tile < at + n) { s_item[0] = i; s_item[1] = (tile - at) * kT; s_item[2] = counts[i]; }
-                at += n;
-            }
-    }
-    __syncthreads();
-    if (tile >= total) return;                             // the same in all CTAs of a cluster
-    const int slot = s_item[0], from = s_item[1], cnt = min(s_item[2] - from, kT);
-    {
-        const int per = (p.seqs + kThreads - 1) / kThreads, s0 = min(t * per, p.seqs), s1 = min(s0 + per, p.seqs);
-        int mine = 0, all;
-        for (int s = s0; s < s1; ++s) mine += p.group(s) == slot ? p.count(s) : 0;
-        int at = block_scan(mine, s_red, all) - from;      // of the tile's first row
-        if (mine > 0 && at < kT && at + mine > 0)
-            for (int s = s0; s < s1; ++s) {
-                if (p.group(s) != slot) continue;
-                const int n = p.count(s), f = p.first(s);
-                for (int i = max(0, -at); i < n && at + i < kT; ++i) s_rows[at + i] = f + i;
-                at += n;
-            }
-    }
-    __syncthreads();
-    const int rank = p.rank_of(slot), mtiles = (cnt + 15) / 16, rtiles = (rank + 7) / 8;
+    Item item;
+    if (!find_item<kThreads, kT>(p, tile, smem, s_red, s_item, s_rows, item)) return;   // the same in all CTAs of a cluster
+    const int slot = item.slot, cnt = item.cnt, rank = item.rank;
+    const int mtiles = (cnt + 15) / 16 - m0, rtiles = (rank + 7) / 8;      // tiles of rows of this warp, of ranks
 
     float* s_part = reinterpret_cast<float*>(smem);
-    float* s_sum = reinterpret_cast<float*>(smem + Lay::first_area(p.slots));
-    __nv_bfloat16* s_inner = reinterpret_cast<__nv_bfloat16*>(s_sum + kT * kS);
+    float* s_sum = reinterpret_cast<float*>(smem + S::first_area(p.slots));
+    __nv_bfloat16* s_inner = reinterpret_cast<__nv_bfloat16*>(s_sum + S::kSum / 4);
+    const __nv_bfloat16* weights = p.B + int64_t(slot) * p.N * p.max_rank;
+    const T* base = static_cast<const T*>(p.base);
+    T* out = static_cast<T*>(p.out);
+    const int nunits = (p.N + 31) / 32, v0 = nunits * part >> p.cluster_log2, v1 = nunits * (part + 1) >> p.cluster_log2;     // K, N < 2^31: 31 bits
+
+    // the second product's operands start on their way to L2 under the first one
+    const int units = (p.K + 31) / 32, u0 = units * part >> p.cluster_log2, u1 = units * (part + 1) >> p.cluster_log2;
+    if (rank > 0) {
+        const int n0 = 32 * v0, n1 = min(32 * v1, p.N);
+        if (2 * rank > p.max_rank) {
+            const char* from = reinterpret_cast<const char*>(weights + int64_t(n0) * p.max_rank);
+            for (int i = 128 * t; i < (n1 - n0) * p.max_rank * 2; i += 128 * kThreads) prefetch_line(from + i);
+        } else {
+            for (int n = n0 + t; n < n1; n += kThreads) prefetch_line(weights + int64_t(n) * p.max_rank);
+        }
+    }
+
+    // ---- what the second product reads: this CTA's part of N, the groups taking kLoadN x 32 columns in turn
+    constexpr int kLN = S::kLoadN;
+    uint32_t bw[kLN][4][kSteps][kQ];
+    Cells<T> cell[kLN][MT][2];
+    // (every lane loads, as above; entries of B beyond the rank count for nothing, whatever they are: the masks below)
+    int brow[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) brow[s] = kQ == 4 ? min(32 * s + 8 * q, max(rank - 1, 0) & ~7) : min(4 * q, max(rank - 1, 0) & ~3);
+    const T* bp[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = s_rows[16 * (m0 + m) + 8 * h + g];
+            bp[m][h] = base + int64_t(row < 0 ? max(s_rows[0], 0) : row) * p.base_stride;
+        }
+    const auto load_columns = [&](int v) {
+#pragma unroll
+        for (int l = 0; l < kLN; ++l) {
+            if (v + l >= v1) break;
+            if (rank > 0) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const __nv_bfloat16* wp = weights + int64_t(min(32 * (v + l) + 8 * (g >> 1) + 2 * j + (g & 1), p.N - 1)) * p.max_rank;
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) {
+                        if (s > 0 && 32 * s >= rank) break;
+                        if constexpr (kQ == 4) {
+                            const uint4 w = __ldg(reinterpret_cast<const uint4*>(wp + brow[s]));
+                            bw[l][j][s][0] = w.x; bw[l][j][s][1] = w.y; bw[l][j][s][2] = w.z; bw[l][j][s][3] = w.w;
+                        } else {
+                            const uint2 w = __ldg(reinterpret_cast<const uint2*>(wp + brow[s]));
+                            bw[l][j][s][0] = w.x; bw[l][j][s][1] = w.y;
+                        }
+                    }
+                }
+            }
+            if (base) {
+                const int col = min(32 * (v + l) + 8 * q, p.N - 8);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (m > 0 && m >= mtiles) break;
+                        cell[l][m][h].load(bp[m][h] + col);
+                    }
+            } else {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) { cell[l][m][0].zero(); cell[l][m][1].zero(); }
+            }
+        }
+    };
 
     if (rank > 0) {
-        // ---- first product: sums over this CTA's part of K, the warps taking 32 columns in turn
+        // ---- first product: sums over this CTA's part of K, the groups taking kLoadK x 32 columns in turn
         float acc[MT][RN][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -250,47 +414,64 @@ adapters_add_kernel(const AdapterArgs p) {
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int row = s_rows[16 * m + 8 * h + g];
-                xp[m][h] = static_cast<const T*>(p.x) + (row < 0 ? int64_t(max(s_rows[0], 0)) : int64_t(row)) * p.x_stride + 8 * q;
+                const int row = s_rows[16 * (m0 + m) + 8 * h + g];
+                xp[m][h] = static_cast<const T*>(p.x) + int64_t(row < 0 ? max(s_rows[0], 0) : row) * p.x_stride;
             }
-        const __nv_bfloat16* ap = p.A + (int64_t(slot) * p.max_rank + g) * p.K + 8 * q;
-        const int units = (p.K + 31) / 32, u1 = int(int64_t(units) * (part + 1) / cl);
-        constexpr int kP = Operand<T>::kParts;
-#pragma unroll 2
-        for (int u = int(int64_t(units) * part / cl) + warp; u < u1; u += kWarps) {
-            const bool in = 32 * u + 8 * q < p.K;
-            Operand<T> xv[MT][2];
-            uint4 av[RN];
+        // Every lane loads: where there is no such rank, the last one's row again (those sums are dropped below), behind the last
+        // column the last 8 again (zeroed).
+        const __nv_bfloat16* ap[RN];
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+        for (int j = 0; j < RN; ++j) ap[j] = p.A + (int64_t(slot) * p.max_rank + min(8 * j + g, rank - 1)) * p.K;
+        constexpr int kP = Operand<T>::kParts, kL = S::kLoadK;
+        if (mtiles > 0)
+            for (int u = u0 + group * kL; u < u1; u += kGroups * kL) {
+                Operand<T> xv[kL][MT][2];
+                uint4 av[kL][RN];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    xv[m][h].zero();
-                    if (in && m < mtiles) xv[m][h].load(xp[m][h] + 32 * u);
+                for (int l = 0; l < kL; ++l) {
+                    if (l > 0 && u + l >= u1) break;
+                    const int k = min(32 * (u + l) + 8 * q, p.K - 8);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (m > 0 && m >= mtiles) break;
+                            xv[l][m][h].load(xp[m][h] + k);
+                        }
+#pragma unroll
+                    for (int j = 0; j < RN; ++j) {
+                        if (j > 0 && j >= rtiles) break;
+                        av[l][j] = __ldg(reinterpret_cast<const uint4*>(ap[j] + k));
+                    }
                 }
 #pragma unroll
-            for (int j = 0; j < RN; ++j) {
-                av[j] = make_uint4(0, 0, 0, 0);
-                if (in && 8 * j + g < rank) av[j] = __ldg(reinterpret_cast<const uint4*>(ap + int64_t(8 * j) * p.K + 32 * u));
-            }
+                for (int l = 0; l < kL; ++l) {
+                    if (l > 0 && u + l >= u1) break;
+                    if (32 * (u + l) + 32 > p.K && 32 * (u + l) + 8 * q >= p.K) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                if (m >= mtiles) break;
-                uint32_t w0[kP][4], w1[kP][4];
-                xv[m][0].split(w0);
-                xv[m][1].split(w1);
+                        for (int m = 0; m < MT; ++m) { xv[l][m][0].zero(); xv[l][m][1].zero(); }
 #pragma unroll
-                for (int j = 0; j < RN; ++j) {
-                    if (j >= rtiles) break;
+                        for (int j = 0; j < RN; ++j) av[l][j] = make_uint4(0, 0, 0, 0);
+                    }
 #pragma unroll
-                    for (int k = 0; k < kP; ++k) {
-                        mma_bf16(acc[m][j], w0[k][0], w1[k][0], w0[k][1], w1[k][1], av[j].x, av[j].y);
-                        mma_bf16(acc[m][j], w0[k][2], w1[k][2], w0[k][3], w1[k][3], av[j].z, av[j].w);
+                    for (int m = 0; m < MT; ++m) {
+                        if (m > 0 && m >= mtiles) break;
+                        uint32_t w0[kP][4], w1[kP][4];
+                        xv[l][m][0].split(w0);
+                        xv[l][m][1].split(w1);
+#pragma unroll
+                        for (int j = 0; j < RN; ++j) {
+                            if (j > 0 && j >= rtiles) break;
+#pragma unroll
+                            for (int k = 0; k < kP; ++k) {
+                                mma_bf16(acc[m][j], w0[k][0], w1[k][0], w0[k][1], w1[k][1], av[l][j].x, av[l][j].y);
+                                mma_bf16(acc[m][j], w0[k][2], w1[k][2], w0[k][3], w1[k][3], av[l][j].z, av[l][j].w);
+                            }
+                        }
                     }
                 }
             }
-        }
-        // ---- the warps' sums, then the cluster's: CTA `part` adds every cl-th group of four and hands it to all
+        // ---- the groups' sums, then the cluster's: CTA `part` adds every cl-th group of four and hands it to all
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             if (m >= mtiles) break;
@@ -298,50 +479,70 @@ adapters_add_kernel(const AdapterArgs p) {
             for (int j = 0; j < RN; ++j)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
-                    *reinterpret_cast<float2*>(s_part + warp * kT * kS + (16 * m + 8 * h + g) * kS + 8 * j + 2 * q) = make_float2(acc[m][j][2 * h], acc[m][j][2 * h + 1]);
+                    *reinterpret_cast<float2*>(s_part + group * kT * kS + (16 * (m0 + m) + 8 * h + g) * kS + 8 * j + 2 * q) = make_float2(acc[m][j][2 * h], acc[m][j][2 * h + 1]);
         }
+        load_columns(v0 + group * kLN);                    // under the exchange
         __syncthreads();
-        for (int e = t; e < cnt * (kR / 4); e += kThreads) {
+        if (cl > 1) cluster_wait();
+        // Each CTA adds its groups' sums, in fours.  Small tiles: every CTA hands all of its sums to all CTAs, which add them up, each for
+        // itself.  Others: the e-th four goes to CTA e % cl, which adds the cl parts and hands the result to all; one more barrier,
+        // an cl-th of the traffic.
+        const int fours = cnt * (kR / 4);
+        const uint32_t sum_addr = ptx::smem_addr(s_sum), inner_addr = ptx::smem_addr(s_inner);
+        const float scale = p.scale[slot];
+        for (int e = t; e < fours; e += kThreads) {
             const int at = e / (kR / 4) * kS + e % (kR / 4) * 4;
             float4 s = *reinterpret_cast<const float4*>(s_part + at);
 #pragma unroll
-            for (int w = 1; w < kWarps; ++w) {
+            for (int w = 1; w < kGroups; ++w) {
                 const float4 o = *reinterpret_cast<const float4*>(s_part + w * kT * kS + at);
                 s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
             }
-            *reinterpret_cast<float4*>(s_sum + at) = s;
+            if constexpr (S::kAll) {
+                for (int c = 0; c < cl; ++c) st_cluster4(ptx::map_to_cta(sum_addr + (e * cl + part) * 16, c), s);
+            } else {
+                st_cluster4(ptx::map_to_cta(sum_addr + ((e & -cl) + part) * 16, e & (cl - 1)), s);
+            }
         }
         __syncwarp();
         if (cl > 1) ptx::cluster_sync(); else __syncthreads();
-        const float scale = p.scale[slot];
-        const uint32_t sum_addr = ptx::smem_addr(s_sum), inner_addr = ptx::smem_addr(s_inner);
-        for (int e = part + cl * t; e < cnt * (kR / 4); e += cl * kThreads) {
-            const int at = e / (kR / 4) * kS + e % (kR / 4) * 4;
+        for (int k = t; S::kAll ? k < fours : part + (k << p.cluster_log2) < fours; k += kThreads) {
+            const int e = S::kAll ? k : part + (k << p.cluster_log2), at = e / (kR / 4) * kS + e % (kR / 4) * 4;
             float f[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
             for (int c = 0; c < cl; ++c) {
-                const float4 o = ld_cluster4(ptx::map_to_cta(sum_addr + at * 4, c));
+                const float4 o = *reinterpret_cast<const float4*>(s_sum + ((k << p.cluster_log2) + c) * 4);
                 f[0] += o.x; f[1] += o.y; f[2] += o.z; f[3] += o.w;
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] *= scale;
+            for (int i = 0; i < 4; ++i) f[i] = e % (kR / 4) * 4 + i < rank ? f[i] * scale : 0.f;
             uint32_t w[kParts][2];
 #pragma unroll
-            for (int k = 0; k < kParts; ++k) {
-                w[k][0] = k + 1 < kParts ? upper(f[0], f[1]) : rounded(f[0], f[1]);
-                w[k][1] = k + 1 < kParts ? upper(f[2], f[3]) : rounded(f[2], f[3]);
+            for (int i = 0; i < kParts; ++i) {
+                w[i][0] = i + 1 < kParts ? upper(f[0], f[1]) : rounded(f[0], f[1]);
+                w[i][1] = i + 1 < kParts ? upper(f[2], f[3]) : rounded(f[2], f[3]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) f[i] = rest(f[i]);
+                for (int j = 0; j < 4; ++j) f[j] = rest(f[j]);
+                if constexpr (S::kAll) {
+                    *reinterpret_cast<uint2*>(s_inner + i * kT * kS + at) = make_uint2(w[i][0], w[i][1]);
+                } else {
+                    for (int c = 0; c < cl; ++c) st_cluster2(ptx::map_to_cta(inner_addr + (i * kT * kS + at) * 2, c), w[i][0], w[i][1]);
+                }
             }
-            for (int c = 0; c < cl; ++c)
-#pragma unroll
-                for (int k = 0; k < kParts; ++k) st_cluster2(ptx::map_to_cta(inner_addr + (k * kT * kS + at) * 2, c), w[k][0], w[k][1]);
         }
-        __syncwarp();
-        if (cl > 1) ptx::cluster_sync(); else __syncthreads();
+        if constexpr (S::kAll) {
+            __syncthreads();
+        } else {
+            __syncwarp();
+            if (cl > 1) ptx::cluster_sync(); else __syncthreads();
+        }
+    } else {
+        load_columns(v0 + group * kLN);
     }
+    if (mtiles <= 0) return;
 
-    // ---- second product: this CTA's part of N, 32 columns a warp
-    uint32_t mask[kSteps][kQ];                             // entries of B beyond the rank count for nothing, whatever they are
+    // ---- second product
+    uint32_t mask[kSteps][kQ];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
 #pragma unroll
@@ -349,116 +550,114 @@ adapters_add_kernel(const AdapterArgs p) {
             const int k = 32 * s + 2 * kQ * q + 2 * i;
             mask[s][i] = (k < rank ? 0xFFFFu : 0u) | (k + 1 < rank ? 0xFFFF0000u : 0u);
         }
-    const T* base = static_cast<const T*>(p.base);
-    T* out = static_cast<T*>(p.out);
-    const int units = (p.N + 31) / 32, v1 = int(int64_t(units) * (part + 1) / cl);
-    for (int v = int(int64_t(units) * part / cl) + warp; v < v1; v += kWarps) {
-        const int col = 32 * v + 8 * q;
-        uint32_t bw[4][kSteps][kQ];
+    for (int v = v0 + group * kLN; v < v1; v += kGroups * kLN) {
+        if (v != v0 + group * kLN) load_columns(v);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int n = 32 * v + 8 * (g >> 1) + 2 * j + (g & 1);
-            const __nv_bfloat16* bp = p.B + (int64_t(slot) * p.N + n) * p.max_rank + 2 * kQ * q;
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                if constexpr (kQ == 4) {
-                    uint4 w = make_uint4(0, 0, 0, 0);
-                    if (n < p.N && 32 * s + 8 * q < rank) w = __ldg(reinterpret_cast<const uint4*>(bp + 32 * s));
-                    bw[j][s][0] = w.x & mask[s][0]; bw[j][s][1] = w.y & mask[s][1];
-                    bw[j][s][2] = w.z & mask[s][2]; bw[j][s][3] = w.w & mask[s][3];
-                } else {
-                    uint2 w = make_uint2(0, 0);
-                    if (n < p.N && 4 * q < rank) w = __ldg(reinterpret_cast<const uint2*>(bp));
-                    bw[j][s][0] = w.x & mask[s][0]; bw[j][s][1] = w.y & mask[s][1];
-                }
-            }
-        }
-        Cells<T> cell[MT][2];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int i = 16 * m + 8 * h + g, row = s_rows[i];
-                cell[m][h].zero();
-                if (base && i < cnt && row >= 0 && col < p.N) cell[m][h].load(base + int64_t(row) * p.base_stride + col);
-            }
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if (m >= mtiles) break;
-            float acc[4][4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+        for (int l = 0; l < kLN; ++l) {
+            if (v + l >= v1) break;
+            const int col = 32 * (v + l) + 8 * q;
             if (rank > 0) {
 #pragma unroll
-                for (int k = 0; k < kParts; ++k)
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int s = 0; s < kSteps; ++s) {
-                        if (32 * s >= rank) break;
-                        const __nv_bfloat16* hp = s_inner + k * kT * kS + (16 * m + g) * kS + 32 * s + 2 * kQ * q;
-                        uint32_t w0[kQ], w1[kQ];
-                        if constexpr (kQ == 4) {
-                            const uint4 a = *reinterpret_cast<const uint4*>(hp), b = *reinterpret_cast<const uint4*>(hp + 8 * kS);
-                            w0[0] = a.x; w0[1] = a.y; w0[2] = a.z; w0[3] = a.w;
-                            w1[0] = b.x; w1[1] = b.y; w1[2] = b.z; w1[3] = b.w;
-                        } else {
-                            const uint2 a = *reinterpret_cast<const uint2*>(hp), b = *reinterpret_cast<const uint2*>(hp + 8 * kS);
-                            w0[0] = a.x; w0[1] = a.y;
-                            w1[0] = b.x; w1[1] = b.y;
-                        }
+                        if (s > 0 && 32 * s >= rank) break;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-#pragma unroll
-                            for (int i = 0; i < kQ; i += 2) mma_bf16(acc[j], w0[i], w1[i], w0[i + 1], w1[i + 1], bw[j][s][i], bw[j][s][i + 1]);
+                        for (int i = 0; i < kQ; ++i) bw[l][j][s][i] &= mask[s][i];
                     }
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int i = 16 * m + 8 * h + g, row = s_rows[i];
-                const float d[8] = {acc[0][2 * h], acc[0][2 * h + 1], acc[1][2 * h], acc[1][2 * h + 1],
-                                    acc[2][2 * h], acc[2][2 * h + 1], acc[3][2 * h], acc[3][2 * h + 1]};
-                if (i < cnt && row >= 0 && col < p.N) cell[m][h].add_store(out + int64_t(row) * p.out_stride + col, d);
+            for (int m = 0; m < MT; ++m) {
+                if (m > 0 && m >= mtiles) break;
+                float acc[4][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+                if (rank > 0) {
+#pragma unroll
+                    for (int k = 0; k < kParts; ++k)
+#pragma unroll
+                        for (int s = 0; s < kSteps; ++s) {
+                            if (s > 0 && 32 * s >= rank) break;
+                            const __nv_bfloat16* hp = s_inner + k * kT * kS + (16 * (m0 + m) + g) * kS + 32 * s + 2 * kQ * q;
+                            uint32_t w0[kQ], w1[kQ];
+                            if constexpr (kQ == 4) {
+                                const uint4 a = *reinterpret_cast<const uint4*>(hp), b = *reinterpret_cast<const uint4*>(hp + 8 * kS);
+                                w0[0] = a.x; w0[1] = a.y; w0[2] = a.z; w0[3] = a.w;
+                                w1[0] = b.x; w1[1] = b.y; w1[2] = b.z; w1[3] = b.w;
+                            } else {
+                                const uint2 a = *reinterpret_cast<const uint2*>(hp), b = *reinterpret_cast<const uint2*>(hp + 8 * kS);
+                                w0[0] = a.x; w0[1] = a.y;
+                                w1[0] = b.x; w1[1] = b.y;
+                            }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                                for (int i = 0; i < kQ; i += 2) mma_bf16(acc[j], w0[i], w1[i], w0[i + 1], w1[i + 1], bw[l][j][s][i], bw[l][j][s][i + 1]);
+                        }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int i = 16 * (m0 + m) + 8 * h + g, row = s_rows[i];
+                    const float d[8] = {acc[0][2 * h], acc[0][2 * h + 1], acc[1][2 * h], acc[1][2 * h + 1],
+                                        acc[2][2 * h], acc[2][2 * h + 1], acc[3][2 * h], acc[3][2 * h + 1]};
+                    if (i < cnt && row >= 0 && col < p.N) cell[l][m][h].add_store(out + int64_t(row) * p.out_stride + col, d);
+                }
             }
         }
     }
 }
 
-template <typename T, int MT, int RN>
+// Allows a kernel clusters of 16, once per kernel and device.
+template <auto Kern>
+cudaError_t allow_large_clusters() {
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1)) return cudaSuccess;
+    const cudaError_t r = cudaFuncSetAttribute(Kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (r == cudaSuccess && dev < 64) done.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+    return r;
+}
+
+template <typename T, int MT, int HM, int RN>
 int launch_tiles(AdapterArgs p, cudaStream_t st) {
-    using Lay = Layout<T, MT, RN>;
-    const int64_t tiles = p.rows / Lay::kTokens + std::min(p.seqs, p.slots + 1);
-    const int bytes = Lay::bytes(p.slots), sms = device_sm_count();
+    using S = Shape<T, MT, HM, RN>;
+    constexpr auto kern = adapters_add_kernel<T, MT, HM, RN>;
+    const int64_t tiles = p.rows / S::kTokens + std::min(p.seqs, p.slots + 1);
+    const int bytes = S::bytes(p.slots), sms = device_sm_count();
     // as many CTAs to a tile as keep the launch near two CTAs on every SM
-    p.cluster = 8;
-    while (p.cluster > 1 && tiles * p.cluster > 2 * sms) p.cluster /= 2;
-    const cudaError_t e = allow_smem<adapters_add_kernel<T, MT, RN>>(Lay::bytes(8192));
-    if (e != cudaSuccess) return cuda_fail(e);
+    p.cluster_log2 = S::kMostLog2;
+    while (p.cluster_log2 > 0 && tiles << p.cluster_log2 > (p.cluster_log2 == 4 ? sms / 2 : 2 * sms)) --p.cluster_log2;
+    QLLM_CUDA_TRY(allow_smem<kern>(S::bytes(8192)));
+    if (p.cluster_log2 > 3) QLLM_CUDA_TRY(allow_large_clusters<kern>());
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(tiles * p.cluster));
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3(unsigned(tiles << p.cluster_log2));
+    cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = size_t(bytes);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = unsigned(p.cluster);
+    attr[0].val.clusterDim.x = 1u << p.cluster_log2;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    const cudaError_t r = cudaLaunchKernelEx(&cfg, adapters_add_kernel<T, MT, RN>, p);
-    return r == cudaSuccess ? after_launch() : cuda_fail(r);
+    QLLM_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, p));
+    return after_launch();
 }
 
 template <typename T>
 int launch_adapters(const AdapterArgs& p, cudaStream_t st) {
     // tiles of 16 rows while groups are that small on average
     const bool few = p.rows <= int64_t(16) * std::min(p.seqs, p.slots + 1);
-    if (p.max_rank <= 16) return few ? launch_tiles<T, 1, 2>(p, st) : launch_tiles<T, 4, 2>(p, st);
-    if (p.max_rank <= 32) return few ? launch_tiles<T, 1, 4>(p, st) : launch_tiles<T, 4, 4>(p, st);
-    if (p.max_rank <= 64) return few ? launch_tiles<T, 1, 8>(p, st) : launch_tiles<T, 4, 8>(p, st);
-    return few ? launch_tiles<T, 1, 16>(p, st) : launch_tiles<T, 2, 16>(p, st);
+    if (p.max_rank <= 16) return few ? launch_tiles<T, 1, 1, 2>(p, st) : launch_tiles<T, 2, 2, 2>(p, st);
+    if (p.max_rank <= 32) return few ? launch_tiles<T, 1, 1, 4>(p, st) : launch_tiles<T, 2, 2, 4>(p, st);
+    if (p.max_rank <= 64) return few ? launch_tiles<T, 1, 1, 8>(p, st) : launch_tiles<T, 2, 2, 8>(p, st);
+    return few ? launch_tiles<T, 1, 1, 16>(p, st) : launch_tiles<T, 2, 1, 16>(p, st);
 }
 
 int check_rows(const void* p, int64_t stride, int width, int dtype) {
@@ -488,7 +687,7 @@ extern "C" int qllm_adapters_add(const qllm_adapters_t* ad, const void* x, int64
     int* status = device_status_word();
     if (!status) return QLLM_ERR_CUDA;
     const AdapterArgs p{static_cast<const __nv_bfloat16*>(ad->A), static_cast<const __nv_bfloat16*>(ad->B), ad->scale, ad->rank, ad->slots, ad->max_rank,
-                        ad->K, ad->N, q_start, adapter, seqs, 1, rows, x, base, out, x_stride, base_stride, out_stride, status};
+                        ad->K, ad->N, q_start, adapter, seqs, 0, rows, x, base, out, x_stride, base_stride, out_stride, status};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return dtype == QLLM_BF16 ? launch_adapters<__nv_bfloat16>(p, st) : launch_adapters<float>(p, st);
 }
