@@ -19,72 +19,19 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
-#include <atomic>
 
-#include "common.h"
-#include "kv_cache.cuh"
-#include "ptx_sm100.cuh"
+#include "adapters.cuh"
 
 namespace qllm {
 namespace {
 
-struct AdapterArgs {
-    const __nv_bfloat16 *A, *B;
-    const float* scale;
-    const int32_t* rank;                                   // null: max_rank
-    int slots, max_rank, K, N;
-    const int32_t *start, *adapter;
-    int seqs, cluster_log2;                                // CTAs of a tile: 1, 2, 4, 8 or 16
-    int64_t rows;
-    const void *x, *base;
-    void* out;
-    int64_t x_stride, base_stride, out_stride;
-    int* status;
-    // row ranges, cut to what exists
-    __device__ __forceinline__ int first(int s) const { return int(min(max(int64_t(start[s]), int64_t(0)), rows)); }
-    __device__ __forceinline__ int count(int s) const { return max(first(s + 1) - first(s), 0); }
-    // the group that rows with adapter[s] = a belong to: the adapter, `slots` for none, -1 for rows that stay as they are
-    __device__ __forceinline__ int group_of(int a) const { return a >= 0 && a < slots ? a : base == out ? -1 : slots; }
-    __device__ __forceinline__ int raw_rank(int a) const { return rank ? rank[a] : max_rank; }
-    __device__ __forceinline__ int cut_rank(int r) const { return min(max(r, 0), max_rank); }
-};
-
-// exclusive prefix sum over the CTA's threads; total for everyone.  red: an int for each warp
-template <int THREADS>
-__device__ __forceinline__ int block_scan(int v, int* red, int& total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int p = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int n = __shfl_up_sync(0xffffffffu, p, o);
-        if (lane >= o) p += n;
-    }
-    __syncthreads();                                       // red may still be read from the last call
-    if (lane == 31) red[warp] = p;
-    __syncthreads();
-    int before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < warp) before += red[w];
-        total += red[w];
-    }
-    return before + p - v;
-}
+using namespace lora;
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-
-// the upper halves of two floats as a bf16 pair (low element first): truncation, 8 bits of each
-__device__ __forceinline__ uint32_t upper(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
-__device__ __forceinline__ uint32_t rounded(float lo, float hi) {
-    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&b);
-}
-__device__ __forceinline__ float rest(float f) { return f - __uint_as_float(__float_as_uint(f) & 0xFFFF0000u); }
 
 // 8 neighbouring values of a row as MMA operand words: P parts
 template <typename XT>
@@ -149,20 +96,7 @@ struct Cells<float> {
     }
 };
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_line(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-__device__ __forceinline__ void st_cluster4(uint32_t addr, float4 v) {
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
-}
-__device__ __forceinline__ void st_cluster2(uint32_t addr, uint32_t a, uint32_t b) {
-    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
-}
-
-constexpr int kFew = 256;                                  // sequences, and adapters, that find_item's short way takes
-// bytes of shared memory that find_item uses
-__host__ __device__ constexpr int find_bytes(int slots) { return (slots + 2) / 2 * 16 + 3 * kFew * 4; }
-
 // Eight groups of warps split K in the first product and N in the second; HM warps of a group take MT tiles of 16 rows each.
 constexpr int kGroups = 8;
 
@@ -174,7 +108,7 @@ struct Shape {
     static constexpr int kPart = kTokens * kStride * 4;    // one group's sums; the CTA's
     static constexpr int kInner = kTokens * kStride * 2;   // one part of the tile's sums
     // the counts and ranks of all adapters, later the groups' sums
-    static __host__ __device__ constexpr int first_area(int slots) { return kGroups * kPart > find_bytes(slots) ? kGroups * kPart : find_bytes(slots); }
+    static __host__ __device__ constexpr int first_area(int slots) { return kGroups * kPart > find_bytes(slots, kThreads) ? kGroups * kPart : find_bytes(slots, kThreads); }
     static constexpr bool kAll = MT * HM == 1;             // every CTA adds up all parts of the sums
     static constexpr int kMostLog2 = kAll && RN <= 4 ? 4 : 3;          // CTAs of a cluster: what shared memory holds twice over
     static constexpr int kSum = kPart * (kAll ? 1 << kMostLog2 : 1);
@@ -186,128 +120,6 @@ struct Shape {
     static constexpr int kLoadN = fit(72, 8 * MT * kWide + (RN >= 4 ? 4 * RN : 8));
 };
 
-// rows f .. f + n - 1 at place `to` of the tile's list, as far as they fall into it
-template <int T>
-__device__ __forceinline__ void list_rows(int* s_rows, int to, int n, int f) {
-    for (int i = max(0, -to); i < n && to + i < T; ++i) s_rows[to + i] = f + i;
-}
-struct Item {
-    int slot, cnt, rank;                                   // adapter, rows of the tile, the adapter's rank
-};
-// The tile's item and its rows (packed row numbers in s_rows, -1 behind the last).  false: there is no such tile.  Ends with the CTA
-// synchronised.  Groups of rows are ordered by adapter, the rows of one by sequence.  Up to kFew sequences and adapters take one round of
-// loads, after which every warp finds the item for itself from the counts and the first one lists the rows.
-template <int THREADS, int T>
-__device__ __forceinline__ bool find_item(const AdapterArgs& p, int tile, uint8_t* area, int* s_red, int* s_item, int* s_rows, Item& item) {
-    const int t = threadIdx.x, lane = t & 31, groups = p.slots + 1;
-    int* counts = reinterpret_cast<int*>(area);
-    int* ranks = counts + groups;
-    int* seq_first = reinterpret_cast<int*>(area + (p.slots + 2) / 2 * 16);
-    int* seq_rows = seq_first + kFew;
-    int* seq_group = seq_rows + kFew;
-    for (int i = t; i < groups; i += THREADS) counts[i] = 0;
-    if (t < T) s_rows[t] = -1;
-    __syncthreads();
-    asm volatile("griddepcontrol.wait;" ::: "memory");     // launched as a dependent: nothing above touched global memory
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (p.seqs <= kFew && groups <= kFew) {
-        const bool on = t < p.seqs;
-        const int s = on ? t : 0;
-        const int b0 = p.start[s], b1 = p.start[s + 1], ad = p.adapter[s], raw = t < p.slots ? p.raw_rank(t) : 0;
-        const int f = int(min(max(int64_t(b0), int64_t(0)), p.rows)), n = on ? max(int(min(max(int64_t(b1), int64_t(0)), p.rows)) - f, 0) : 0;
-        const int a = n > 0 ? p.group_of(ad) : -1;
-        if (a >= 0) atomicAdd(counts + a, n);
-        if (t < groups) ranks[t] = p.cut_rank(raw);
-        if (blockIdx.x == 0 && on && (b0 < 0 || b1 < b0 || b1 > p.rows || ad >= p.slots)) kv::raise_page(p.status);
-        if (t < kFew) { seq_first[t] = f; seq_rows[t] = n; seq_group[t] = a; }
-        __syncthreads();
-        if (blockIdx.x == 0 && t < p.slots && counts[t] > 0 && raw != ranks[t]) kv::raise_page(p.status);
-        const int eachg = (groups + 31) / 32, eachs = (p.seqs + 31) / 32;       // of a lane
-        int tiles = 0;
-        for (int k = lane * eachg; k < min((lane + 1) * eachg, groups); ++k) tiles += (counts[k] + T - 1) / T;
-        int at = tiles;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, at, o);
-            if (lane >= o) at += v;
-        }
-        if (tile >= __shfl_sync(0xffffffffu, at, 31)) return false;
-        at -= tiles;
-        const bool mine = tile >= at && tile < at + tiles;
-        int slot = 0, from = 0;
-        if (mine)
-            for (int k = lane * eachg; k < min((lane + 1) * eachg, groups); ++k) {
-                const int c = (counts[k] + T - 1) / T;
-                if (tile >= at && tile < at + c) { slot = k; from = (tile - at) * T; }
-                at += c;
-            }
-        const int who = __ffs(__ballot_sync(0xffffffffu, mine)) - 1;
-        slot = __shfl_sync(0xffffffffu, slot, who);
-        from = __shfl_sync(0xffffffffu, from, who);
-        item.slot = slot;
-        item.cnt = min(counts[slot] - from, T);
-        item.rank = ranks[slot];
-        if (t < 32) {
-            const int k0 = lane * eachs, k1 = min(k0 + eachs, p.seqs);
-            int have = 0;
-            for (int k = k0; k < k1; ++k) have += seq_group[k] == slot ? seq_rows[k] : 0;
-            int to = have;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, to, o);
-                if (lane >= o) to += v;
-            }
-            to -= have + from;                             // of the tile's first row
-            if (have > 0 && to < T && to + have > 0)
-                for (int k = k0; k < k1; ++k) {
-                    if (seq_group[k] != slot) continue;
-                    list_rows<T>(s_rows, to, seq_rows[k], seq_first[k]);
-                    to += seq_rows[k];
-                }
-        }
-    } else {
-        // a thread's run of sequences, and of adapters
-        const int per = (p.seqs + THREADS - 1) / THREADS, s0 = min(t * per, p.seqs), s1 = min(s0 + per, p.seqs);
-        for (int i = t; i < groups; i += THREADS) ranks[i] = i < p.slots ? p.cut_rank(p.raw_rank(i)) : 0;
-        for (int s = s0; s < s1; ++s) {
-            const int n = p.count(s), b0 = p.start[s], b1 = p.start[s + 1], ad = p.adapter[s], a = p.group_of(ad);
-            if (n > 0 && a >= 0) atomicAdd(counts + a, n);
-            if (blockIdx.x == 0 && (b0 < 0 || b1 < b0 || b1 > p.rows || ad >= p.slots)) kv::raise_page(p.status);
-        }
-        __syncthreads();
-        if (blockIdx.x == 0)
-            for (int i = t; i < p.slots; i += THREADS)
-                if (counts[i] > 0 && p.raw_rank(i) != ranks[i]) kv::raise_page(p.status);
-        const int each = (groups + THREADS - 1) / THREADS, g0 = min(t * each, groups), g1 = min(g0 + each, groups);
-        int tiles = 0, total, have = 0, all;
-        for (int i = g0; i < g1; ++i) tiles += (counts[i] + T - 1) / T;
-        int at = block_scan<THREADS>(tiles, s_red, total);
-        if (tile >= total) return false;
-        if (tile >= at && tile < at + tiles)
-            for (int i = g0; i < g1; ++i) {
-                const int n = (counts[i] + T - 1) / T;
-                if (tile >= at && tile < at + n) { s_item[0] = i; s_item[1] = (tile - at) * T; }
-                at += n;
-            }
-        __syncthreads();
-        const int slot = s_item[0], from = s_item[1];
-        item.slot = slot;
-        item.cnt = min(counts[slot] - from, T);
-        item.rank = ranks[slot];
-        for (int s = s0; s < s1; ++s) have += p.group_of(p.adapter[s]) == slot ? p.count(s) : 0;
-        int to = block_scan<THREADS>(have, s_red, all) - from;
-        if (have > 0 && to < T && to + have > 0)
-            for (int s = s0; s < s1; ++s) {
-                if (p.group_of(p.adapter[s]) != slot) continue;
-                const int n = p.count(s);
-                list_rows<T>(s_rows, to, n, p.first(s));
-                to += n;
-            }
-    }
-    __syncthreads();
-    return true;
-}
-
 template <typename T, int MT, int HM, int RN>
 __global__ void __launch_bounds__(32 * kGroups * HM, HM == 1 && RN <= 8 ? 2 : 1)
 adapters_add_kernel(const AdapterArgs p) {
@@ -318,7 +130,7 @@ adapters_add_kernel(const AdapterArgs p) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int s_red[kThreads / 32], s_item[4], s_rows[kT];
     const int t = threadIdx.x, lane = t & 31, group = (t >> 5) / HM, m0 = (t >> 5) % HM * MT, g = lane >> 2, q = lane & 3;
-    const int cl = 1 << p.cluster_log2, part = int(blockIdx.x) & (cl - 1), tile = int(blockIdx.x) >> p.cluster_log2;
+    const int cl = p.cluster, tile = int(blockIdx.x) / cl, part = int(blockIdx.x) - tile * cl;
     if (cl > 1) cluster_arrive();                          // waited for before the first write to another CTA's memory: all have started
 
     // ---- the tile's adapter and rows
@@ -333,10 +145,10 @@ adapters_add_kernel(const AdapterArgs p) {
     const __nv_bfloat16* weights = p.B + int64_t(slot) * p.N * p.max_rank;
     const T* base = static_cast<const T*>(p.base);
     T* out = static_cast<T*>(p.out);
-    const int nunits = (p.N + 31) / 32, v0 = nunits * part >> p.cluster_log2, v1 = nunits * (part + 1) >> p.cluster_log2;     // K, N < 2^31: 31 bits
+    const int nunits = (p.N + 31) / 32, v0 = nunits * part / cl, v1 = nunits * (part + 1) / cl;     // K, N < 2^31: 31 bits
 
     // the second product's operands start on their way to L2 under the first one
-    const int units = (p.K + 31) / 32, u0 = units * part >> p.cluster_log2, u1 = units * (part + 1) >> p.cluster_log2;
+    const int units = (p.K + 31) / 32, u0 = units * part / cl, u1 = units * (part + 1) / cl;
     if (rank > 0) {
         const int n0 = 32 * v0, n1 = min(32 * v1, p.N);
         if (2 * rank > p.max_rank) {
@@ -506,12 +318,12 @@ adapters_add_kernel(const AdapterArgs p) {
         }
         __syncwarp();
         if (cl > 1) ptx::cluster_sync(); else __syncthreads();
-        for (int k = t; S::kAll ? k < fours : part + (k << p.cluster_log2) < fours; k += kThreads) {
-            const int e = S::kAll ? k : part + (k << p.cluster_log2), at = e / (kR / 4) * kS + e % (kR / 4) * 4;
+        for (int k = t; S::kAll ? k < fours : part + k * cl < fours; k += kThreads) {
+            const int e = S::kAll ? k : part + k * cl, at = e / (kR / 4) * kS + e % (kR / 4) * 4;
             float f[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
             for (int c = 0; c < cl; ++c) {
-                const float4 o = *reinterpret_cast<const float4*>(s_sum + ((k << p.cluster_log2) + c) * 4);
+                const float4 o = *reinterpret_cast<const float4*>(s_sum + (k * cl + c) * 4);
                 f[0] += o.x; f[1] += o.y; f[2] += o.z; f[3] += o.w;
             }
 #pragma unroll
@@ -609,38 +421,25 @@ adapters_add_kernel(const AdapterArgs p) {
     }
 }
 
-// Allows a kernel clusters of 16, once per kernel and device.
-template <auto Kern>
-cudaError_t allow_large_clusters() {
-    static std::atomic<uint64_t> done{0};
-    int dev = 0;
-    const cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1)) return cudaSuccess;
-    const cudaError_t r = cudaFuncSetAttribute(Kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (r == cudaSuccess && dev < 64) done.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
-    return r;
-}
-
 template <typename T, int MT, int HM, int RN>
 int launch_tiles(AdapterArgs p, cudaStream_t st) {
     using S = Shape<T, MT, HM, RN>;
     constexpr auto kern = adapters_add_kernel<T, MT, HM, RN>;
-    const int64_t tiles = p.rows / S::kTokens + std::min(p.seqs, p.slots + 1);
+    const int64_t groups = std::min<int64_t>({p.seqs, p.slots + 1, p.rows}), tiles = groups + (p.rows - groups) / S::kTokens;
     const int bytes = S::bytes(p.slots), sms = device_sm_count();
     // as many CTAs to a tile as keep the launch near two CTAs on every SM
-    p.cluster_log2 = S::kMostLog2;
-    while (p.cluster_log2 > 0 && tiles << p.cluster_log2 > (p.cluster_log2 == 4 ? sms / 2 : 2 * sms)) --p.cluster_log2;
+    p.cluster = 1 << S::kMostLog2;
+    while (p.cluster > 1 && tiles * p.cluster > (p.cluster == 16 ? sms / 2 : 2 * sms)) p.cluster /= 2;
     QLLM_CUDA_TRY(allow_smem<kern>(S::bytes(8192)));
-    if (p.cluster_log2 > 3) QLLM_CUDA_TRY(allow_large_clusters<kern>());
+    if (p.cluster > 8) QLLM_CUDA_TRY(allow_large_clusters<kern>());
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(tiles << p.cluster_log2));
+    cfg.gridDim = dim3(unsigned(tiles * p.cluster));
     cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = size_t(bytes);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 1u << p.cluster_log2;
+    attr[0].val.clusterDim.x = unsigned(p.cluster);
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
@@ -650,14 +449,34 @@ int launch_tiles(AdapterArgs p, cudaStream_t st) {
     return after_launch();
 }
 
+// Which kernel serves a bf16 call.  Large tiles: the tensor-core kernel, but where the rank is small and so are the groups of rows (8192 x
+// 10240, rank 32: 256 rows of one adapter 20 us here, 26 there; 1024 rows 46 and 30; rank 64, 17 rows: 29 and 20).  Few rows for each adapter: it
+// has the longer way to its first byte and streams faster behind it (rank 64, 8192 x 10240: one token 12 us here, 13 there; 96 tokens on 24 adapters 25 and
+// 21; rank 16: 10 and 15).
+bool tensor_cores(const AdapterArgs& p, bool few) {
+    const int64_t groups = std::min(p.seqs, p.slots + 1), weights = groups * (int64_t(p.K) + p.N) * p.max_rank;
+    if (!few) return p.max_rank > 32 || (p.rows >= 512 && p.rows >= 128 * groups);
+    return p.max_rank > 64 ? groups >= 12 : p.max_rank > 32 && weights >= 9000000;
+}
+
 template <typename T>
 int launch_adapters(const AdapterArgs& p, cudaStream_t st) {
     // tiles of 16 rows while groups are that small on average
     const bool few = p.rows <= int64_t(16) * std::min(p.seqs, p.slots + 1);
-    if (p.max_rank <= 16) return few ? launch_tiles<T, 1, 1, 2>(p, st) : launch_tiles<T, 2, 2, 2>(p, st);
-    if (p.max_rank <= 32) return few ? launch_tiles<T, 1, 1, 4>(p, st) : launch_tiles<T, 2, 2, 4>(p, st);
-    if (p.max_rank <= 64) return few ? launch_tiles<T, 1, 1, 8>(p, st) : launch_tiles<T, 2, 2, 8>(p, st);
-    return few ? launch_tiles<T, 1, 1, 16>(p, st) : launch_tiles<T, 2, 1, 16>(p, st);
+    if (sizeof(T) == 2 && tensor_cores(p, few)) return launch_tiles_tc(p, few, st);
+    if (few) {
+        if (p.max_rank <= 16) return launch_tiles<T, 1, 1, 2>(p, st);
+        if (p.max_rank <= 32) return launch_tiles<T, 1, 1, 4>(p, st);
+        if (p.max_rank <= 64) return launch_tiles<T, 1, 1, 8>(p, st);
+        return launch_tiles<T, 1, 1, 16>(p, st);
+    }
+    if (p.max_rank <= 16) return launch_tiles<T, 2, 2, 2>(p, st);
+    if (p.max_rank <= 32) return launch_tiles<T, 2, 2, 4>(p, st);
+    if constexpr (sizeof(T) == 4) {
+        if (p.max_rank <= 64) return launch_tiles<T, 2, 2, 8>(p, st);
+        return launch_tiles<T, 2, 1, 16>(p, st);
+    }
+    return QLLM_ERR_UNSUPPORTED;                           // (not reached: large ranks are the other kernel's)
 }
 
 int check_rows(const void* p, int64_t stride, int width, int dtype) {
@@ -687,7 +506,7 @@ extern "C" int qllm_adapters_add(const qllm_adapters_t* ad, const void* x, int64
     int* status = device_status_word();
     if (!status) return QLLM_ERR_CUDA;
     const AdapterArgs p{static_cast<const __nv_bfloat16*>(ad->A), static_cast<const __nv_bfloat16*>(ad->B), ad->scale, ad->rank, ad->slots, ad->max_rank,
-                        ad->K, ad->N, q_start, adapter, seqs, 0, rows, x, base, out, x_stride, base_stride, out_stride, status};
+                        ad->K, ad->N, q_start, adapter, seqs, 1, rows, x, base, out, x_stride, base_stride, out_stride, status};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return dtype == QLLM_BF16 ? launch_adapters<__nv_bfloat16>(p, st) : launch_adapters<float>(p, st);
 }

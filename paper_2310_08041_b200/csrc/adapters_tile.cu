@@ -1,0 +1,503 @@
+// qllm_adapters_add for bf16 on the tensor cores (tcgen05): up to 128 rows of one adapter are the M side of both products,
+//
+//   D1[rows x ranks] = X A^T over this CTA's part of K,  H = scale * (sum of the cluster's D1),  D2[rows x 128] = H B^T, out = base + D2.
+//
+// A cluster owns a tile (adapters.cuh finds its rows); each CTA takes a part of K in the first product and a part of N in the second, the
+// sums over K are exchanged over distributed shared memory.  Eight warps feed a ring of stages by asynchronous copies of 16 bytes a thread,
+// swizzled as the tensor core reads operands (rows of 128 bytes, 16-byte pieces at piece ^ (row & 7)): first 128 columns of A and of the
+// tile's rows of x a stage, then, without waiting for the sums, 128 rows of B and 128 columns of base.  Copies fill with zeros what lies behind
+// K and, in B, behind the rank, so operands need no masks; rows behind the tile and the rank are whatever is there: they only reach
+// sums that are dropped.  Two threads issue the MMAs, every second stage each; two teams of four warps, a thread for each row of the tile, read the sums back from tensor
+// memory, 128 columns of the second product in turn.  H enters
+// the second product as two bf16 parts, 16 bits.
+//
+// ROWS: rows of the tile that stages have room for.  With 16 (a step's single tokens) the first product's other 112 rows are whatever follows in
+// shared memory, the second's are H three times more: a warp reaches a quarter of the rows in tensor memory, so each of four has all 16
+// rows and takes a quarter of the columns.  The tensor core has time for it, and stages are small enough that eight are in flight.
+//
+// What bounds it: memory.  The MMAs of a tile take a tenth of its time; the warp-level MMA (adapters.cu) took a third of it for prompts
+// (some 20 cycles for each m16n8k16 and quarter of an SM).
+#include <algorithm>
+
+#include "adapters.cuh"
+#include "qgemm_tc_common.cuh"
+
+namespace qllm {
+namespace lora {
+namespace {
+
+using tc::Abort;
+using tc::wait_bounded;
+
+constexpr int kFeeders = 256, kTeam = 128, kWorkers = 2 * kTeam, kIssuers = 2, kThreads = kWorkers + 32 * kIssuers + kFeeders, kCols = 128;
+
+template <int R, int ROWS>
+struct Shape {
+    static constexpr int kBlocks = (R + 63) / 64;          // operand blocks (64 elements of 128 bytes) of a row of B
+    static constexpr bool kSide = R <= 32;                 // both parts of H in one block
+    static constexpr int kHBlocks = kSide ? 1 : 2 * kBlocks;
+    static constexpr bool kAll = ROWS == 16;               // few rows: every CTA adds up all parts of the sums; H four times, for four warps
+    static constexpr int kABlock = R * 128, kXBlock = ROWS * 128, kBBlock = kCols * 128, kHBlock = kAll ? 128 * 128 : kXBlock;
+    static constexpr int kPitch = kCols * 2 + 16;          // bytes between rows of base: 16-byte accesses of 8 rows in different banks
+    static constexpr int kStageK = 2 * (kABlock + kXBlock), kStageN = kBlocks * kBBlock + ROWS * kPitch;
+    static constexpr int kStage = ((kStageK > kStageN ? kStageK : kStageN) + 1023) / 1024 * 1024;
+    static constexpr int kPart = kAll ? ROWS * R * 4 : 0, kSum = kAll ? 8 * ROWS * R * 4 : ROWS * R * 4 + 8 * 16;
+    static constexpr int kFixed = kHBlocks * kHBlock + kPart + kSum + (ROWS < 128 ? 128 * 128 : 0) + 1024;      // (operands are read 128 rows deep)
+    static constexpr int kMost = (223 * 1024 - kFixed) / kStage, kStages = kMost > 8 ? 8 : kMost;
+    static constexpr int kBytes = kFixed + kStages * kStage;
+    static_assert(kStages >= 2, "two stages at least");
+};
+
+// kind::f16: bf16 x bf16, both K-major, float32 sums
+__host__ __device__ constexpr uint32_t idesc_bf16(int m, int n) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
+}
+// Operands by the low words of their descriptors (128-byte swizzle, K-major, groups of 8 rows 1024 bytes apart; the high word is the same for
+// all): a step along an operand is one addition for the one thread that issues.
+constexpr uint32_t kDescHigh = uint32_t((uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61) >> 32);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr) { return (addr & 0x3FFFFu) >> 4 | 1u << 16; }
+__device__ __forceinline__ void mma_bf16_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
+                 : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+__device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+// 16 bytes, of which the first `bytes` are copied and the others become zeros
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// This thread's arrival on `bar`, once all copies that it has asked for have landed.
+__device__ __forceinline__ void arrive_with_copies(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(ptx::smem_addr(bar)) : "memory");
+}
+// wait_bounded for a barrier's first phase that CTAs of the cluster arrive on: what they wrote before is seen behind it
+__device__ __forceinline__ bool wait_cluster(uint64_t* bar, const Abort& ab) {
+    const bool ok = wait_bounded(bar, 0, ab);
+    asm volatile("fence.acq_rel.cluster;" ::: "memory");
+    return ok;
+}
+// shared memory by 32-bit address
+__device__ __forceinline__ uint4 lds4(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ void sts4(uint32_t a, uint4 v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ bool all(bool ok) { return __all_sync(0xffffffffu, ok); }
+
+template <int R, int ROWS>
+__global__ void __launch_bounds__(kThreads, 1)
+adapters_tile_kernel(const AdapterArgs p) {
+    using S = Shape<R, ROWS>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t s_full[S::kStages], s_empty[S::kStages], s_ready[2], s_d1, s_h, s_d2[2], s_d2_free[2];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_red[kThreads / 32], s_item[2], s_rows[ROWS], s_abort;
+    uint8_t* smem = smem_raw + (1024 - (ptx::smem_addr(smem_raw) & 1023)) % 1024;
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int cl = p.cluster, tile = int(blockIdx.x) / cl, part = int(blockIdx.x) - tile * cl;
+    if (t == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            ptx::mbar_init(&s_full[i], kFeeders);
+            ptx::mbar_init(&s_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            ptx::mbar_init(&s_ready[i], cl);
+            ptx::mbar_init(&s_d2[i], 1);
+            ptx::mbar_init(&s_d2_free[i], kTeam / 32);
+        }
+        ptx::mbar_init(&s_d1, kIssuers);
+        ptx::mbar_init(&s_h, kWorkers);
+        ptx::fence_barrier_init();
+        s_abort = 0;
+    }
+    __syncwarp();
+    if (cl > 1) cluster_arrive();                          // waited for below: all CTAs have started, their barriers are set
+    Item item;
+    if (!find_item<kThreads, ROWS>(p, tile, smem, s_red, s_item, s_rows, item)) return;  // the same in all CTAs of a cluster
+    if (cl > 1) cluster_wait();
+    if (warp == 0) {
+        ptx::tmem_alloc(&s_tmem, 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = s_tmem;                          // two D2 in columns 0 .. 255, two D1 from 256 on
+    const int slot = item.slot, cnt = item.cnt, rank = item.rank;
+    // this CTA's parts of K and N, in units of 64 and 128 (K, N < 2^31)
+    const int ku = (p.K + 63) / 64, nu = (p.N + kCols - 1) / kCols;
+    const int k0 = 64 * (ku * part / cl), k1 = rank > 0 ? min(64 * (ku * (part + 1) / cl), p.K) : k0;
+    const int n0 = kCols * (nu * part / cl), n1 = min(kCols * (nu * (part + 1) / cl), p.N);
+    uint8_t* s_hop = smem + S::kStages * S::kStage;        // H as operand
+    float* s_part = reinterpret_cast<float*>(s_hop + S::kHBlocks * S::kHBlock);
+    float* s_sum = s_part + S::kPart / 4;
+    const Abort ab{&s_abort, p.status};
+    int sg = 0;
+    uint32_t turn = 0;
+    const auto advance = [&] {
+        if (++sg == S::kStages) { sg = 0; turn ^= 1; }
+    };
+
+    if (warp >= kWorkers / 32 + kIssuers) {
+        // ---------------------------------------------------------------- feeders: a thread has the same 16 bytes of its rows in all stages
+        const int me = t - kWorkers - 32 * kIssuers, piece = me & 15, row0 = me >> 4;              // 16 rows of 256 bytes at a time
+        constexpr int kX = ROWS / 16, kA = R / 16;
+        const uint8_t* src[kX];
+        const auto set_rows = [&](const void* m, int64_t stride, int at) {
+#pragma unroll
+            for (int i = 0; i < kX; ++i)
+                src[i] = static_cast<const uint8_t*>(m) + (int64_t(max(s_rows[min(row0 + 16 * i, cnt - 1)], 0)) * stride + at + 8 * piece) * 2;
+        };
+        // place in an operand block of the row and 16-byte piece that this thread copies
+        const uint32_t swz = uint32_t(row0 * 128 + (((piece & 7) ^ (row0 & 7)) << 4)), base_addr = ptx::smem_addr(smem);
+        bool ok = true;
+        set_rows(p.x, p.x_stride, k0);
+        const uint8_t* a = reinterpret_cast<const uint8_t*>(p.A + (int64_t(slot) * p.max_rank + row0) * p.K + k0 + 8 * piece);
+        const int64_t a_step = int64_t(16) * p.K * 2;
+        for (int k = k0; k < k1; k += kCols) {
+            if (!(ok = all(wait_bounded(&s_empty[sg], turn ^ 1, ab)))) break;
+            const uint32_t to = base_addr + sg * S::kStage + swz;
+            const int bytes = k + 8 * piece < k1 ? 16 : 0;             // behind the last column: zeros
+            const int64_t back = bytes ? 0 : int64_t(k1 - 8 - k - 8 * piece) * 2;       // (from an address that exists)
+            const uint32_t block = piece >> 3;
+#pragma unroll
+            for (int i = 0; i < kA; ++i)
+                if (row0 + 16 * i < rank) cp_async16(to + block * S::kABlock + i * 2048, a + i * a_step + back, bytes);
+#pragma unroll
+            for (int i = 0; i < kX; ++i) {
+                if (row0 + 16 * i < cnt) cp_async16(to + 2 * S::kABlock + block * S::kXBlock + i * 2048, src[i] + back, bytes);
+                src[i] += kCols * 2;
+            }
+            a += kCols * 2;
+            arrive_with_copies(&s_full[sg]);
+            advance();
+        }
+        // rows of B: R / 8 pieces of each, side by side; what lies behind the rank in the last 16 that are used becomes zero
+        constexpr int kP = R / 8, kRows = kFeeders / kP, kTimes = kCols / kRows;
+        const int bp = me % kP, br = me / kP, bytes = min(max(rank - 8 * bp, 0), 8) * 2;
+        const bool used = 8 * bp < (rank + 15) / 16 * 16;
+        const uint8_t* w = reinterpret_cast<const uint8_t*>(p.B + (int64_t(slot) * p.N + n0 + br) * p.max_rank) + (bytes ? 16 * bp : 0);
+        const int64_t w_step = int64_t(kRows) * p.max_rank * 2, w_stage = int64_t(kCols) * p.max_rank * 2;
+        if (p.base) set_rows(p.base, p.base_stride, n0);
+        for (int n = n0; ok && n < n1; n += kCols) {
+            if (!(ok = all(wait_bounded(&s_empty[sg], turn ^ 1, ab)))) break;
+            const uint32_t to = base_addr + sg * S::kStage;
+            if (used) {
+#pragma unroll
+                for (int i = 0; i < kTimes; ++i) {
+                    const int r = br + i * kRows;
+                    if (n + r < n1) cp_async16(to + (bp >> 3) * S::kBBlock + r * 128 + (((bp & 7) ^ (r & 7)) << 4), w + i * w_step, bytes);
+                }
+            }
+            w += w_stage;
+            if (p.base) {
+                const uint32_t cell = to + S::kBlocks * S::kBBlock + row0 * S::kPitch + piece * 16;
+#pragma unroll
+                for (int i = 0; i < kX; ++i) {
+                    if (row0 + 16 * i < cnt && n + 8 * piece < n1) cp_async16(cell + 16 * i * S::kPitch, src[i], 16);
+                    src[i] += kCols * 2;
+                }
+            }
+            arrive_with_copies(&s_full[sg]);
+            advance();
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        return;
+    }
+
+    if (warp >= kWorkers / 32) {
+        // ---------------------------------------------------------------- one thread of each of two warps issues the MMAs of every second
+        // stage, to sums of its own (all lanes walk along, so that operands are the warp's, not a thread's)
+        const int me = warp - kWorkers / 32;
+        if (rank > 0) {
+            constexpr uint32_t id1 = idesc_bf16(128, R), id2 = idesc_bf16(128, kCols);
+            const uint32_t base_addr = ptx::smem_addr(smem), h_low = desc_low(ptx::smem_addr(s_hop)), d = __shfl_sync(0xffffffffu, tmem, 0);
+            const uint32_t d1 = d + 256 + me * R, d2 = d + me * kCols;
+            const bool lead = elect_one();
+            bool ok = true;
+            uint32_t more = 0;
+            int turns = 0;
+            for (int k = k0; k < k1; k += kCols, advance(), ++turns) {
+                if ((turns & 1) != me) continue;
+                if (!(ok = all(wait_bounded(&s_full[sg], turn, ab)))) break;
+                ptx::fence_proxy_async_smem();             // copies of the generic proxy, read by the tensor core
+                ptx::tc_fence_after_sync();
+                const uint32_t ranks = desc_low(base_addr + sg * S::kStage), rows = ranks + (2 * S::kABlock >> 4);
+                if (lead) {
+#pragma unroll
+                    for (int s = 0; s < 8; ++s)
+                        mma_bf16_ss(d1, rows + (((s >> 2) * S::kXBlock + (s & 3) * 32) >> 4), ranks + (((s >> 2) * S::kABlock + (s & 3) * 32) >> 4), id1,
+                                    s > 0 ? 1u : more);
+                    ptx::mma_commit(&s_empty[sg]);
+                }
+                __syncwarp();
+                more = 1;
+            }
+            if (ok && lead) ptx::mma_commit(&s_d1);
+            if (ok) ok = all(wait_bounded(&s_h, 0, ab));
+            ptx::fence_proxy_async_smem();
+            ptx::tc_fence_after_sync();
+            const int steps = (rank + 15) / 16;
+            uint32_t round = 0;
+            turns = 0;
+            for (int n = n0; ok && n < n1; n += kCols, advance(), ++turns) {
+                if ((turns & 1) != me) continue;
+                ok = all(wait_bounded(&s_full[sg], turn, ab) && wait_bounded(&s_d2_free[me], round ^ 1, ab));
+                if (!ok) break;
+                ptx::fence_proxy_async_smem();
+                ptx::tc_fence_after_sync();
+                const uint32_t columns = desc_low(base_addr + sg * S::kStage);
+                if (lead) {
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int s = 0; s < R / 16; ++s) {
+                            if (s > 0 && s >= steps) break;
+                            mma_bf16_ss(d2, h_low + ((S::kSide ? half * 2 * R + s * 32 : (half * S::kBlocks + (s >> 2)) * S::kHBlock + (s & 3) * 32) >> 4),
+                                        columns + (((s >> 2) * S::kBBlock + (s & 3) * 32) >> 4), id2, half > 0 || s > 0);
+                        }
+                    ptx::mma_commit(&s_d2[me]);
+                }
+                __syncwarp();
+                round ^= 1;
+            }
+        }
+        return;
+    }
+
+    // -------------------------------------------------------------------- workers: two teams, thread `row` of a team has that row of the tile
+    const int team = t / kTeam, row = t % kTeam, quarter = warp & 3;
+    const uint32_t my_tmem = tmem + (uint32_t(quarter * 32) << 16);
+    bool ok = true;                                        // false: a wait ran out; go through the motions without waiting
+    for (int k = k0; k < k1; k += kCols) advance();        // the stages of the first product are the MMAs'
+    if (rank > 0) {
+        ok = all(wait_bounded(&s_d1, 0, ab));
+        ptx::tc_fence_after_sync();
+        const int parts = min((k1 - k0 + kCols - 1) / kCols, 2);       // issuers that had a stage
+        // Sums in fours.  Small tiles: every CTA hands all of its sums to all CTAs, which add them up, each for itself.  Others: the e-th four
+        // goes to CTA e % cl, which adds the cl parts and hands the result to all; a cl-th of the traffic, one more exchange.
+        const int fours = cnt * (R / 4);
+        const uint32_t sum_addr = ptx::smem_addr(s_sum), h_addr = ptx::smem_addr(s_hop);
+        const float scale = p.scale[slot];
+        if (quarter * 32 < cnt) {
+#pragma unroll 1
+            for (int c = 16 * team; c < R; c += 32) {
+                float d[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) d[i] = 0.f;
+                for (int i = 0; i < parts; ++i) {
+                    uint32_t w[16];
+                    tmem_ld_x16(my_tmem + 256 + i * R + c, w);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) d[j] += __uint_as_float(w[j]);
+                }
+                if (row < cnt) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = row * (R / 4) + c / 4 + i;
+                        const float4 v = make_float4(d[4 * i], d[4 * i + 1], d[4 * i + 2], d[4 * i + 3]);
+                        if constexpr (S::kAll) reinterpret_cast<float4*>(s_part)[e] = v;
+                        else st_cluster4(ptx::map_to_cta(sum_addr + (e / cl * cl + part) * 16, e % cl), v);
+                    }
+                }
+            }
+        }
+        ptx::named_bar_sync(1, kWorkers);
+        if constexpr (S::kAll) {
+            for (int i = t; i < fours * cl; i += kWorkers) {
+                const int e = i / cl, to = i - e * cl;
+                st_cluster4(ptx::map_to_cta(sum_addr + (e * cl + part) * 16, to), reinterpret_cast<const float4*>(s_part)[e]);
+            }
+            ptx::named_bar_sync(1, kWorkers);
+        }
+        if (t < cl) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_addr(&s_ready[0]), t));
+        ok = all(ok && wait_cluster(&s_ready[0], ab));
+        for (int k = t; S::kAll ? k < fours : part + k * cl < fours; k += kWorkers) {
+            const int e = S::kAll ? k : part + k * cl, at_row = e / (R / 4), col = e % (R / 4) * 4;
+            float f[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int c = 0; c < cl; ++c) {
+                const float4 o = *reinterpret_cast<const float4*>(s_sum + (k * cl + c) * 4);
+                f[0] += o.x; f[1] += o.y; f[2] += o.z; f[3] += o.w;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = col + i < rank ? f[i] * scale : 0.f;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const uint32_t w0 = half ? rounded(f[0], f[1]) : upper(f[0], f[1]), w1 = half ? rounded(f[2], f[3]) : upper(f[2], f[3]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[j] = rest(f[j]);
+                const int byte = S::kSide ? half * 2 * R + 2 * col : 2 * (col & 63), block = S::kSide ? 0 : half * S::kBlocks + (col >> 6);
+                const uint32_t at = h_addr + block * S::kHBlock + at_row * 128 + (((byte >> 4) ^ (at_row & 7)) << 4) + (byte & 15);
+                if constexpr (S::kAll) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + i * 4096), "r"(w0), "r"(w1) : "memory");
+                } else {
+                    for (int c = 0; c < cl; ++c) st_cluster2(ptx::map_to_cta(at, c), w0, w1);
+                }
+            }
+        }
+        if constexpr (!S::kAll) {
+            ptx::named_bar_sync(1, kWorkers);
+            if (t < cl) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_addr(&s_ready[1]), t));
+            ok = all(ok && wait_cluster(&s_ready[1], ab));
+        }
+        ptx::fence_proxy_async_smem();                     // H is read by the tensor core
+        ptx::mbar_arrive(&s_h);
+    }
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out);
+    const bool has_base = p.base != nullptr;
+    const uint32_t smem_base = ptx::smem_addr(smem);
+    const bool wide = ROWS > 16;                           // a thread per row and all columns; else 16 rows and a quarter of them
+    const int own = wide ? row : lane;                     // the tile's row that this thread has
+    const int my_row = own < cnt ? s_rows[own % ROWS] : -1;
+    __nv_bfloat16* my_out = out + int64_t(max(my_row, 0)) * p.out_stride;
+    int out_row[wide ? ROWS / 8 : 1];                      // rows that this thread copies out
+    if constexpr (wide) {
+#pragma unroll
+        for (int i = 0; i < ROWS / 8; ++i) out_row[i] = (row >> 4) + 8 * i < cnt ? s_rows[(row >> 4) + 8 * i] : -1;
+    }
+    uint32_t round = 0;
+    int turns = 0;
+    for (int n = n0; n < n1; n += kCols, advance(), ++turns) {
+        if ((turns & 1) != team) continue;                 // the other team's
+        ok = all(ok && wait_bounded(&s_full[sg], turn, ab) && (rank == 0 || wait_bounded(&s_d2[team], round, ab)));
+        ptx::tc_fence_after_sync();
+        const uint32_t cells = smem_base + sg * S::kStage + S::kBlocks * S::kBBlock, cell_addr = cells + own * S::kPitch;
+        if (ok && (!wide || quarter * 32 < cnt)) {
+#pragma unroll 1
+            for (int c = wide ? 0 : 32 * quarter; c < (wide ? kCols : 32 * quarter + 32); c += 32) {
+                uint32_t d[32];
+                if (rank > 0) {
+                    ptx::tmem_ld_32x32b_x32(my_tmem + team * kCols + c, d);
+                    ptx::tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) d[i] = 0;
+                }
+                if (own < cnt) {
+                    uint4 o[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = has_base ? lds4(cell_addr + c * 2 + 16 * i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t w[4] = {o[i].x, o[i].y, o[i].z, o[i].w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            w[j] = rounded(__uint_as_float(w[j] << 16) + __uint_as_float(d[8 * i + 2 * j]),
+                                           __uint_as_float(w[j] & 0xFFFF0000u) + __uint_as_float(d[8 * i + 2 * j + 1]));
+                        o[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (wide) {
+                            sts4(cell_addr + c * 2 + 16 * i, o[i]);
+                        } else {                           // few rows: straight to memory
+                            if (my_row >= 0 && n + c + 8 * i < n1) *reinterpret_cast<uint4*>(my_out + n + c + 8 * i) = o[i];
+                        }
+                    }
+                }
+            }
+        }
+        ptx::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&s_d2_free[team]);
+        ptx::named_bar_sync(2 + team, kTeam);
+        if constexpr (wide) {
+            // 16 threads a row, 8 rows at a time
+            if (ok && n + 8 * (row & 15) < n1) {
+                const uint32_t from = cells + (row >> 4) * S::kPitch + (row & 15) * 16;
+#pragma unroll
+                for (int i0 = 0; i0 < ROWS / 8; i0 += 4) {
+                    uint4 o[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = lds4(from + (i0 + i) * 8 * S::kPitch);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (out_row[i0 + i] >= 0) *reinterpret_cast<uint4*>(out + int64_t(out_row[i0 + i]) * p.out_stride + n + 8 * (row & 15)) = o[i];
+                }
+            }
+            ptx::named_bar_sync(2 + team, kTeam);
+        }
+        if (row == 0) ptx::mbar_arrive(&s_empty[sg]);
+        round ^= 1;
+    }
+    if (!ok) {                                             // MMAs that were issued before a wait ran out
+        const long long since = clock64();
+        while (clock64() - since < (1ll << 20)) {}
+    }
+    ptx::tc_fence_before_sync();
+    ptx::named_bar_sync(1, kWorkers);
+    ptx::tc_fence_after_sync();
+    if (warp == 0) ptx::tmem_dealloc(tmem, 512);
+}
+
+template <int R, int ROWS>
+int launch_shape(AdapterArgs p, cudaStream_t st) {
+    using S = Shape<R, ROWS>;
+    constexpr auto kern = adapters_tile_kernel<R, ROWS>;
+    static_assert(find_bytes(8192, kThreads) + 1024 <= S::kBytes, "the counts of 8192 adapters lie where the stages will be");
+    // tiles: at most, and about (a group's last tile is half full, but every group has one)
+    const int64_t groups = std::min<int64_t>({p.seqs, p.slots + 1, p.rows}), tiles = groups + (p.rows - groups) / ROWS;
+    const int64_t likely = std::max(groups, (p.rows + groups * (ROWS / 2)) / ROWS);
+    QLLM_CUDA_TRY(allow_smem<kern>(S::kBytes));
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = S::kBytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    // as many CTAs to a tile as let all tiles run at once (clusters of 4: 33 of 148 SMs' possible 37, whatever their parts of the chip)
+    static std::atomic<int> known[64][9];
+    int dev = 0;
+    QLLM_CUDA_TRY(cudaGetDevice(&dev));
+    for (p.cluster = 8; p.cluster > 1; --p.cluster) {
+        int most = dev < 64 ? known[dev][p.cluster].load(std::memory_order_relaxed) : 0;
+        if (!most) {
+            attr[0].val.clusterDim.x = unsigned(p.cluster);
+            cfg.gridDim = dim3(unsigned(p.cluster));
+            cfg.numAttrs = 1;
+            QLLM_CUDA_TRY(cudaOccupancyMaxActiveClusters(&most, kern, &cfg));
+            most = std::max(most, 1);
+            if (dev < 64) known[dev][p.cluster].store(most, std::memory_order_relaxed);
+        }
+        if (likely <= most) break;
+    }
+    attr[0].val.clusterDim.x = unsigned(p.cluster);
+    cfg.gridDim = dim3(unsigned(tiles * p.cluster));
+    cfg.numAttrs = 2;
+    QLLM_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, p));
+    return after_launch();
+}
+
+}  // namespace
+
+int launch_tiles_tc(const AdapterArgs& p, bool few, cudaStream_t st) {
+    if (p.max_rank <= 16) return launch_shape<16, 128>(p, st);
+    if (p.max_rank <= 32) return launch_shape<32, 128>(p, st);
+    if (p.max_rank <= 64) return few ? launch_shape<64, 16>(p, st) : launch_shape<64, 128>(p, st);
+    return launch_shape<128, 64>(p, st);                   // (shared memory has no room for four times H)
+}
+
+}  // namespace lora
+}  // namespace qllm

@@ -2,7 +2,7 @@
 
 Bound.  A x: products of exact operands, summed in float32 by 16-term MMAs, eight warps and up to eight CTAs: at most K / 16 + 32
 additions in a row with a relative error of 2^-23 each (an MMA's own additions may be truncated), of what the terms come to without
-signs; that error goes through B.  The sums enter the second product with 16 bits for bf16 (two truncated-then-rounded parts: 2^-16),
+signs; that error goes through B.  The sums enter the second product with 16 bits for bf16 (a truncated and a rounded part: 2^-16),
 24 for float32.  The second product: max_rank / 16 x parts MMA steps.  Then base is added (a float32 rounding) and the result rounded to
 its type."""
 import numpy as np
@@ -106,6 +106,31 @@ def test_a_step_of_many_requests(dtype, K, N, top):
 def test_prompts_and_tokens(dtype, K, N, top):
     """Runs of rows longer and shorter than a tile, the same adapter in sequences far apart."""
     case(dtype, K, N, top, [top, top // 2, top - 1], [130, 1, 64, 0, 17, 300, 1, 65, 16], [0, 1, 2, 0, 0, 1, -1, 2, 1], lead=1, tail=5)
+
+
+@pytest.mark.parametrize("K,N,top,slots", [(8192, 10240, 64, 14), (8200, 10248, 40, 18), (8136, 10120, 56, 15), (1032, 264, 128, 13), (40, 72, 72, 30), (4096, 1288, 120, 20)])
+@pytest.mark.parametrize("rows", ["ones", "some"])
+def test_steps_of_large_adapters(K, N, top, slots, rows):
+    """Few rows for each of many large adapters, ranks from 0 to all, groups of 1 to 30 rows."""
+    rng = np.random.RandomState(K + top)
+    seqs = 40 if rows == "ones" else 25
+    news = np.ones(seqs, int) if rows == "ones" else rng.choice([0, 1, 3, 9], seqs)
+    ranks = [top, 0, 1, top - 1, top // 2] + [int(r) for r in rng.randint(1, top + 1, slots - 5)]
+    case("bf16", K, N, top, ranks, news, rng.randint(-1, slots, seqs), lead=2, tail=1)
+    case("bf16", K, N, top, ranks, news, rng.randint(-1, slots, seqs), inplace=True)
+
+
+@pytest.mark.parametrize("K,N", [(40, 72), (1032, 264), (4104, 2056)])
+@pytest.mark.parametrize("top", [8, 16, 24, 32, 40, 64, 72, 128])
+def test_long_prompts(K, N, top):
+    """Tiles of 64 and 128 rows, full and ragged, all of one adapter or cut by others; strided, in place, without a base."""
+    case("bf16", K, N, top, [top, max(1, top - 5)], [513, 1, 700], [0, 1, 1], pad=(8, 16, 24))
+    case("bf16", K, N, top, [top], [1111], [0], inplace=True, pad=(0, 0, 8))
+    start, adapter = [0, 600, 640, 1300], [0, -1, 0]
+    x = torch.randn(1300, K, device=G.DEV).bfloat16()
+    ad = make(1, top, K, N, [top])
+    got, _ = run(ad, x, None, start, adapter)
+    check(got, ad, [top], x, torch.zeros_like(got), start, adapter)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
