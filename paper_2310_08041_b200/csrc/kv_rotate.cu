@@ -8,8 +8,8 @@
 // It moves bytes: queries in and out, keys and values in, (head_dim / 2 + 8) bytes a row out, 4 rot_dim bytes of table a token.
 // head_dim / 16 lanes own a row, 16 channels each in two runs of 8, so chosen that both channels of a pair lie in one lane: for pairs
 // (p, p + rot_dim / 2) lane l < rot_dim / 16 has the runs l and l + rot_dim / 16, for pairs (2p, 2p + 1) two neighbouring runs; either way its
-// pairs are 8l .. 8l + 7, one 64-byte piece of the table.  A unit of work is kRows rows of one token: their loads are in flight
-// together and share the cosines and sines in registers.  Rows of a token are ordered [queries][keys][values].
+// pairs are 8l .. 8l + 7, one 64-byte piece of the table.  A unit of work is a few rows of one token and one kind (queries, keys or values):
+// their loads are in flight together, before the token's place has been found, and share the cosines and sines in registers.
 
 #include <algorithm>
 
@@ -32,147 +32,203 @@ struct Turn {
     int q_heads;
 };
 
-// 8 channels; plain loads (queries may be turned in place)
-__device__ __forceinline__ void get8(const float* p, float (&f)[8]) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
-__device__ __forceinline__ void get8(const __nv_bfloat16* p, float (&f)[8]) {
-    const uint4 r = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+// 8 channels as they lie in memory; plain loads (queries may be turned in place)
+template <typename T>
+struct Run8;
+template <>
+struct Run8<__nv_bfloat16> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        f[2 * k] = __uint_as_float(w[k] << 16);
-        f[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-    }
-}
-__device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s) {
-    const float x = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s)), y = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
-    a = x;
-    b = y;
-}
-
-constexpr int kRows = 4;
-
-template <typename T, int D>
-__global__ void __launch_bounds__(256)
-kv_rotate_append_kernel(const Turn a, const Cache c, const Batch b, const Angles ang, int run, int* status) {
-    constexpr int L = D / 16, G = 256 / L;                 // lanes of a row, units of a CTA in flight
-    __shared__ int4 s_place[kMostTokens];                  // page (or -1: nobody's row, -2: no place), place in it, position or -1
-    const int lane = threadIdx.x % L, group = threadIdx.x / L;
-    const int heads = c.heads, rows = a.q_heads + 2 * heads, blocks = (rows + kRows - 1) / kRows;
-    const int64_t t0 = int64_t(blockIdx.x) * run;
-    const int tokens = int(min(int64_t(run), b.rows - t0)), units = tokens * blocks;
-    asm volatile("griddepcontrol.wait;" ::: "memory");     // launched as a dependent
-    if (threadIdx.x < 32) {
-        const int i = threadIdx.x;
-        const int s = seq_of_lane(b, t0, tokens, i);
-        if (i < tokens) {
-            int4 at = make_int4(-1, 0, -1, 0);
-            if (s >= 0) {
-                const int64_t pos = int64_t(b.len(s)) - b.count(s) + (t0 + i - b.row(s));
-                at.x = -2;
-                if (pos >= ang.positions) {
-                    raise_page(status);
-                } else if (pos >= 0) {
-                    at.z = int(pos);
-                    const int page = b.table[int64_t(s) * b.width + (pos >> b.page_log2)];
-                    if (page >= 0 && page < c.pages) { at.x = page; at.y = int(pos) & ((1 << b.page_log2) - 1); }
-                    else raise_page(status);
-                }
-            }
-            s_place[i] = at;
+        for (int k = 0; k < 4; ++k) {
+            f[2 * k] = __uint_as_float(w[k] << 16);
+            f[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
         }
     }
-    if (blockIdx.x == 0) b.report(status, threadIdx.x, 256);
-    __syncthreads();
+};
+template <>
+struct Run8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
+    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    }
+};
+
+// the least of three, NaN if one is
+__device__ __forceinline__ float min3_nan(float a, float b, float c) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// The lane's pairs (a, b) by cosine and sine, one rounding an operation.  (The packed operations on two floats would be half as many
+// instructions, but a packed product and sum come out fused, whatever rounding they name.)
+struct Sines {
+    float4 w[4];                                           // cos, sin of two pairs
+    __device__ __forceinline__ void load(const float4* p) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = __ldg(p + j);
+    }
+    __device__ __forceinline__ void turn(float c, float s, float& a, float& b) const {
+        const float x = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
+        b = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
+        a = x;
+    }
+    __device__ __forceinline__ void turn_row(float (&f)[2][8], bool interleaved) const {
+        if (interleaved) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                turn(w[j].x, w[j].y, f[j >> 1][4 * (j & 1)], f[j >> 1][4 * (j & 1) + 1]);
+                turn(w[j].z, w[j].w, f[j >> 1][4 * (j & 1) + 2], f[j >> 1][4 * (j & 1) + 3]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                turn(w[j].x, w[j].y, f[0][2 * j], f[1][2 * j]);
+                turn(w[j].z, w[j].w, f[0][2 * j + 1], f[1][2 * j + 1]);
+            }
+        }
+    }
+};
+
+// A CTA's tokens and units: U rows of one kind each, ordered [token][queries, keys, values].
+struct Work {
+    int tokens, q_blocks, kv_blocks;
+    uint32_t inverse;                                      // ceil(2^32 / blocks): unit -> token, units < 2^16
+};
+
+template <typename T, int D, int U>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2)
+kv_rotate_append_kernel(const Turn a, const Cache c, const Batch b, const Angles ang, const Work work, int* status) {
+    constexpr int L = D / 16, G = 256 / L;                 // lanes of a row, units of a CTA in flight
+    __shared__ int4 s_place[kMostTokens];                  // page (or -1: nobody's row, -2: no place), place in it, position or -1
+    const int lane = threadIdx.x % L, group = threadIdx.x / L, blocks = work.q_blocks + 2 * work.kv_blocks;
+    const int64_t t0 = int64_t(blockIdx.x) * work.tokens;
+    const int tokens = int(min(int64_t(work.tokens), b.rows - t0)), units = tokens * blocks;
     const int turned = ang.rot_dim / 16;                   // lanes that turn
     int ra = 2 * lane, rb = 2 * lane + 1;                  // the lane's runs of 8 channels
     if (!ang.interleaved && lane < turned) { ra = lane; rb = lane + turned; }
-
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // launched as a dependent: nothing above touched global memory
     for (int base = 0; base < units; base += G) {
-        const int unit = base + group, tok = min(unit / blocks, tokens - 1), first = (unit - unit / blocks * blocks) * kRows;
-        const int4 at = s_place[tok];
-        const bool on = unit < units && at.x != -1;
+        const int unit = min(base + group, units - 1), tok = int(__umulhi(uint32_t(unit), work.inverse)), block = unit - tok * blocks;
         const int64_t t = t0 + tok;
-        float f[kRows][2][8];
-        int kind[kRows], head[kRows];                      // 0 query, 1 key, 2 value, -1 nothing to do
+        const int kind = block < work.q_blocks ? 0 : block < work.q_blocks + work.kv_blocks ? 1 : 2;       // query, key, value
+        const int head = (kind == 0 ? block : kind == 1 ? block - work.q_blocks : block - work.q_blocks - work.kv_blocks) * U;
+        const int rows = base + group < units ? min(U, (kind == 0 ? a.q_heads : c.heads) - head) : 0;
+        const T* p = (kind == 0 ? static_cast<const T*>(a.q) + t * a.q_stride
+                    : kind == 1 ? static_cast<const T*>(a.k) + t * a.k_stride : static_cast<const T*>(a.v) + t * a.v_stride) + head * D;
+        Run8<T> x[U][2];
 #pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            const int r = first + u;
-            kind[u] = !on || r >= rows ? -1 : r < a.q_heads ? 0 : r < a.q_heads + heads ? 1 : 2;
-            head[u] = r < a.q_heads ? r : r < a.q_heads + heads ? r - a.q_heads : r - a.q_heads - heads;
-            if (kind[u] > 0 && at.x < 0) kind[u] = -1;     // no place to store it
-#pragma unroll
-            for (int j = 0; j < 16; ++j) f[u][j >> 3][j & 7] = 0.f;
-            if (kind[u] >= 0 && at.z >= 0) {
-                const T* p = kind[u] == 0 ? static_cast<const T*>(a.q) + t * a.q_stride
-                           : kind[u] == 1 ? static_cast<const T*>(a.k) + t * a.k_stride : static_cast<const T*>(a.v) + t * a.v_stride;
-                p += head[u] * D;
-                get8(p + 8 * ra, f[u][0]);
-                get8(p + 8 * rb, f[u][1]);
+        for (int u = 0; u < U; ++u) {
+            if (u < rows) {
+                x[u][0].load(p + u * D + 8 * ra);
+                x[u][1].load(p + u * D + 8 * rb);
+            } else {
+                x[u][0].zero();
+                x[u][1].zero();
             }
         }
-        float cs[16];                                      // cos, sin of the lane's 8 pairs
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { cs[2 * j] = 1.f; cs[2 * j + 1] = 0.f; }
-        const bool turns = on && at.z >= 0 && lane < turned && first < a.q_heads + heads;
-        if (turns) {
-            const float4* p = ang.table + int64_t(at.z) * (ang.rot_dim / 4) + 4 * lane;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 w = __ldg(p + j);
-                cs[4 * j] = w.x; cs[4 * j + 1] = w.y; cs[4 * j + 2] = w.z; cs[4 * j + 3] = w.w;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            if (turns && kind[u] >= 0 && kind[u] < 2) {
-                if (ang.interleaved) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) turn_pair(f[u][j >> 2][2 * (j & 3)], f[u][j >> 2][2 * (j & 3) + 1], cs[2 * j], cs[2 * j + 1]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) turn_pair(f[u][0][j], f[u][1][j], cs[2 * j], cs[2 * j + 1]);
+        if (base == 0) {                                   // under the first loads
+            if (threadIdx.x < 32) {
+                const int i = threadIdx.x;
+                const int s = seq_of_lane(b, t0, tokens, i);
+                if (i < tokens) {
+                    int4 at = make_int4(-1, 0, -1, 0);
+                    if (s >= 0) {
+                        const int64_t pos = int64_t(b.len(s)) - b.count(s) + (t0 + i - b.row(s));
+                        at.x = -2;
+                        if (pos >= ang.positions) {
+                            raise_page(status);
+                        } else if (pos >= 0) {
+                            at.z = int(pos);
+                            const int page = b.table[int64_t(s) * b.width + (pos >> b.page_log2)];
+                            if (page >= 0 && page < c.pages) { at.x = page; at.y = int(pos) & ((1 << b.page_log2) - 1); }
+                            else raise_page(status);
+                        }
+                    }
+                    s_place[i] = at;
                 }
             }
-            if (kind[u] == 0) {
-                T* p = static_cast<T*>(a.q_out) + t * a.q_out_stride + head[u] * D;
-                store8(p + 8 * ra, f[u][0]);
-                store8(p + 8 * rb, f[u][1]);
-            }
-            if (!__any_sync(0xffffffffu, kind[u] > 0)) continue;
-            float lo = f[u][0][0], hi = lo;
+            if (blockIdx.x == 0) b.report(status, threadIdx.x, 256);
+            __syncthreads();
+        }
+        const int4 at = s_place[tok];
+        const bool turns = kind < 2 && at.z >= 0 && lane < turned;
+        Sines sc;
+        if (turns) sc.load(ang.table + int64_t(at.z) * (ang.rot_dim / 4) + 4 * lane);
+        if (kind == 0 && at.x != -1) {
+            T* to = static_cast<T*>(a.q_out) + t * a.q_out_stride + head * D;
 #pragma unroll
-            for (int j = 1; j < 16; ++j) { lo = min_nan(lo, f[u][j >> 3][j & 7]); hi = fmaxf(hi, f[u][j >> 3][j & 7]); }
+            for (int u = 0; u < U; ++u) {
+                if (u >= rows) break;
+                if (at.z < 0) { x[u][0].zero(); x[u][1].zero(); }
+                float f[2][8];
+                x[u][0].get(f[0]);
+                x[u][1].get(f[1]);
+                if (turns) sc.turn_row(f, ang.interleaved);
+                store8(to + u * D + 8 * ra, f[0]);
+                store8(to + u * D + 8 * rb, f[1]);
+            }
+        }
+        const bool stores = kind > 0 && at.x >= 0 && rows > 0;
+        if (!__any_sync(0xffffffffu, stores)) continue;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[2][8];
+            x[u][0].get(f[0]);
+            x[u][1].get(f[1]);
+            if (turns && kind == 1) sc.turn_row(f, ang.interleaved);
+            float lo = f[0][0], hi = lo;
+#pragma unroll
+            for (int j = 1; j < 15; j += 2) {
+                lo = min3_nan(lo, f[j >> 3][j & 7], f[(j + 1) >> 3][(j + 1) & 7]);
+                hi = max3(hi, f[j >> 3][j & 7], f[(j + 1) >> 3][(j + 1) & 7]);
+            }
+            lo = min_nan(lo, f[1][7]);
+            hi = fmaxf(hi, f[1][7]);
 #pragma unroll
             for (int o = L / 2; o > 0; o >>= 1) {
                 lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
                 hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
             }
-            if (kind[u] > 0) {
+            if (stores && u < rows) {
                 float alpha, inv, zero;
-                row_params(f[u], lo, hi, alpha, inv, zero);
-                const int64_t row = c.row(at.x, head[u], at.y);
-                uint32_t* to = reinterpret_cast<uint32_t*>((kind[u] == 1 ? c.kc : c.vc) + row * (D / 2));
-                to[ra] = codes8(f[u][0], lo, hi, inv, zero);
-                to[rb] = codes8(f[u][1], lo, hi, inv, zero);
-                if (lane == 0) (kind[u] == 1 ? c.kp : c.vp)[row] = make_float2(alpha, zero);
+                row_params(f, lo, hi, alpha, inv, zero);
+                const int64_t row = c.row(at.x, head + u, at.y);
+                uint32_t* to = reinterpret_cast<uint32_t*>((kind == 1 ? c.kc : c.vc) + row * (D / 2));
+                to[ra] = codes8(f[0], lo, hi, inv, zero);
+                to[rb] = codes8(f[1], lo, hi, inv, zero);
+                if (lane == 0) (kind == 1 ? c.kp : c.vp)[row] = make_float2(alpha, zero);
             }
         }
     }
 }
 
-// Tokens of a CTA: as many as keep eight CTAs on every SM, at least one step's worth where a token has few rows.
+// Tokens of a CTA: as many as give every SM sixteen CTAs, at least one step's worth where a token has few rows.  U: rows of a unit; two and
+// four CTAs on an SM (64 registers, bf16) were better than 4 and 3, or 1 and 5: 79, 104, 112 us for 9708 tokens of 32 + 2 x 32 heads of 128.  Small
+// calls have units of one row, on as many SMs as there are.
+template <typename T, int D, int U>
+int launch_units(const Turn& a, const Cache& c, const Batch& b, const Angles& ang, int* status, cudaStream_t st) {
+    const int qb = (a.q_heads + U - 1) / U, kb = (c.heads + U - 1) / U, blocks = qb + 2 * kb, group = 256 / (D / 16);
+    int64_t n = b.rows / (int64_t(device_sm_count()) * 16);
+    n = std::min<int64_t>(n, std::max(1, 8 * group / blocks));
+    n = std::max<int64_t>(n, std::min(group / blocks, 8));
+    n = std::min<int64_t>(std::max<int64_t>(n, 1), std::min(kMostTokens, 65535 / blocks));
+    const Work work{int(n), qb, kb, uint32_t(((uint64_t(1) << 32) + blocks - 1) / blocks)};
+    QLLM_CUDA_TRY(launch_dependent(kv_rotate_append_kernel<T, D, U>, dim3(unsigned((b.rows + n - 1) / n)), dim3(256), 0, st, a, c, b, ang, work, status));
+    return after_launch();
+}
 template <typename T, int D>
 int launch_rotate(const Turn& a, const Cache& c, const Batch& b, const Angles& ang, int* status, cudaStream_t st) {
-    const int blocks = (a.q_heads + 2 * c.heads + kRows - 1) / kRows, group = 256 / (D / 16);
-    int64_t n = b.rows / (int64_t(device_sm_count()) * 8);
-    n = std::min<int64_t>(n, std::max(1, 4 * group / blocks));
-    n = std::max<int64_t>(n, std::min(group / blocks, 8));
-    n = std::min<int64_t>(std::max<int64_t>(n, 1), kMostTokens);
-    QLLM_CUDA_TRY(launch_dependent(kv_rotate_append_kernel<T, D>, dim3(unsigned((b.rows + n - 1) / n)), dim3(256), 0, st, a, c, b, ang, int(n), status));
-    return after_launch();
+    constexpr int U = 2;
+    const int64_t rows = b.rows * (a.q_heads + 2 * c.heads);
+    if (rows * (D / 16) <= int64_t(device_sm_count()) * 256) return launch_units<T, D, 1>(a, c, b, ang, status, st);
+    return launch_units<T, D, U>(a, c, b, ang, status, st);
 }
 
 // cos and sin of position / divisor * base^(-2 p / rot_dim), the angle in 64 bits
