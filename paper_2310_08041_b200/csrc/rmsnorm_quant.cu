@@ -83,28 +83,23 @@ struct Raw<float> {
     }
 };
 
-// x / d correctly rounded for d = 15, 63, 255 and inv = 1 / d: the product corrected by its exact residual (Markstein), checked for
-// every mantissa; where something might underflow, the division.
-__device__ __forceinline__ float by_levels(float x, float d, float inv) {
-    const float q = x * inv;
-    return x > 1e-30f && x < 1e38f ? fmaf(fmaf(-d, q, x), inv, q) : x / d;
-}
-// Eq. 2's parameters of u' and the row's factor.  ok = false: the row's numbers are too large or too small for float32 squares or
-// for a reciprocal of the scale (2^-120: its reciprocal and the products with it stay finite).
+// Eq. 2's parameters of u' and the row's factor.  ok = false: the row's numbers are too large or too small for float32 squares, or for
+// the short ways here; `plain` takes the long ones.  x / (2^bits - 1) is the product with the reciprocal corrected by its exact residual (Markstein),
+// correctly rounded for 15, 63 and 255 (checked for every mantissa).  The scale is 2^-100 at least, whose reciprocal and the products with it are finite.
 struct RowStats {
     float alpha, inv, zero, r;
     bool ok;
     RowStats() = default;
     __device__ __forceinline__ RowStats(float ssq, float lo, float hi, const NormArgs& a, float qmax) {
-        const float ms = fmaf(ssq, a.inv_c, a.eps);
-        alpha = by_levels(hi - lo, qmax, a.inv_levels);
-        if (!(hi > lo)) alpha = lo != 0.f ? fabsf(lo) : 1.f;
+        const float ms = fmaf(ssq, a.inv_c, a.eps), range = hi - lo, q = range * a.inv_levels;
+        alpha = range > 0.f ? fmaf(fmaf(-qmax, q, range), a.inv_levels, q) : fabsf(lo);
         inv = __frcp_rn(alpha);
         zero = -rintf(lo * inv);
-        r = rsqrtf(ms);                                    // two steps of float32 off at most; corrected once
-        r = fmaf(0.5f * r, fmaf(-ms * r, r, 1.f), r);
-        ok = ms < INFINITY && ms >= 0x1p-80f && hi - lo < INFINITY && alpha >= 0x1p-120f;
+        asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(ms));
+        r = fmaf(0.5f * r, fmaf(-ms * r, r, 1.f), r);      // two steps of float32 off at most before
+        ok = ms < 0x1p100f && ms >= 0x1p-80f && alpha < 0x1p100f && alpha >= 0x1p-100f;
     }
+    __device__ __forceinline__ void plain(float lo, float hi, float qmax) { eq2_params(lo, hi, qmax, alpha, inv, zero); }
 };
 // The factor of a row whose channels have been multiplied by `by` (a power of two), in 64 bits.  0 for a row of zeros with eps = 0 and
 // for one with an infinity, NaN for one with a NaN.
@@ -119,17 +114,11 @@ __device__ __forceinline__ float scale_of(float top) {
 }
 
 // Shared memory of the kernel below: S rows as they arrive, each thread's pieces side by side; with a map u (8 words for each of the
-// CTA's vector places), behind it the values of merged outputs, then the merged outputs' entries as (address of u's word, coefficient)
-// and where each one's entries begin and end.
-constexpr int merged_cap(int places) { return 2 * places; }                 // of 8 * places outputs
-constexpr int entry_cap(int places) { return 4 * places; }
-constexpr int map_smem(int places) { return (8 * places + merged_cap(places)) * 4 + entry_cap(places) * 8 + merged_cap(places) * 4; }
-
-__device__ __forceinline__ float shared_at(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
+// CTA's vector places), behind it the values of merged outputs, then two 16-byte records for each merged output (words of its first four
+// entries, coefficients, where further entries begin and end) and the further entries as (word, coefficient).
+constexpr int merged_cap(int places) { return places * 3 / 2; }             // of 8 * places outputs
+constexpr int entry_cap(int places) { return 2 * places; }
+constexpr int map_smem(int places) { return (8 * places + merged_cap(places)) * 4 + merged_cap(places) * 32 + entry_cap(places) * 8; }
 
 // A thread's NV vectors of 8 channels: its own pieces of the next S - 1 rows are on their way into shared memory (asynchronous copies of
 // 16 bytes that only the thread itself reads again: no barrier) while it works on the present one.
@@ -210,12 +199,14 @@ rmsnorm_quant_kernel(const NormArgs a) {
         for (int j = 0; j < 8; ++j) gamma[i][j] = t + i * T < nvec ? __ldg(a.gamma + 8 * (t + i * T) + j) : 0.f;
 
     float* s_u = reinterpret_cast<float*>(smem + S * stage);
-    uint2* s_entry = reinterpret_cast<uint2*>(s_u + 8 * P + merged_cap(P));
-    uint32_t* s_list = reinterpret_cast<uint32_t*>(s_entry + entry_cap(P));
-    const uint32_t u_addr = uint32_t(__cvta_generic_to_shared(s_u));
+    uint4* s_first = reinterpret_cast<uint4*>(s_u + 8 * P + merged_cap(P));        // words 0 | 1 << 16, 2 | 3 << 16, coefficients 0, 1
+    uint4* s_second = s_first + merged_cap(P);             // coefficients 2, 3, further entries
+    uint2* s_entry = reinterpret_cast<uint2*>(s_second + merged_cap(P));
+    const auto shared_at = [&](uint32_t bytes) { return *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(s_u) + bytes); };
     uint32_t addr[MAP ? NV : 1][8], walked[MAP ? NV : 1];
     float coef[MAP ? NV : 1][8];
-    const auto addr_of = [&](int k) { return u_addr + 4u * ((uint32_t(k) & 7u) * P + (uint32_t(k) >> 3)); };
+    const auto word_of = [&](int k) { return (uint32_t(k) & 7u) * P + (uint32_t(k) >> 3); };
+    const auto addr_of = [&](int k) { return 4u * word_of(k); };
     int merged = 0;
     if (MAP) {
         if (t < 2) s_count[t] = 0;
@@ -231,13 +222,13 @@ rmsnorm_quant_kernel(const NormArgs a) {
             several[i] = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                addr[i][j] = g < nvec ? addr_of(__ldg(a.src + from[j])) : u_addr;
+                addr[i][j] = g < nvec ? addr_of(__ldg(a.src + from[j])) : 0;
                 coef[i][j] = g < nvec ? __ldg(a.coef + from[j]) : 0.f;
                 const int n = from[j + 1] - from[j];
                 if (n > 1) {
                     several[i] |= 1u << j;
                     ++rows;
-                    entries += min(n, entry_cap(P) + 1);
+                    entries += min(max(n - 4, 0), entry_cap(P) + 1);
                 }
             }
             walked[i] = 0;
@@ -255,20 +246,29 @@ rmsnorm_quant_kernel(const NormArgs a) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (own >> j & 1) {
-                    addr[i][j] = u_addr + 4u * uint32_t(8 * P + slot + __popc(own & ((1u << j) - 1)));
+                    addr[i][j] = 4u * uint32_t(8 * P + slot + __popc(own & ((1u << j) - 1)));
                     coef[i][j] = 1.f;
                 }
 #pragma unroll 1
             for (uint32_t left = own; left; left &= left - 1) {
                 const int c = 8 * (t + i * T) + __ffs(left) - 1, b = __ldg(a.ptr + c), e = __ldg(a.ptr + c + 1);
-                s_list[slot++] = uint32_t(at) | uint32_t(at + e - b) << 16;
+                uint32_t w[4];
+                float f[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {              // (a missing entry is the first one times 0)
+                    const bool is = b + k < e;
+                    w[k] = word_of(__ldg(a.src + (is ? b + k : b)));
+                    f[k] = is ? __ldg(a.coef + b + k) : 0.f;
+                }
+                s_first[slot] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, __float_as_uint(f[0]), __float_as_uint(f[1]));
+                s_second[slot++] = make_uint4(__float_as_uint(f[2]), __float_as_uint(f[3]), at, at + max(e - b - 4, 0));
 #pragma unroll 1
-                for (int k = b; k < e; ++k) s_entry[at++] = make_uint2(addr_of(__ldg(a.src + k)), __float_as_uint(__ldg(a.coef + k)));
+                for (int k = b + 4; k < e; ++k) s_entry[at++] = make_uint2(addr_of(__ldg(a.src + k)), __float_as_uint(__ldg(a.coef + k)));
             }
         }
         if (!room)
             for (int k = 0; k < rows; ++k)
-                if (slot + k < merged_cap(P)) s_list[slot + k] = 0;          // no entries
+                if (slot + k < merged_cap(P)) s_first[slot + k] = s_second[slot + k] = make_uint4(0, 0, 0, 0);
         __syncthreads();
         merged = min(s_count[0], merged_cap(P));
     }
@@ -312,15 +312,21 @@ rmsnorm_quant_kernel(const NormArgs a) {
                 }
             }
             if (MAP) {
+                uint4 one = make_uint4(0, 0, 0, 0), two = one;             // the thread's first record, in front of the barrier
+                if (t < merged) { one = s_first[t]; two = s_second[t]; }
                 __syncthreads();
                 for (int i = t; i < merged; i += T) {
-                    const uint32_t range = s_list[i];
-                    double s = 0.0;
-                    for (uint32_t k = range & 0xFFFFu; k < range >> 16; ++k) {
+                    const float u0 = shared_at(4u * (one.x & 0xFFFFu)), u1 = shared_at(4u * (one.x >> 16));
+                    const float u2 = shared_at(4u * (one.y & 0xFFFFu)), u3 = shared_at(4u * (one.y >> 16));
+                    double s = fma(double(__uint_as_float(one.w)), double(u1), double(__uint_as_float(one.z)) * double(u0));
+                    if (two.x) s = fma(double(__uint_as_float(two.x)), double(u2), s);
+                    if (two.y) s = fma(double(__uint_as_float(two.y)), double(u3), s);
+                    for (uint32_t k = two.z; k < two.w; ++k) {
                         const uint2 e = s_entry[k];
                         s = fma(double(__uint_as_float(e.y)), double(shared_at(e.x)), s);
                     }
                     s_u[8 * P + i] = float(s);
+                    if (i + T < merged) { one = s_first[i + T]; two = s_second[i + T]; }
                 }
                 __syncthreads();
 #pragma unroll
@@ -381,6 +387,7 @@ rmsnorm_quant_kernel(const NormArgs a) {
         if (quant && before >= 0 && warp == 0) flush(s_sum[turn ^ 1], before);
         float r = rs.r, scale = rs.alpha * rs.r;
         if (!rs.ok || by != 1.f) {
+            if (!rs.ok) rs.plain(lo, hi, qmax);
             const double wide = scaled_factor(ssq, C, a.eps, by);
             r = float(wide);
             scale = float(wide * double(rs.alpha));
@@ -477,9 +484,10 @@ rmsnorm_quant_any(const NormArgs a) {
             block_minmax(none, top, red);
             if (top > 0.f && top < INFINITY) by = scale_of(top);
         }
-        const RowStats st(ssq, lo, hi, a, qmax);
+        RowStats st(ssq, lo, hi, a, qmax);
         float r = st.r, scale = st.alpha * st.r;
         if (!st.ok || by != 1.f) {
+            if (!st.ok) st.plain(lo, hi, qmax);
             const double wide = scaled_factor(ssq, C, a.eps, by);
             r = float(wide);
             scale = float(wide * double(st.alpha));
