@@ -190,7 +190,7 @@ rmsnorm_quant_kernel(const NormArgs a) {
     };
     int64_t m = blockIdx.x;
 #pragma unroll
-    for (int i = 0; i + 1 < S; ++i) request(i, m + i * step);
+    for (int i = 0; i < (S > 1 ? S - 1 : 1); ++i) request(i, m + i * step);
 
     float gamma[NV][8];
 #pragma unroll
@@ -280,7 +280,7 @@ rmsnorm_quant_kernel(const NormArgs a) {
     int parity = 0, turn = 0, st = 0;
     int64_t before = -1;                                   // the row whose code sums wait in s_sum[turn ^ 1]
     for (; m < a.M; m += step) {
-        request(st == 0 ? S - 1 : st - 1, m + (S - 1) * step);             // into what the last row was taken from
+        if (S > 1) request(st == 0 ? S - 1 : st - 1, m + (S - 1) * step);  // into what the last row was taken from
         asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
         float f[MAP ? 1 : NV][8], v[MAP ? NV : 1][8], by = 1.f;
         float ssq, lo, hi;
@@ -431,6 +431,7 @@ rmsnorm_quant_kernel(const NormArgs a) {
         before = m;
         turn ^= 1;
         st = st + 1 == S ? 0 : st + 1;
+        if (S == 1) request(0, m + step);
     }
     if (quant && before >= 0) {
         __syncthreads();
