@@ -11,9 +11,9 @@
 // memory, 128 columns of the second product in turn.  H enters
 // the second product as two bf16 parts, 16 bits.
 //
-// ROWS: rows of the tile that stages have room for.  With 16 (a step's single tokens) the first product's other 112 rows are whatever follows in
-// shared memory, the second's are H three times more: a warp reaches a quarter of the rows in tensor memory, so each of four has all 16
-// rows and takes a quarter of the columns.  The tensor core has time for it, and stages are small enough that eight are in flight.
+// ROWS: rows of the tile that stages have room for.  With 16 (a step's single tokens) the products are transposed, D1[ranks x rows] and
+// D2[128 columns x rows]: the weights are the M side, the rows an N of 16.  An MMA's time is that of its operands' bytes from shared memory, and
+// 128 rows of which 16 are real would be most of them (96 tokens on 24 adapters of rank 64, 8192 x 10240: 21 us so).
 //
 // What bounds it: memory.  The MMAs of a tile take a tenth of its time; the warp-level MMA (adapters.cu) took a third of it for prompts
 // (some 20 cycles for each m16n8k16 and quarter of an SM).
@@ -34,14 +34,14 @@ constexpr int kFeeders = 256, kTeam = 128, kWorkers = 2 * kTeam, kIssuers = 2, k
 template <int R, int ROWS>
 struct Shape {
     static constexpr int kBlocks = (R + 63) / 64;          // operand blocks (64 elements of 128 bytes) of a row of B
-    static constexpr bool kSide = R <= 32;                 // both parts of H in one block
-    static constexpr int kHBlocks = kSide ? 1 : 2 * kBlocks;
-    static constexpr bool kAll = ROWS == 16;               // few rows: every CTA adds up all parts of the sums; H four times, for four warps
-    static constexpr int kABlock = R * 128, kXBlock = ROWS * 128, kBBlock = kCols * 128, kHBlock = kAll ? 128 * 128 : kXBlock;
+    static constexpr bool kFew = ROWS == 16;               // transposed products; every CTA adds up all parts of the sums
+    static constexpr bool kSide = R <= 32;                 // both parts of H in one block, side by side
+    static constexpr int kHBlocks = kFew ? kBlocks : kSide ? 1 : 2 * kBlocks;
+    static constexpr int kABlock = R * 128, kXBlock = ROWS * 128, kBBlock = kCols * 128, kHBlock = kFew ? 2 * kXBlock : kXBlock;
     static constexpr int kPitch = kCols * 2 + 16;          // bytes between rows of base: 16-byte accesses of 8 rows in different banks
     static constexpr int kStageK = 2 * (kABlock + kXBlock), kStageN = kBlocks * kBBlock + ROWS * kPitch;
     static constexpr int kStage = ((kStageK > kStageN ? kStageK : kStageN) + 1023) / 1024 * 1024;
-    static constexpr int kPart = kAll ? ROWS * R * 4 : 0, kSum = kAll ? 8 * ROWS * R * 4 : ROWS * R * 4 + 8 * 16;
+    static constexpr int kPart = kFew ? ROWS * R * 4 : 0, kSum = kFew ? 8 * ROWS * R * 4 : ROWS * R * 4 + 8 * 16;
     static constexpr int kFixed = kHBlocks * kHBlock + kPart + kSum + (ROWS < 128 ? 128 * 128 : 0) + 1024;      // (operands are read 128 rows deep)
     static constexpr int kMost = (223 * 1024 - kFixed) / kStage, kStages = kMost > 8 ? 8 : kMost;
     static constexpr int kBytes = kFixed + kStages * kStage;
@@ -92,6 +92,11 @@ __device__ __forceinline__ bool wait_cluster(uint64_t* bar, const Abort& ab) {
 __device__ __forceinline__ uint4 lds4(uint32_t a) {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds_half(uint32_t a) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
     return v;
 }
 __device__ __forceinline__ void sts4(uint32_t a, uint4 v) {
@@ -225,9 +230,13 @@ adapters_tile_kernel(const AdapterArgs p) {
         // stage, to sums of its own (all lanes walk along, so that operands are the warp's, not a thread's)
         const int me = warp - kWorkers / 32;
         if (rank > 0) {
-            constexpr uint32_t id1 = idesc_bf16(128, R), id2 = idesc_bf16(128, kCols);
+            constexpr uint32_t id1 = idesc_bf16(128, S::kFew ? ROWS : R), id2 = idesc_bf16(128, S::kFew ? 2 * ROWS : kCols);
             const uint32_t base_addr = ptx::smem_addr(smem), h_low = desc_low(ptx::smem_addr(s_hop)), d = __shfl_sync(0xffffffffu, tmem, 0);
             const uint32_t d1 = d + 256 + me * R, d2 = d + me * kCols;
+            const auto issue = [&](uint32_t to, uint32_t rows, uint32_t weights, uint32_t id, uint32_t more) {
+                if constexpr (S::kFew) mma_bf16_ss(to, weights, rows, id, more);
+                else mma_bf16_ss(to, rows, weights, id, more);
+            };
             const bool lead = elect_one();
             bool ok = true;
             uint32_t more = 0;
@@ -241,8 +250,8 @@ adapters_tile_kernel(const AdapterArgs p) {
                 if (lead) {
 #pragma unroll
                     for (int s = 0; s < 8; ++s)
-                        mma_bf16_ss(d1, rows + (((s >> 2) * S::kXBlock + (s & 3) * 32) >> 4), ranks + (((s >> 2) * S::kABlock + (s & 3) * 32) >> 4), id1,
-                                    s > 0 ? 1u : more);
+                        issue(d1, rows + (((s >> 2) * S::kXBlock + (s & 3) * 32) >> 4), ranks + (((s >> 2) * S::kABlock + (s & 3) * 32) >> 4), id1,
+                              s > 0 ? 1u : more);
                     ptx::mma_commit(&s_empty[sg]);
                 }
                 __syncwarp();
@@ -264,12 +273,12 @@ adapters_tile_kernel(const AdapterArgs p) {
                 const uint32_t columns = desc_low(base_addr + sg * S::kStage);
                 if (lead) {
 #pragma unroll
-                    for (int half = 0; half < 2; ++half)
+                    for (int half = 0; half < (S::kFew ? 1 : 2); ++half)       // (few rows: both parts are N of one MMA)
 #pragma unroll
                         for (int s = 0; s < R / 16; ++s) {
                             if (s > 0 && s >= steps) break;
-                            mma_bf16_ss(d2, h_low + ((S::kSide ? half * 2 * R + s * 32 : (half * S::kBlocks + (s >> 2)) * S::kHBlock + (s & 3) * 32) >> 4),
-                                        columns + (((s >> 2) * S::kBBlock + (s & 3) * 32) >> 4), id2, half > 0 || s > 0);
+                            issue(d2, h_low + ((S::kSide && !S::kFew ? half * 2 * R + s * 32 : (half * S::kBlocks + (s >> 2)) * S::kHBlock + (s & 3) * 32) >> 4),
+                                  columns + (((s >> 2) * S::kBBlock + (s & 3) * 32) >> 4), id2, half > 0 || s > 0);
                         }
                     ptx::mma_commit(&s_d2[me]);
                 }
@@ -294,32 +303,43 @@ adapters_tile_kernel(const AdapterArgs p) {
         const int fours = cnt * (R / 4);
         const uint32_t sum_addr = ptx::smem_addr(s_sum), h_addr = ptx::smem_addr(s_hop);
         const float scale = p.scale[slot];
-        if (quarter * 32 < cnt) {
+        const auto sums = [&](int c, float (&d)[16]) {     // 16 columns of this thread's row of D1
+#pragma unroll
+            for (int i = 0; i < 16; ++i) d[i] = 0.f;
+            for (int i = 0; i < parts; ++i) {
+                uint32_t w[16];
+                tmem_ld_x16(my_tmem + 256 + i * R + c, w);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) d[j] += __uint_as_float(w[j]);
+            }
+        };
+        if constexpr (S::kFew) {
+            if (team == 0 && quarter * 32 < R) {           // thread `row` has rank `row`
+                float d[16];
+                sums(0, d);
+                if (row < R) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (i < cnt) s_part[i * R + row] = d[i];
+                }
+            }
+        } else if (quarter * 32 < cnt) {
 #pragma unroll 1
             for (int c = 16 * team; c < R; c += 32) {
                 float d[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) d[i] = 0.f;
-                for (int i = 0; i < parts; ++i) {
-                    uint32_t w[16];
-                    tmem_ld_x16(my_tmem + 256 + i * R + c, w);
-                    ptx::tmem_ld_wait();
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) d[j] += __uint_as_float(w[j]);
-                }
+                sums(c, d);
                 if (row < cnt) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int e = row * (R / 4) + c / 4 + i;
-                        const float4 v = make_float4(d[4 * i], d[4 * i + 1], d[4 * i + 2], d[4 * i + 3]);
-                        if constexpr (S::kAll) reinterpret_cast<float4*>(s_part)[e] = v;
-                        else st_cluster4(ptx::map_to_cta(sum_addr + (e / cl * cl + part) * 16, e % cl), v);
+                        st_cluster4(ptx::map_to_cta(sum_addr + (e / cl * cl + part) * 16, e % cl), make_float4(d[4 * i], d[4 * i + 1], d[4 * i + 2], d[4 * i + 3]));
                     }
                 }
             }
         }
         ptx::named_bar_sync(1, kWorkers);
-        if constexpr (S::kAll) {
+        if constexpr (S::kFew) {
             for (int i = t; i < fours * cl; i += kWorkers) {
                 const int e = i / cl, to = i - e * cl;
                 st_cluster4(ptx::map_to_cta(sum_addr + (e * cl + part) * 16, to), reinterpret_cast<const float4*>(s_part)[e]);
@@ -328,8 +348,8 @@ adapters_tile_kernel(const AdapterArgs p) {
         }
         if (t < cl) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_addr(&s_ready[0]), t));
         ok = all(ok && wait_cluster(&s_ready[0], ab));
-        for (int k = t; S::kAll ? k < fours : part + k * cl < fours; k += kWorkers) {
-            const int e = S::kAll ? k : part + k * cl, at_row = e / (R / 4), col = e % (R / 4) * 4;
+        for (int k = t; S::kFew ? k < fours : part + k * cl < fours; k += kWorkers) {
+            const int e = S::kFew ? k : part + k * cl, at_row = e / (R / 4), col = e % (R / 4) * 4;
             float f[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
             for (int c = 0; c < cl; ++c) {
@@ -343,17 +363,18 @@ adapters_tile_kernel(const AdapterArgs p) {
                 const uint32_t w0 = half ? rounded(f[0], f[1]) : upper(f[0], f[1]), w1 = half ? rounded(f[2], f[3]) : upper(f[2], f[3]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) f[j] = rest(f[j]);
-                const int byte = S::kSide ? half * 2 * R + 2 * col : 2 * (col & 63), block = S::kSide ? 0 : half * S::kBlocks + (col >> 6);
-                const uint32_t at = h_addr + block * S::kHBlock + at_row * 128 + (((byte >> 4) ^ (at_row & 7)) << 4) + (byte & 15);
-                if constexpr (S::kAll) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + i * 4096), "r"(w0), "r"(w1) : "memory");
+                const bool side = S::kSide && !S::kFew;
+                const int byte = side ? half * 2 * R + 2 * col : 2 * (col & 63), block = side ? 0 : (S::kFew ? 0 : half * S::kBlocks) + (col >> 6);
+                const int line = at_row + (S::kFew ? 16 * half : 0);
+                const uint32_t at = h_addr + block * S::kHBlock + line * 128 + (((byte >> 4) ^ (line & 7)) << 4) + (byte & 15);
+                if constexpr (S::kFew) {
+                    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(w0), "r"(w1) : "memory");
                 } else {
                     for (int c = 0; c < cl; ++c) st_cluster2(ptx::map_to_cta(at, c), w0, w1);
                 }
             }
         }
-        if constexpr (!S::kAll) {
+        if constexpr (!S::kFew) {
             ptx::named_bar_sync(1, kWorkers);
             if (t < cl) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_addr(&s_ready[1]), t));
             ok = all(ok && wait_cluster(&s_ready[1], ab));
@@ -364,25 +385,55 @@ adapters_tile_kernel(const AdapterArgs p) {
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out);
     const bool has_base = p.base != nullptr;
     const uint32_t smem_base = ptx::smem_addr(smem);
-    const bool wide = ROWS > 16;                           // a thread per row and all columns; else 16 rows and a quarter of them
-    const int own = wide ? row : lane;                     // the tile's row that this thread has
-    const int my_row = own < cnt ? s_rows[own % ROWS] : -1;
-    __nv_bfloat16* my_out = out + int64_t(max(my_row, 0)) * p.out_stride;
-    int out_row[wide ? ROWS / 8 : 1];                      // rows that this thread copies out
-    if constexpr (wide) {
+    const int mine = !S::kFew && row < cnt ? row : -1;     // the tile's row that this thread has (few rows: a column of all of them)
+    int out_row[S::kFew ? 16 : ROWS / 8];                  // rows that this thread writes
 #pragma unroll
-        for (int i = 0; i < ROWS / 8; ++i) out_row[i] = (row >> 4) + 8 * i < cnt ? s_rows[(row >> 4) + 8 * i] : -1;
+    for (int i = 0; i < (S::kFew ? 16 : ROWS / 8); ++i) {
+        const int r = S::kFew ? i : (row >> 4) + 8 * i;
+        out_row[i] = r < cnt ? s_rows[r] : -1;
     }
+    const auto release = [&] {                             // this team's D2 has been read
+        ptx::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&s_d2_free[team]);
+    };
     uint32_t round = 0;
     int turns = 0;
     for (int n = n0; n < n1; n += kCols, advance(), ++turns) {
         if ((turns & 1) != team) continue;                 // the other team's
         ok = all(ok && wait_bounded(&s_full[sg], turn, ab) && (rank == 0 || wait_bounded(&s_d2[team], round, ab)));
         ptx::tc_fence_after_sync();
-        const uint32_t cells = smem_base + sg * S::kStage + S::kBlocks * S::kBBlock, cell_addr = cells + own * S::kPitch;
-        if (ok && (!wide || quarter * 32 < cnt)) {
+        const uint32_t cells = smem_base + sg * S::kStage + S::kBlocks * S::kBBlock;
+        if constexpr (S::kFew) {
+            uint32_t d[16], e[16];
+            if (rank > 0) {
+                tmem_ld_x16(my_tmem + team * kCols, d);
+                tmem_ld_x16(my_tmem + team * kCols + 16, e);
+                ptx::tmem_ld_wait();
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) d[i] = e[i] = 0;
+            }
+            release();                                     // the next MMAs run under the rest
+            __nv_bfloat16* to = out + n + row;
+            if (ok && n + row < n1) {
+#pragma unroll
+                for (int i0 = 0; i0 < 16; i0 += 4) {       // four rows at a time, as many as there are
+                    if (i0 >= cnt) break;
+                    uint32_t o[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = has_base ? lds_half(cells + (i0 + i) * S::kPitch + row * 2) : 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (out_row[i0 + i] >= 0)
+                            to[int64_t(out_row[i0 + i]) * p.out_stride] =
+                                __float2bfloat16_rn(__uint_as_float(o[i] << 16) + (__uint_as_float(d[i0 + i]) + __uint_as_float(e[i0 + i])));
+                }
+            }
+        } else if (ok && quarter * 32 < cnt) {
+            const uint32_t cell = cells + row * S::kPitch;
 #pragma unroll 1
-            for (int c = wide ? 0 : 32 * quarter; c < (wide ? kCols : 32 * quarter + 32); c += 32) {
+            for (int c = 0; c < kCols; c += 32) {
                 uint32_t d[32];
                 if (rank > 0) {
                     ptx::tmem_ld_32x32b_x32(my_tmem + team * kCols + c, d);
@@ -391,10 +442,10 @@ adapters_tile_kernel(const AdapterArgs p) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) d[i] = 0;
                 }
-                if (own < cnt) {
+                if (mine >= 0) {
                     uint4 o[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[i] = has_base ? lds4(cell_addr + c * 2 + 16 * i) : make_uint4(0, 0, 0, 0);
+                    for (int i = 0; i < 4; ++i) o[i] = has_base ? lds4(cell + c * 2 + 16 * i) : make_uint4(0, 0, 0, 0);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         uint32_t w[4] = {o[i].x, o[i].y, o[i].z, o[i].w};
@@ -402,24 +453,14 @@ adapters_tile_kernel(const AdapterArgs p) {
                         for (int j = 0; j < 4; ++j)
                             w[j] = rounded(__uint_as_float(w[j] << 16) + __uint_as_float(d[8 * i + 2 * j]),
                                            __uint_as_float(w[j] & 0xFFFF0000u) + __uint_as_float(d[8 * i + 2 * j + 1]));
-                        o[i] = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if constexpr (wide) {
-                            sts4(cell_addr + c * 2 + 16 * i, o[i]);
-                        } else {                           // few rows: straight to memory
-                            if (my_row >= 0 && n + c + 8 * i < n1) *reinterpret_cast<uint4*>(my_out + n + c + 8 * i) = o[i];
-                        }
+                        sts4(cell + c * 2 + 16 * i, make_uint4(w[0], w[1], w[2], w[3]));
                     }
                 }
             }
         }
-        ptx::tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&s_d2_free[team]);
+        if constexpr (!S::kFew) release();
         ptx::named_bar_sync(2 + team, kTeam);
-        if constexpr (wide) {
+        if constexpr (!S::kFew) {
             // 16 threads a row, 8 rows at a time
             if (ok && n + 8 * (row & 15) < n1) {
                 const uint32_t from = cells + (row >> 4) * S::kPitch + (row & 15) * 16;
@@ -496,7 +537,7 @@ int launch_tiles_tc(const AdapterArgs& p, bool few, cudaStream_t st) {
     if (p.max_rank <= 16) return launch_shape<16, 128>(p, st);
     if (p.max_rank <= 32) return launch_shape<32, 128>(p, st);
     if (p.max_rank <= 64) return few ? launch_shape<64, 16>(p, st) : launch_shape<64, 128>(p, st);
-    return launch_shape<128, 64>(p, st);                   // (shared memory has no room for four times H)
+    return few ? launch_shape<128, 16>(p, st) : launch_shape<128, 64>(p, st);
 }
 
 }  // namespace lora
