@@ -449,34 +449,34 @@ int launch_tiles(AdapterArgs p, cudaStream_t st) {
     return after_launch();
 }
 
-// Which kernel serves a bf16 call.  Large tiles: the tensor-core kernel, but where the rank is small and so are the groups of rows (8192 x
-// 10240, rank 32: 256 rows of one adapter 20 us here, 26 there; 1024 rows 46 and 30; rank 64, 17 rows: 29 and 20).  Few rows for each adapter: it
-// has the longer way to its first byte and streams faster behind it (rank 64, 8192 x 10240: one token 12 us here, 13 there; 96 tokens on 24 adapters 25 and
-// 21; rank 16: 10 and 15).
+// Which kernel serves a bf16 call: this file's warp-level MMA with operands straight from memory, or the tensor cores' (adapters_tile.cu), which
+// have the longer way to their first byte and stream faster behind it.  Measured with random adapters, us here / there:
+//   tiles of many rows  rank 32, 8192 x 10240: 256 rows of one adapter 20 / 26, 24 adapters of 40 rows 34 / 33, 1024 rows of one 46 / 30
+//                       rank 64: 17 rows 29 / 20, 1024 rows 87 / 34
+//   few rows each       rank 32, 8192 x 10240: one token 6.7 / 10.8, 96 tokens on 24 adapters 16 / 16; 4096 x 4096: 6.1 / 7.8, 8.8 / 11
+//                       rank 64, 8192 x 10240: 12.3 / 11.2, 25 / 18; 4096 x 4096: 7.8 / 8.3, 12.8 / 12.2
+//                       rank 128: 1024 x 1000 6.5 / 7.0, 17 / 9.3; 4096 x 4096 11 / 9.5, 33 / 18
 bool tensor_cores(const AdapterArgs& p, bool few) {
-    const int64_t groups = std::min(p.seqs, p.slots + 1), weights = groups * (int64_t(p.K) + p.N) * p.max_rank;
+    const int64_t groups = std::min(p.seqs, p.slots + 1), sides = int64_t(p.K) + p.N;
     if (!few) return p.max_rank > 32 || (p.rows >= 512 && p.rows >= 128 * groups);
-    return p.max_rank > 64 ? groups >= 12 : p.max_rank > 32 && weights >= 9000000;
+    return p.max_rank > 64 || (p.max_rank > 32 && (sides >= 16384 || groups * sides * p.max_rank >= 8000000));
 }
 
 template <typename T>
 int launch_adapters(const AdapterArgs& p, cudaStream_t st) {
     // tiles of 16 rows while groups are that small on average
     const bool few = p.rows <= int64_t(16) * std::min(p.seqs, p.slots + 1);
-    if (sizeof(T) == 2 && tensor_cores(p, few)) return launch_tiles_tc(p, few, st);
+    constexpr bool half = sizeof(T) == 2;                  // (whose larger ranks are the other kernel's)
+    if (half && tensor_cores(p, few)) return launch_tiles_tc(p, few, st);
     if (few) {
         if (p.max_rank <= 16) return launch_tiles<T, 1, 1, 2>(p, st);
         if (p.max_rank <= 32) return launch_tiles<T, 1, 1, 4>(p, st);
-        if (p.max_rank <= 64) return launch_tiles<T, 1, 1, 8>(p, st);
-        return launch_tiles<T, 1, 1, 16>(p, st);
+        if (half || p.max_rank <= 64) return launch_tiles<T, 1, 1, 8>(p, st);
+        if constexpr (!half) return launch_tiles<T, 1, 1, 16>(p, st);
     }
     if (p.max_rank <= 16) return launch_tiles<T, 2, 2, 2>(p, st);
-    if (p.max_rank <= 32) return launch_tiles<T, 2, 2, 4>(p, st);
-    if constexpr (sizeof(T) == 4) {
-        if (p.max_rank <= 64) return launch_tiles<T, 2, 2, 8>(p, st);
-        return launch_tiles<T, 2, 1, 16>(p, st);
-    }
-    return QLLM_ERR_UNSUPPORTED;                           // (not reached: large ranks are the other kernel's)
+    if (half || p.max_rank <= 32) return launch_tiles<T, 2, 2, 4>(p, st);
+    if constexpr (!half) return p.max_rank <= 64 ? launch_tiles<T, 2, 2, 8>(p, st) : launch_tiles<T, 2, 1, 16>(p, st);
 }
 
 int check_rows(const void* p, int64_t stride, int width, int dtype) {
