@@ -165,15 +165,16 @@ def test_part_of_a_fused_projection():
     assert torch.equal(out[:, 256:512], before[:, 256:512])
 
 
-@pytest.mark.parametrize("seqs,slots", [(257, 3), (1000, 700), (3000, 8192), (5000, 1)])
-def test_more_sequences_and_slots_than_threads(seqs, slots):
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("seqs,slots,top", [(257, 3, 8), (1000, 700, 8), (3000, 8192, 8), (5000, 1, 8), (700, 900, 72), (1500, 8192, 72), (2000, 2, 40)])
+def test_more_sequences_and_slots_than_threads(dtype, seqs, slots, top):
     rng = np.random.RandomState(seqs)
-    K, N, top = 64, 40, 8
+    K, N = 64, 40
     A, Bm = torch.randn(slots, top, K, device=G.DEV).bfloat16(), torch.randn(slots, N, top, device=G.DEV).bfloat16()
     ad = B.Adapters(A, Bm, torch.rand(slots, device=G.DEV), ints(rng.randint(0, top + 1, slots)))
     news, adapter = rng.choice([0, 1, 1, 2, 5], seqs), rng.randint(-1, slots, seqs)
     start = np.concatenate([[0], np.cumsum(news)]).tolist()
-    x, base = torch.randn(start[-1], K, device=G.DEV), torch.randn(start[-1], N, device=G.DEV)
+    x, base = torch.randn(start[-1], K, device=G.DEV).to(DT[dtype]), torch.randn(start[-1], N, device=G.DEV).to(DT[dtype])
     got, _ = run(ad, x, base, start, adapter)
     row_ad = torch.from_numpy(np.repeat(adapter, news)).to(G.DEV)
     rank = ad.rank[row_ad.clamp(min=0)]
@@ -183,21 +184,36 @@ def test_more_sequences_and_slots_than_threads(seqs, slots):
     mid = torch.einsum("mk,mrk->mr", x.double(), aa)
     want = base + sc[:, None] * torch.einsum("mr,mnr->mn", mid, bb)
     first = sc[:, None] * torch.einsum("mr,mnr->mn", torch.einsum("mk,mrk->mr", x.double().abs(), aa.abs()), bb.abs())
-    assert ((got - want).abs() <= (K / 16 + 32 + 8 + 4) * 2.0 ** -23 * first + 2.0 ** -23 * want.abs()).all()
+    second = sc[:, None] * torch.einsum("mr,mnr->mn", mid.abs(), bb.abs())
+    half, split = torch.finfo(DT[dtype]).eps / 2, 2.0 ** -16 if dtype == "bf16" else 2.0 ** -23
+    assert ((got - want).abs() <= (K / 16 + 32) * 2.0 ** -23 * first + (split + (top / 16 * 3 + 4) * 2.0 ** -23) * second + (half + 2.0 ** -24) * want.abs()).all()
     assert B.qllm_poll_status() == B.QLLM_OK
 
 
-def test_contents_out_of_range_are_reported_and_harmless():
+@pytest.mark.parametrize("seed", range(16))
+def test_random_shapes(seed):
+    r = np.random.RandomState(500 + seed)
+    top, slots = 8 * r.randint(1, 17), r.randint(1, 30)
+    K, N = 8 * r.randint(1, 400), 8 * r.randint(1, 400)
+    seqs = r.randint(1, 50)
+    news = [int(x) for x in (r.randint(0, 4, seqs) if seed % 3 else r.randint(0, 90, seqs))]
+    ranks = [int(x) for x in r.randint(0, top + 1, slots)]
+    case(["bf16", "f32"][seed % 2], K, N, top, ranks, news, r.randint(-1, slots, seqs), lead=r.randint(0, 3), tail=r.randint(0, 3),
+         pad=tuple(8 * int(v) for v in r.randint(0, 3, 3)))
+
+
+@pytest.mark.parametrize("dtype,top", [("f32", 16), ("bf16", 16), ("bf16", 72)])
+def test_contents_out_of_range_are_reported_and_harmless(dtype, top):
     """Slots that do not exist count as none, ranks are cut, row ranges are cut to the tensors; the other sequences are served."""
-    K, N, top, rows = 256, 128, 16, 40
-    x, base = torch.randn(rows, K, device=G.DEV), torch.randn(rows, N, device=G.DEV)
+    K, N, rows = 256, 128, 40
+    x, base = torch.randn(rows, K, device=G.DEV).to(DT[dtype]), torch.randn(rows, N, device=G.DEV).to(DT[dtype])
     good = dict(start=[0, 10, 20, 30, 40], adapter=[0, 1, 0, -1], ranks=[16, 12])
-    for change in (dict(adapter=[0, 2, 0, -1]), dict(adapter=[0, 2 ** 30, 0, -1]), dict(ranks=[16, 17]), dict(ranks=[16, -5]), dict(start=[0, 10, 20, 30, 1000]),
+    for change in (dict(adapter=[0, 2, 0, -1]), dict(adapter=[0, 2 ** 30, 0, -1]), dict(ranks=[16, top + 1]), dict(ranks=[16, -5]), dict(start=[0, 10, 20, 30, 1000]),
                    dict(start=[-7, 10, 20, 30, 40]), dict(start=[0, 10, 2 ** 31 - 1, 30, 40]), dict(start=[0, 10, -2 ** 31, 30, 40])):
         c = dict(good, **change)
         ad = make(2, top, K, N, good["ranks"], junk=0.0)
         ad.rank.copy_(ints(c["ranks"]))
-        out = G.Guarded((rows, N), torch.float32, 3.0)
+        out = G.Guarded((rows, N), DT[dtype], 3.0)
         B.qllm_adapters_add(ad, x, base, out.t, ints(c["start"]), ints(c["adapter"]))
         assert B.qllm_poll_status() == B.QLLM_ERR_PAGE, change
         out.check()
@@ -208,13 +224,13 @@ def test_contents_out_of_range_are_reported_and_harmless():
         if "adapter" in change:
             assert torch.equal(out.t[10:20], base[10:20])
         if "ranks" in change:
-            check(out.t[10:20], ad, [16, min(max(change["ranks"][1], 0), 16)], x[10:20], base[10:20], [0, 10], [1])
+            check(out.t[10:20], ad, [16, min(max(change["ranks"][1], 0), top)], x[10:20], base[10:20], [0, 10], [1])
     assert B.qllm_poll_status() == B.QLLM_OK
 
 
 def test_rows_with_nan_and_infinities_stay_by_themselves():
-    for dtype in ("bf16", "f32"):
-        ad = make(1, 16, 256, 128, [16])
+    for dtype, top in (("bf16", 16), ("f32", 16), ("bf16", 72)):
+        ad = make(1, top, 256, 128, [16])
         x, base = torch.randn(40, 256, device=G.DEV).to(DT[dtype]), torch.randn(40, 128, device=G.DEV).to(DT[dtype])
         x[3, 7], x[20, 9] = float("nan"), float("inf")
         out = torch.empty_like(base)
