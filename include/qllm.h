@@ -236,7 +236,7 @@ int qllm_qgemm_acc(const uint8_t* codes, const uint8_t* w_codes, int32_t* acc,
  *   A      bf16 [slots][max_rank][K],  B  bf16 [slots][N][max_rank], 16-byte aligned
  *   rank   int32 [slots] or NULL (all max_rank): what A holds behind row rank[a] and B behind column rank[a] counts for nothing
  *   scale  float [slots]
- * max_rank is a multiple of 8 up to 128, K and N are multiples of 8, slots <= 8192 (QLLM_ERR_UNSUPPORTED).
+ * max_rank is a multiple of 8 up to 128, K and N are multiples of 8 up to 2^20, slots <= 8192 (QLLM_ERR_UNSUPPORTED).
  *  x          device [rows][K], base, out device [rows][N], all of dtype (QLLM_F32 or QLLM_BF16); *_stride: distance between rows in
  *             elements, so that one call can serve a part of a fused projection's columns.  Addresses and strides are multiples of 16 bytes.
  *             base may be out (with the same stride, QLLM_ERR_SHAPE otherwise), or NULL (zeros); x must not overlap out.
@@ -244,7 +244,7 @@ int qllm_qgemm_acc(const uint8_t* codes, const uint8_t* w_codes, int32_t* acc,
  *  adapter    device int32 [seqs]: the sequence's slot; negative: none (its rows of out become those of base)
  * Read on the device when the kernel runs, so a captured graph follows their contents.  Row ranges that decrease or leave the
  * tensors are cut, slots out of range count as none, ranks are cut to 0 .. max_rank, and the status word becomes QLLM_ERR_PAGE
- * (qllm_poll_status).  seqs <= 2^20, rows <= 2^30.
+ * (qllm_poll_status); ranges that decrease may overlap others, whose rows of out are then one or the other's, or left.  seqs <= 2^20, rows <= 2^30.
  * Precision: sums in float32; of A_a x, 16 bits (QLLM_BF16) or 24 bits (QLLM_F32) enter the second product.  QLLM_F32 rows with an
  * infinity give NaN. */
 typedef struct qllm_adapters {

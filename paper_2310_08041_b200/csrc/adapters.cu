@@ -145,7 +145,7 @@ adapters_add_kernel(const AdapterArgs p) {
     const __nv_bfloat16* weights = p.B + int64_t(slot) * p.N * p.max_rank;
     const T* base = static_cast<const T*>(p.base);
     T* out = static_cast<T*>(p.out);
-    const int nunits = (p.N + 31) / 32, v0 = nunits * part / cl, v1 = nunits * (part + 1) / cl;     // K, N < 2^31: 31 bits
+    const int nunits = (p.N + 31) / 32, v0 = nunits * part / cl, v1 = nunits * (part + 1) / cl;     // K, N <= 2^20
 
     // the second product's operands start on their way to L2 under the first one
     const int units = (p.K + 31) / 32, u0 = units * part / cl, u1 = units * (part + 1) / cl;
@@ -298,7 +298,7 @@ adapters_add_kernel(const AdapterArgs p) {
         if (cl > 1) cluster_wait();
         // Each CTA adds its groups' sums, in fours.  Small tiles: every CTA hands all of its sums to all CTAs, which add them up, each for
         // itself.  Others: the e-th four goes to CTA e % cl, which adds the cl parts and hands the result to all; one more barrier,
-        // an cl-th of the traffic.
+        // a cl-th of the traffic.
         const int fours = cnt * (kR / 4);
         const uint32_t sum_addr = ptx::smem_addr(s_sum), inner_addr = ptx::smem_addr(s_inner);
         const float scale = p.scale[slot];
@@ -493,7 +493,8 @@ extern "C" int qllm_adapters_add(const qllm_adapters_t* ad, const void* x, int64
     if (!dtype_ok(dtype)) return QLLM_ERR_DTYPE;
     if (!ad) return QLLM_ERR_NULL;
     if (ad->slots <= 0 || ad->max_rank <= 0 || ad->K <= 0 || ad->N <= 0 || seqs < 0 || rows < 0) return QLLM_ERR_SHAPE;
-    if (ad->slots > 8192 || ad->max_rank > 128 || ad->max_rank % 8 || ad->K % 8 || ad->N % 8 || seqs > (1 << 20) || rows > (int64_t(1) << 30))
+    if (ad->slots > 8192 || ad->max_rank > 128 || ad->max_rank % 8 || ad->K % 8 || ad->N % 8 || ad->K > (1 << 20) || ad->N > (1 << 20) ||
+        seqs > (1 << 20) || rows > (int64_t(1) << 30))
         return QLLM_ERR_UNSUPPORTED;
     if (rows == 0 || seqs == 0) return QLLM_OK;
     if (!ad->A || !ad->B || !ad->scale || !x || !out || !q_start || !adapter) return QLLM_ERR_NULL;

@@ -102,6 +102,8 @@ struct Item {
 // The tile's item and its rows (packed row numbers in s_rows, -1 behind the last).  false: there is no such tile.  Ends with the CTA
 // synchronised.  Groups of rows are ordered by adapter, the rows of one by sequence.  As many sequences and adapters as threads take one round of
 // loads, after which every warp finds the item for itself from the counts and the first one lists the rows.
+// Ranges that increase hold `rows` rows at most.  Others overlap and could sum up to more than an int holds: where rows x seqs allows that,
+// a batch with a decreasing range has no tiles.
 template <int THREADS, int T>
 __device__ __forceinline__ bool find_item(const AdapterArgs& p, int tile, uint8_t* area, int* s_red, int* s_item, int* s_rows, Item& item) {
     const int t = threadIdx.x, lane = t & 31, groups = p.slots + 1;
@@ -115,10 +117,15 @@ __device__ __forceinline__ bool find_item(const AdapterArgs& p, int tile, uint8_
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");     // launched as a dependent: nothing above touched global memory
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const bool vast = p.rows * p.seqs > (int64_t(1) << 30);
     if (p.seqs <= THREADS && groups <= THREADS) {
         const bool on = t < p.seqs;
         const int s = on ? t : 0;
         const int b0 = p.start[s], b1 = p.start[s + 1], ad = p.adapter[s], raw = t < p.slots ? p.raw_rank(t) : 0;
+        if (vast && __syncthreads_or(on && b1 < b0)) {
+            if (blockIdx.x == 0 && t == 0) kv::raise_page(p.status);
+            return false;
+        }
         const int f = int(min(max(int64_t(b0), int64_t(0)), p.rows)), n = on ? max(int(min(max(int64_t(b1), int64_t(0)), p.rows)) - f, 0) : 0;
         const int a = n > 0 ? p.group_of(ad) : -1;
         if (a >= 0) atomicAdd(counts + a, n);
@@ -176,6 +183,14 @@ __device__ __forceinline__ bool find_item(const AdapterArgs& p, int tile, uint8_
     } else {
         // a thread's run of sequences, and of adapters
         const int per = (p.seqs + THREADS - 1) / THREADS, s0 = min(t * per, p.seqs), s1 = min(s0 + per, p.seqs);
+        if (vast) {
+            bool down = false;
+            for (int s = t; s < p.seqs; s += THREADS) down |= p.start[s + 1] < p.start[s];
+            if (__syncthreads_or(down)) {
+                if (blockIdx.x == 0 && t == 0) kv::raise_page(p.status);
+                return false;
+            }
+        }
         for (int i = t; i < groups; i += THREADS) ranks[i] = i < p.slots ? p.cut_rank(p.raw_rank(i)) : 0;
         for (int s = s0; s < s1; ++s) {
             const int n = p.count(s), b0 = p.start[s], b1 = p.start[s + 1], ad = p.adapter[s], a = p.group_of(ad);

@@ -144,7 +144,7 @@ adapters_tile_kernel(const AdapterArgs p) {
     ptx::tc_fence_after_sync();
     const uint32_t tmem = s_tmem;                          // two D2 in columns 0 .. 255, two D1 from 256 on
     const int slot = item.slot, cnt = item.cnt, rank = item.rank;
-    // this CTA's parts of K and N, in units of 64 and 128 (K, N < 2^31)
+    // this CTA's parts of K and N, in units of 64 and 128
     const int ku = (p.K + 63) / 64, nu = (p.N + kCols - 1) / kCols;
     const int k0 = 64 * (ku * part / cl), k1 = rank > 0 ? min(64 * (ku * (part + 1) / cl), p.K) : k0;
     const int n0 = kCols * (nu * part / cl), n1 = min(kCols * (nu * (part + 1) / cl), p.N);
@@ -482,6 +482,10 @@ adapters_tile_kernel(const AdapterArgs p) {
     if (!ok) {                                             // MMAs that were issued before a wait ran out
         const long long since = clock64();
         while (clock64() - since < (1ll << 20)) {}
+        if (cl > 1) {                                      // others may still write to this CTA: until they are here, or gone
+            cluster_arrive();
+            cluster_wait();
+        }
     }
     ptx::tc_fence_before_sync();
     ptx::named_bar_sync(1, kWorkers);
@@ -493,7 +497,7 @@ template <int R, int ROWS>
 int launch_shape(AdapterArgs p, cudaStream_t st) {
     using S = Shape<R, ROWS>;
     constexpr auto kern = adapters_tile_kernel<R, ROWS>;
-    static_assert(find_bytes(8192, kThreads) + 1024 <= S::kBytes, "the counts of 8192 adapters lie where the stages will be");
+    static_assert(find_bytes(8192, kThreads) <= S::kStages * S::kStage, "the counts of 8192 adapters lie where the stages will be, in front of what other CTAs write");
     // tiles: at most, and about (a group's last tile is half full, but every group has one)
     const int64_t groups = std::min<int64_t>({p.seqs, p.slots + 1, p.rows}), tiles = groups + (p.rows - groups) / ROWS;
     const int64_t likely = std::max(groups, (p.rows + groups * (ROWS / 2)) / ROWS);

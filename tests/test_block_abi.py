@@ -55,7 +55,8 @@ def add(x=ONE, xs=256, base=ONE, bs=512, out=ONE, os=512, dtype=1, start=ONE, ad
     (dict(A=None), "NULL"), (dict(B=None), "NULL"), (dict(scale=None), "NULL"), (dict(x=None), "NULL"), (dict(out=None), "NULL"), (dict(start=None), "NULL"),
     (dict(adapter=None), "NULL"), (dict(A=8), "ALIGN"), (dict(B=8), "ALIGN"), (dict(x=8), "ALIGN"), (dict(base=8), "ALIGN"), (dict(out=24), "ALIGN"),
     (dict(xs=255), "SHAPE"), (dict(bs=511), "SHAPE"), (dict(os=504), "SHAPE"), (dict(xs=260), "ALIGN"), (dict(bs=516, base=32), "ALIGN"), (dict(os=516), "ALIGN"),
-    (dict(xs=258, dtype=0), "ALIGN"), (dict(os=520), "SHAPE")])
+    (dict(xs=258, dtype=0), "ALIGN"), (dict(K=(1 << 20) + 8, xs=1 << 21), "UNSUPPORTED"),
+    (dict(N=(1 << 20) + 8, bs=1 << 21, os=1 << 21), "UNSUPPORTED"), (dict(os=520), "SHAPE")])
 def test_adapters_refused(kw, e):
     """(the last one: base is out, with another stride)"""
     assert add(**kw) == err(e)

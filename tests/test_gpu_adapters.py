@@ -228,6 +228,25 @@ def test_contents_out_of_range_are_reported_and_harmless(dtype, top):
     assert B.qllm_poll_status() == B.QLLM_OK
 
 
+@pytest.mark.parametrize("seqs,rows,top", [(40000, 200000, 16), (200, 1 << 25, 16), (40000, 200000, 72), (200, 1 << 25, 72)])
+def test_decreasing_ranges_that_would_pass_31_bits(seqs, rows, top):
+    """Every second range is the whole tensor: the rows of one adapter add up to 2^31 and more."""
+    ad = make(2, top, 8, 8, [8, 8])
+    x, base = torch.ones(rows, 8, device=G.DEV).bfloat16(), torch.ones(rows, 8, device=G.DEV).bfloat16()
+    out = G.Guarded((rows, 8), torch.bfloat16, 3.0)
+    B.qllm_adapters_add(ad, x, base, out.t, ints([rows * (s % 2) for s in range(seqs + 1)]), ints([1] * seqs))
+    assert B.qllm_poll_status() == B.QLLM_ERR_PAGE
+    out.check()
+    assert (out.t == 3.0).all()
+    # the same sizes with ranges that increase
+    cut = [rows * s // seqs for s in range(seqs + 1)]
+    B.qllm_adapters_add(ad, x, base, out.t, ints(cut), ints([s % 2 for s in range(seqs)]))
+    assert B.qllm_poll_status() == B.QLLM_OK
+    for s in (0, 1, 2, 77, seqs - 2, seqs - 1):
+        lo, hi = cut[s], min(cut[s] + 40, cut[s + 1])
+        check(out.t[lo:hi], ad, [8, 8], x[lo:hi], base[lo:hi], [0, hi - lo], [s % 2])
+
+
 def test_rows_with_nan_and_infinities_stay_by_themselves():
     for dtype, top in (("bf16", 16), ("f32", 16), ("bf16", 72)):
         ad = make(1, top, 256, 128, [16])
