@@ -135,7 +135,7 @@ adapters_add_kernel(const AdapterArgs p) {
 
     // ---- the tile's adapter and rows
     Item item;
-    if (!find_item<kThreads, kT>(p, tile, smem, s_red, s_item, s_rows, item)) return;   // the same in all CTAs of a cluster
+    if (!find_item<kThreads, kT>(p, tile, kT, smem, s_red, s_item, s_rows, item)) return;   // the same in all CTAs of a cluster
     const int slot = item.slot, cnt = item.cnt, rank = item.rank;
     const int mtiles = (cnt + 15) / 16 - m0, rtiles = (rank + 7) / 8;      // tiles of rows of this warp, of ranks
 
@@ -507,7 +507,7 @@ extern "C" int qllm_adapters_add(const qllm_adapters_t* ad, const void* x, int64
     int* status = device_status_word();
     if (!status) return QLLM_ERR_CUDA;
     const AdapterArgs p{static_cast<const __nv_bfloat16*>(ad->A), static_cast<const __nv_bfloat16*>(ad->B), ad->scale, ad->rank, ad->slots, ad->max_rank,
-                        ad->K, ad->N, q_start, adapter, seqs, 1, rows, x, base, out, x_stride, base_stride, out_stride, status};
+                        ad->K, ad->N, q_start, adapter, seqs, 1, 0, 0, 0, rows, x, base, out, x_stride, base_stride, out_stride, status};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return dtype == QLLM_BF16 ? launch_adapters<__nv_bfloat16>(p, st) : launch_adapters<float>(p, st);
 }

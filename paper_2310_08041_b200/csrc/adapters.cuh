@@ -22,6 +22,7 @@ struct AdapterArgs {
     int slots, max_rank, K, N;
     const int32_t *start, *adapter;
     int seqs, cluster;                                     // CTAs of a tile
+    int tile_rows, stage, stages;                          // adapters_tile.cu: rows of a tile, bytes of a stage, stages
     int64_t rows;
     const void *x, *base;
     void* out;
@@ -80,13 +81,11 @@ __device__ __forceinline__ void st_cluster2(uint32_t addr, uint32_t a, uint32_t 
 __host__ __device__ constexpr int find_bytes(int slots, int threads) { return (slots + 2) / 2 * 16 + 3 * threads * 4; }
 
 // Rows f .. f + n - 1 at place `to` of the tile's list, as far as they fall into it: by one thread.
-template <int T>
-__device__ __forceinline__ void list_rows(int* s_rows, int to, int n, int f) {
+__device__ __forceinline__ void list_rows(int* s_rows, int T, int to, int n, int f) {
     for (int i = max(0, -to); i < n && to + i < T; ++i) s_rows[to + i] = f + i;
 }
 // The same by a warp, a run of rows for each lane (n = 0: none): short runs by their lanes, long ones by all lanes one after the other.
-template <int T>
-__device__ __forceinline__ void list_rows_warp(int* s_rows, int to, int n, int f, int lane) {
+__device__ __forceinline__ void list_rows_warp(int* s_rows, int T, int to, int n, int f, int lane) {
     const int first = max(0, -to), last = min(n, T - to);
     if (last - first <= 8)
         for (int i = first; i < last; ++i) s_rows[to + i] = f + i;
@@ -99,13 +98,13 @@ __device__ __forceinline__ void list_rows_warp(int* s_rows, int to, int n, int f
 struct Item {
     int slot, cnt, rank;                                   // adapter, rows of the tile, the adapter's rank
 };
-// The tile's item and its rows (packed row numbers in s_rows, -1 behind the last).  false: there is no such tile.  Ends with the CTA
+// The tile's item and its rows (packed row numbers in s_rows, -1 behind the last; T rows to a tile, MOST places).  false: there is no such tile.  Ends with the CTA
 // synchronised.  Groups of rows are ordered by adapter, the rows of one by sequence.  As many sequences and adapters as threads take one round of
 // loads, after which every warp finds the item for itself from the counts and the first one lists the rows.
 // Ranges that increase hold `rows` rows at most.  Others overlap and could sum up to more than an int holds: where rows x seqs allows that,
 // a batch with a decreasing range has no tiles.
-template <int THREADS, int T>
-__device__ __forceinline__ bool find_item(const AdapterArgs& p, int tile, uint8_t* area, int* s_red, int* s_item, int* s_rows, Item& item) {
+template <int THREADS, int MOST>
+__device__ __forceinline__ bool find_item(const AdapterArgs& p, int tile, int T, uint8_t* area, int* s_red, int* s_item, int* s_rows, Item& item) {
     const int t = threadIdx.x, lane = t & 31, groups = p.slots + 1;
     int* counts = reinterpret_cast<int*>(area);
     int* ranks = counts + groups;
@@ -113,7 +112,7 @@ __device__ __forceinline__ bool find_item(const AdapterArgs& p, int tile, uint8_
     int* seq_rows = seq_first + THREADS;
     int* seq_group = seq_rows + THREADS;
     for (int i = t; i < groups; i += THREADS) counts[i] = 0;
-    for (int i = t; i < T; i += THREADS) s_rows[i] = -1;
+    for (int i = t; i < MOST; i += THREADS) s_rows[i] = -1;
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");     // launched as a dependent: nothing above touched global memory
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -176,7 +175,7 @@ __device__ __forceinline__ bool find_item(const AdapterArgs& p, int tile, uint8_
                 const int k = k0 + i;
                 const bool in = k < k1 && seq_group[k] == slot;
                 const int n = in ? seq_rows[k] : 0;
-                list_rows_warp<T>(s_rows, to, n, in ? seq_first[k] : 0, lane);
+                list_rows_warp(s_rows, T, to, n, in ? seq_first[k] : 0, lane);
                 to += n;
             }
         }
@@ -223,7 +222,7 @@ __device__ __forceinline__ bool find_item(const AdapterArgs& p, int tile, uint8_
             for (int s = s0; s < s1; ++s) {
                 if (p.group_of(p.adapter[s]) != slot) continue;
                 const int n = p.count(s);
-                list_rows<T>(s_rows, to, n, p.first(s));
+                list_rows(s_rows, T, to, n, p.first(s));
                 to += n;
             }
     }

@@ -39,13 +39,19 @@ struct Shape {
     static constexpr int kHBlocks = kFew ? kBlocks : kSide ? 1 : 2 * kBlocks;
     static constexpr int kABlock = R * 128, kXBlock = ROWS * 128, kBBlock = kCols * 128, kHBlock = kFew ? 2 * kXBlock : kXBlock;
     static constexpr int kPitch = kCols * 2 + 16;          // bytes between rows of base: 16-byte accesses of 8 rows in different banks
-    static constexpr int kStageK = 2 * (kABlock + kXBlock), kStageN = kBlocks * kBBlock + ROWS * kPitch;
-    static constexpr int kStage = ((kStageK > kStageN ? kStageK : kStageN) + 1023) / 1024 * 1024;
     static constexpr int kPart = kFew ? ROWS * R * 4 : 0, kSum = kFew ? 8 * ROWS * R * 4 : ROWS * R * 4 + 8 * 16;
     static constexpr int kFixed = kHBlocks * kHBlock + kPart + kSum + (ROWS < 128 ? 128 * 128 : 0) + 1024;      // (operands are read 128 rows deep)
-    static constexpr int kMost = (223 * 1024 - kFixed) / kStage, kStages = kMost > 8 ? 8 : kMost;
-    static constexpr int kBytes = kFixed + kStages * kStage;
-    static_assert(kStages >= 2, "two stages at least");
+    static constexpr int kRing = (223 * 1024 - kFixed) / 1024 * 1024, kBytes = kFixed + kRing, kMostStages = 8;
+    // the ring's stages for tiles of `rows` rows: the fewer, the more of them
+    static __host__ __device__ constexpr int stage_bytes(int rows) {
+        const int k = 2 * (kABlock + rows * 128), n = kBlocks * kBBlock + rows * kPitch;
+        return ((k > n ? k : n) + 1023) / 1024 * 1024;
+    }
+    static __host__ __device__ constexpr int stages(int rows) {
+        const int n = kRing / stage_bytes(rows);
+        return n > kMostStages ? kMostStages : n;
+    }
+    static_assert(kRing / stage_bytes(ROWS) >= 2, "two stages at least");
 };
 
 // kind::f16: bf16 x bf16, both K-major, float32 sums
@@ -109,19 +115,21 @@ __global__ void __launch_bounds__(kThreads, 1)
 adapters_tile_kernel(const AdapterArgs p) {
     using S = Shape<R, ROWS>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t s_full[S::kStages], s_empty[S::kStages], s_ready[2], s_d1, s_h, s_d2[2], s_d2_free[2];
+    __shared__ uint64_t s_full[S::kMostStages], s_empty[S::kMostStages], s_ready[2], s_d1, s_h, s_d2[4], s_d2_free[4];
     __shared__ uint32_t s_tmem;
     __shared__ int s_red[kThreads / 32], s_item[2], s_rows[ROWS], s_abort;
     uint8_t* smem = smem_raw + (1024 - (ptx::smem_addr(smem_raw) & 1023)) % 1024;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const int cl = p.cluster, tile = int(blockIdx.x) / cl, part = int(blockIdx.x) - tile * cl;
+    const int tile_rows = S::kFew ? ROWS : p.tile_rows, x_block = tile_rows * 128;
+    const int stage = S::kFew ? S::stage_bytes(ROWS) : p.stage, stages = S::kFew ? S::stages(ROWS) : p.stages;
     if (t == 0) {
-        for (int i = 0; i < S::kStages; ++i) {
+        for (int i = 0; i < stages; ++i) {
             ptx::mbar_init(&s_full[i], kFeeders);
-            ptx::mbar_init(&s_empty[i], 1);
+            ptx::mbar_init(&s_empty[i], kTeam / 32);       // a team's warps; in the first product the MMAs, for all of them
         }
-        for (int i = 0; i < 2; ++i) {
-            ptx::mbar_init(&s_ready[i], cl);
+        for (int i = 0; i < 2; ++i) ptx::mbar_init(&s_ready[i], cl);
+        for (int i = 0; i < 4; ++i) {
             ptx::mbar_init(&s_d2[i], 1);
             ptx::mbar_init(&s_d2_free[i], kTeam / 32);
         }
@@ -133,7 +141,7 @@ adapters_tile_kernel(const AdapterArgs p) {
     __syncwarp();
     if (cl > 1) cluster_arrive();                          // waited for below: all CTAs have started, their barriers are set
     Item item;
-    if (!find_item<kThreads, ROWS>(p, tile, smem, s_red, s_item, s_rows, item)) return;  // the same in all CTAs of a cluster
+    if (!find_item<kThreads, ROWS>(p, tile, tile_rows, smem, s_red, s_item, s_rows, item)) return;  // the same in all CTAs of a cluster
     if (cl > 1) cluster_wait();
     if (warp == 0) {
         ptx::tmem_alloc(&s_tmem, 512);
@@ -142,20 +150,21 @@ adapters_tile_kernel(const AdapterArgs p) {
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
-    const uint32_t tmem = s_tmem;                          // two D2 in columns 0 .. 255, two D1 from 256 on
+    // Tensor memory: D1, one of each issuer, from column 256 on; D2, two of each team: team + 2 k at 128 times that, over D1 once it has been read
+    const uint32_t tmem = s_tmem;
     const int slot = item.slot, cnt = item.cnt, rank = item.rank;
     // this CTA's parts of K and N, in units of 64 and 128
     const int ku = (p.K + 63) / 64, nu = (p.N + kCols - 1) / kCols;
     const int k0 = 64 * (ku * part / cl), k1 = rank > 0 ? min(64 * (ku * (part + 1) / cl), p.K) : k0;
     const int n0 = kCols * (nu * part / cl), n1 = min(kCols * (nu * (part + 1) / cl), p.N);
-    uint8_t* s_hop = smem + S::kStages * S::kStage;        // H as operand
+    uint8_t* s_hop = smem + S::kRing;        // H as operand
     float* s_part = reinterpret_cast<float*>(s_hop + S::kHBlocks * S::kHBlock);
     float* s_sum = s_part + S::kPart / 4;
     const Abort ab{&s_abort, p.status};
     int sg = 0;
     uint32_t turn = 0;
     const auto advance = [&] {
-        if (++sg == S::kStages) { sg = 0; turn ^= 1; }
+        if (++sg == stages) { sg = 0; turn ^= 1; }
     };
 
     if (warp >= kWorkers / 32 + kIssuers) {
@@ -176,7 +185,7 @@ adapters_tile_kernel(const AdapterArgs p) {
         const int64_t a_step = int64_t(16) * p.K * 2;
         for (int k = k0; k < k1; k += kCols) {
             if (!(ok = all(wait_bounded(&s_empty[sg], turn ^ 1, ab)))) break;
-            const uint32_t to = base_addr + sg * S::kStage + swz;
+            const uint32_t to = base_addr + sg * stage + swz;
             const int bytes = k + 8 * piece < k1 ? 16 : 0;             // behind the last column: zeros
             const int64_t back = bytes ? 0 : int64_t(k1 - 8 - k - 8 * piece) * 2;       // (from an address that exists)
             const uint32_t block = piece >> 3;
@@ -185,7 +194,7 @@ adapters_tile_kernel(const AdapterArgs p) {
                 if (row0 + 16 * i < rank) cp_async16(to + block * S::kABlock + i * 2048, a + i * a_step + back, bytes);
 #pragma unroll
             for (int i = 0; i < kX; ++i) {
-                if (row0 + 16 * i < cnt) cp_async16(to + 2 * S::kABlock + block * S::kXBlock + i * 2048, src[i] + back, bytes);
+                if (row0 + 16 * i < cnt) cp_async16(to + 2 * S::kABlock + block * x_block + i * 2048, src[i] + back, bytes);
                 src[i] += kCols * 2;
             }
             a += kCols * 2;
@@ -201,7 +210,7 @@ adapters_tile_kernel(const AdapterArgs p) {
         if (p.base) set_rows(p.base, p.base_stride, n0);
         for (int n = n0; ok && n < n1; n += kCols) {
             if (!(ok = all(wait_bounded(&s_empty[sg], turn ^ 1, ab)))) break;
-            const uint32_t to = base_addr + sg * S::kStage;
+            const uint32_t to = base_addr + sg * stage;
             if (used) {
 #pragma unroll
                 for (int i = 0; i < kTimes; ++i) {
@@ -232,7 +241,7 @@ adapters_tile_kernel(const AdapterArgs p) {
         if (rank > 0) {
             constexpr uint32_t id1 = idesc_bf16(128, S::kFew ? ROWS : R), id2 = idesc_bf16(128, S::kFew ? 2 * ROWS : kCols);
             const uint32_t base_addr = ptx::smem_addr(smem), h_low = desc_low(ptx::smem_addr(s_hop)), d = __shfl_sync(0xffffffffu, tmem, 0);
-            const uint32_t d1 = d + 256 + me * R, d2 = d + me * kCols;
+            const uint32_t d1 = d + 256 + me * R;
             const auto issue = [&](uint32_t to, uint32_t rows, uint32_t weights, uint32_t id, uint32_t more) {
                 if constexpr (S::kFew) mma_bf16_ss(to, weights, rows, id, more);
                 else mma_bf16_ss(to, rows, weights, id, more);
@@ -246,12 +255,13 @@ adapters_tile_kernel(const AdapterArgs p) {
                 if (!(ok = all(wait_bounded(&s_full[sg], turn, ab)))) break;
                 ptx::fence_proxy_async_smem();             // copies of the generic proxy, read by the tensor core
                 ptx::tc_fence_after_sync();
-                const uint32_t ranks = desc_low(base_addr + sg * S::kStage), rows = ranks + (2 * S::kABlock >> 4);
+                const uint32_t ranks = desc_low(base_addr + sg * stage), rows = ranks + (2 * S::kABlock >> 4);
                 if (lead) {
 #pragma unroll
                     for (int s = 0; s < 8; ++s)
-                        issue(d1, rows + (((s >> 2) * S::kXBlock + (s & 3) * 32) >> 4), ranks + (((s >> 2) * S::kABlock + (s & 3) * 32) >> 4), id1,
+                        issue(d1, rows + (((s >> 2) * x_block + (s & 3) * 32) >> 4), ranks + (((s >> 2) * S::kABlock + (s & 3) * 32) >> 4), id1,
                               s > 0 ? 1u : more);
+                    for (int i = 1; i < kTeam / 32; ++i) ptx::mbar_arrive(&s_empty[sg]);
                     ptx::mma_commit(&s_empty[sg]);
                 }
                 __syncwarp();
@@ -262,15 +272,16 @@ adapters_tile_kernel(const AdapterArgs p) {
             ptx::fence_proxy_async_smem();
             ptx::tc_fence_after_sync();
             const int steps = (rank + 15) / 16;
-            uint32_t round = 0;
             turns = 0;
             for (int n = n0; ok && n < n1; n += kCols, advance(), ++turns) {
                 if ((turns & 1) != me) continue;
-                ok = all(wait_bounded(&s_full[sg], turn, ab) && wait_bounded(&s_d2_free[me], round ^ 1, ab));
+                const int buf = turns & 3;                 // team + 2 k
+                ok = all(wait_bounded(&s_full[sg], turn, ab) && wait_bounded(&s_d2_free[buf], (turns >> 2 & 1) ^ 1, ab));
                 if (!ok) break;
+                const uint32_t d2 = d + buf * kCols;
                 ptx::fence_proxy_async_smem();
                 ptx::tc_fence_after_sync();
-                const uint32_t columns = desc_low(base_addr + sg * S::kStage);
+                const uint32_t columns = desc_low(base_addr + sg * stage);
                 if (lead) {
 #pragma unroll
                     for (int half = 0; half < (S::kFew ? 1 : 2); ++half)       // (few rows: both parts are N of one MMA)
@@ -280,10 +291,9 @@ adapters_tile_kernel(const AdapterArgs p) {
                             issue(d2, h_low + ((S::kSide && !S::kFew ? half * 2 * R + s * 32 : (half * S::kBlocks + (s >> 2)) * S::kHBlock + (s & 3) * 32) >> 4),
                                   columns + (((s >> 2) * S::kBBlock + (s & 3) * 32) >> 4), id2, half > 0 || s > 0);
                         }
-                    ptx::mma_commit(&s_d2[me]);
+                    ptx::mma_commit(&s_d2[buf]);
                 }
                 __syncwarp();
-                round ^= 1;
             }
         }
         return;
@@ -380,41 +390,44 @@ adapters_tile_kernel(const AdapterArgs p) {
             ok = all(ok && wait_cluster(&s_ready[1], ab));
         }
         ptx::fence_proxy_async_smem();                     // H is read by the tensor core
+        ptx::tc_fence_before_sync();                       // D1 is written over
         ptx::mbar_arrive(&s_h);
     }
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out);
     const bool has_base = p.base != nullptr;
     const uint32_t smem_base = ptx::smem_addr(smem);
-    const int mine = !S::kFew && row < cnt ? row : -1;     // the tile's row that this thread has (few rows: a column of all of them)
-    int out_row[S::kFew ? 16 : ROWS / 8];                  // rows that this thread writes
+    // rows that this thread writes: few rows: a column of all of them; others: pieces of every second row of its warp's 32
+    const int first_row = S::kFew ? 0 : 32 * quarter + (lane >> 4);
+    int out_row[16];
 #pragma unroll
-    for (int i = 0; i < (S::kFew ? 16 : ROWS / 8); ++i) {
-        const int r = S::kFew ? i : (row >> 4) + 8 * i;
+    for (int i = 0; i < 16; ++i) {
+        const int r = S::kFew ? i : first_row + 2 * i;
         out_row[i] = r < cnt ? s_rows[r] : -1;
     }
-    const auto release = [&] {                             // this team's D2 has been read
-        ptx::tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&s_d2_free[team]);
-    };
-    uint32_t round = 0;
     int turns = 0;
     for (int n = n0; n < n1; n += kCols, advance(), ++turns) {
         if ((turns & 1) != team) continue;                 // the other team's
-        ok = all(ok && wait_bounded(&s_full[sg], turn, ab) && (rank == 0 || wait_bounded(&s_d2[team], round, ab)));
+        const int buf = turns & 3;
+        const uint32_t d2 = my_tmem + buf * kCols;
+        ok = all(ok && wait_bounded(&s_full[sg], turn, ab) && (rank == 0 || wait_bounded(&s_d2[buf], turns >> 2 & 1, ab)));
         ptx::tc_fence_after_sync();
-        const uint32_t cells = smem_base + sg * S::kStage + S::kBlocks * S::kBBlock;
+        const uint32_t cells = smem_base + sg * stage + S::kBlocks * S::kBBlock;
+        const auto release = [&] {                         // D2 has been read: the MMAs after the next run under the rest
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&s_d2_free[buf]);
+        };
         if constexpr (S::kFew) {
             uint32_t d[16], e[16];
             if (rank > 0) {
-                tmem_ld_x16(my_tmem + team * kCols, d);
-                tmem_ld_x16(my_tmem + team * kCols + 16, e);
+                tmem_ld_x16(d2, d);
+                tmem_ld_x16(d2 + 16, e);
                 ptx::tmem_ld_wait();
             } else {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) d[i] = e[i] = 0;
             }
-            release();                                     // the next MMAs run under the rest
+            release();
             __nv_bfloat16* to = out + n + row;
             if (ok && n + row < n1) {
 #pragma unroll
@@ -430,19 +443,19 @@ adapters_tile_kernel(const AdapterArgs p) {
                                 __float2bfloat16_rn(__uint_as_float(o[i] << 16) + (__uint_as_float(d[i0 + i]) + __uint_as_float(e[i0 + i])));
                 }
             }
-        } else if (ok && quarter * 32 < cnt) {
+        } else if (ok && quarter * 32 < cnt) {             // a warp's rows are its own from the sums to the stores
             const uint32_t cell = cells + row * S::kPitch;
 #pragma unroll 1
             for (int c = 0; c < kCols; c += 32) {
                 uint32_t d[32];
                 if (rank > 0) {
-                    ptx::tmem_ld_32x32b_x32(my_tmem + team * kCols + c, d);
+                    ptx::tmem_ld_32x32b_x32(d2 + c, d);
                     ptx::tmem_ld_wait();
                 } else {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) d[i] = 0;
                 }
-                if (mine >= 0) {
+                if (row < cnt) {
                     uint4 o[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[i] = has_base ? lds4(cell + c * 2 + 16 * i) : make_uint4(0, 0, 0, 0);
@@ -457,27 +470,27 @@ adapters_tile_kernel(const AdapterArgs p) {
                     }
                 }
             }
-        }
-        if constexpr (!S::kFew) release();
-        ptx::named_bar_sync(2 + team, kTeam);
-        if constexpr (!S::kFew) {
-            // 16 threads a row, 8 rows at a time
-            if (ok && n + 8 * (row & 15) < n1) {
-                const uint32_t from = cells + (row >> 4) * S::kPitch + (row & 15) * 16;
+            release();
+            // 16 threads a row, 2 rows at a time
+            if (n + 8 * (lane & 15) < n1) {
+                const uint32_t from = cells + first_row * S::kPitch + (lane & 15) * 16;
+                __nv_bfloat16* to = out + n + 8 * (lane & 15);
 #pragma unroll
-                for (int i0 = 0; i0 < ROWS / 8; i0 += 4) {
+                for (int i0 = 0; i0 < 16; i0 += 4) {
+                    if (32 * quarter + 2 * i0 >= cnt) break;
                     uint4 o[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[i] = lds4(from + (i0 + i) * 8 * S::kPitch);
+                    for (int i = 0; i < 4; ++i) o[i] = lds4(from + (i0 + i) * 2 * S::kPitch);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (out_row[i0 + i] >= 0) *reinterpret_cast<uint4*>(out + int64_t(out_row[i0 + i]) * p.out_stride + n + 8 * (row & 15)) = o[i];
+                        if (out_row[i0 + i] >= 0) *reinterpret_cast<uint4*>(to + int64_t(out_row[i0 + i]) * p.out_stride) = o[i];
                 }
             }
-            ptx::named_bar_sync(2 + team, kTeam);
+        } else {
+            release();
         }
-        if (row == 0) ptx::mbar_arrive(&s_empty[sg]);
-        round ^= 1;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&s_empty[sg]);
     }
     if (!ok) {                                             // MMAs that were issued before a wait ran out
         const long long since = clock64();
@@ -497,10 +510,7 @@ template <int R, int ROWS>
 int launch_shape(AdapterArgs p, cudaStream_t st) {
     using S = Shape<R, ROWS>;
     constexpr auto kern = adapters_tile_kernel<R, ROWS>;
-    static_assert(find_bytes(8192, kThreads) <= S::kStages * S::kStage, "the counts of 8192 adapters lie where the stages will be, in front of what other CTAs write");
-    // tiles: at most, and about (a group's last tile is half full, but every group has one)
-    const int64_t groups = std::min<int64_t>({p.seqs, p.slots + 1, p.rows}), tiles = groups + (p.rows - groups) / ROWS;
-    const int64_t likely = std::max(groups, (p.rows + groups * (ROWS / 2)) / ROWS);
+    static_assert(find_bytes(8192, kThreads) <= S::kRing, "the counts of 8192 adapters lie where the stages will be, in front of what other CTAs write");
     QLLM_CUDA_TRY(allow_smem<kern>(S::kBytes));
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(kThreads);
@@ -512,22 +522,38 @@ int launch_shape(AdapterArgs p, cudaStream_t st) {
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    // as many CTAs to a tile as let all tiles run at once (clusters of 4: 33 of 148 SMs' possible 37, whatever their parts of the chip)
+    // All tiles at once, on as many SMs as that takes: for each size of a cluster, the fewest rows to a tile with which about all of them run
+    // together (a group's last tile is about half full), and of these the pair with which a CTA has the least to read.  (Clusters of 4: 33 of 148
+    // SMs' possible 37, whatever their parts of the chip.)  3900 rows on 9 adapters: 3 CTAs and 104 rows; 1024 rows of one: 8 and 80.
+    const int64_t groups = std::min<int64_t>({p.seqs, p.slots + 1, p.rows});
     static std::atomic<int> known[64][9];
     int dev = 0;
     QLLM_CUDA_TRY(cudaGetDevice(&dev));
-    for (p.cluster = 8; p.cluster > 1; --p.cluster) {
-        int most = dev < 64 ? known[dev][p.cluster].load(std::memory_order_relaxed) : 0;
+    double least = 1e30;
+    for (int cl = 8; cl >= 1; --cl) {
+        int most = dev < 64 ? known[dev][cl].load(std::memory_order_relaxed) : 0;
         if (!most) {
-            attr[0].val.clusterDim.x = unsigned(p.cluster);
-            cfg.gridDim = dim3(unsigned(p.cluster));
+            attr[0].val.clusterDim.x = unsigned(cl);
+            cfg.gridDim = dim3(unsigned(cl));
             cfg.numAttrs = 1;
             QLLM_CUDA_TRY(cudaOccupancyMaxActiveClusters(&most, kern, &cfg));
             most = std::max(most, 1);
-            if (dev < 64) known[dev][p.cluster].store(most, std::memory_order_relaxed);
+            if (dev < 64) known[dev][cl].store(most, std::memory_order_relaxed);
         }
-        if (likely <= most) break;
+        int64_t rows = ROWS;
+        const int64_t room = 4 * most - 3 * groups;        // fours of tiles beside the groups' last ones
+        if (groups <= most && ROWS > 16 && room > 0) rows = std::min<int64_t>((4 * p.rows / room + 16) / 16 * 16, ROWS);
+        const bool fits = std::max(groups, p.rows / rows + (ROWS > 16 ? 3 * groups / 4 : groups / 2)) <= most;
+        const double cost = double(rows + R) / cl;
+        if ((fits && cost < least) || (cl == 1 && least == 1e30)) {
+            least = cost;
+            p.cluster = cl;
+            p.tile_rows = int(rows);
+        }
     }
+    p.stage = S::stage_bytes(p.tile_rows);
+    p.stages = S::stages(p.tile_rows);
+    const int64_t tiles = groups + (p.rows - groups) / p.tile_rows;        // at most
     attr[0].val.clusterDim.x = unsigned(p.cluster);
     cfg.gridDim = dim3(unsigned(tiles * p.cluster));
     cfg.numAttrs = 2;
