@@ -451,14 +451,17 @@ int launch_tiles(AdapterArgs p, cudaStream_t st) {
 
 // Which kernel serves a bf16 call: this file's warp-level MMA with operands straight from memory, or the tensor cores' (adapters_tile.cu), which
 // have the longer way to their first byte and stream faster behind it.  Measured with random adapters, us here / there:
-//   tiles of many rows  rank 32, 8192 x 10240: 256 rows of one adapter 20 / 26, 24 adapters of 40 rows 34 / 33, 1024 rows of one 46 / 30
-//                       rank 64: 17 rows 29 / 20, 1024 rows 87 / 34
+//   tiles of many rows  rank 16, 4096 x 4096, rows of one adapter: 256 10.2 / 13.1, 768 10.6 / 14.1, 1024 (16 of this kernel's tiles, of whose clusters
+//                       15 fit at once) 20.5 / 14.5; 4 adapters of 300 22 / 16, 24 of 20 18.1 / 16.5; 4096 rows, 1024 x 1000: 17.6 / 12.6
+//                       rank 32, 8192 x 10240: 24 rows 16.2 / 17.8, 64 20.0 / 17.9, 1024 46 / 24, 24 adapters of 40 34.3 / 34.8, 12 of 100 46 / 33;
+//                       5120 x 5120: 64 rows 14.7 / 13.5, 768 16.3 / 16.0
+//                       rank 64, 8192 x 10240: 17 rows 29 / 19, 1024 rows 87 / 28
 //   few rows each       rank 32, 8192 x 10240: one token 6.7 / 10.8, 96 tokens on 24 adapters 16 / 16; 4096 x 4096: 6.1 / 7.8, 8.8 / 11
 //                       rank 64, 8192 x 10240: 12.3 / 11.2, 25 / 18; 4096 x 4096: 7.8 / 8.3, 12.8 / 12.2
 //                       rank 128: 1024 x 1000 6.5 / 7.0, 17 / 9.3; 4096 x 4096 11 / 9.5, 33 / 18
 bool tensor_cores(const AdapterArgs& p, bool few) {
     const int64_t groups = std::min(p.seqs, p.slots + 1), sides = int64_t(p.K) + p.N;
-    if (!few) return p.max_rank > 32 || (p.rows >= 512 && p.rows >= 128 * groups);
+    if (!few) return p.max_rank > 32 || groups + p.rows / 64 > 15 || (p.max_rank > 16 && p.rows >= 48);
     return p.max_rank > 64 || (p.max_rank > 32 && (sides >= 16384 || groups * sides * p.max_rank >= 8000000));
 }
 

@@ -29,7 +29,7 @@ namespace {
 using tc::Abort;
 using tc::wait_bounded;
 
-constexpr int kFeeders = 256, kTeam = 128, kWorkers = 2 * kTeam, kIssuers = 2, kThreads = kWorkers + 32 * kIssuers + kFeeders, kCols = 128;
+constexpr int kFeeders = 256, kTeam = 128, kTeams = 3, kWorkers = kTeams * kTeam, kIssuers = kTeams, kThreads = kWorkers + 32 * kIssuers + kFeeders, kCols = 128;
 
 template <int R, int ROWS>
 struct Shape {
@@ -94,6 +94,13 @@ __device__ __forceinline__ bool wait_cluster(uint64_t* bar, const Abort& ab) {
     asm volatile("fence.acq_rel.cluster;" ::: "memory");
     return ok;
 }
+// a bf16 pair plus two floats, rounded (the sums as one packed addition)
+__device__ __forceinline__ uint32_t add_rounded(uint32_t pair, uint32_t d0, uint32_t d1) {
+    uint32_t s0, s1;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=r"(s0), "=r"(s1) : "r"(pair << 16), "r"(pair & 0xFFFF0000u), "r"(d0), "r"(d1));
+    return rounded(__uint_as_float(s0), __uint_as_float(s1));
+}
 // shared memory by 32-bit address
 __device__ __forceinline__ uint4 lds4(uint32_t a) {
     uint4 v;
@@ -115,9 +122,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 adapters_tile_kernel(const AdapterArgs p) {
     using S = Shape<R, ROWS>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t s_full[S::kMostStages], s_empty[S::kMostStages], s_ready[2], s_d1, s_h, s_d2[4], s_d2_free[4];
+    __shared__ uint64_t s_full[S::kMostStages], s_empty[S::kMostStages], s_ready[2], s_d1, s_h, s_d2[kTeams], s_d2_free[kTeams];
     __shared__ uint32_t s_tmem;
     __shared__ int s_red[kThreads / 32], s_item[2], s_rows[ROWS], s_abort;
+    __shared__ int64_t s_off[ROWS];                        // bytes from out to the tile's rows, -1 behind the last
     uint8_t* smem = smem_raw + (1024 - (ptx::smem_addr(smem_raw) & 1023)) % 1024;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const int cl = p.cluster, tile = int(blockIdx.x) / cl, part = int(blockIdx.x) - tile * cl;
@@ -129,7 +137,7 @@ adapters_tile_kernel(const AdapterArgs p) {
             ptx::mbar_init(&s_empty[i], kTeam / 32);       // a team's warps; in the first product the MMAs, for all of them
         }
         for (int i = 0; i < 2; ++i) ptx::mbar_init(&s_ready[i], cl);
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kTeams; ++i) {
             ptx::mbar_init(&s_d2[i], 1);
             ptx::mbar_init(&s_d2_free[i], kTeam / 32);
         }
@@ -143,6 +151,7 @@ adapters_tile_kernel(const AdapterArgs p) {
     Item item;
     if (!find_item<kThreads, ROWS>(p, tile, tile_rows, smem, s_red, s_item, s_rows, item)) return;  // the same in all CTAs of a cluster
     if (cl > 1) cluster_wait();
+    if (t < ROWS) s_off[t] = s_rows[t] < 0 ? -1 : s_rows[t] * p.out_stride * 2;
     if (warp == 0) {
         ptx::tmem_alloc(&s_tmem, 512);
         ptx::tmem_relinquish();
@@ -150,7 +159,7 @@ adapters_tile_kernel(const AdapterArgs p) {
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
-    // Tensor memory: D1, one of each issuer, from column 256 on; D2, two of each team: team + 2 k at 128 times that, over D1 once it has been read
+    // Tensor memory: D1, one of each issuer; D2, one of each team, over D1 once it has been read
     const uint32_t tmem = s_tmem;
     const int slot = item.slot, cnt = item.cnt, rank = item.rank;
     // this CTA's parts of K and N, in units of 64 and 128
@@ -161,10 +170,11 @@ adapters_tile_kernel(const AdapterArgs p) {
     float* s_part = reinterpret_cast<float*>(s_hop + S::kHBlocks * S::kHBlock);
     float* s_sum = s_part + S::kPart / 4;
     const Abort ab{&s_abort, p.status};
-    int sg = 0;
+    int sg = 0, owner = 0;                                 // place in the ring, its team
     uint32_t turn = 0;
     const auto advance = [&] {
-        if (++sg == stages) { sg = 0; turn ^= 1; }
+        if (++owner == kTeams) owner = 0;
+        if (++sg == stages) { sg = owner = 0; turn ^= 1; }
     };
 
     if (warp >= kWorkers / 32 + kIssuers) {
@@ -235,13 +245,14 @@ adapters_tile_kernel(const AdapterArgs p) {
     }
 
     if (warp >= kWorkers / 32) {
-        // ---------------------------------------------------------------- one thread of each of two warps issues the MMAs of every second
-        // stage, to sums of its own (all lanes walk along, so that operands are the warp's, not a thread's)
+        // ---------------------------------------------------------------- one thread of each of two warps issues the MMAs of every second place
+        // of the ring, to sums of its own (all lanes walk along, so that operands are the warp's, not a thread's).  A place has the same issuer and
+        // team for good: who waits for its next phase has seen the last one end, which a bit of parity alone would not tell.
         const int me = warp - kWorkers / 32;
         if (rank > 0) {
             constexpr uint32_t id1 = idesc_bf16(128, S::kFew ? ROWS : R), id2 = idesc_bf16(128, S::kFew ? 2 * ROWS : kCols);
             const uint32_t base_addr = ptx::smem_addr(smem), h_low = desc_low(ptx::smem_addr(s_hop)), d = __shfl_sync(0xffffffffu, tmem, 0);
-            const uint32_t d1 = d + 256 + me * R;
+            const uint32_t d1 = d + me * R, d2 = d + me * kCols;
             const auto issue = [&](uint32_t to, uint32_t rows, uint32_t weights, uint32_t id, uint32_t more) {
                 if constexpr (S::kFew) mma_bf16_ss(to, weights, rows, id, more);
                 else mma_bf16_ss(to, rows, weights, id, more);
@@ -249,9 +260,8 @@ adapters_tile_kernel(const AdapterArgs p) {
             const bool lead = elect_one();
             bool ok = true;
             uint32_t more = 0;
-            int turns = 0;
-            for (int k = k0; k < k1; k += kCols, advance(), ++turns) {
-                if ((turns & 1) != me) continue;
+            for (int k = k0; k < k1; k += kCols, advance()) {
+                if (owner != me) continue;
                 if (!(ok = all(wait_bounded(&s_full[sg], turn, ab)))) break;
                 ptx::fence_proxy_async_smem();             // copies of the generic proxy, read by the tensor core
                 ptx::tc_fence_after_sync();
@@ -261,7 +271,7 @@ adapters_tile_kernel(const AdapterArgs p) {
                     for (int s = 0; s < 8; ++s)
                         issue(d1, rows + (((s >> 2) * x_block + (s & 3) * 32) >> 4), ranks + (((s >> 2) * S::kABlock + (s & 3) * 32) >> 4), id1,
                               s > 0 ? 1u : more);
-                    for (int i = 1; i < kTeam / 32; ++i) ptx::mbar_arrive(&s_empty[sg]);
+                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(ptx::smem_addr(&s_empty[sg])), "n"(kTeam / 32 - 1) : "memory");
                     ptx::mma_commit(&s_empty[sg]);
                 }
                 __syncwarp();
@@ -272,13 +282,12 @@ adapters_tile_kernel(const AdapterArgs p) {
             ptx::fence_proxy_async_smem();
             ptx::tc_fence_after_sync();
             const int steps = (rank + 15) / 16;
-            turns = 0;
-            for (int n = n0; ok && n < n1; n += kCols, advance(), ++turns) {
-                if ((turns & 1) != me) continue;
-                const int buf = turns & 3;                 // team + 2 k
-                ok = all(wait_bounded(&s_full[sg], turn, ab) && wait_bounded(&s_d2_free[buf], (turns >> 2 & 1) ^ 1, ab));
+            uint32_t uses = 0;                             // the phase of the team's D2
+            for (int n = n0; ok && n < n1; n += kCols, advance()) {
+                if (owner != me) continue;
+                ok = all(wait_bounded(&s_full[sg], turn, ab) && wait_bounded(&s_d2_free[me], uses ^ 1, ab));
                 if (!ok) break;
-                const uint32_t d2 = d + buf * kCols;
+                uses ^= 1;
                 ptx::fence_proxy_async_smem();
                 ptx::tc_fence_after_sync();
                 const uint32_t columns = desc_low(base_addr + sg * stage);
@@ -291,7 +300,7 @@ adapters_tile_kernel(const AdapterArgs p) {
                             issue(d2, h_low + ((S::kSide && !S::kFew ? half * 2 * R + s * 32 : (half * S::kBlocks + (s >> 2)) * S::kHBlock + (s & 3) * 32) >> 4),
                                   columns + (((s >> 2) * S::kBBlock + (s & 3) * 32) >> 4), id2, half > 0 || s > 0);
                         }
-                    ptx::mma_commit(&s_d2[buf]);
+                    ptx::mma_commit(&s_d2[me]);
                 }
                 __syncwarp();
             }
@@ -307,7 +316,7 @@ adapters_tile_kernel(const AdapterArgs p) {
     if (rank > 0) {
         ok = all(wait_bounded(&s_d1, 0, ab));
         ptx::tc_fence_after_sync();
-        const int parts = min((k1 - k0 + kCols - 1) / kCols, 2);       // issuers that had a stage
+        const int parts = min((k1 - k0 + kCols - 1) / kCols, min(kIssuers, stages));     // issuers that had a stage
         // Sums in fours.  Small tiles: every CTA hands all of its sums to all CTAs, which add them up, each for itself.  Others: the e-th four
         // goes to CTA e % cl, which adds the cl parts and hands the result to all; a cl-th of the traffic, one more exchange.
         const int fours = cnt * (R / 4);
@@ -318,7 +327,7 @@ adapters_tile_kernel(const AdapterArgs p) {
             for (int i = 0; i < 16; ++i) d[i] = 0.f;
             for (int i = 0; i < parts; ++i) {
                 uint32_t w[16];
-                tmem_ld_x16(my_tmem + 256 + i * R + c, w);
+                tmem_ld_x16(my_tmem + i * R + c, w);
                 ptx::tmem_ld_wait();
 #pragma unroll
                 for (int j = 0; j < 16; ++j) d[j] += __uint_as_float(w[j]);
@@ -336,7 +345,7 @@ adapters_tile_kernel(const AdapterArgs p) {
             }
         } else if (quarter * 32 < cnt) {
 #pragma unroll 1
-            for (int c = 16 * team; c < R; c += 32) {
+            for (int c = 16 * team; c < R; c += 16 * kTeams) {
                 float d[16];
                 sums(c, d);
                 if (row < cnt) {
@@ -393,29 +402,21 @@ adapters_tile_kernel(const AdapterArgs p) {
         ptx::tc_fence_before_sync();                       // D1 is written over
         ptx::mbar_arrive(&s_h);
     }
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out);
+    uint8_t* out = static_cast<uint8_t*>(p.out);
     const bool has_base = p.base != nullptr;
     const uint32_t smem_base = ptx::smem_addr(smem);
-    // rows that this thread writes: few rows: a column of all of them; others: pieces of every second row of its warp's 32
-    const int first_row = S::kFew ? 0 : 32 * quarter + (lane >> 4);
-    int out_row[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = S::kFew ? i : first_row + 2 * i;
-        out_row[i] = r < cnt ? s_rows[r] : -1;
-    }
-    int turns = 0;
-    for (int n = n0; n < n1; n += kCols, advance(), ++turns) {
-        if ((turns & 1) != team) continue;                 // the other team's
-        const int buf = turns & 3;
-        const uint32_t d2 = my_tmem + buf * kCols;
-        ok = all(ok && wait_bounded(&s_full[sg], turn, ab) && (rank == 0 || wait_bounded(&s_d2[buf], turns >> 2 & 1, ab)));
+    const int first_row = 32 * quarter + (lane >> 4);
+    uint32_t uses = 0;
+    for (int n = n0; n < n1; n += kCols, advance()) {
+        if (owner != team) continue;                 // another team's
+        const uint32_t d2 = my_tmem + team * kCols;
+        ok = all(ok && wait_bounded(&s_full[sg], turn, ab) && (rank == 0 || wait_bounded(&s_d2[team], uses, ab)));
         ptx::tc_fence_after_sync();
         const uint32_t cells = smem_base + sg * stage + S::kBlocks * S::kBBlock;
-        const auto release = [&] {                         // D2 has been read: the MMAs after the next run under the rest
+        const auto release = [&] {                         // D2 has been read: the team's next MMAs run under the rest
             ptx::tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&s_d2_free[buf]);
+            if (lane == 0) ptx::mbar_arrive(&s_d2_free[team]);
         };
         if constexpr (S::kFew) {
             uint32_t d[16], e[16];
@@ -428,7 +429,7 @@ adapters_tile_kernel(const AdapterArgs p) {
                 for (int i = 0; i < 16; ++i) d[i] = e[i] = 0;
             }
             release();
-            __nv_bfloat16* to = out + n + row;
+            uint8_t* to = out + (n + row) * 2;
             if (ok && n + row < n1) {
 #pragma unroll
                 for (int i0 = 0; i0 < 16; i0 += 4) {       // four rows at a time, as many as there are
@@ -437,10 +438,12 @@ adapters_tile_kernel(const AdapterArgs p) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[i] = has_base ? lds_half(cells + (i0 + i) * S::kPitch + row * 2) : 0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (out_row[i0 + i] >= 0)
-                            to[int64_t(out_row[i0 + i]) * p.out_stride] =
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t at = s_off[i0 + i];
+                        if (at >= 0)
+                            *reinterpret_cast<__nv_bfloat16*>(to + at) =
                                 __float2bfloat16_rn(__uint_as_float(o[i] << 16) + (__uint_as_float(d[i0 + i]) + __uint_as_float(e[i0 + i])));
+                    }
                 }
             }
         } else if (ok && quarter * 32 < cnt) {             // a warp's rows are its own from the sums to the stores
@@ -463,9 +466,7 @@ adapters_tile_kernel(const AdapterArgs p) {
                     for (int i = 0; i < 4; ++i) {
                         uint32_t w[4] = {o[i].x, o[i].y, o[i].z, o[i].w};
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            w[j] = rounded(__uint_as_float(w[j] << 16) + __uint_as_float(d[8 * i + 2 * j]),
-                                           __uint_as_float(w[j] & 0xFFFF0000u) + __uint_as_float(d[8 * i + 2 * j + 1]));
+                        for (int j = 0; j < 4; ++j) w[j] = add_rounded(w[j], d[8 * i + 2 * j], d[8 * i + 2 * j + 1]);
                         sts4(cell + c * 2 + 16 * i, make_uint4(w[0], w[1], w[2], w[3]));
                     }
                 }
@@ -474,7 +475,7 @@ adapters_tile_kernel(const AdapterArgs p) {
             // 16 threads a row, 2 rows at a time
             if (n + 8 * (lane & 15) < n1) {
                 const uint32_t from = cells + first_row * S::kPitch + (lane & 15) * 16;
-                __nv_bfloat16* to = out + n + 8 * (lane & 15);
+                uint8_t* to = out + (n + 8 * (lane & 15)) * 2;
 #pragma unroll
                 for (int i0 = 0; i0 < 16; i0 += 4) {
                     if (32 * quarter + 2 * i0 >= cnt) break;
@@ -482,8 +483,10 @@ adapters_tile_kernel(const AdapterArgs p) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[i] = lds4(from + (i0 + i) * 2 * S::kPitch);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (out_row[i0 + i] >= 0) *reinterpret_cast<uint4*>(to + int64_t(out_row[i0 + i]) * p.out_stride) = o[i];
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t at = s_off[(first_row + 2 * (i0 + i)) % ROWS];
+                        if (at >= 0) *reinterpret_cast<uint4*>(to + at) = o[i];
+                    }
                 }
             }
         } else {
@@ -491,6 +494,7 @@ adapters_tile_kernel(const AdapterArgs p) {
         }
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&s_empty[sg]);
+        uses ^= 1;
     }
     if (!ok) {                                             // MMAs that were issued before a wait ran out
         const long long since = clock64();
@@ -523,8 +527,10 @@ int launch_shape(AdapterArgs p, cudaStream_t st) {
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     // All tiles at once, on as many SMs as that takes: for each size of a cluster, the fewest rows to a tile with which about all of them run
-    // together (a group's last tile is about half full), and of these the pair with which a CTA has the least to read.  (Clusters of 4: 33 of 148
-    // SMs' possible 37, whatever their parts of the chip.)  3900 rows on 9 adapters: 3 CTAs and 104 rows; 1024 rows of one: 8 and 80.
+    // together, be the groups random (their last tiles are half full, some more) or alike, and of these the pair with the shortest CTAs: 128 columns of both products together
+    // take (180 + rows) 5.6 ns (rank 32).  3792 rows on 9 adapters, 8192 x 8192: 3 CTAs to 104 rows, 53 us; 3 to 128 58, 2 to 64 55, 4 to
+    // 128 (two rounds) 64.  1024 rows of one, 8192 x 10240: 8 to 80, 25 us; 8 to 128 30, 6 to 48 29, 2 to 16 54.
+    // (Clusters of 4: 33 of 148 SMs' possible 37, whatever their parts of the chip.)
     const int64_t groups = std::min<int64_t>({p.seqs, p.slots + 1, p.rows});
     static std::atomic<int> known[64][9];
     int dev = 0;
@@ -541,10 +547,14 @@ int launch_shape(AdapterArgs p, cudaStream_t st) {
             if (dev < 64) known[dev][cl].store(most, std::memory_order_relaxed);
         }
         int64_t rows = ROWS;
-        const int64_t room = 4 * most - 3 * groups;        // fours of tiles beside the groups' last ones
-        if (groups <= most && ROWS > 16 && room > 0) rows = std::min<int64_t>((4 * p.rows / room + 16) / 16 * 16, ROWS);
-        const bool fits = std::max(groups, p.rows / rows + (ROWS > 16 ? 3 * groups / 4 : groups / 2)) <= most;
-        const double cost = double(rows + R) / cl;
+        const int64_t room = 4 * most - 3 * groups, each = (p.rows + groups - 1) / groups;         // fours of tiles beside the groups' last ones
+        if (ROWS > 16 && groups <= most && room > 0) {
+            const int64_t even = (each + most / groups - 1) / (most / groups);
+            rows = std::min<int64_t>((std::max(4 * p.rows / room + 1, even) + 7) / 8 * 8, ROWS);
+        }
+        const bool fits = ROWS > 16 ? 4 * (p.rows / rows) <= room && groups * ((each + rows - 1) / rows) <= most
+                                    : std::max(groups, p.rows / rows + groups / 2) <= most;
+        const double cost = double(rows + 180) / cl;
         if ((fits && cost < least) || (cl == 1 && least == 1e30)) {
             least = cost;
             p.cluster = cl;
