@@ -151,7 +151,7 @@ int qllm_quantize_rows(const void* x, int x_dtype, int64_t M, int C, int bits,
  * The norm's factor r is common to a token's channels, so codes and zero-point are those of u' = map(gamma h) and a_scale is r times
  * u's alpha (1 for a row of zeros).  Which code a value gets is thus decided by float32 operations that do not depend on an order: the sum x + residual
  * (not rounded to x_dtype before it is normalised), the product with gamma, the map's coefficient (rows with several members: summed
- * in 64 bits, rounded once), and Eq. 2 as in qllm_quantize_rows.  Finite rows whose squares pass float32, or fall below 2^-80, are
+ * in 64 bits, rounded once), and Eq. 2 as in qllm_quantize_rows.  Finite rows whose mean square leaves 2^-80 .. 2^100 are
  * scaled by a power of two on the way; gamma's entries are expected within 2^-60 .. 2^60.  A row with a NaN has a NaN
  * as a_scale; a row with an infinity has the factor 0, as the formula says, and a_scale 0 or NaN.
  * Multiples of 8 channels up to 16384 (with a map: 8192) stay in registers between reading and writing; others go through shared memory. */

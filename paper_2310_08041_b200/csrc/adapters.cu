@@ -14,6 +14,10 @@
 // two k pairs of two MMAs, and every load is a full sector.  No element is loaded twice by a CTA: in the first product the warps
 // split K, in the second N.  The columns of an MMA's 8-wide tile are dealt out so that a lane ends up with 8 neighbouring columns of out.
 //
+// This kernel serves float32 and what is small in bf16; tensor_cores() below says which, with both sides measured.  What bounds it: latency (one
+// token of 4096 -> 12288, rank 16: 5.8 us, of which a launch is 3; 35 rows of float32, 5120 x 5120, rank 32: 9.2 us), and, for larger calls, the
+// operand registers, which hold too few loads to keep memory busy (48 to 72 words a lane: kLoadK, kLoadN).
+//
 // Precision: sums in float32.  x and the weights are exact operands (float32 x as three bf16 parts of 8 bits each); the sums over K
 // are split into two bf16 parts (16 bits) for bf16 outputs, three (24 bits) for float32 ones, before they multiply B.
 #include <cuda_bf16.h>

@@ -7,16 +7,21 @@
 // swizzled as the tensor core reads operands (rows of 128 bytes, 16-byte pieces at piece ^ (row & 7)): first 128 columns of A and of the
 // tile's rows of x a stage, then, without waiting for the sums, 128 rows of B and 128 columns of base.  Copies fill with zeros what lies behind
 // K and, in B, behind the rank, so operands need no masks; rows behind the tile and the rank are whatever is there: they only reach
-// sums that are dropped.  Two threads issue the MMAs, every second stage each; two teams of four warps, a thread for each row of the tile, read the sums back from tensor
-// memory, 128 columns of the second product in turn.  H enters
-// the second product as two bf16 parts, 16 bits.
+// sums that are dropped.  Three threads issue the MMAs, each for the places of the ring that are its own; in the second product each of them has a
+// team of four warps, a thread for each row of the tile, that reads the sums back from tensor memory, adds them to base where it lies
+// and stores the rows of out (a warp's rows are its own: no barrier among warps).  H enters the second product as two bf16 parts, 16 bits.
 //
-// ROWS: rows of the tile that stages have room for.  With 16 (a step's single tokens) the products are transposed, D1[ranks x rows] and
+// The rows of a tile and the CTAs of a cluster are chosen together (launch_shape); fewer rows leave the ring more stages.
+//
+// ROWS: rows of the tile that there is room for.  With 16 (a step's single tokens) the products are transposed, D1[ranks x rows] and
 // D2[128 columns x rows]: the weights are the M side, the rows an N of 16.  An MMA's time is that of its operands' bytes from shared memory, and
-// 128 rows of which 16 are real would be most of them (96 tokens on 24 adapters of rank 64, 8192 x 10240: 21 us so).
+// 128 rows of which 16 are real would be most of them (96 tokens on 24 adapters of rank 64, 8192 x 10240: 21.2 us so, 19.7 now).
 //
-// What bounds it: memory.  The MMAs of a tile take a tenth of its time; the warp-level MMA (adapters.cu) took a third of it for prompts
-// (some 20 cycles for each m16n8k16 and quarter of an SM).
+// What bounds it.  3792 rows on 9 adapters of rank <= 32, 8192 x 8192 (53 us, 192 MB: 3.6 TB/s; the floor is 29): 0.4 us for 128 columns of the
+// first product, the ring's bytes in flight, and up to 1.3 of the second, the instructions of the teams (3900 for 128 x 128 numbers of out), on
+// three quarters of the SMs; finding the tile 2.5, first data 2, the exchange 3.7.  Two teams with barriers among their warps took 57.3 us; four teams, or
+// the teams' loop unrolled, were slower (instruction fetch).  The warp-level MMA (adapters.cu) took 63 (some 20 cycles for each m16n8k16 and quarter
+// of an SM).  A step of 96 tokens: the chain search, first data, exchange, and 125 SMs for 25 adapters of 5 CTAs.
 #include <algorithm>
 
 #include "adapters.cuh"

@@ -11,9 +11,12 @@
 // bits) and Eq. 2 in float32.  Sums of squares are float32 sums of float32 products: at most 8 NV terms per lane in order, then
 // trees; C terms of one sign are off by at most (8 NV + 12) 2^-24.
 //
-// What bounds it: HBM.  A row is read once, kept in registers, and written once.  The CTAs stay and walk the rows (gamma stays in
-// registers, the next rows are on their way); the code sum of a row leaves with the next row's exchange.
-
+// What bounds it.  A row is read once and written once.  The CTAs stay and walk the rows (gamma stays in registers, the next rows are on their way
+// into shared memory); the code sum of a row leaves with the next row's exchange.  2048 rows of 8192 in bf16 with residual, h, y and 8-bit codes:
+// 31 us for 151 MB, 4.9 TB/s of a copy's 6.6; two thirds of the issue slots.  With the map, 6011 rows of 4096: 61.5 us for 172 MB, instructions: 35.6 M, half of the issue
+// slots at 16 warps an SM; the exchange, the merged outputs and Eq. 2 cost a warp 300 to 390 of its 740 a row.  gamma from L1 instead of registers
+// took 79 us there (L1 is what shared memory leaves), one vector a thread and 512 threads 72.  A few rows: one vector a thread, one row a CTA, 2.7 us for a
+// row of 4096, 7.3 with a map of 8192 (reading it).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -566,7 +569,7 @@ int launch_norm(const NormArgs& a, cudaStream_t st) {
 
 // ---- the values that codes stand for -------------------------------------------------------------------------------------
 // out = a_scale (code - a_zero), one rounding for the difference (none for codes of zero-points below 2^22), one for the product and
-// one to the output's type.  16 codes a thread: 8 or 16 bytes in, 32 or 64 out; two rows of a CTA in flight.
+// one to the output's type.  16 codes a thread: 8 or 16 bytes in, 32 or 64 out.  2048 rows of 8192 in 8 bits to bf16: 10.4 us, 4.8 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256)
 dequantize_rows_kernel(const uint8_t* codes, const float* a_scale, const float* a_zero, int64_t M, int C, int bits, T* out) {
