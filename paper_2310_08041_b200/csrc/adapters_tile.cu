@@ -531,15 +531,17 @@ int launch_shape(AdapterArgs p, cudaStream_t st) {
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    // All tiles at once, on as many SMs as that takes: for each size of a cluster, the fewest rows to a tile with which about all of them run
-    // together, be the groups random (their last tiles are half full, some more) or alike, and of these the pair with the shortest CTAs: 128 columns of both products together
-    // take (180 + rows) 5.6 ns (rank 32).  3792 rows on 9 adapters, 8192 x 8192: 3 CTAs to 104 rows, 53 us; 3 to 128 58, 2 to 64 55, 4 to
-    // 128 (two rounds) 64.  1024 rows of one, 8192 x 10240: 8 to 80, 25 us; 8 to 128 30, 6 to 48 29, 2 to 16 54.
+    // For each size of a cluster: the rounds that the fewest tiles take, the fewest rows to a tile with which they do, be the groups random (their
+    // last tiles are half full, some more) or alike; of these the shortest launch: 128 columns of both products together take a CTA
+    // (180 + rows) 5.6 ns (rank 32; 100 + rows transposed), and a round has 8 us of its own.  3792 rows on 9 adapters, 8192 x 8192: 3 CTAs to 104 rows, 53 us; 3 to
+    // 128 58, 2 to 64 55, 4 to 128 (two rounds) 64.  1024 rows of one, 8192 x 10240: 8 to 80, 24 us; 8 to 128 30, 6 to 48 29, 2 to 16 54.  20000 rows of
+    // one, 4096 x 4096, rank 16: 3 rounds of 2 CTAs to 96 rows 114, 2 rounds of single CTAs to 128 146.
     // (Clusters of 4: 33 of 148 SMs' possible 37, whatever their parts of the chip.)
     const int64_t groups = std::min<int64_t>({p.seqs, p.slots + 1, p.rows});
     static std::atomic<int> known[64][9];
     int dev = 0;
     QLLM_CUDA_TRY(cudaGetDevice(&dev));
+    const int64_t each = (p.rows + groups - 1) / groups;
     double least = 1e30;
     for (int cl = 8; cl >= 1; --cl) {
         int most = dev < 64 ? known[dev][cl].load(std::memory_order_relaxed) : 0;
@@ -551,19 +553,15 @@ int launch_shape(AdapterArgs p, cudaStream_t st) {
             most = std::max(most, 1);
             if (dev < 64) known[dev][cl].store(most, std::memory_order_relaxed);
         }
-        int64_t rows = ROWS;
-        const int64_t room = 4 * most - 3 * groups, each = (p.rows + groups - 1) / groups;         // fours of tiles beside the groups' last ones
-        if (ROWS > 16 && groups <= most && room > 0) {
-            const int64_t even = (each + most / groups - 1) / (most / groups);
-            rows = std::min<int64_t>((std::max(4 * p.rows / room + 1, even) + 7) / 8 * 8, ROWS);
-        }
-        const bool fits = ROWS > 16 ? 4 * (p.rows / rows) <= room && groups * ((each + rows - 1) / rows) <= most
-                                    : std::max(groups, p.rows / rows + groups / 2) <= most;
-        const double cost = double(rows + 180) / cl;
-        if ((fits && cost < least) || (cl == 1 && least == 1e30)) {
-            least = cost;
+        const int64_t fewest = std::max(p.rows / ROWS + 3 * groups / 4, groups * ((each + ROWS - 1) / ROWS)), rounds = (fewest + most - 1) / most;
+        const int64_t room = 4 * most * rounds - 3 * groups;               // fours of tiles beside the groups' last ones
+        const int64_t rows = std::max(4 * p.rows / room + 1, (each + most * rounds / groups - 1) / (most * rounds / groups));
+        const int tile_rows = S::kFew ? ROWS : int(std::min<int64_t>((rows + 7) / 8 * 8, ROWS));
+        const double time = double(rounds) * (double(tile_rows + (S::kFew ? 100 : 180)) / cl + 366e3 / (double(p.K) + p.N));
+        if (time < least) {
+            least = time;
             p.cluster = cl;
-            p.tile_rows = int(rows);
+            p.tile_rows = tile_rows;
         }
     }
     p.stage = S::stage_bytes(p.tile_rows);

@@ -190,6 +190,12 @@ def test_more_sequences_and_slots_than_threads(dtype, seqs, slots, top):
     assert B.qllm_poll_status() == B.QLLM_OK
 
 
+@pytest.mark.parametrize("dtype,top,news", [("bf16", 16, [20000]), ("bf16", 40, [9000, 1, 12000]), ("bf16", 128, [10000, 7000]), ("bf16", 128, [1] * 700), ("f32", 16, [9000, 3000])])
+def test_more_tiles_than_run_at_once(dtype, top, news):
+    slots = min(len(news), 500)
+    case(dtype, 64, 136, top, [top] * slots, news, [i % slots for i in range(len(news))])
+
+
 @pytest.mark.parametrize("seed", range(16))
 def test_random_shapes(seed):
     r = np.random.RandomState(500 + seed)
