@@ -79,3 +79,28 @@ def test_captured_without_a_call_before(i):
     """In a process of its own."""
     r = subprocess.run([sys.executable, "-c", CAPTURE % sys.path, str(i)], capture_output=True, text=True, timeout=240)
     assert r.returncode == 0, r.stderr[-1500:]
+
+
+CAPTURE_TILES = """
+import sys, torch
+sys.path[:0] = %r
+from paper_2310_08041_b200 import binding as B
+top, rows = int(sys.argv[1]), int(sys.argv[2])
+ad = B.Adapters(torch.ones(2, top, 256, device="cuda").bfloat16(), torch.ones(2, 128, top, device="cuda").bfloat16(), torch.ones(2, device="cuda"))
+x, out = torch.ones(rows, 256, device="cuda").bfloat16(), torch.zeros(rows, 128, device="cuda").bfloat16()
+start, which = torch.tensor([0, rows], dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+g, st = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+with torch.cuda.graph(g, stream=st):
+    B.qllm_adapters_add(ad, x, None, out, start, which)
+g.replay()
+torch.cuda.synchronize()
+assert B.qllm_poll_status() == B.QLLM_OK and (out == 256.0 * top).all()
+"""
+
+
+@pytest.mark.parametrize("top,rows", [(16, 3), (128, 3), (40, 200), (16, 2000)])
+def test_adapters_captured_without_a_call_before(top, rows):
+    """Every kind of launch asks the device what it holds; 256 * rank is a bf16 number."""
+    r = subprocess.run([sys.executable, "-c", CAPTURE_TILES % sys.path, str(top), str(rows)], capture_output=True, text=True, timeout=240)
+    assert r.returncode == 0, r.stderr[-1500:]
