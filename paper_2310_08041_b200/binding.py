@@ -35,6 +35,7 @@ EXPORTS = [
     "qllm_kv_append", "qllm_kv_read", "qllm_kv_attention", "qllm_kv_attention_workspace",
     "qllm_kv_pages_extend", "qllm_kv_pages_fork", "qllm_kv_pages_free", "qllm_kv_pages_compact", "qllm_kv_pages_copy",
     "qllm_status_string", "qllm_last_cuda_error", "qllm_poll_status", "qllm_launch_count", "qllm_debug_wait_expiry",
+    "qllm_debug_exit_expiry",
 ]
 
 if not os.path.exists(LIB_PATH):
@@ -82,6 +83,7 @@ _lib.qllm_status_string.argtypes = [_i]
 _lib.qllm_status_string.restype = ctypes.c_char_p
 _lib.qllm_launch_count.restype = _i64
 _lib.qllm_debug_wait_expiry.argtypes = [_vp, _vp]
+_lib.qllm_debug_exit_expiry.argtypes = [_vp, _vp]
 _lib.qllm_rmsnorm_quant.argtypes = [_vp, _vp, _i, _i64, _i, _vp, _f, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.qllm_dequantize_rows.argtypes = [_vp, _vp, _vp, _i64, _i, _i, _vp, _i, _vp]
 _lib.qllm_adapters_add.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _i, _vp, _vp, _i, _i64, _vp]
@@ -298,6 +300,11 @@ def qllm_poll_status():
 def qllm_debug_wait_expiry(gave_up, stream=None):
     """Runs a bounded device-side wait into its (short) limit; gave_up: device int32 tensor, set to 1."""
     _check(_lib.qllm_debug_wait_expiry(_dp(gave_up), _stream(stream)))
+
+
+def qllm_debug_exit_expiry(left, stream=None):
+    """Runs the exit behind such a wait in a cluster of two CTAs; left: device int32 [2], each CTA adds its warps that left (3)."""
+    _check(_lib.qllm_debug_exit_expiry(_dp(left), _stream(stream)))
 
 
 def qllm_launch_count():

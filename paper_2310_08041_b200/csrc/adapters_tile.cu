@@ -501,16 +501,8 @@ adapters_tile_kernel(const AdapterArgs p) {
         if (lane == 0) ptx::mbar_arrive(&s_empty[sg]);
         uses ^= 1;
     }
-    if (!ok) {                                             // MMAs that were issued before a wait ran out
-        const long long since = clock64();
-        while (clock64() - since < (1ll << 20)) {}
-        if (cl > 1) {                                      // others may still write to this CTA: until they are here, or gone
-            cluster_arrive();
-            cluster_wait();
-        }
-    }
     ptx::tc_fence_before_sync();
-    ptx::named_bar_sync(1, kWorkers);
+    tc::leave_cluster(ok, 1, kWorkers, cl);
     ptx::tc_fence_after_sync();
     if (warp == 0) ptx::tmem_dealloc(tmem, 512);
 }

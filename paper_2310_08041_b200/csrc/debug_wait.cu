@@ -6,6 +6,9 @@
 // tensor memory, nothing in flight, no trap and no unbounded spin.  What the host sees afterwards (the launch
 // returns, qllm_poll_status reports the timeout once, the next call works) is what it would see after a real
 // expiry.
+//
+// qllm_debug_exit_expiry: the exit that the adapters' tensor-core kernel takes behind such a wait, among warps of which only one
+// saw it run out, in one of a cluster's two CTAs.
 
 #include "qgemm_tc_common.cuh"
 
@@ -26,8 +29,36 @@ __global__ void __launch_bounds__(32) wait_expiry_kernel(int* status, int* gave_
     if (threadIdx.x == 0) *gave_up = arrived ? 0 : 1;
 }
 
+constexpr int kExitWarps = 4, kExitWorkers = 3;            // the last warp leaves at once, as feeders and issuers do
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * kExitWarps) exit_expiry_kernel(int* status, int* left) {
+    __shared__ __align__(8) uint64_t bar;
+    __shared__ int flag;
+    if (threadIdx.x == 0) {
+        flag = 0;
+        ptx::mbar_init(&bar, 1);
+        ptx::fence_barrier_init();
+    }
+    __syncthreads();
+    const int warp = int(threadIdx.x) / 32;
+    if (warp >= kExitWorkers) return;
+    bool ok = true;
+    if (blockIdx.x == 0 && warp == 1) ok = __all_sync(0xffffffffu, tc::wait_bounded(&bar, 0, tc::Abort{&flag, status}, 1ll << 20));
+    tc::leave_cluster(ok, 1, 32 * kExitWorkers, 2);
+    if (threadIdx.x % 32 == 0) atomicAdd(left + blockIdx.x, 1);
+}
+
 }  // namespace
 }  // namespace qllm
+
+extern "C" int qllm_debug_exit_expiry(int* left, void* stream) {
+    using namespace qllm;
+    if (!left) return QLLM_ERR_NULL;
+    int* status = device_status_word();
+    if (!status) return QLLM_ERR_CUDA;
+    exit_expiry_kernel<<<2, 32 * kExitWarps, 0, static_cast<cudaStream_t>(stream)>>>(status, left);
+    return after_launch();
+}
 
 extern "C" int qllm_debug_wait_expiry(int* gave_up, void* stream) {
     using namespace qllm;

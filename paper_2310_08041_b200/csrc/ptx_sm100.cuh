@@ -218,6 +218,13 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t cluster_addr) {
 __device__ __forceinline__ void named_bar_sync(int id, int nthreads) {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
 }
+// the same, and whether `p` holds for any of them
+__device__ __forceinline__ bool named_bar_or(int id, int nthreads, bool p) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(uint32_t(p)), "r"(id), "r"(nthreads) : "memory");
+    return r != 0;
+}
 
 }  // namespace ptx
 }  // namespace qllm
