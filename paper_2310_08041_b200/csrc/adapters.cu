@@ -18,8 +18,8 @@
 // token of 4096 -> 12288, rank 16: 5.8 us, of which a launch is 3; 35 rows of float32, 5120 x 5120, rank 32: 9.2 us), and, for larger calls, the
 // operand registers, which hold too few loads to keep memory busy (48 to 72 words a lane: kLoadK, kLoadN).
 //
-// Precision: sums in float32.  x and the weights are exact operands (float32 x as three bf16 parts of 8 bits each); the sums over K
-// are split into two bf16 parts (16 bits) for bf16 outputs, three (24 bits) for float32 ones, before they multiply B.
+// Precision: sums in float32.  x and the weights are exact operands (float32 x as three bf16 parts of 8 bits each); so are the sums over K
+// when they multiply B, as three parts.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -108,7 +108,7 @@ template <typename T, int MT, int HM, int RN>
 struct Shape {
     static constexpr int kThreads = 32 * kGroups * HM, kTokens = 16 * MT * HM, kRank = 8 * RN;
     static constexpr int kStride = kRank + 8;              // floats / bf16 of a row: rows of a fragment in different banks
-    static constexpr int kParts = sizeof(T) == 2 ? 2 : 3;  // of the sums over K
+    static constexpr int kParts = kSumParts;               // of the sums over K
     static constexpr int kPart = kTokens * kStride * 4;    // one group's sums; the CTA's
     static constexpr int kInner = kTokens * kStride * 2;   // one part of the tile's sums
     // the counts and ranks of all adapters, later the groups' sums
@@ -455,14 +455,13 @@ int launch_tiles(AdapterArgs p, cudaStream_t st) {
 
 // Which kernel serves a bf16 call: this file's warp-level MMA with operands straight from memory, or the tensor cores' (adapters_tile.cu), which
 // have the longer way to their first byte and stream faster behind it.  Measured with random adapters, us here / there:
-//   tiles of many rows  rank 16, 4096 x 4096, rows of one adapter: 256 10.2 / 13.1, 768 10.6 / 14.1, 1024 (16 of this kernel's tiles, of whose clusters
-//                       15 fit at once) 20.5 / 14.5; 4 adapters of 300 22 / 16, 24 of 20 18.1 / 16.5; 4096 rows, 1024 x 1000: 17.6 / 12.6
-//                       rank 32, 8192 x 10240: 24 rows 16.2 / 17.8, 64 20.0 / 17.9, 1024 46 / 24, 24 adapters of 40 34.3 / 34.8, 12 of 100 46 / 33;
-//                       5120 x 5120: 64 rows 14.7 / 13.5, 768 16.3 / 16.0
-//                       rank 64, 8192 x 10240: 17 rows 29 / 19, 1024 rows 87 / 28
-//   few rows each       rank 32, 8192 x 10240: one token 6.7 / 10.8, 96 tokens on 24 adapters 16 / 16; 4096 x 4096: 6.1 / 7.8, 8.8 / 11
-//                       rank 64, 8192 x 10240: 12.3 / 11.2, 25 / 18; 4096 x 4096: 7.8 / 8.3, 12.8 / 12.2
-//                       rank 128: 1024 x 1000 6.5 / 7.0, 17 / 9.3; 4096 x 4096 11 / 9.5, 33 / 18
+//   tiles of many rows  rank 16, 4096 x 4096, rows of one adapter: 256 11.1 / 13.5, 768 11.5 / 14.5, 1024 (16 of this kernel's tiles, of whose clusters
+//                       15 fit at once) 21.8 / 15.0; 4 adapters of 300 23 / 16.5, 24 of 20 19.6 / 18.2; 4096 rows, 1024 x 1000: 19.1 / 13.1
+//                       rank 32, 8192 x 10240: 24 rows 18.2 / 18.4, 64 22.2 / 18.5, 1024 51 / 25, 24 adapters of 40 38.2 / 36.1, 12 of 100 51 / 34;
+//                       5120 x 5120: 64 rows 16.0 / 14.1, 768 18.1 / 16.8
+//   few rows each       rank 32, 8192 x 10240: one token 7.3 / 17.7, 96 tokens on 24 adapters 17.3 / 25.8; 4096 x 4096: 6.7 / 12.4, 9.7 / 17.4
+//                       rank 64, 8192 x 10240: 13.8 / 11.8, 27 / 18.8; 4096 x 4096: 8.5 / 8.8, 13.9 / 12.7
+// (Larger ranks were farther apart: rank 64, 8192 x 10240, 1024 rows 87 / 28; rank 128, 4096 x 4096, 96 tokens 33 / 18, with two parts of the sums.)
 bool tensor_cores(const AdapterArgs& p, bool few) {
     const int64_t groups = std::min(p.seqs, p.slots + 1), sides = int64_t(p.K) + p.N;
     if (!few) return p.max_rank > 32 || groups + p.rows / 64 > 15 || (p.max_rank > 16 && p.rows >= 48);
@@ -514,7 +513,7 @@ extern "C" int qllm_adapters_add(const qllm_adapters_t* ad, const void* x, int64
     int* status = device_status_word();
     if (!status) return QLLM_ERR_CUDA;
     const AdapterArgs p{static_cast<const __nv_bfloat16*>(ad->A), static_cast<const __nv_bfloat16*>(ad->B), ad->scale, ad->rank, ad->slots, ad->max_rank,
-                        ad->K, ad->N, q_start, adapter, seqs, 1, 0, 0, 0, rows, x, base, out, x_stride, base_stride, out_stride, status};
+                        ad->K, ad->N, q_start, adapter, seqs, 1, 0, 0, 0, 0, rows, x, base, out, x_stride, base_stride, out_stride, status};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return dtype == QLLM_BF16 ? launch_adapters<__nv_bfloat16>(p, st) : launch_adapters<float>(p, st);
 }

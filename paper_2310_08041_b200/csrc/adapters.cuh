@@ -22,7 +22,7 @@ struct AdapterArgs {
     int slots, max_rank, K, N;
     const int32_t *start, *adapter;
     int seqs, cluster;                                     // CTAs of a tile
-    int tile_rows, stage, stages;                          // adapters_tile.cu: rows of a tile, bytes of a stage, stages
+    int tile_rows, ring, stage, stages;                    // adapters_tile.cu: rows of a tile, bytes of the ring, of a stage, stages
     int64_t rows;
     const void *x, *base;
     void* out;
@@ -36,6 +36,11 @@ struct AdapterArgs {
     __device__ __forceinline__ int raw_rank(int a) const { return rank ? rank[a] : max_rank; }
     __device__ __forceinline__ int cut_rank(int r) const { return min(max(r, 0), max_rank); }
 };
+
+// Parts of 8 bits in which the sums over K enter the second product: all of a float32.  With two (16 bits) an output that is small next to
+// the adapter's product, base taking most of it away, was off by up to two steps of bf16, and 0.3 % of ordinary outputs came out as the neighbour of
+// the number that float32 sums give.
+constexpr int kSumParts = 3;
 
 // exclusive prefix sum over the CTA's threads; total for everyone.  red: an int for each warp
 template <int THREADS>

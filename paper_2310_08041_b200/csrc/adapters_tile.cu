@@ -9,7 +9,7 @@
 // K and, in B, behind the rank, so operands need no masks; rows behind the tile and the rank are whatever is there: they only reach
 // sums that are dropped.  Three threads issue the MMAs, each for the places of the ring that are its own; in the second product each of them has a
 // team of four warps, a thread for each row of the tile, that reads the sums back from tensor memory, adds them to base where it lies
-// and stores the rows of out (a warp's rows are its own: no barrier among warps).  H enters the second product as two bf16 parts, 16 bits.
+// and stores the rows of out (a warp's rows are its own: no barrier among warps).  H enters the second product as three bf16 parts, all of its bits.
 //
 // The rows of a tile and the CTAs of a cluster are chosen together (launch_shape); fewer rows leave the ring more stages.
 //
@@ -40,23 +40,30 @@ template <int R, int ROWS>
 struct Shape {
     static constexpr int kBlocks = (R + 63) / 64;          // operand blocks (64 elements of 128 bytes) of a row of B
     static constexpr bool kFew = ROWS == 16;               // transposed products; every CTA adds up all parts of the sums
-    static constexpr bool kSide = R <= 32;                 // both parts of H in one block, side by side
-    static constexpr int kHBlocks = kFew ? kBlocks : kSide ? 1 : 2 * kBlocks;
-    static constexpr int kABlock = R * 128, kXBlock = ROWS * 128, kBBlock = kCols * 128, kHBlock = kFew ? 2 * kXBlock : kXBlock;
+    // H: the elements of its parts side by side (R of each), few rows: the rows of its parts below one another
+    static constexpr int kHBlocks = kFew ? kBlocks : (kSumParts * R + 63) / 64;
+    static constexpr int kABlock = R * 128, kBBlock = kCols * 128, kPart = kFew ? ROWS * R * 4 : 0;
     static constexpr int kPitch = kCols * 2 + 16;          // bytes between rows of base: 16-byte accesses of 8 rows in different banks
-    static constexpr int kPart = kFew ? ROWS * R * 4 : 0, kSum = kFew ? 8 * ROWS * R * 4 : ROWS * R * 4 + 8 * 16;
-    static constexpr int kFixed = kHBlocks * kHBlock + kPart + kSum + (ROWS < 128 ? 128 * 128 : 0) + 1024;      // (operands are read 128 rows deep)
-    static constexpr int kRing = (223 * 1024 - kFixed) / 1024 * 1024, kBytes = kFixed + kRing, kMostStages = 8;
-    // the ring's stages for tiles of `rows` rows: the fewer, the more of them
+    static constexpr int kBytes = 223 * 1024, kMostStages = 8;
+    // What tiles of `rows` rows leave the ring, and the ring's stages: the fewer rows, the more of them
+    static __host__ __device__ constexpr int h_block(int rows) { return (kFew ? kSumParts * ROWS : rows) * 128; }
+    static __host__ __device__ constexpr int sum_bytes(int rows) { return kFew ? 8 * ROWS * R * 4 : rows * R * 4 + 8 * 16; }
+    static __host__ __device__ constexpr int ring_bytes(int rows) {
+        const int deep = kFew ? 0 : (128 - rows) * 128 - sum_bytes(rows);      // H as an operand is read 128 rows deep
+        return (kBytes - kHBlocks * h_block(rows) - kPart - sum_bytes(rows) - (deep > 0 ? deep : 0) - 1024) / 1024 * 1024;
+    }
     static __host__ __device__ constexpr int stage_bytes(int rows) {
         const int k = 2 * (kABlock + rows * 128), n = kBlocks * kBBlock + rows * kPitch;
         return ((k > n ? k : n) + 1023) / 1024 * 1024;
     }
     static __host__ __device__ constexpr int stages(int rows) {
-        const int n = kRing / stage_bytes(rows);
+        const int n = ring_bytes(rows) / stage_bytes(rows);
         return n > kMostStages ? kMostStages : n;
     }
-    static_assert(kRing / stage_bytes(ROWS) >= 2, "two stages at least");
+    // rows of a tile at most: with 128 of rank 64 the ring would have two stages instead of three (8 adapters of 128 rows, 8192 x 10240: 42.6 us
+    // with tiles of 128, 35.4 with two of 64 each)
+    static constexpr int kMostRows = ROWS == 128 && stages(128) < 3 ? 120 : ROWS;
+    static_assert(stages(kMostRows) >= 2, "two stages at least");
 };
 
 // kind::f16: bf16 x bf16, both K-major, float32 sums
@@ -136,6 +143,7 @@ adapters_tile_kernel(const AdapterArgs p) {
     const int cl = p.cluster, tile = int(blockIdx.x) / cl, part = int(blockIdx.x) - tile * cl;
     const int tile_rows = S::kFew ? ROWS : p.tile_rows, x_block = tile_rows * 128;
     const int stage = S::kFew ? S::stage_bytes(ROWS) : p.stage, stages = S::kFew ? S::stages(ROWS) : p.stages;
+    const int ring = S::kFew ? S::ring_bytes(ROWS) : p.ring, h_block = S::h_block(tile_rows);
     if (t == 0) {
         for (int i = 0; i < stages; ++i) {
             ptx::mbar_init(&s_full[i], kFeeders);
@@ -171,8 +179,8 @@ adapters_tile_kernel(const AdapterArgs p) {
     const int ku = (p.K + 63) / 64, nu = (p.N + kCols - 1) / kCols;
     const int k0 = 64 * (ku * part / cl), k1 = rank > 0 ? min(64 * (ku * (part + 1) / cl), p.K) : k0;
     const int n0 = kCols * (nu * part / cl), n1 = min(kCols * (nu * (part + 1) / cl), p.N);
-    uint8_t* s_hop = smem + S::kRing;        // H as operand
-    float* s_part = reinterpret_cast<float*>(s_hop + S::kHBlocks * S::kHBlock);
+    uint8_t* s_hop = smem + ring;                          // H as operand
+    float* s_part = reinterpret_cast<float*>(s_hop + S::kHBlocks * h_block);
     float* s_sum = s_part + S::kPart / 4;
     const Abort ab{&s_abort, p.status};
     int sg = 0, owner = 0;                                 // place in the ring, its team
@@ -255,7 +263,7 @@ adapters_tile_kernel(const AdapterArgs p) {
         // team for good: who waits for its next phase has seen the last one end, which a bit of parity alone would not tell.
         const int me = warp - kWorkers / 32;
         if (rank > 0) {
-            constexpr uint32_t id1 = idesc_bf16(128, S::kFew ? ROWS : R), id2 = idesc_bf16(128, S::kFew ? 2 * ROWS : kCols);
+            constexpr uint32_t id1 = idesc_bf16(128, S::kFew ? ROWS : R), id2 = idesc_bf16(128, S::kFew ? kSumParts * ROWS : kCols);
             const uint32_t base_addr = ptx::smem_addr(smem), h_low = desc_low(ptx::smem_addr(s_hop)), d = __shfl_sync(0xffffffffu, tmem, 0);
             const uint32_t d1 = d + me * R, d2 = d + me * kCols;
             const auto issue = [&](uint32_t to, uint32_t rows, uint32_t weights, uint32_t id, uint32_t more) {
@@ -298,12 +306,13 @@ adapters_tile_kernel(const AdapterArgs p) {
                 const uint32_t columns = desc_low(base_addr + sg * stage);
                 if (lead) {
 #pragma unroll
-                    for (int half = 0; half < (S::kFew ? 1 : 2); ++half)       // (few rows: both parts are N of one MMA)
+                    for (int i = 0; i < (S::kFew ? 1 : kSumParts); ++i)        // (few rows: all parts are N of one MMA)
 #pragma unroll
                         for (int s = 0; s < R / 16; ++s) {
                             if (s > 0 && s >= steps) break;
-                            issue(d2, h_low + ((S::kSide && !S::kFew ? half * 2 * R + s * 32 : (half * S::kBlocks + (s >> 2)) * S::kHBlock + (s & 3) * 32) >> 4),
-                                  columns + (((s >> 2) * S::kBBlock + (s & 3) * 32) >> 4), id2, half > 0 || s > 0);
+                            const int at = i * R + 16 * s;                     // element of a row of H
+                            issue(d2, h_low + (((at >> 6) * h_block + (at & 63) * 2) >> 4), columns + (((s >> 2) * S::kBBlock + (s & 3) * 32) >> 4), id2,
+                                  i > 0 || s > 0);
                         }
                     ptx::mma_commit(&s_d2[me]);
                 }
@@ -383,14 +392,13 @@ adapters_tile_kernel(const AdapterArgs p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) f[i] = col + i < rank ? f[i] * scale : 0.f;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const uint32_t w0 = half ? rounded(f[0], f[1]) : upper(f[0], f[1]), w1 = half ? rounded(f[2], f[3]) : upper(f[2], f[3]);
+            for (int i = 0; i < kSumParts; ++i) {
+                const bool last = i + 1 == kSumParts;
+                const uint32_t w0 = last ? rounded(f[0], f[1]) : upper(f[0], f[1]), w1 = last ? rounded(f[2], f[3]) : upper(f[2], f[3]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) f[j] = rest(f[j]);
-                const bool side = S::kSide && !S::kFew;
-                const int byte = side ? half * 2 * R + 2 * col : 2 * (col & 63), block = side ? 0 : (S::kFew ? 0 : half * S::kBlocks) + (col >> 6);
-                const int line = at_row + (S::kFew ? 16 * half : 0);
-                const uint32_t at = h_addr + block * S::kHBlock + line * 128 + (((byte >> 4) ^ (line & 7)) << 4) + (byte & 15);
+                const int element = (S::kFew ? 0 : i * R) + col, byte = 2 * (element & 63), line = at_row + (S::kFew ? ROWS * i : 0);
+                const uint32_t at = h_addr + (element >> 6) * h_block + line * 128 + (((byte >> 4) ^ (line & 7)) << 4) + (byte & 15);
                 if constexpr (S::kFew) {
                     asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(w0), "r"(w1) : "memory");
                 } else {
@@ -424,14 +432,16 @@ adapters_tile_kernel(const AdapterArgs p) {
             if (lane == 0) ptx::mbar_arrive(&s_d2_free[team]);
         };
         if constexpr (S::kFew) {
-            uint32_t d[16], e[16];
-            if (rank > 0) {
-                tmem_ld_x16(d2, d);
-                tmem_ld_x16(d2 + 16, e);
-                ptx::tmem_ld_wait();
-            } else {
+            float d[16];                                   // the parts' products, the smallest first
 #pragma unroll
-                for (int i = 0; i < 16; ++i) d[i] = e[i] = 0;
+            for (int i = 0; i < 16; ++i) d[i] = 0.f;
+            if (rank > 0) {
+                uint32_t w[kSumParts][16];
+#pragma unroll
+                for (int i = 0; i < kSumParts; ++i) tmem_ld_x16(d2 + 16 * i, w[i]);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) d[i] = __uint_as_float(w[0][i]) + (__uint_as_float(w[1][i]) + __uint_as_float(w[2][i]));
             }
             release();
             uint8_t* to = out + (n + row) * 2;
@@ -447,7 +457,7 @@ adapters_tile_kernel(const AdapterArgs p) {
                         const int64_t at = s_off[i0 + i];
                         if (at >= 0)
                             *reinterpret_cast<__nv_bfloat16*>(to + at) =
-                                __float2bfloat16_rn(__uint_as_float(o[i] << 16) + (__uint_as_float(d[i0 + i]) + __uint_as_float(e[i0 + i])));
+                                __float2bfloat16_rn(__uint_as_float(o[i] << 16) + d[i0 + i]);
                     }
                 }
             }
@@ -511,7 +521,7 @@ template <int R, int ROWS>
 int launch_shape(AdapterArgs p, cudaStream_t st) {
     using S = Shape<R, ROWS>;
     constexpr auto kern = adapters_tile_kernel<R, ROWS>;
-    static_assert(find_bytes(8192, kThreads) <= S::kRing, "the counts of 8192 adapters lie where the stages will be, in front of what other CTAs write");
+    static_assert(find_bytes(8192, kThreads) <= S::ring_bytes(S::kMostRows), "the counts of 8192 adapters lie where the stages will be, in front of what other CTAs write");
     QLLM_CUDA_TRY(allow_smem<kern>(S::kBytes));
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(kThreads);
@@ -545,10 +555,10 @@ int launch_shape(AdapterArgs p, cudaStream_t st) {
             most = std::max(most, 1);
             if (dev < 64) known[dev][cl].store(most, std::memory_order_relaxed);
         }
-        const int64_t fewest = std::max(p.rows / ROWS + 3 * groups / 4, groups * ((each + ROWS - 1) / ROWS)), rounds = (fewest + most - 1) / most;
+        const int64_t fewest = std::max(p.rows / S::kMostRows + 3 * groups / 4, groups * ((each + S::kMostRows - 1) / S::kMostRows)), rounds = (fewest + most - 1) / most;
         const int64_t room = 4 * most * rounds - 3 * groups;               // fours of tiles beside the groups' last ones
         const int64_t rows = std::max(4 * p.rows / room + 1, (each + most * rounds / groups - 1) / (most * rounds / groups));
-        const int tile_rows = S::kFew ? ROWS : int(std::min<int64_t>((rows + 7) / 8 * 8, ROWS));
+        const int tile_rows = S::kFew ? ROWS : int(std::min<int64_t>((rows + 7) / 8 * 8, S::kMostRows));
         const double time = double(rounds) * (double(tile_rows + (S::kFew ? 100 : 180)) / cl + 366e3 / (double(p.K) + p.N));
         if (time < least) {
             least = time;
@@ -556,6 +566,7 @@ int launch_shape(AdapterArgs p, cudaStream_t st) {
             p.tile_rows = tile_rows;
         }
     }
+    p.ring = S::ring_bytes(p.tile_rows);
     p.stage = S::stage_bytes(p.tile_rows);
     p.stages = S::stages(p.tile_rows);
     const int64_t tiles = groups + (p.rows - groups) / p.tile_rows;        // at most
