@@ -395,7 +395,7 @@ rmsnorm_quant_kernel(const NormArgs a) {
             r = float(wide);
             scale = float(wide * double(rs.alpha));
         }
-        if (lo == 0.f && hi == 0.f) scale = 1.f;           // Eq. 2's choice for a row of zeros
+        if (lo == 0.f && hi == 0.f && ssq < INFINITY) scale = 1.f;         // Eq. 2's choice for a row of zeros (lo and hi know no NaN, ssq does)
         const RowQuant rq(lo, hi, rs.inv, rs.zero, qmax);
         uint8_t* row = a.codes + m * (a.bits == 4 ? C / 2 : C);
         int sum = 0;
@@ -496,7 +496,7 @@ rmsnorm_quant_any(const NormArgs a) {
             r = float(wide);
             scale = float(wide * double(st.alpha));
         }
-        if (lo == 0.f && hi == 0.f) scale = 1.f;
+        if (lo == 0.f && hi == 0.f && ssq < INFINITY) scale = 1.f;
         if (a.y)
             for (int k = t; k < C; k += T) static_cast<XT*>(a.y)[m * C + k] = XT(s_u[k] * by * a.gamma[k] * r);
         if (a.codes) {
