@@ -391,11 +391,12 @@ rmsnorm_quant_kernel(const NormArgs a) {
         float r = rs.r, scale = rs.alpha * rs.r;
         if (!rs.ok || by != 1.f) {
             if (!rs.ok) rs.plain(lo, hi, qmax);
-            const double wide = scaled_factor(ssq, C, a.eps, by);
+            double wide = scaled_factor(ssq, C, a.eps, by);
             r = float(wide);
+            // a row of zeros, which is never ok: Eq. 2's alpha of 1 itself (lo and hi know no NaN, ssq does)
+            if (lo == 0.f && hi == 0.f && ssq < INFINITY) wide = 1.0;
             scale = float(wide * double(rs.alpha));
         }
-        if (lo == 0.f && hi == 0.f && ssq < INFINITY) scale = 1.f;         // Eq. 2's choice for a row of zeros (lo and hi know no NaN, ssq does)
         const RowQuant rq(lo, hi, rs.inv, rs.zero, qmax);
         uint8_t* row = a.codes + m * (a.bits == 4 ? C / 2 : C);
         int sum = 0;
@@ -492,11 +493,11 @@ rmsnorm_quant_any(const NormArgs a) {
         float r = st.r, scale = st.alpha * st.r;
         if (!st.ok || by != 1.f) {
             if (!st.ok) st.plain(lo, hi, qmax);
-            const double wide = scaled_factor(ssq, C, a.eps, by);
+            double wide = scaled_factor(ssq, C, a.eps, by);
             r = float(wide);
+            if (lo == 0.f && hi == 0.f && ssq < INFINITY) wide = 1.0;
             scale = float(wide * double(st.alpha));
         }
-        if (lo == 0.f && hi == 0.f && ssq < INFINITY) scale = 1.f;
         if (a.y)
             for (int k = t; k < C; k += T) static_cast<XT*>(a.y)[m * C + k] = XT(s_u[k] * by * a.gamma[k] * r);
         if (a.codes) {
