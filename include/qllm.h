@@ -246,7 +246,7 @@ int qllm_qgemm_acc(const uint8_t* codes, const uint8_t* w_codes, int32_t* acc,
  * tensors are cut, slots out of range count as none, ranks are cut to 0 .. max_rank, and the status word becomes QLLM_ERR_PAGE
  * (qllm_poll_status); ranges that decrease may overlap others, whose rows of out are then one or the other's, or left.  seqs <= 2^20, rows <= 2^30.
  * Precision: sums in float32, all of whose bits enter the second product.  QLLM_F32 rows with an
- * infinity give NaN. */
+ * infinity give NaN (QLLM_BF16 ones what the formula gives).  The weights are finite. */
 typedef struct qllm_adapters {
     const void*    A;
     const void*    B;

@@ -338,7 +338,7 @@ adapters_add_kernel(const AdapterArgs p) {
                 w[i][0] = i + 1 < kParts ? upper(f[0], f[1]) : rounded(f[0], f[1]);
                 w[i][1] = i + 1 < kParts ? upper(f[2], f[3]) : rounded(f[2], f[3]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) f[j] = rest(f[j]);
+                for (int j = 0; j < 4; ++j) f[j] = rest_of_sum(f[j]);
                 if constexpr (S::kAll) {
                     *reinterpret_cast<uint2*>(s_inner + i * kT * kS + at) = make_uint2(w[i][0], w[i][1]);
                 } else {

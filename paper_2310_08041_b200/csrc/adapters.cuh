@@ -73,6 +73,9 @@ __device__ __forceinline__ uint32_t rounded(float lo, float hi) {
 }
 __device__ __forceinline__ float rest(float f) { return f - __uint_as_float(__float_as_uint(f) & 0xFFFF0000u); }
 
+// of a sum over K: an infinity is its first part, whose product with B is the formula's
+__device__ __forceinline__ float rest_of_sum(float f) { return fabsf(f) == INFINITY ? 0.f : rest(f); }
+
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void st_cluster4(uint32_t addr, float4 v) {

@@ -396,7 +396,7 @@ adapters_tile_kernel(const AdapterArgs p) {
                 const bool last = i + 1 == kSumParts;
                 const uint32_t w0 = last ? rounded(f[0], f[1]) : upper(f[0], f[1]), w1 = last ? rounded(f[2], f[3]) : upper(f[2], f[3]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) f[j] = rest(f[j]);
+                for (int j = 0; j < 4; ++j) f[j] = rest_of_sum(f[j]);
                 const int element = (S::kFew ? 0 : i * R) + col, byte = 2 * (element & 63), line = at_row + (S::kFew ? ROWS * i : 0);
                 const uint32_t at = h_addr + (element >> 6) * h_block + line * 128 + (((byte >> 4) ^ (line & 7)) << 4) + (byte & 15);
                 if constexpr (S::kFew) {
