@@ -612,7 +612,7 @@ int qllm_poll_status(void);
  * QLLM_ERR_TIMEOUT once and QLLM_OK again; other calls are unaffected.  Asynchronous on `stream`. */
 int qllm_debug_wait_expiry(int* gave_up, void* stream);
 /* The exit of qllm_adapters_add's tensor-core kernel behind such a wait: of a cluster of two CTAs, one warp's wait runs out and the others'
- * do not; all of them leave together.  left (device int[2]): each CTA adds the number of its warps that left, three.  Status and launch as above. */
+ * do not; all of them leave together.  left (device int[2]): each CTA adds the number of its warps that left, four.  Status and launch as above. */
 int qllm_debug_exit_expiry(int* left, void* stream);
 /* Number of kernel launches issued by this library in this process (all threads). */
 int64_t qllm_launch_count(void);

@@ -303,7 +303,7 @@ def qllm_debug_wait_expiry(gave_up, stream=None):
 
 
 def qllm_debug_exit_expiry(left, stream=None):
-    """Runs the exit behind such a wait in a cluster of two CTAs; left: device int32 [2], each CTA adds its warps that left (3)."""
+    """Runs the exit behind such a wait in a cluster of two CTAs; left: device int32 [2], each CTA adds its warps that left (4)."""
     _check(_lib.qllm_debug_exit_expiry(_dp(left), _stream(stream)))
 
 

@@ -185,6 +185,7 @@ adapters_tile_kernel(const AdapterArgs p) {
     const Abort ab{&s_abort, p.status};
     int sg = 0, owner = 0;                                 // place in the ring, its team
     uint32_t turn = 0;
+    const auto leave = [&](bool ok) { tc::leave_cluster(ok, 2, kThreads, cl); };
     const auto advance = [&] {
         if (++owner == kTeams) owner = 0;
         if (++sg == stages) { sg = owner = 0; turn ^= 1; }
@@ -254,6 +255,7 @@ adapters_tile_kernel(const AdapterArgs p) {
             advance();
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
+        leave(ok);
         return;
     }
 
@@ -262,6 +264,7 @@ adapters_tile_kernel(const AdapterArgs p) {
         // of the ring, to sums of its own (all lanes walk along, so that operands are the warp's, not a thread's).  A place has the same issuer and
         // team for good: who waits for its next phase has seen the last one end, which a bit of parity alone would not tell.
         const int me = warp - kWorkers / 32;
+        bool ok = true;
         if (rank > 0) {
             constexpr uint32_t id1 = idesc_bf16(128, S::kFew ? ROWS : R), id2 = idesc_bf16(128, S::kFew ? kSumParts * ROWS : kCols);
             const uint32_t base_addr = ptx::smem_addr(smem), h_low = desc_low(ptx::smem_addr(s_hop)), d = __shfl_sync(0xffffffffu, tmem, 0);
@@ -271,7 +274,6 @@ adapters_tile_kernel(const AdapterArgs p) {
                 else mma_bf16_ss(to, rows, weights, id, more);
             };
             const bool lead = elect_one();
-            bool ok = true;
             uint32_t more = 0;
             for (int k = k0; k < k1; k += kCols, advance()) {
                 if (owner != me) continue;
@@ -319,6 +321,7 @@ adapters_tile_kernel(const AdapterArgs p) {
                 __syncwarp();
             }
         }
+        leave(ok);
         return;
     }
 
@@ -512,7 +515,7 @@ adapters_tile_kernel(const AdapterArgs p) {
         uses ^= 1;
     }
     ptx::tc_fence_before_sync();
-    tc::leave_cluster(ok, 1, kWorkers, cl);
+    leave(ok);
     ptx::tc_fence_after_sync();
     if (warp == 0) ptx::tmem_dealloc(tmem, 512);
 }

@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(32) wait_expiry_kernel(int* status, int* gave_
     if (threadIdx.x == 0) *gave_up = arrived ? 0 : 1;
 }
 
-constexpr int kExitWarps = 4, kExitWorkers = 3;            // the last warp leaves at once, as feeders and issuers do
+constexpr int kExitWarps = 4;
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * kExitWarps) exit_expiry_kernel(int* status, int* left) {
     __shared__ __align__(8) uint64_t bar;
@@ -40,11 +40,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * kExitWarps) exi
         ptx::fence_barrier_init();
     }
     __syncthreads();
-    const int warp = int(threadIdx.x) / 32;
-    if (warp >= kExitWorkers) return;
     bool ok = true;
-    if (blockIdx.x == 0 && warp == 1) ok = __all_sync(0xffffffffu, tc::wait_bounded(&bar, 0, tc::Abort{&flag, status}, 1ll << 20));
-    tc::leave_cluster(ok, 1, 32 * kExitWorkers, 2);
+    if (blockIdx.x == 0 && threadIdx.x / 32 == 1) ok = __all_sync(0xffffffffu, tc::wait_bounded(&bar, 0, tc::Abort{&flag, status}, 1ll << 20));
+    tc::leave_cluster(ok, 2, 32 * kExitWarps, 2);
     if (threadIdx.x % 32 == 0) atomicAdd(left + blockIdx.x, 1);
 }
 

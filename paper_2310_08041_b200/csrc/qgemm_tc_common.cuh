@@ -44,11 +44,12 @@ __device__ __forceinline__ bool wait_bounded(uint64_t* bar, uint32_t parity, con
     }
 }
 
-// The end of a CTA of a cluster whose waits may have run out: by `threads` threads, whole warps, on named barrier `id`; its other threads exit
-// without it.  ok is a warp's own (a wait can run out for one warp and end for the next), what follows is decided by all of them in
-// one barrier: none may stand at the cluster's barrier for a warp that stands at this one for it.  Where a wait ran out, MMAs that were issued
-// before end in the time spent here, and the CTA stays until the cluster's others, which may still write to it, are here or gone.
+// The end of a CTA of a cluster whose waits may have run out: by all of its `threads` threads, each where its role ends, on named barrier `id`.
+// ok is a warp's own (a wait can run out for one warp and end for the next), what follows is decided by all of them in one barrier: none may
+// stand at the cluster's barrier for a warp that stands at this one for it, and none may still issue MMAs.  Where a wait ran out, those that were
+// issued before end in the time spent here, and the CTA stays until the cluster's others, which may still write to it, are here or gone.
 __device__ __forceinline__ void leave_cluster(bool ok, int id, int threads, int cluster) {
+    __syncwarp();
     if (!ptx::named_bar_or(id, threads, !ok)) return;
     const long long since = clock64();
     while (clock64() - since < (1ll << 20)) {}

@@ -15,7 +15,7 @@ def test_one_warp_whose_wait_ran_out_takes_the_others_along():
     for times in (1, 2, 3):
         B.qllm_debug_exit_expiry(left)
         assert B.qllm_poll_status() == B.QLLM_ERR_TIMEOUT
-        assert left.tolist() == [3 * times, 3 * times]
+        assert left.tolist() == [4 * times, 4 * times]
     assert B.qllm_poll_status() == B.QLLM_OK
     # rank 72, few rows: the tensor-core kernel in clusters.  Sums of eight ones times one half: exact
     top, K, N, rows = 72, 256, 512, 3
