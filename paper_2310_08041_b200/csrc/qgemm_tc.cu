@@ -180,6 +180,7 @@ qgemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const int quad = warp & 3;                        // TMEM lanes 32*quad .. +31
         const int et = threadIdx.x - 32 * kFirstEpiWarp;  // 0..127
         uint32_t lt = 0;
+        bool ok = true;                                   // false: a wait ran out; on to the barriers where the other warps still meet this one
         asm volatile("griddepcontrol.wait;" ::: "memory");   // the row terms below come from the kernel before
         for (int tile = blockIdx.x; tile < num_tiles; tile += gridDim.x, ++lt) {
             const uint32_t abuf = lt & 1, aph = (lt >> 1) & 1;
@@ -190,7 +191,8 @@ qgemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             const int64_t m = int64_t(m0) + quad * 32 + lane;
             RowTerm rt{0.f, 0, 0};
             if (!ep.raw_acc && m < M) rt = make_row_term(ep.a_scale, ep.a_zero, ep.a_rowsum, m);
-            if (!wait_bounded(&acc_full[abuf], aph, ab)) break;
+            ok = __all_sync(0xffffffffu, ok && wait_bounded(&acc_full[abuf], aph, ab));
+            if (!ok) continue;
             ptx::tc_fence_after_sync();
 #pragma unroll 1
             for (int ch = 0; ch < BN / 32; ++ch) {

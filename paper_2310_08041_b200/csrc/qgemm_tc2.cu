@@ -201,6 +201,7 @@ qgemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                                            ptx::map_to_cta(ptx::smem_addr(&acc_empty[1]), 0)};
         uint8_t* mybuf = outbuf + (warp - kFirstEpiWarp) * 2048;
         uint32_t lt = 0;
+        bool ok = true;                                   // false: a wait ran out; on to the barriers where the other warps still meet this one
         asm volatile("griddepcontrol.wait;" ::: "memory");   // the row terms below come from the kernel before
         for (int tile = pair; tile < num_tiles; tile += npairs, ++lt) {
             const uint32_t abuf = lt & 1, aph = (lt >> 1) & 1;
@@ -217,7 +218,8 @@ qgemm_tc2_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                 rt[i] = RowTerm{0.f, 0, 0};
                 if (!ep.raw_acc && m < M) rt[i] = make_row_term(ep.a_scale, ep.a_zero, ep.a_rowsum, m);
             }
-            if (!wait_bounded(&acc_full[abuf], aph, ab)) break;
+            ok = __all_sync(0xffffffffu, ok && wait_bounded(&acc_full[abuf], aph, ab));
+            if (!ok) continue;
             ptx::tc_fence_after_sync();
 #pragma unroll 1
             for (int ch = half; ch < BN / 32; ch += 2) {
