@@ -15,13 +15,15 @@
 //
 // ROWS: rows of the tile that there is room for.  With 16 (a step's single tokens) the products are transposed, D1[ranks x rows] and
 // D2[128 columns x rows]: the weights are the M side, the rows an N of 16.  An MMA's time is that of its operands' bytes from shared memory, and
-// 128 rows of which 16 are real would be most of them (96 tokens on 24 adapters of rank 64, 8192 x 10240: 21.2 us so, 19.7 now).
+// 128 rows of which 16 are real would be most of them (96 tokens on 24 adapters of rank 64, 8192 x 10240: 21.2 us so, 19.4 now).
 //
 // What bounds it.  3792 rows on 9 adapters of rank <= 32, 8192 x 8192 (53 us, 192 MB: 3.6 TB/s; the floor is 29): 0.4 us for 128 columns of the
 // first product, the ring's bytes in flight, and up to 1.3 of the second, the instructions of the teams (3900 for 128 x 128 numbers of out), on
-// three quarters of the SMs; finding the tile 2.5, first data 2, the exchange 3.7.  Two teams with barriers among their warps took 57.3 us; four teams, or
-// the teams' loop unrolled, were slower (instruction fetch).  The warp-level MMA (adapters.cu) took 63 (some 20 cycles for each m16n8k16 and quarter
-// of an SM).  A step of 96 tokens: the chain search, first data, exchange, and 125 SMs for 25 adapters of 5 CTAs.
+// three quarters of the SMs; finding the tile 2.5, first data 2, the exchange 3.7.  The third part of the sums is 1.3 us of the 53 (its MMAs and
+// stores); where MMAs are more of the time it is more: 1024 rows of rank 64, 8192 x 10240, 28.2 -> 30.4, of rank 128, 4096 x 4096, 24.8 -> 28.3.  With two
+// parts, when they came to 52: two teams with barriers among their warps took 57.3 us; four teams, or the teams' loop unrolled, were slower
+// (instruction fetch); the warp-level MMA (adapters.cu) took 63 (some 20 cycles for each m16n8k16 and quarter of an SM).  A step of 96 tokens: the chain
+// search, first data, exchange, and 125 SMs for 25 adapters of 5 CTAs.
 #include <algorithm>
 
 #include "adapters.cuh"
@@ -260,7 +262,7 @@ adapters_tile_kernel(const AdapterArgs p) {
     }
 
     if (warp >= kWorkers / 32) {
-        // ---------------------------------------------------------------- one thread of each of two warps issues the MMAs of every second place
+        // ---------------------------------------------------------------- one thread of each of three warps issues the MMAs of every third place
         // of the ring, to sums of its own (all lanes walk along, so that operands are the warp's, not a thread's).  A place has the same issuer and
         // team for good: who waits for its next phase has seen the last one end, which a bit of parity alone would not tell.
         const int me = warp - kWorkers / 32;
@@ -325,7 +327,7 @@ adapters_tile_kernel(const AdapterArgs p) {
         return;
     }
 
-    // -------------------------------------------------------------------- workers: two teams, thread `row` of a team has that row of the tile
+    // -------------------------------------------------------------------- workers: three teams, thread `row` of a team has that row of the tile
     const int team = t / kTeam, row = t % kTeam, quarter = warp & 3;
     const uint32_t my_tmem = tmem + (uint32_t(quarter * 32) << 16);
     bool ok = true;                                        // false: a wait ran out; go through the motions without waiting
@@ -538,9 +540,10 @@ int launch_shape(AdapterArgs p, cudaStream_t st) {
     cfg.attrs = attr;
     // For each size of a cluster: the rounds that the fewest tiles take, the fewest rows to a tile with which they do, be the groups random (their
     // last tiles are half full, some more) or alike; of these the shortest launch: 128 columns of both products together take a CTA
-    // (180 + rows) 5.6 ns (rank 32; 100 + rows transposed), and a round has 8 us of its own.  3792 rows on 9 adapters, 8192 x 8192: 3 CTAs to 104 rows, 53 us; 3 to
-    // 128 58, 2 to 64 55, 4 to 128 (two rounds) 64.  1024 rows of one, 8192 x 10240: 8 to 80, 24 us; 8 to 128 30, 6 to 48 29, 2 to 16 54.  20000 rows of
-    // one, 4096 x 4096, rank 16: 3 rounds of 2 CTAs to 96 rows 114, 2 rounds of single CTAs to 128 146.
+    // (180 + rows) 5.6 ns (rank 32; 100 + rows transposed), and a round has 8 us of its own.  3792 rows on 9 adapters, 8192 x 8192: 3 CTAs to 104 rows 56.1 us (timed
+    // like the following), 3 to 112 57.5, 3 to 128 59.6, 2 to 64 56.2, 4 to 128 (two rounds) 65.4.  1024 rows of one, 8192 x 10240: 8 to 72 25.6; 8 to 128 33.8,
+    // 6 to 48 27.4, 2 to 16 48.7; rank 64: 8 to 72 30.5, 8 to 120 38.7, 6 to 48 30.9.  20000 rows of one, 4096 x 4096, rank 16: 3 rounds of 2 CTAs to 96 rows 116,
+    // 2 rounds of single CTAs to 128 148.
     // (Clusters of 4: 33 of 148 SMs' possible 37, whatever their parts of the chip.)
     const int64_t groups = std::min<int64_t>({p.seqs, p.slots + 1, p.rows});
     static std::atomic<int> known[64][9];
